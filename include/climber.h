@@ -225,6 +225,91 @@ int climber_attn_sumi_bias(const climber_config *cfg, const float *tau_layer,
                            const int32_t *cand_beh, void *o_c, const climber_rel_bias *bias,
                            void *stream);
 
+/* ---- paged history cache ----------------------------------------------------------------------
+ * climber_kv_cache holds histories that are encoded once.  A history that grows -- a behaviour, a
+ * session at a time -- or that is too long to keep whole lives in pages instead: one layer's keys and
+ * values in a pool of pages, and for every sequence (user) the list of its pages.  Three calls work on it:
+ *   climber_attn_history_paged  stores a chunk of new behaviours per sequence and attends from them
+ *   climber_attn_sumi_paged     candidates against the stored history (the mask of Sec. 3.2)
+ *   climber_paged_evict         cuts every sequence to a budget, the tokens with the least weight first
+ * All memory belongs to the caller; there is no handle, and a layout that the caller may read and write:
+ *   k, v        dev [n_pages][n_kv_heads][page_size][d_head], config dtype, 16-byte aligned
+ *   page_table  dev int32 [n_seqs][table_ld]: token `slot` of sequence b is row slot % page_size of page
+ *               page_table[b][slot / page_size].  Entries behind the pages in use may hold anything.
+ *   len         dev int32 [n_seqs]: tokens in the cache before the call.  No call but climber_paged_evict
+ *               changes a length: after an append the caller adds the chunk's rows.
+ *   max_len     host: no sequence has more tokens than this after the call.  It sizes the launches (a
+ *               HIP graph keeps working while lengths grow up to it) and is at most table_ld * page_size.
+ *   mass        dev fp32 [n_pages][page_size] or NULL: accumulated attention weight per token.  Where it is
+ *               not NULL, both attention calls add to a token's entry its softmax weights in all of the call's
+ *               rows and heads (not a candidate's weight on itself); an appended token starts from 0.  Sums are
+ *               made in fp32 in an order that only depends on the sizes of the call.  Two calls that add to
+ *               the same tokens must not overlap.
+ *   stamp       dev int32 [n_pages][page_size] or NULL: a number of the caller's per token (its time, its
+ *               position), stored by climber_attn_history_paged and kept with its token by climber_paged_evict.
+ * page_size: a power of two, 16 .. 4096.  n_kv_heads divides cfg->n_heads: query head h reads cache head
+ * h / (n_heads / n_kv_heads).  CLIMBER_BF16: d_head 64 or 128; CLIMBER_F32: d_head <= 128, a multiple of 4.
+ * A page may be listed by several sequences (a shared prefix) as long as no call writes into it: an append
+ * writes the pages of slots len[b] .. len[b] + rows - 1, an eviction those of slots below the budget.
+ * Contents of slots from len[b] on are never used: they may hold anything, NaN included.
+ * Lengths, offsets and page numbers are device memory and cannot be checked on the host: lengths are clamped to
+ * max_len, offsets to m_total, page numbers that are read to the pool, and a token whose page number lies outside the
+ * pool is not stored.  climber_check_paged reports such values.
+ * Rows (q, k, v, o): row r starts r * ld elements behind the pointer and holds its heads one after the other;
+ * pointers and row pitches are multiples of 16 bytes; o must not share an element with q, k or v.  Rows of no
+ * sequence (behind off[n_seqs]) stay as they are. */
+typedef struct climber_paged_kv {
+    void *k, *v;
+    float *mass;
+    int32_t *stamp;
+    const int32_t *page_table, *len;
+    int32_t n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len;
+} climber_paged_kv;
+
+/* Bytes of scratch that any call on this cache needs for up to m_total rows, at most m_max per sequence (0, 0: eviction only).
+ * Reads the sizes, and whether mass is NULL.  0 on an invalid argument. */
+size_t climber_paged_workspace_bytes(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total, int32_t m_max);
+
+/* A chunk of new behaviours.  off: dev int32 [n_seqs + 1], rows off[b] .. off[b + 1] - 1 are sequence b's next tokens (m_total, m_max
+ * as in climber_attn_sumi; a sequence may have none).  Their k, v (and stamp: dev int32 [m_total], needed if kv->stamp) are stored as
+ * slots len[b] + i, and
+ *     o_i = softmax over { cached tokens of b, new tokens j <= i of b } of qk_scale <q_i, k_j> / tau[scen_i][beh_i], applied to v
+ * (CLIMBER_HIST_CAUSAL; without it, all new tokens of b).  With len = 0 this is the attention of whole histories.  A token that a row
+ * does not see has no influence on it, whatever it holds.  cfg->sub_len must be 0: a sequence is one subsequence.
+ * q, o: [m_total][ld] of n_heads * d_head; k, v: [m_total][ld_kv] of n_kv_heads * d_head.
+ * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _TAU, _BUFSIZE, _UNSUPPORTED (d_head, sub_len, o on q, k or v), _RUNTIME. */
+int climber_attn_history_paged(const climber_config *cfg, const float *tau_layer, const climber_paged_kv *kv, const void *q,
+                               int64_t ld_q, const void *k, const void *v, int64_t ld_kv, const int32_t *off, int32_t m_total,
+                               int32_t m_max, const int32_t *scen, const int32_t *beh, const int32_t *stamp, void *o,
+                               int64_t ld_o, void *workspace, size_t ws_bytes, void *stream);
+
+/* Candidates: climber_attn_sumi over the paged history.  Every candidate sees all cached tokens of its sequence and itself; nothing
+ * is stored.  cfg->sub_len and CLIMBER_HIST_CAUSAL do not concern it.  Errors as above. */
+int climber_attn_sumi_paged(const climber_config *cfg, const float *tau_layer, const climber_paged_kv *kv, const void *q_c,
+                            int64_t ld_q, const void *k_c, const void *v_c, int64_t ld_kv, const int32_t *cand_off,
+                            int32_t m_total, int32_t m_max, const int32_t *cand_scen, const int32_t *cand_beh, void *o_c,
+                            int64_t ld_o, void *workspace, size_t ws_bytes, void *stream);
+
+/* Sequence b keeps min(budget[b], len[b]) tokens (budget: dev int32 [n_seqs]; below 0 counts as 0).  Tokens rank by
+ *     stamp >= keep_from[b] before all others (keep_from: dev int32 [n_seqs], or NULL: no such rule; needs kv->stamp),
+ *     then rank descending (rank: dev fp32 laid out as kv->mass, or NULL: kv->mass; NaN ranks below everything),
+ *     then slot ascending.
+ * The cache of a sequence is a set: kept tokens of slots below the new length stay where they are, and the places of evicted tokens
+ * among them are filled, in ascending order, with the kept tokens of the slots behind.  k, v, and mass and stamp where they are
+ * not NULL, move with their token; `rank` is only read.  Slots from the new length on keep what they held.
+ * len_out: dev int32 [n_seqs], the new lengths (may be kv->len).  src: dev int32 [n_seqs][table_ld * page_size] or NULL: for each slot below
+ * the new length the slot that its token had before, -1 from there on.  A caller with more data per token moves it by src.
+ * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _BUFSIZE, _UNSUPPORTED (d_head), _RUNTIME. */
+int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, const float *rank, const int32_t *budget,
+                        const int32_t *keep_from, int32_t *len_out, int32_t *src, void *workspace, size_t ws_bytes, void *stream);
+
+/* climber_check_inputs for a paged cache: one small kernel that reads page_table, len and, if not NULL, off against the rules
+ * above for a call of m_total rows that stores them (appends != 0) or does not, and ORs CLIMBER_BAD_* bits into *status. */
+#define CLIMBER_BAD_PAGE 32 /* a page number of a token outside [0, n_pages) */
+#define CLIMBER_BAD_LEN 64  /* a length below 0, or over max_len after the call */
+int climber_check_paged(const climber_config *cfg, const climber_paged_kv *kv, const int32_t *off, int32_t m_total, int32_t m_max,
+                        int32_t appends, int32_t *status, void *stream);
+
 /* ---- debug check of device-resident inputs -----------------------------------------------------
  * Eq. (3) divides a row's logits by tau[scen][beh]: the ids must lie inside the table and the entry
  * must be finite and > 0.  Ids, offsets and the table live in device memory, so the compute calls

@@ -53,6 +53,12 @@ class BgfWeights(C.Structure):
                 ("tau_scen", C.c_void_p), ("b_head", C.c_float), ("n_blocks", C.c_int32), ("d_gate", C.c_int32)]
 
 
+class PagedKV(C.Structure):
+    """Mirror of ``climber_paged_kv`` (device pointers).  Build with ``paged_kv(...)``."""
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "mass", "stamp", "page_table", "len")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "n_seqs", "table_ld", "max_len")]
+
+
 class _Weights(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("layers", C.POINTER(LayerWeights)), ("packed", C.c_void_p)]
 
@@ -127,6 +133,17 @@ def load_library():
     lib.climber_sumi_score_static.restype = C.c_int
     lib.climber_sumi_score_static.argtypes = [cfgp, C.POINTER(_Weights), vp, vp, vp, vp, i32, i32, vp,
                                               vp, vp, vp]
+    pkv = C.POINTER(PagedKV)
+    lib.climber_paged_workspace_bytes.restype = sz
+    lib.climber_paged_workspace_bytes.argtypes = [cfgp, pkv, i32, i32]
+    lib.climber_attn_history_paged.restype = C.c_int
+    lib.climber_attn_history_paged.argtypes = [cfgp, vp, pkv, vp, i64, vp, vp, i64, vp, i32, i32, vp, vp, vp, vp, i64, vp, sz, vp]
+    lib.climber_attn_sumi_paged.restype = C.c_int
+    lib.climber_attn_sumi_paged.argtypes = [cfgp, vp, pkv, vp, i64, vp, vp, i64, vp, i32, i32, vp, vp, vp, i64, vp, sz, vp]
+    lib.climber_paged_evict.restype = C.c_int
+    lib.climber_paged_evict.argtypes = [cfgp, pkv, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.climber_check_paged.restype = C.c_int
+    lib.climber_check_paged.argtypes = [cfgp, pkv, vp, i32, i32, i32, vp, vp]
     try:
         _load_native(lib)
     except ImportError:  # the host's calls do without; an attention call raises it
@@ -169,6 +186,10 @@ def _stream(stream) -> Optional[int]:
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def _i32arr(xs: Sequence[int]):
@@ -248,7 +269,7 @@ def climber_attn_sumi(cfg: Config, tau_layer, cache: KVCache, layer: int, q_c, k
         raise ClimberError(code, "climber_attn_sumi")
 
 
-BAD_SCEN, BAD_BEH, BAD_TAU, BAD_OFFSETS, BAD_M_MAX = 1, 2, 4, 8, 16
+BAD_SCEN, BAD_BEH, BAD_TAU, BAD_OFFSETS, BAD_M_MAX, BAD_PAGE, BAD_LEN = 1, 2, 4, 8, 16, 32, 64
 
 
 def climber_check_inputs(cfg: Config, tau_layer, scen, beh, cache: Optional[KVCache], m_total: int,
@@ -385,3 +406,75 @@ def climber_bgf_score(cfg: Config, atl_layer, w_down, w_up, w_head, tau_scen, b_
     _ok(load_library().climber_bgf_score(C.byref(cfg), C.byref(w), _ptr(e), _ptr(cand_scen), m_total, _ptr(y),
                                          _ptr(score), _ptr(workspace), workspace.numel() * workspace.element_size(),
                                          _stream(stream)), "climber_bgf_score")
+
+
+def paged_kv(k, v, page_table, len, max_len: int, mass=None, stamp=None) -> PagedKV:
+    """climber_paged_kv from contiguous device tensors: k, v [n_pages, n_kv_heads, page_size, d_head]; page_table int32 [n_seqs, table_ld];
+    len int32 [n_seqs]; mass fp32, stamp int32 [n_pages, page_size]."""
+    for t in (k, v, page_table, len, mass, stamp):
+        if t is not None and not t.is_contiguous():
+            raise ValueError("a paged cache is described by contiguous tensors")
+    n_pages, n_kv_heads, page_size, _ = k.shape
+    n_seqs, table_ld = page_table.shape
+    if v.shape != k.shape or len.numel() != n_seqs or any(t is not None and t.numel() != n_pages * page_size for t in (mass, stamp)):
+        raise ValueError("k, v, page_table, len, mass and stamp are not of one cache")
+    kv = PagedKV(_ptr(k), _ptr(v), _ptr(mass), _ptr(stamp), _ptr(page_table), _ptr(len), n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len)
+    kv._keep = (k, v, mass, stamp, page_table, len)
+    return kv
+
+
+def climber_paged_workspace_bytes(cfg: Config, kv: PagedKV, m_total: int, m_max: int) -> int:
+    return int(load_library().climber_paged_workspace_bytes(C.byref(cfg), C.byref(kv), m_total, m_max))
+
+
+def _pitch(t, width: int) -> int:
+    """Elements from one row to the next: of a tensor its first stride (its other dimensions lie one behind the other), of a pointer `width`."""
+    if t is None or isinstance(t, int):
+        return width
+    shape, stride = t.shape, t.stride()
+    inner = 1
+    for n, st in zip(reversed(shape[1:]), reversed(stride[1:])):
+        if n != 1 and st != inner:
+            raise ValueError("the elements of a row have to be contiguous")
+        inner *= n
+    return stride[0] if shape[0] > 1 else max(width, inner)
+
+
+def _same_pitch(k, v, width: int) -> int:
+    ld = _pitch(k, width)
+    if v is not None and not isinstance(v, int) and v.shape[0] > 1 and _pitch(v, width) != ld:
+        raise ValueError("k and v have different row pitches")
+    return ld
+
+
+def climber_attn_history_paged(cfg: Config, tau_layer, kv: PagedKV, q, k, v, off, m_total: int, m_max: int, scen, beh, stamp, o,
+                               workspace, stream=None) -> None:
+    """Append a chunk of new behaviours to the paged cache and attend from them.  q, k, v, o: row r is [r] of the tensor (row pitches are
+    taken from it, so that columns of one projection's output can be passed as they are)."""
+    d, dk = cfg.d_model, kv.n_kv_heads * cfg.d_head
+    _ok(load_library().climber_attn_history_paged(
+        C.byref(cfg), _ptr(tau_layer), C.byref(kv), _ptr(q), _pitch(q, d), _ptr(k), _ptr(v), _same_pitch(k, v, dk), _ptr(off), m_total, m_max,
+        _ptr(scen), _ptr(beh), _ptr(stamp), _ptr(o), _pitch(o, d), _ptr(workspace), _nbytes(workspace), _stream(stream)),
+        "climber_attn_history_paged")
+
+
+def climber_attn_sumi_paged(cfg: Config, tau_layer, kv: PagedKV, q_c, k_c, v_c, cand_off, m_total: int, m_max: int, cand_scen, cand_beh,
+                            o_c, workspace, stream=None) -> None:
+    """Candidates against the paged cache (rows as in climber_attn_history_paged)."""
+    d, dk = cfg.d_model, kv.n_kv_heads * cfg.d_head
+    _ok(load_library().climber_attn_sumi_paged(
+        C.byref(cfg), _ptr(tau_layer), C.byref(kv), _ptr(q_c), _pitch(q_c, d), _ptr(k_c), _ptr(v_c), _same_pitch(k_c, v_c, dk), _ptr(cand_off),
+        m_total, m_max, _ptr(cand_scen), _ptr(cand_beh), _ptr(o_c), _pitch(o_c, d), _ptr(workspace), _nbytes(workspace), _stream(stream)),
+        "climber_attn_sumi_paged")
+
+
+def climber_paged_evict(cfg: Config, kv: PagedKV, rank, budget, keep_from, len_out, src, workspace, stream=None) -> None:
+    """Cut every sequence of the paged cache to its budget, least weight first."""
+    _ok(load_library().climber_paged_evict(C.byref(cfg), C.byref(kv), _ptr(rank), _ptr(budget), _ptr(keep_from), _ptr(len_out), _ptr(src),
+                                           _ptr(workspace), _nbytes(workspace), _stream(stream)), "climber_paged_evict")
+
+
+def climber_check_paged(cfg: Config, kv: PagedKV, off, m_total: int, m_max: int, appends: bool, status, stream=None) -> None:
+    """Device-side check of page numbers / lengths / offsets; ORs BAD_* bits into status (int32 tensor)."""
+    _ok(load_library().climber_check_paged(C.byref(cfg), C.byref(kv), _ptr(off), m_total, m_max, int(appends), _ptr(status), _stream(stream)),
+        "climber_check_paged")

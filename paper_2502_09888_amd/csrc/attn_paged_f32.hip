@@ -1,0 +1,407 @@
+// Attention over the paged history cache in fp32 (gfx950): a chunk of new behaviours, or candidates, of every sequence against
+// its cached tokens and its own rows (Eq. (3) of Climber, arXiv 2502.09888; the mask of Sec. 3.2 for candidates), the join of partial
+// results, and the accumulation of the attention weights per cached token.
+#include "paged.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace climber {
+namespace {
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+
+constexpr int kKeys = 32;              // keys of a tile
+constexpr float kNoRef = -1.0e30f;     // "no reference yet", below any finite logit
+
+static __device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4 *)p; }
+static __device__ __forceinline__ f32x4 load4(const __bf16 *p)
+{
+    const uint2 u = *(const uint2 *)p;
+    f32x4 x;
+    x[0] = __uint_as_float(u.x << 16);
+    x[1] = __uint_as_float(u.x & 0xffff0000u);
+    x[2] = __uint_as_float(u.y << 16);
+    x[3] = __uint_as_float(u.y & 0xffff0000u);
+    return x;
+}
+static __device__ __forceinline__ void store4(float *p, f32x4 x) { *(f32x4 *)p = x; }
+static __device__ __forceinline__ void store4(__bf16 *p, f32x4 x)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = (__bf16)x[i];
+}
+
+static __device__ __forceinline__ float half_max(float x) { return fmaxf(x, __shfl_xor(x, 32, 64)); }
+
+// 32 keys (rows pointed to by key_ptr) into LDS, pitch DP + 4 floats, zeros beyond d
+template <typename E, int DP, int NT, typename Ptr>
+static __device__ __forceinline__ void load_tile(float *to, int d, Ptr key_ptr)
+{
+    constexpr int C = DP / 4;
+    for (int i = threadIdx.x; i < kKeys * C; i += NT) {
+        const int r = i / C, c = (i % C) * 4;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (c < d) x = load4((const E *)key_ptr(r) + c);
+        *(f32x4 *)(to + r * (DP + 4) + c) = x;
+    }
+}
+
+// The transposed problem, as in the bf16 kernels: S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x2_f32.  A lane owns one packed
+// row (lane % 32), its probabilities leave the accumulator as the operand of the value product (step r of it takes the keys of
+// accumulator register r).  The sum over the dimensions is taken in an order that lets a lane read four of them at once.
+template <typename E, int DP, int NW, bool SUMI>
+__global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs p)
+{
+    constexpr int kPitch = DP + 4, NB = DP / 32;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    float *tk = lds, *tv = lds + kKeys * kPitch;
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    if (!paged_work(p, w)) return;
+    const PagedSeq s = paged_seq(p, w.b);
+    const int rows = s.T * p.G, r_tile = w.tile * NW * 32;
+    if (r_tile >= rows) return;
+    const int r_wave = r_tile + wave * 32, r = min(r_wave + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
+    const int64_t row = s.row0 + t;
+    const bool causal = !SUMI && p.causal;
+    const int k_all = SUMI ? s.n : s.n + s.T;
+    // this lane's row sees keys below lim; the tile's and the wave's bounds
+    const int lim = causal ? s.n + t + 1 : k_all;
+    const int t_tile = min(r_tile + NW * 32 - 1, rows - 1) / p.G, k_end = causal ? s.n + t_tile + 1 : k_all;
+    const int lim_lo = causal ? s.n + min(r_wave, rows - 1) / p.G + 1 : k_all, lim_hi = causal ? s.n + min(r_wave + 31, rows - 1) / p.G + 1 : k_all;
+    int k_lo, k_hi;
+    paged_part(p, w.split, k_end, kKeys, k_lo, k_hi);
+
+    if (!SUMI && w.split == 0) {  // the tile's new tokens go into their pages (no call reads them from there before this one is done)
+        const int t0 = (r_tile + p.G - 1) / p.G, t1 = (min(r_tile + NW * 32, rows) + p.G - 1) / p.G, C = p.row_bytes / 8;
+        for (int i = threadIdx.x; i < (t1 - t0) * C; i += NW * 64) {
+            const int tt = t0 + i / C, c = (i % C) * 8, slot = s.n + tt;
+            const int raw = p.table[(int64_t)w.b * p.table_ld + (slot >> p.page_shift)];
+            if (raw < 0 || raw >= p.n_pages) continue;
+            const int64_t at = paged_row(p, raw, w.hk, slot) + c, from = (s.row0 + tt) * p.ld_kv + (int64_t)w.hk * p.row_bytes + c;
+            *(uint2 *)(p.k_pages + at) = *(const uint2 *)(p.k + from);
+            *(uint2 *)(p.v_pages + at) = *(const uint2 *)(p.v + from);
+            if (w.hk == 0 && c == 0 && p.stamp) p.stamp[((int64_t)raw << p.page_shift) + (slot & ((1 << p.page_shift) - 1))] = p.stamp_new[s.row0 + tt];
+        }
+    }
+
+    f32x4 q[DP / 8];
+    const E *qp = (const E *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) q[i] = 8 * i + 4 * hf < p.d ? load4(qp + 8 * i + 4 * hf) : f32x4{0.f, 0.f, 0.f, 0.f};
+    const float c = paged_row_scale(p, row);
+    float m = kNoRef, l = 0.f;
+    f32x16 O[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
+    if (SUMI && w.split == 0) {  // the row's own key and value: the first member of its softmax
+        const E *kp = (const E *)(p.k + row * p.ld_kv) + (int64_t)w.hk * p.d, *vp = (const E *)(p.v + row * p.ld_kv) + (int64_t)w.hk * p.d;
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i)
+            if (8 * i + 4 * hf < p.d) {
+                const f32x4 x = load4(kp + 8 * i + 4 * hf);
+                dot += q[i][0] * x[0] + q[i][1] * x[1] + q[i][2] * x[2] + q[i][3] * x[3];
+            }
+        m = dot + __shfl_xor(dot, 32, 64);
+        l = hf == 0 ? 1.f : 0.f;
+        if (m != m) l = m, m = kNoRef;  // (a logit that is no number makes the row none)
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (32 * db + 8 * g + 4 * hf < p.d) {
+                    const f32x4 x = load4(vp + 32 * db + 8 * g + 4 * hf);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) O[db][4 * g + e] = x[e];
+                }
+    }
+
+    for (int k0 = k_lo; k0 < k_hi; k0 += kKeys) {
+        // keys behind the last one are read as the last one, and masked
+        auto ptr = [&](const uint8_t *pages, const uint8_t *fresh) {
+            return [&, pages, fresh](int i) {
+                const int j = min(k0 + i, k_hi - 1);
+                if (j < s.n) return pages + paged_row(p, paged_page(p, w.b, j), w.hk, j);
+                return fresh + (s.row0 + j - s.n) * p.ld_kv + (int64_t)w.hk * p.row_bytes;
+            };
+        };
+        __syncthreads();
+        load_tile<E, DP, NW * 64>(tk, p.d, ptr(p.k_pages, p.k));
+        load_tile<E, DP, NW * 64>(tv, p.d, ptr(p.v_pages, p.v));
+        __syncthreads();
+        if (r_wave >= rows || k0 >= lim_hi) continue;  // (no row here, or none that sees a key of the tile)
+        f32x16 S;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) {
+            const f32x4 x = *(const f32x4 *)(tk + l32 * kPitch + 8 * i + 4 * hf);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[i][e], S, 0, 0, 0);
+        }
+        const int top = min(lim, k_hi);
+        const bool masked = k0 + kKeys > min(lim_lo, k_hi);
+        auto key_of = [&](int i) { return k0 + 8 * (i >> 2) + 4 * hf + (i & 3); };
+        if (masked) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (key_of(i) >= top) S[i] = -INFINITY;
+        }
+        float mx = S[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
+        mx = fmaxf(half_max(mx), m);
+        const float alpha = __builtin_amdgcn_exp2f((m - mx) * c);
+        m = mx;
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) O[db][i] *= alpha;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            S[i] = __builtin_amdgcn_exp2f((S[i] - m) * c);
+            l += S[i];
+        }
+        if (!masked) {
+#pragma unroll
+            for (int db = 0; db < NB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(tv[(8 * (i >> 2) + 4 * hf + (i & 3)) * kPitch + 32 * db + l32], S[i], O[db], 0, 0, 0);
+        } else {
+            // A row must not meet the values of keys that it does not see, not even with probability 0, where they are infinite or
+            // no numbers: those take part as zeros, and the rows that do see one get it by a count of such values.
+#pragma unroll
+            for (int db = 0; db < NB; ++db) {
+                bool odd = false;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = tv[(8 * (i >> 2) + 4 * hf + (i & 3)) * kPitch + 32 * db + l32];
+                    const bool fine = fabsf(x) < INFINITY;
+                    odd |= !fine;
+                    O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(fine ? x : 0.f, S[i], O[db], 0, 0, 0);
+                }
+                if (__builtin_amdgcn_ballot_w64(odd) == 0) continue;
+                for (int kind = 0; kind < 3; ++kind) {
+                    f32x16 n;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) n[i] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float x = tv[(8 * (i >> 2) + 4 * hf + (i & 3)) * kPitch + 32 * db + l32];
+                        const bool is = kind == 0 ? x == INFINITY : kind == 1 ? x == -INFINITY : x != x;
+                        n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.f : 0.f, key_of(i) < top ? 1.f : 0.f, n, 0, 0, 0);
+                    }
+                    const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (n[i] > 0.f) O[db][i] += add;
+                }
+            }
+        }
+    }
+
+    if (r_wave + l32 >= rows) return;
+    l += __shfl_xor(l, 32, 64);
+    const int64_t rh = row * p.H + h;
+    if (p.n_split > 1) {
+        float *po = p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * p.d;
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (32 * db + 8 * g + 4 * hf < p.d)
+                    *(f32x4 *)(po + 32 * db + 8 * g + 4 * hf) = f32x4{O[db][4 * g], O[db][4 * g + 1], O[db][4 * g + 2], O[db][4 * g + 3]};
+        if (hf == 0) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{m * c, l};
+        return;
+    }
+    const float inv = 1.f / l;
+    E *op = (E *)(p.o + row * p.ld_o) + (int64_t)h * p.d;
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            if (32 * db + 8 * g + 4 * hf < p.d)
+                store4(op + 32 * db + 8 * g + 4 * hf, f32x4{O[db][4 * g] * inv, O[db][4 * g + 1] * inv, O[db][4 * g + 2] * inv, O[db][4 * g + 3] * inv});
+    if (hf == 0 && p.lse) p.lse[rh] = m * c + __builtin_amdgcn_logf(l);
+}
+
+// Partial results of the parts of the keys, joined: a wave per row and head.
+template <typename E>
+__global__ __launch_bounds__(256) void paged_combine_kernel(const PagedArgs p)
+{
+    const int64_t all = (int64_t)p.m_total * p.H, rh = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (rh >= all) return;
+    const int64_t row = rh / p.H;
+    if (row < max(p.off[0], 0) || row >= p.off[p.n_seqs]) return;  // a row of no sequence stays as it is
+    const int h = (int)(rh % p.H);
+    float M = -INFINITY;
+    for (int i = 0; i < p.n_split; ++i) {
+        const float2 ml = *(const float2 *)(p.part_ml + (i * all + rh) * 2);
+        if (ml.y != 0.f) M = fmaxf(M, ml.x);
+    }
+    float L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    const int c = lane * 4;
+    for (int i = 0; i < p.n_split; ++i) {
+        const float2 ml = *(const float2 *)(p.part_ml + (i * all + rh) * 2);
+        if (ml.y == 0.f) continue;  // (no key of the part is seen)
+        const float w = __builtin_amdgcn_exp2f(ml.x - M);
+        L += w * ml.y;
+        if (c < p.d) {
+            const f32x4 x = *(const f32x4 *)(p.part_o + (i * all + rh) * p.d + c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += w * x[e];
+        }
+    }
+    const float inv = 1.f / L;
+    if (c < p.d) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] *= inv;
+        store4((E *)(p.o + row * p.ld_o) + (int64_t)h * p.d + c, acc);
+    }
+    if (lane == 0 && p.lse) p.lse[rh] = M + __builtin_amdgcn_logf(L);
+}
+
+// Attention weights per cached token.  One workgroup: 32 keys of one (sequence, cache head), which stay in registers; its waves
+// take the packed rows in turn, p = exp2(s c - lse) again from the logits, and each lane adds up those of its keys.  The sums of a
+// cache head go to part[b][hk][slot], without atomics: a second kernel adds the heads up in their order.
+template <typename E, int DP>
+__global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, float *part)
+{
+    constexpr int kPitch = DP + 4;
+    __shared__ __attribute__((aligned(16))) float tk[kKeys * kPitch];
+    __shared__ float sums[4][kKeys];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = threadIdx.x >> 6;
+    const int tiles = (p.max_len + kKeys - 1) / kKeys, tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / p.Hkv, hk = bh % p.Hkv;
+    const PagedSeq s = paged_seq(p, b);
+    const int keys = p.sumi ? s.n : s.n + s.T, k0 = tile * kKeys, rows = s.T * p.G;
+    if (k0 >= keys || rows == 0) return;
+    load_tile<E, DP, 256>(tk, p.d, [&](int i) {
+        const int j = min(k0 + i, keys - 1);
+        if (j >= s.n) return p.k + (s.row0 + j - s.n) * p.ld_kv + (int64_t)hk * p.row_bytes;
+        return (const uint8_t *)p.k_pages + paged_row(p, paged_page(p, b, j), hk, j);
+    });
+    __syncthreads();
+    float sum[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+    const bool causal = !p.sumi && p.causal;
+    const int first = causal ? max(0, k0 - s.n) * p.G : 0;  // rows before it see none of these keys
+    for (int r0 = first / 32 * 32 + wave * 32; r0 < rows; r0 += 128) {
+        const int r = min(r0 + l32, rows - 1), t = r / p.G, h = hk * p.G + r % p.G;
+        const int64_t row = s.row0 + t;
+        const int lim = r0 + l32 >= rows ? 0 : causal ? s.n + t + 1 : keys;
+        const E *qp = (const E *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
+        f32x16 S;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < DP / 8; ++i) {
+            const f32x4 q = 8 * i + 4 * hf < p.d ? load4(qp + 8 * i + 4 * hf) : f32x4{0.f, 0.f, 0.f, 0.f};
+            const f32x4 x = *(const f32x4 *)(tk + l32 * kPitch + 8 * i + 4 * hf);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[e], S, 0, 0, 0);
+        }
+        const float c = paged_row_scale(p, row), lse = p.lse[row * p.H + h];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float w = __builtin_amdgcn_exp2f(fmaf(S[i], c, -lse));
+            if (k0 + 8 * (i >> 2) + 4 * hf + (i & 3) < lim) sum[i] += w;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        float x = sum[i];
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) x += __shfl_xor(x, o, 64);
+        if (l32 == 0) sums[wave][8 * (i >> 2) + 4 * hf + (i & 3)] = x;
+    }
+    __syncthreads();
+    if (threadIdx.x < kKeys && k0 + (int)threadIdx.x < keys)
+        part[(int64_t)bh * p.max_len + k0 + threadIdx.x] =
+            (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
+}
+
+__global__ __launch_bounds__(256) void paged_mass_add_kernel(const PagedArgs p, const float *part)
+{
+    const int per = (p.max_len + 255) / 256, b = blockIdx.x / per, j = (blockIdx.x % per) * 256 + threadIdx.x;
+    const PagedSeq s = paged_seq(p, b);
+    if (s.T == 0 || j >= (p.sumi ? s.n : s.n + s.T)) return;
+    const int raw = p.table[(int64_t)b * p.table_ld + (j >> p.page_shift)];
+    if (raw < 0 || raw >= p.n_pages) return;
+    float x = 0.f;
+    for (int h = 0; h < p.Hkv; ++h) x += part[((int64_t)b * p.Hkv + h) * p.max_len + j];
+    float *to = p.mass + ((int64_t)raw << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+    *to = j < s.n ? *to + x : x;  // a new token has none yet, whatever its slot holds
+}
+
+template <typename E, int DP>
+hipError_t launch(const PagedArgs &a, hipStream_t s)
+{
+    PagedArgs p = a;
+    const int64_t rows = (int64_t)a.m_max * a.G;
+    const size_t lds = 2 * kKeys * (DP + 4) * sizeof(float);
+    auto go = [&](auto nw, auto sumi) {
+        constexpr int NW = decltype(nw)::value;
+        constexpr bool SUMI = decltype(sumi)::value;
+        p.n_tiles = (int)((rows + NW * 32 - 1) / (NW * 32));
+        hipLaunchKernelGGL((attn_paged_f32_kernel<E, DP, NW, SUMI>), dim3(paged_grid(p)), dim3(NW * 64), lds, s, p);
+    };
+    if (rows <= 32) {
+        if (a.sumi) go(std::integral_constant<int, 1>{}, std::true_type{});
+        else go(std::integral_constant<int, 1>{}, std::false_type{});
+    } else {
+        if (a.sumi) go(std::integral_constant<int, 4>{}, std::true_type{});
+        else go(std::integral_constant<int, 4>{}, std::false_type{});
+    }
+    return hipGetLastError();
+}
+
+template <typename E, int DP>
+void launch_mass(const PagedArgs &p, float *part, hipStream_t s)
+{
+    const int64_t tiles = (p.max_len + kKeys - 1) / kKeys;
+    hipLaunchKernelGGL((paged_mass_kernel<E, DP>), dim3((unsigned)(tiles * p.n_seqs * p.Hkv)), dim3(256), 0, s, p, part);
+}
+
+}  // namespace
+
+hipError_t launch_attn_paged_f32(const PagedArgs &a, bool bf16, hipStream_t s)
+{
+    if (bf16) return a.d == 64 ? launch<__bf16, 64>(a, s) : launch<__bf16, 128>(a, s);
+    return a.d <= 32 ? launch<float, 32>(a, s) : a.d <= 64 ? launch<float, 64>(a, s) : launch<float, 128>(a, s);
+}
+
+hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s)
+{
+    const unsigned blocks = (unsigned)(((int64_t)a.m_total * a.H + 3) / 4);
+    if (bf16) hipLaunchKernelGGL(paged_combine_kernel<__bf16>, dim3(blocks), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(paged_combine_kernel<float>, dim3(blocks), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_mass_f32(const PagedArgs &a, bool bf16, float *part, hipStream_t s)
+{
+    if (bf16) {
+        if (a.d == 64) launch_mass<__bf16, 64>(a, part, s);
+        else launch_mass<__bf16, 128>(a, part, s);
+    } else {
+        if (a.d <= 32) launch_mass<float, 32>(a, part, s);
+        else if (a.d <= 64) launch_mass<float, 64>(a, part, s);
+        else launch_mass<float, 128>(a, part, s);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_mass_add_kernel, dim3((unsigned)((a.max_len + 255) / 256 * a.n_seqs)), dim3(256), 0, s, a, part);
+    return hipGetLastError();
+}
+
+}  // namespace climber

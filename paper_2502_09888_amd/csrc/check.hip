@@ -62,7 +62,39 @@ __global__ __launch_bounds__(256) void check_inputs_kernel(const CheckParams p)
     if (bad) atomicOr(p.status, bad);
 }
 
+// A workgroup per sequence: its offsets, its length, and the pages that hold its tokens (and, if it appends, its new ones).
+__global__ __launch_bounds__(256) void check_paged_kernel(const int32_t *table, const int32_t *len, const int32_t *off, int n_seqs, int n_pages,
+                                                          int page_shift, int table_ld, int max_len, int m_total, int m_max, int appends,
+                                                          int32_t *status)
+{
+    const int b = blockIdx.x;
+    int bad = 0;
+    int64_t rows = 0;
+    if (off) {
+        const int lo = off[b], hi = off[b + 1];
+        if (hi < lo || lo < 0 || (b == 0 && lo != 0) || hi > m_total || (b == n_seqs - 1 && hi != m_total)) bad |= CLIMBER_BAD_OFFSETS;
+        rows = (int64_t)hi - lo;
+        if (rows > m_max) bad |= CLIMBER_BAD_M_MAX;
+    }
+    const int64_t n = len[b], need = n + (appends && rows > 0 ? rows : 0);
+    if (n < 0 || need > max_len) bad |= CLIMBER_BAD_LEN;
+    const int64_t pages = min(((need + (1 << page_shift) - 1) >> page_shift), (int64_t)table_ld);
+    for (int64_t i = threadIdx.x; i < pages; i += 256) {
+        const int id = table[(int64_t)b * table_ld + i];
+        if (id < 0 || id >= n_pages) bad |= CLIMBER_BAD_PAGE;
+    }
+    if (bad) atomicOr(status, bad);
+}
+
 }  // namespace
+
+hipError_t launch_check_paged(const int32_t *table, const int32_t *len, const int32_t *off, int n_seqs, int n_pages, int page_shift,
+                              int table_ld, int max_len, int m_total, int m_max, int appends, int32_t *status, hipStream_t s)
+{
+    hipLaunchKernelGGL(check_paged_kernel, dim3((unsigned)n_seqs), dim3(256), 0, s, table, len, off, n_seqs, n_pages, page_shift, table_ld, max_len,
+                       m_total, m_max, appends, status);
+    return hipGetLastError();
+}
 
 hipError_t launch_check_inputs(const float *tau, const int32_t *scen, const int32_t *beh, int64_t n_rows,
                                const int32_t *hist_len, const int32_t *tok_off, const int32_t *cand_off,

@@ -35,13 +35,8 @@ bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 int check_config(const climber_config *c)
 {
-    if (!c) return CLIMBER_ERR_NULL;
-    if (c->n_layers < 1 || c->n_heads < 1 || c->d_head < 1 || c->n_scen < 1 || c->n_beh < 1 ||
-        c->sub_len < 0 || c->d_model != c->n_heads * c->d_head)
-        return CLIMBER_ERR_SHAPE;
-    if (c->dtype != CLIMBER_F32 && c->dtype != CLIMBER_BF16) return CLIMBER_ERR_SHAPE;
-    if (!(c->qk_scale > 0.f) || !std::isfinite(c->qk_scale)) return CLIMBER_ERR_TAU;
-    if (c->flags & ~(CLIMBER_HIST_CAUSAL | CLIMBER_HIST_TWO_KERNEL | CLIMBER_QKV_VIA_ROWS)) return CLIMBER_ERR_SHAPE;
+    const int e = check_config_values(c);
+    if (e) return e;
     if (c->dtype == CLIMBER_BF16) {
         if (c->d_head != kDHead) return CLIMBER_ERR_UNSUPPORTED;
         if (c->sub_len % 128 != 0) return CLIMBER_ERR_ALIGN;
@@ -127,8 +122,20 @@ int check_cache_use(const climber_config *cfg, const climber_kv_cache *cache, in
 
 }  // namespace
 
-// ---- internal entry points used by the stack driver (stack.hip) ---------------------------------
+// ---- internal entry points used by the stack driver (stack.hip) and the paged cache (paged_api.hip) ----
 namespace climber {
+
+int check_config_values(const climber_config *c)
+{
+    if (!c) return CLIMBER_ERR_NULL;
+    if (c->n_layers < 1 || c->n_heads < 1 || c->d_head < 1 || c->n_scen < 1 || c->n_beh < 1 ||
+        c->sub_len < 0 || c->d_model != c->n_heads * c->d_head)
+        return CLIMBER_ERR_SHAPE;
+    if (c->dtype != CLIMBER_F32 && c->dtype != CLIMBER_BF16) return CLIMBER_ERR_SHAPE;
+    if (!(c->qk_scale > 0.f) || !std::isfinite(c->qk_scale)) return CLIMBER_ERR_TAU;
+    if (c->flags & ~(CLIMBER_HIST_CAUSAL | CLIMBER_HIST_TWO_KERNEL | CLIMBER_QKV_VIA_ROWS)) return CLIMBER_ERR_SHAPE;
+    return CLIMBER_OK;
+}
 
 int attn_history_strided(const climber_config *cfg, const float *tau_layer, const void *q,
                          const void *k, const void *v, int64_t ld, const int32_t *scen,

@@ -6,7 +6,12 @@
 
 #include "bias.h"
 
+struct climber_config;
+
 namespace climber {
+
+// what every call asks of a configuration, whichever precision path or cache it is for (climber_api.hip)
+int check_config_values(const climber_config *c);
 
 // ---- bf16 KV-cache geometry (d_head = 64) ---------------------------------------------------
 // A (user, head) owns L_pad/32 consecutive 8 KiB blocks.  Block kb holds keys 32kb .. 32kb+31:
@@ -99,5 +104,8 @@ hipError_t launch_kv_write_f32(const CacheView &c, const void *k, const void *v,
 hipError_t launch_check_inputs(const float *tau, const int32_t *scen, const int32_t *beh, int64_t n_rows,
                                const int32_t *hist_len, const int32_t *tok_off, const int32_t *cand_off,
                                int B, int n_scen, int n_beh, int m_max, int32_t *status, hipStream_t s);
+// the same for page tables, lengths and offsets of a paged cache; off may be nullptr
+hipError_t launch_check_paged(const int32_t *table, const int32_t *len, const int32_t *off, int n_seqs, int n_pages, int page_shift,
+                              int table_ld, int max_len, int m_total, int m_max, int appends, int32_t *status, hipStream_t s);
 
 }  // namespace climber

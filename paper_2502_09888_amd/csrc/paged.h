@@ -1,0 +1,127 @@
+// The paged history cache: what its kernels are given, and the geometry that they share (internal).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+namespace climber {
+
+// One call on a paged cache.  Rows of the call: new behaviours (history) or candidates (SUMI) of n_seqs sequences, packed by `off`.
+// The G = H / Hkv query heads that share a cache head are rows of one problem: "packed row" r of (sequence, cache head) is row r / G,
+// query head r % G of the group, so that a tile of packed rows reads keys and values once for all of them.
+struct PagedArgs {
+    uint8_t *k_pages, *v_pages;  // [n_pages][Hkv][page][d]
+    float *mass;                 // [n_pages][page] or nullptr
+    int32_t *stamp;              // [n_pages][page] or nullptr
+    const int32_t *table, *len;  // [n_seqs][table_ld], [n_seqs]
+    const uint8_t *q, *k, *v;    // the call's rows
+    int64_t ld_q, ld_kv, ld_o;   // bytes
+    const int32_t *off, *scen, *beh, *stamp_new;
+    const float *tau;
+    uint8_t *o;
+    int n_seqs, n_pages, page_shift, table_ld, max_len;
+    int H, Hkv, G, d, row_bytes;  // row_bytes: of one key of one head
+    int n_scen, n_beh, m_total, m_max;
+    int causal, sumi;
+    float scale_log2e;
+    // work split: tiles of packed rows, parts of the keys
+    int n_tiles, n_split, bh_major;
+    float *part_o, *part_ml;  // [n_split][m_total H][d], [n_split][m_total H][2] (n_split > 1)
+    float *lse;               // [m_total H], log2 units, or nullptr: not wanted
+};
+
+struct PagedSeq {
+    int n, T;      // cached tokens, rows of the call
+    int64_t row0;  // first row
+};
+
+// Lengths and offsets live in device memory: whatever they hold, nothing is read or written outside the arrays.
+static __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs &p, int b)
+{
+    PagedSeq s;
+    const int r0 = min(max(p.off[b], 0), p.m_total);
+    s.T = min(min(max(p.off[b + 1] - r0, 0), p.m_total - r0), p.m_max);
+    if (!p.sumi) s.T = min(s.T, p.max_len);
+    s.n = min(max(p.len[b], 0), p.sumi ? p.max_len : p.max_len - s.T);
+    s.row0 = r0;
+    return s;
+}
+
+static __device__ __forceinline__ int paged_page(const PagedArgs &p, int b, int slot)
+{
+    return min(max(p.table[(int64_t)b * p.table_ld + (slot >> p.page_shift)], 0), p.n_pages - 1);
+}
+
+// byte offset of a slot's row of head h in the key or value pages
+static __device__ __forceinline__ int64_t paged_row(const PagedArgs &p, int page, int h, int slot)
+{
+    return ((((int64_t)page * p.Hkv + h) << p.page_shift) + (slot & ((1 << p.page_shift) - 1))) * p.row_bytes;
+}
+
+// Workgroup -> (sequence, cache head), tile, part of the keys.  Tiles of one head read the same keys: they follow each other on one XCD
+// (workgroups are dealt to the eight in turn), where there are heads enough to have each XCD work; the last tiles, which see the
+// most keys under the causal mask, first.
+struct PagedWork {
+    int b, hk, tile, split;
+};
+static __device__ __forceinline__ bool paged_work(const PagedArgs &p, PagedWork &w)
+{
+    const int per = p.n_tiles * p.n_split, n_bh = p.n_seqs * p.Hkv;
+    int bh, in;
+    if (p.bh_major) {
+        const int j = blockIdx.x >> 3;
+        bh = (j / per) * 8 + (blockIdx.x & 7);
+        in = j % per;
+    } else {
+        bh = blockIdx.x / per;
+        in = blockIdx.x % per;
+    }
+    if (bh >= n_bh) return false;
+    w.b = bh / p.Hkv;
+    w.hk = bh % p.Hkv;
+    w.tile = p.n_tiles - 1 - in / p.n_split;
+    w.split = in % p.n_split;
+    return true;
+}
+static inline unsigned paged_grid(PagedArgs &p)
+{
+    const int64_t bh = (int64_t)p.n_seqs * p.Hkv;
+    p.bh_major = bh % 8 == 0 || bh >= 64;
+    return (unsigned)((p.bh_major ? (bh + 7) / 8 * 8 : bh) * p.n_tiles * p.n_split);
+}
+
+// the keys [lo, hi) of part `split` of the first k_end keys, in whole tiles of `unit`
+static __device__ __forceinline__ void paged_part(const PagedArgs &p, int split, int k_end, int unit, int &lo, int &hi)
+{
+    const int tiles = (k_end + unit - 1) / unit, per = (tiles + p.n_split - 1) / p.n_split;
+    lo = min(split * per * unit, k_end);
+    hi = min(lo + per * unit, k_end);
+}
+
+// log2(e) qk_scale / temperature of a row
+static __device__ __forceinline__ float paged_row_scale(const PagedArgs &p, int64_t row)
+{
+    const int sc = min(max(p.scen[row], 0), p.n_scen - 1), bh = min(max(p.beh[row], 0), p.n_beh - 1);
+    return p.scale_log2e / p.tau[sc * p.n_beh + bh];
+}
+
+hipError_t launch_attn_paged_f32(const PagedArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s);
+hipError_t launch_paged_mass_f32(const PagedArgs &a, bool bf16, float *part, hipStream_t s);
+
+struct EvictArgs {
+    uint8_t *k_pages, *v_pages;
+    float *mass;
+    const float *rank;
+    int32_t *stamp;
+    const int32_t *table, *len, *budget, *keep_from;
+    int32_t *len_out, *src;
+    int n_seqs, n_pages, page_shift, table_ld, max_len, Hkv, row_bytes;
+    uint32_t *keys;          // workspace [n_seqs][max_len]
+    uint64_t *first;         // workspace [n_seqs][ceil(max_len / 64)]: bit set: ranks before all others
+    int32_t *holes, *movers; // workspace [n_seqs][max_len / 2 + 1]
+    int32_t *n_moves;        // workspace [n_seqs]
+};
+hipError_t launch_paged_evict(const EvictArgs &a, hipStream_t s);
+
+}  // namespace climber

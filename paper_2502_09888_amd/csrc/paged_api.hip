@@ -1,0 +1,274 @@
+// Host side of the paged history cache: argument validation, workspace layout and dispatch of its entry points (include/climber.h)
+// onto the kernels.  Everything is validated before the first launch; nothing here allocates device memory.
+#include "../../include/climber.h"
+
+#include <algorithm>
+
+#include "internal.h"
+#include "paged.h"
+
+using namespace climber;
+
+namespace {
+
+size_t up(size_t x) { return (x + 255) / 256 * 256; }
+bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+int rt(hipError_t e) { return e == hipSuccess ? CLIMBER_OK : CLIMBER_ERR_RUNTIME; }
+size_t elem_of(const climber_config *cfg) { return cfg->dtype == CLIMBER_BF16 ? 2 : 4; }
+
+// sizes of a cache and its configuration, without its pointers
+int check_sizes(const climber_config *cfg, const climber_paged_kv *kv)
+{
+    int e = check_config_values(cfg);
+    if (e) return e;
+    if (!kv) return CLIMBER_ERR_NULL;
+    if (cfg->dtype == CLIMBER_BF16 ? cfg->d_head != 64 && cfg->d_head != 128 : cfg->d_head % 4 != 0 || cfg->d_head > 128)
+        return CLIMBER_ERR_UNSUPPORTED;
+    if (kv->n_pages < 1 || kv->n_seqs < 1 || kv->table_ld < 1 || kv->n_kv_heads < 1 || cfg->n_heads % kv->n_kv_heads != 0 || kv->page_size < 1)
+        return CLIMBER_ERR_SHAPE;
+    if (kv->page_size < 16 || kv->page_size > 4096 || (kv->page_size & (kv->page_size - 1)) != 0) return CLIMBER_ERR_ALIGN;
+    if (kv->max_len < 0 || kv->max_len > (int64_t)kv->table_ld * kv->page_size) return CLIMBER_ERR_RANGE;
+    // slots of a table row, rows of a launch and tokens of the pool are counted in 32 bits
+    if ((int64_t)kv->table_ld * kv->page_size >= (int64_t)1 << 30 || (int64_t)kv->n_pages * kv->page_size >= (int64_t)1 << 31) return CLIMBER_ERR_RANGE;
+    if ((int64_t)kv->n_seqs * kv->n_kv_heads * std::max<int64_t>(1, kv->max_len / 32) >= (int64_t)1 << 31) return CLIMBER_ERR_RANGE;
+    return CLIMBER_OK;
+}
+
+int check_rows(const climber_config *cfg, int32_t m_total, int32_t m_max)
+{
+    if (m_total < 0 || m_max < 0 || m_max > m_total || (m_total > 0 && m_max == 0)) return CLIMBER_ERR_SHAPE;
+    if ((int64_t)m_total * cfg->d_model >= (int64_t)1 << 31) return CLIMBER_ERR_RANGE;
+    return CLIMBER_OK;
+}
+
+int check_pointers(const climber_paged_kv *kv)
+{
+    if (!kv->k || !kv->v || !kv->page_table || !kv->len) return CLIMBER_ERR_NULL;
+    if (!aligned(kv->k, 16) || !aligned(kv->v, 16) || !aligned(kv->page_table, 4) || !aligned(kv->len, 4) || !aligned(kv->mass, 4) || !aligned(kv->stamp, 4))
+        return CLIMBER_ERR_ALIGN;
+    return CLIMBER_OK;
+}
+
+constexpr int64_t kPartRows = 1 << 16;  // rows x heads x parts that a call's partial results have room for at most
+constexpr int64_t kPartKeys = 256;      // and the fewest keys of a part
+
+int64_t most_parts(const climber_paged_kv *kv) { return std::max<int64_t>(1, kv->max_len / kPartKeys); }
+
+// Parts of the keys, so that a launch has two workgroups per CU.
+int parts(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total, int32_t m_max)
+{
+    const int64_t rows = (int64_t)m_max * (cfg->n_heads / kv->n_kv_heads);
+    const int64_t groups = std::max<int64_t>(1, (rows <= 32 ? 1 : (rows + 127) / 128) * kv->n_seqs * kv->n_kv_heads);
+    const int64_t room = kPartRows / std::max<int64_t>(1, (int64_t)m_total * cfg->n_heads);
+    return (int)std::max<int64_t>(1, std::min(std::min(512 / groups, room), most_parts(kv)));
+}
+
+struct Layout {  // of the workspace
+    size_t part_o, part_ml, lse, mass, bytes;
+};
+// for partial results of `part_rows` rows x heads x parts
+Layout layout_of(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total, size_t part_rows)
+{
+    Layout w{};
+    w.part_o = 0;
+    w.part_ml = w.part_o + up(part_rows * cfg->d_head * 4);
+    w.lse = w.part_ml + up(part_rows * 8);
+    w.mass = w.lse + (kv->mass ? up((size_t)m_total * cfg->n_heads * 4) : 0);
+    w.bytes = w.mass + (kv->mass ? up((size_t)kv->n_seqs * kv->n_kv_heads * kv->max_len * 4) : 0);
+    return w;
+}
+
+struct EvictLayout {
+    size_t keys, first, holes, movers, n_moves, bytes;
+};
+EvictLayout evict_layout(const climber_paged_kv *kv)
+{
+    EvictLayout w{};
+    const size_t B = kv->n_seqs, L = kv->max_len;
+    w.keys = 0;
+    w.first = w.keys + up(B * L * 4);
+    w.holes = w.first + up(B * ((L + 63) / 64) * 8);
+    w.movers = w.holes + up(B * (L / 2 + 1) * 4);
+    w.n_moves = w.movers + up(B * (L / 2 + 1) * 4);
+    w.bytes = w.n_moves + up(B * 4);
+    return w;
+}
+
+int page_shift(int page) { return __builtin_ctz((unsigned)page); }
+
+// Two arrays of rows share an element: not if they lie apart, or are columns of the same rows that lie apart.
+bool overlap(const void *a, int64_t ld_a, size_t wide_a, const void *b, int64_t ld_b, size_t wide_b, int64_t rows)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    const uintptr_t x1 = x + (rows - 1) * ld_a + wide_a, y1 = y + (rows - 1) * ld_b + wide_b;
+    if (x1 <= y || y1 <= x) return false;
+    if (ld_a != ld_b) return true;
+    const uintptr_t d = x < y ? y - x : x - y, in = d % (uintptr_t)ld_a;  // the later one's columns behind the earlier one's
+    const size_t first = x < y ? wide_a : wide_b, second = x < y ? wide_b : wide_a;
+    return !(in >= first && in + second <= (uintptr_t)ld_a);
+}
+
+int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_kv *kv, const void *q, int64_t ld_q, const void *k, const void *v,
+               int64_t ld_kv, const int32_t *off, int32_t m_total, int32_t m_max, const int32_t *scen, const int32_t *beh, const int32_t *stamp,
+               void *o, int64_t ld_o, void *workspace, size_t ws_bytes, bool sumi, void *stream)
+{
+    int e = check_sizes(cfg, kv);
+    if (e) return e;
+    e = check_rows(cfg, m_total, m_max);
+    if (e) return e;
+    if (!sumi && cfg->sub_len != 0) return CLIMBER_ERR_UNSUPPORTED;
+    const int64_t elem = (int64_t)elem_of(cfg), wide = cfg->d_model, kv_wide = (int64_t)kv->n_kv_heads * cfg->d_head;
+    if (ld_q < wide || ld_o < wide || ld_kv < kv_wide) return CLIMBER_ERR_SHAPE;
+    const int64_t most = (int64_t)1 << 40;
+    if (ld_q > most || ld_kv > most || ld_o > most) return CLIMBER_ERR_RANGE;
+    if (!tau || !off) return CLIMBER_ERR_NULL;
+    e = check_pointers(kv);
+    if (e) return e;
+    if (m_total == 0) return CLIMBER_OK;  // no rows: their arrays are empty, their pointers free
+    if (!q || !k || !v || !scen || !beh || !o || (!sumi && kv->stamp && !stamp)) return CLIMBER_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || ld_q * elem % 16 || ld_kv * elem % 16 || ld_o * elem % 16)
+        return CLIMBER_ERR_ALIGN;
+    if (!sumi && kv->max_len == 0) return CLIMBER_ERR_RANGE;
+    // outputs are written while other workgroups still read rows
+    if (overlap(o, ld_o * elem, wide * elem, k, ld_kv * elem, kv_wide * elem, m_total) || overlap(o, ld_o * elem, wide * elem, v, ld_kv * elem, kv_wide * elem, m_total) ||
+        overlap(o, ld_o * elem, wide * elem, q, ld_q * elem, wide * elem, m_total))
+        return CLIMBER_ERR_UNSUPPORTED;
+    const int n_split = parts(cfg, kv, m_total, m_max);
+    const Layout w = layout_of(cfg, kv, m_total, n_split > 1 ? (size_t)n_split * m_total * cfg->n_heads : 0);
+    if (w.bytes > 0 && !workspace) return CLIMBER_ERR_NULL;
+    if (!aligned(workspace, 256)) return CLIMBER_ERR_ALIGN;
+    if (ws_bytes < w.bytes) return CLIMBER_ERR_BUFSIZE;
+
+    uint8_t *ws = (uint8_t *)workspace;
+    const bool bf16 = cfg->dtype == CLIMBER_BF16;
+    PagedArgs a{};
+    a.k_pages = (uint8_t *)kv->k;
+    a.v_pages = (uint8_t *)kv->v;
+    a.mass = kv->mass;
+    a.stamp = kv->stamp;
+    a.table = kv->page_table;
+    a.len = kv->len;
+    a.q = (const uint8_t *)q;
+    a.k = (const uint8_t *)k;
+    a.v = (const uint8_t *)v;
+    a.ld_q = ld_q * elem;
+    a.ld_kv = ld_kv * elem;
+    a.ld_o = ld_o * elem;
+    a.off = off;
+    a.scen = scen;
+    a.beh = beh;
+    a.stamp_new = stamp;
+    a.tau = tau;
+    a.o = (uint8_t *)o;
+    a.n_seqs = kv->n_seqs;
+    a.n_pages = kv->n_pages;
+    a.page_shift = page_shift(kv->page_size);
+    a.table_ld = kv->table_ld;
+    a.max_len = kv->max_len;
+    a.H = cfg->n_heads;
+    a.Hkv = kv->n_kv_heads;
+    a.G = cfg->n_heads / kv->n_kv_heads;
+    a.d = cfg->d_head;
+    a.row_bytes = (int)(cfg->d_head * elem);
+    a.n_scen = cfg->n_scen;
+    a.n_beh = cfg->n_beh;
+    a.m_total = m_total;
+    a.m_max = m_max;
+    a.causal = (cfg->flags & CLIMBER_HIST_CAUSAL) ? 1 : 0;
+    a.sumi = sumi;
+    a.scale_log2e = cfg->qk_scale * 1.4426950408889634f;
+    a.n_split = n_split;
+    a.part_o = (float *)(ws + w.part_o);
+    a.part_ml = (float *)(ws + w.part_ml);
+    a.lse = kv->mass ? (float *)(ws + w.lse) : nullptr;
+    const hipStream_t s = (hipStream_t)stream;
+    e = rt(launch_attn_paged_f32(a, bf16, s));
+    if (e) return e;
+    if (a.n_split > 1) e = rt(launch_paged_combine(a, bf16, s));
+    if (e || !kv->mass || kv->max_len == 0) return e;
+    return rt(launch_paged_mass_f32(a, bf16, (float *)(ws + w.mass), s));
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t climber_paged_workspace_bytes(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total, int32_t m_max)
+{
+    if (check_sizes(cfg, kv) != CLIMBER_OK || check_rows(cfg, m_total, m_max) != CLIMBER_OK) return 0;
+    // (a smaller call may have more parts: room for as many as one can have)
+    const int64_t n = most_parts(kv) * m_total * cfg->n_heads;
+    return std::max(layout_of(cfg, kv, m_total, most_parts(kv) > 1 ? (size_t)std::min(n, kPartRows) : 0).bytes, evict_layout(kv).bytes);
+}
+
+int climber_attn_history_paged(const climber_config *cfg, const float *tau_layer, const climber_paged_kv *kv, const void *q, int64_t ld_q,
+                               const void *k, const void *v, int64_t ld_kv, const int32_t *off, int32_t m_total, int32_t m_max,
+                               const int32_t *scen, const int32_t *beh, const int32_t *stamp, void *o, int64_t ld_o, void *workspace,
+                               size_t ws_bytes, void *stream)
+{
+    return attn_paged(cfg, tau_layer, kv, q, ld_q, k, v, ld_kv, off, m_total, m_max, scen, beh, stamp, o, ld_o, workspace, ws_bytes, false, stream);
+}
+
+int climber_attn_sumi_paged(const climber_config *cfg, const float *tau_layer, const climber_paged_kv *kv, const void *q_c, int64_t ld_q,
+                            const void *k_c, const void *v_c, int64_t ld_kv, const int32_t *cand_off, int32_t m_total, int32_t m_max,
+                            const int32_t *cand_scen, const int32_t *cand_beh, void *o_c, int64_t ld_o, void *workspace, size_t ws_bytes,
+                            void *stream)
+{
+    return attn_paged(cfg, tau_layer, kv, q_c, ld_q, k_c, v_c, ld_kv, cand_off, m_total, m_max, cand_scen, cand_beh, nullptr, o_c, ld_o, workspace,
+                      ws_bytes, true, stream);
+}
+
+int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, const float *rank, const int32_t *budget, const int32_t *keep_from,
+                        int32_t *len_out, int32_t *src, void *workspace, size_t ws_bytes, void *stream)
+{
+    int e = check_sizes(cfg, kv);
+    if (e) return e;
+    e = check_pointers(kv);
+    if (e) return e;
+    if (!budget || !len_out || (!rank && !kv->mass) || (keep_from && !kv->stamp)) return CLIMBER_ERR_NULL;
+    if (!aligned(rank, 4) || !aligned(budget, 4) || !aligned(keep_from, 4) || !aligned(len_out, 4) || !aligned(src, 4)) return CLIMBER_ERR_ALIGN;
+    const EvictLayout w = evict_layout(kv);
+    if (!workspace) return CLIMBER_ERR_NULL;
+    if (!aligned(workspace, 256)) return CLIMBER_ERR_ALIGN;
+    if (ws_bytes < w.bytes) return CLIMBER_ERR_BUFSIZE;
+    uint8_t *ws = (uint8_t *)workspace;
+    EvictArgs a{};
+    a.k_pages = (uint8_t *)kv->k;
+    a.v_pages = (uint8_t *)kv->v;
+    a.mass = kv->mass;
+    a.rank = rank ? rank : kv->mass;
+    a.stamp = kv->stamp;
+    a.table = kv->page_table;
+    a.len = kv->len;
+    a.budget = budget;
+    a.keep_from = keep_from;
+    a.len_out = len_out;
+    a.src = src;
+    a.n_seqs = kv->n_seqs;
+    a.n_pages = kv->n_pages;
+    a.page_shift = page_shift(kv->page_size);
+    a.table_ld = kv->table_ld;
+    a.max_len = kv->max_len;
+    a.Hkv = kv->n_kv_heads;
+    a.row_bytes = (int)(cfg->d_head * elem_of(cfg));
+    a.keys = (uint32_t *)(ws + w.keys);
+    a.first = (uint64_t *)(ws + w.first);
+    a.holes = (int32_t *)(ws + w.holes);
+    a.movers = (int32_t *)(ws + w.movers);
+    a.n_moves = (int32_t *)(ws + w.n_moves);
+    return rt(launch_paged_evict(a, (hipStream_t)stream));
+}
+
+int climber_check_paged(const climber_config *cfg, const climber_paged_kv *kv, const int32_t *off, int32_t m_total, int32_t m_max, int32_t appends,
+                        int32_t *status, void *stream)
+{
+    int e = check_sizes(cfg, kv);
+    if (e) return e;
+    e = check_rows(cfg, m_total, m_max);
+    if (e) return e;
+    if (!kv->page_table || !kv->len || !status || (appends && !off)) return CLIMBER_ERR_NULL;
+    return rt(launch_check_paged(kv->page_table, kv->len, off, kv->n_seqs, kv->n_pages, page_shift(kv->page_size), kv->table_ld, kv->max_len, m_total,
+                                 m_max, appends, status, (hipStream_t)stream));
+}
+
+}  // extern "C"
