@@ -1,0 +1,653 @@
+// bf16 MFMA attention over the paged history cache (gfx950): a chunk of new behaviours, or candidates, of every sequence against its
+// cached tokens and its own rows (Eq. (3) of Climber, arXiv 2502.09888; the mask of Sec. 3.2 for candidates).
+//
+// The transposed problem, S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x16_bf16: a lane owns one packed row (row of the call,
+// query head of the group that shares a cache head), softmax statistics are scalars of the lane, and probabilities leave the
+// accumulator as the operand of the value product.  One pass over the keys with a running maximum that moves when a logit exceeds it
+// by 2^8; logits scaled in fp32; probabilities rounded to bf16 for the value product and summed before that in fp32 (the sum also
+// gives the weights per token their denominator, which rounded terms would put off by 3e-5).
+//
+// Keys and values are rows, in pages or of the call: they travel by global_load_lds, 16 keys of 16 at least contiguous ones an
+// instruction group, into LDS rows whose 16-byte pieces are permuted (Rows below) so that both the key fragments (row pieces) and the
+// value fragments (LDS transpose reads) touch every bank once.
+//
+// Two kernels.  Tiles: 4 waves of 32 rows share the keys of a ring of two stages of 64.  Few rows (at most 32 packed rows per
+// sequence and cache head, so that nothing is shared): the waves of a workgroup take different keys, each through a ring of its own and
+// without a barrier, and their results are joined at the end; bound by reading the cache once.
+#include "paged.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace climber {
+namespace {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef const __attribute__((address_space(1))) uint8_t glb_u8;
+typedef const __attribute__((address_space(4))) int32_t const_i32;  // read by scalar loads
+
+constexpr float kNoRef = -1.0e30f;  // "no reference yet", below any finite logit
+constexpr float kSlack = 8.0f;      // log2 units that a logit may exceed the reference by
+
+static __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+static __device__ __forceinline__ float half_max(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Rows of D bf16 in LDS: 16-byte piece c of row r at slot c ^ f(r).  f takes 16 consecutive rows (key fragments: 16 lanes read one
+// piece each) to 16 places of the 64 banks, and 4 consecutive ones (value fragments: 4 pieces of each) to 4 different quarters.
+template <int D>
+struct Rows {
+    static constexpr int kPitch = 2 * D, kPieces = D / 8, kPerLoad = 64 / kPieces, kLoads = 16 / kPerLoad;  // (of 16 rows)
+    static __device__ __forceinline__ int f(int r)
+    {
+        return D == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    }
+    uint32_t k_at[D / 16], v_at[2][D / 32];
+    __device__ __forceinline__ void init(int lane)
+    {
+        const int l32 = lane & 31, hf = lane >> 5, G = lane >> 4, i16 = lane & 15;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) k_at[s] = l32 * kPitch + ((2 * s + hf) ^ f(l32)) * 16;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) {
+                const int r = 8 * hh + 4 * (G >> 1) + (i16 >> 2), c = 4 * db + 2 * (G & 1) + ((i16 >> 1) & 1);
+                v_at[hh][db] = r * kPitch + (c ^ f(r)) * 16 + 8 * (i16 & 1);
+            }
+    }
+};
+
+// Fragments of 32 key rows, and of the 16 value rows from `base` on (A operands of the D / 32 blocks of dimensions).
+template <int D>
+struct KFrags { bf16x8 a[D / 16]; };
+template <int D>
+static __device__ __forceinline__ KFrags<D> read_k(const Rows<D> &w, const lds_u8 *base)
+{
+    KFrags<D> f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) f.a[s] = *(const __attribute__((address_space(3))) bf16x8 *)(base + w.k_at[s]);
+    return f;
+}
+template <int D>
+struct VFrags { u32x4 a[D / 32]; };
+template <int D>
+static __device__ __forceinline__ VFrags<D> read_v(const Rows<D> &w, lds_u8 *base)
+{
+    VFrags<D> f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(base + w.v_at[0][db])));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(base + w.v_at[1][db])));
+        f.a[db] = u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+    return f;
+}
+
+static __device__ __forceinline__ bf16x8 frag(u32x4 x) { return __builtin_bit_cast(bf16x8, x); }
+
+// 16 bytes a lane from anywhere to LDS, 1 KiB in a row
+static __device__ __forceinline__ void copy16(glb_u8 *from, lds_u8 *to) { __builtin_amdgcn_global_load_lds(from, to, 16, 0, 0); }
+
+// What a workgroup knows of its sequence, and the copies of 16 keys and values into LDS.
+template <int D>
+struct Source {
+    const PagedArgs &p;
+    PagedSeq s;
+    int b, hk, k_hi, lane;
+    uint32_t page_off[Rows<D>::kLoads], row_off[Rows<D>::kLoads];  // of this lane's piece, per load: rows of a page, rows of the call
+    const uint8_t *k_new, *v_new;                                  // row 0 of the call's rows of this sequence and head
+
+    __device__ __forceinline__ Source(const PagedArgs &p_, const PagedSeq &s_, int b_, int hk_, int k_hi_, int lane_)
+        : p(p_), s(s_), b(b_), hk(hk_), k_hi(k_hi_), lane(lane_)
+    {
+        using R = Rows<D>;
+#pragma unroll
+        for (int i = 0; i < R::kLoads; ++i) {
+            const int r = i * R::kPerLoad + lane / R::kPieces, c = (lane % R::kPieces) ^ R::f(r);
+            page_off[i] = r * R::kPitch + c * 16;
+            row_off[i] = (uint32_t)r * (uint32_t)p.ld_kv + c * 16;
+        }
+        const int64_t at = s.row0 * p.ld_kv + (int64_t)hk * R::kPitch;
+        k_new = p.k + at;
+        v_new = p.v + at;
+    }
+    // the page of keys g .. g + 15 (a multiple of 16: they lie in one page), or of the last key, which stands for those behind it
+    __device__ __forceinline__ int page_of(int g) const
+    {
+        const int slot = max(0, min(min(g, k_hi - 1), s.n - 1));
+        const const_i32 *t = (const const_i32 *)(p.table + (int64_t)b * p.table_ld);
+        return min(max(t[__builtin_amdgcn_readfirstlane(slot >> p.page_shift)], 0), p.n_pages - 1);
+    }
+    // keys g .. g + 15 to LDS rows at to_k, to_v (wave-uniform)
+    __device__ __forceinline__ void issue(int g, int page, lds_u8 *to_k, lds_u8 *to_v) const
+    {
+        using R = Rows<D>;
+        if (g + 16 <= min(s.n, k_hi)) {
+            const int64_t at = paged_row(p, page, hk, g);
+#pragma unroll
+            for (int i = 0; i < R::kLoads; ++i) {
+                copy16((glb_u8 *)(p.k_pages + at) + page_off[i], to_k + i * 1024);
+                copy16((glb_u8 *)(p.v_pages + at) + page_off[i], to_v + i * 1024);
+            }
+        } else if (g >= s.n && g + 16 <= k_hi) {
+            const int64_t at = (g - s.n) * p.ld_kv;
+#pragma unroll
+            for (int i = 0; i < R::kLoads; ++i) {
+                copy16((glb_u8 *)(k_new + at) + row_off[i], to_k + i * 1024);
+                copy16((glb_u8 *)(v_new + at) + row_off[i], to_v + i * 1024);
+            }
+        } else {  // cached and new ones, or fewer than 16: the last key again in the places behind it
+#pragma unroll
+            for (int i = 0; i < R::kLoads; ++i) {
+                const int r = i * R::kPerLoad + lane / R::kPieces, j = min(g + r, k_hi - 1), c = ((lane % R::kPieces) ^ R::f(r)) * 16;
+                const int64_t cached = paged_row(p, page, hk, j) + c, fresh = (int64_t)(j - s.n) * p.ld_kv + c;
+                const bool old = j < s.n;
+                copy16((glb_u8 *)(old ? p.k_pages + cached : k_new + fresh), to_k + i * 1024);
+                copy16((glb_u8 *)(old ? p.v_pages + cached : v_new + fresh), to_v + i * 1024);
+            }
+        }
+    }
+};
+
+// The softmax state of a wave's QB x 32 packed rows.
+template <int D, int QB>
+struct State {
+    bf16x8 q[QB][D / 16];
+    f32x16 O[QB][D / 32];
+    float c[QB], m[QB], l[QB];  // scale; reference (raw logit); this half-wave's share of the denominator
+
+    __device__ __forceinline__ void start(const PagedArgs &p, int qb, int64_t row, int h, int hf)
+    {
+        const __bf16 *qp = (const __bf16 *)(p.q + row * p.ld_q) + (int64_t)h * D + 8 * hf;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) q[qb][s] = *(const bf16x8 *)(qp + 16 * s);
+        c[qb] = paged_row_scale(p, row);
+        m[qb] = kNoRef;
+        l[qb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) O[qb][db][i] = 0.f;
+    }
+    // the row's own key and value as the first member of the softmax (candidates)
+    __device__ __forceinline__ void own(const PagedArgs &p, int qb, int64_t row, int hk, int hf)
+    {
+        const __bf16 *kp = (const __bf16 *)(p.k + row * p.ld_kv) + (int64_t)hk * D + 8 * hf;
+        const __bf16 *vp = (const __bf16 *)(p.v + row * p.ld_kv) + (int64_t)hk * D + 4 * hf;
+        float dot = 0.f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            const bf16x8 k = *(const bf16x8 *)(kp + 16 * s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot += (float)q[qb][s][e] * (float)k[e];
+        }
+        dot += other_half(dot);
+        l[qb] = hf == 0 ? 1.f : 0.f;
+        m[qb] = dot;
+        if (dot != dot) l[qb] = dot, m[qb] = kNoRef;  // (a logit that is no number makes the row none)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const bf16x4 v = *(const bf16x4 *)(vp + 32 * db + 8 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[qb][db][4 * g + e] = (float)v[e];
+            }
+    }
+    __device__ __forceinline__ void logits(const KFrags<D> &k, f32x16 (&S)[QB]) const
+    {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) S[qb][i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) S[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.a[s], q[qb][s], S[qb], 0, 0, 0);
+    }
+    // S: logits of 32 keys, -inf where masked.  The reference moves where a logit exceeds it by far.
+    __device__ __forceinline__ void reference(const f32x16 (&S)[QB])
+    {
+        float v[QB];
+        bool need[QB], any = false;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            float x = fmaxf(S[qb][0], S[qb][1]);
+#pragma unroll
+            for (int i = 2; i < 16; i += 2) x = fmaxf(fmaxf(x, S[qb][i]), S[qb][i + 1]);
+            v[qb] = half_max(x);
+            need[qb] = (v[qb] - m[qb]) * c[qb] > kSlack;
+            any |= need[qb];
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(any) != 0, 0)) {
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                const float alpha = need[qb] ? __builtin_amdgcn_exp2f((m[qb] - v[qb]) * c[qb]) : 1.f;
+                m[qb] = need[qb] ? v[qb] : m[qb];
+                l[qb] *= alpha;
+#pragma unroll
+                for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) O[qb][db][i] *= alpha;
+            }
+        }
+    }
+    // P: the operand of the value product
+    __device__ __forceinline__ void weights(const f32x16 (&S)[QB], bf16x8 (&P)[QB][2])
+    {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const float sub = m[qb] * c[qb];
+            float sum = 0.f;
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(S[qb][8 * g + e], c[qb], -sub));
+                    sum += x;
+                    P[qb][g][e] = (__bf16)x;
+                }
+            l[qb] += sum;
+        }
+    }
+    // 16 keys' values
+    __device__ __forceinline__ void add(const VFrags<D> &v, const bf16x8 (&P)[QB][2], int g)
+    {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) O[qb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(v.a[db]), P[qb][g], O[qb][db], 0, 0, 0);
+    }
+    // The same for keys of which some rows do not see all: a row must not meet the values of keys that it does not see, not even with
+    // probability 0, where they are infinite or no numbers.  Those take part as zeros, and the rows that do see one get it by a
+    // count of such values.  k: the first key; top: the lane's rows see keys below it.
+    __device__ __forceinline__ void add_masked(VFrags<D> v, const bf16x8 (&P)[QB][2], int g, int k, int hf, const int (&top)[QB])
+    {
+        uint32_t odd = 0;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) odd |= (v.a[db][i] & 0x7f807f80u) + 0x00800080u;  // (all exponent bits set: a carry)
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) == 0, 1)) {
+            add(v, P, g);
+            return;
+        }
+        // 0: the others; 1, 2: infinities of a sign, and what is no number counts as both
+#pragma unroll 1
+        for (int kind = 0; kind < 3; ++kind) {
+            const float put = kind == 1 ? INFINITY : -INFINITY;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db) {
+                u32x4 is;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    asm volatile("" : "+v"(v.a[db][i]));  // (nothing of this is worth a register outside the loop)
+                    auto half = [&](uint32_t u) {
+                        const bool odd_one = (u & 0x7f80u) == 0x7f80u;
+                        return kind == 0 ? (odd_one ? 0u : u) : odd_one && ((u & 0x7fu) != 0 || (int)(u >> 15) == kind - 1) ? 0x3f80u : 0u;
+                    };
+                    is[i] = half(v.a[db][i] & 0xffffu) | half(v.a[db][i] >> 16) << 16;
+                }
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) {
+                    if (kind == 0) {
+                        O[qb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(is), P[qb][g], O[qb][db], 0, 0, 0);
+                        continue;
+                    }
+                    bf16x8 seen;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) seen[e] = (__bf16)(k + 8 * (e >> 2) + 4 * hf + (e & 3) < top[qb] ? 1.f : 0.f);
+                    f32x16 n;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) n[i] = 0.f;
+                    n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(is), seen, n, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (n[i] > 0.f) O[qb][db][i] += put;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+    }
+};
+
+static __device__ __forceinline__ void hide(f32x16 &S, int k, int hf, int top)
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (k + 8 * (i >> 2) + 4 * hf + (i & 3) >= top) S[i] = -INFINITY;
+}
+
+// The new tokens of packed rows r0 .. r1 - 1 go into their pages.  (No call reads them from there before this one is done.)
+template <int D>
+static __device__ __forceinline__ void store_new(const PagedArgs &p, const PagedSeq &s, int b, int hk, int r0, int r1)
+{
+    constexpr int C = D / 8;
+    const int t0 = (r0 + p.G - 1) / p.G, t1 = (r1 + p.G - 1) / p.G;
+    for (int i = threadIdx.x; i < (t1 - t0) * C; i += 256) {
+        const int t = t0 + i / C, c = (i % C) * 16, slot = s.n + t, page = p.table[(int64_t)b * p.table_ld + (slot >> p.page_shift)];
+        if (page < 0 || page >= p.n_pages) continue;
+        const int64_t to = paged_row(p, page, hk, slot) + c, from = (s.row0 + t) * p.ld_kv + (int64_t)hk * (2 * D) + c;
+        *(uint4 *)(p.k_pages + to) = *(const uint4 *)(p.k + from);
+        *(uint4 *)(p.v_pages + to) = *(const uint4 *)(p.v + from);
+        if (hk == 0 && c == 0 && p.stamp) p.stamp[((int64_t)page << p.page_shift) + (slot & ((1 << p.page_shift) - 1))] = p.stamp_new[s.row0 + t];
+    }
+}
+
+// ---- tiles ---------------------------------------------------------------------------------------
+constexpr int kTileKeys = 64;
+
+// 4 waves of QB x 32 packed rows over a ring of three stages of 64 keys.  The keys that every row of the tile sees go through a
+// pipeline over blocks of 32: while the exponentials of block j are made, the matrix pipe has the logits of block j + 1.  The rest (the diagonal of the causal mask, the end of the keys) block by block.
+// D = 128, QB = 2: one wave per SIMD with its 512 registers; each fragment serves 64 rows, without which LDS reads (16 KiB per 32 keys and
+// wave) take as long as the products.
+template <int D, int QB, bool SUMI>
+__global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_tile_kernel(const PagedArgs p)
+{
+    using R = Rows<D>;
+    constexpr int kRows = 128 * QB, kValues = kTileKeys * R::kPitch, kStage = 2 * kValues;  // keys, then values
+    // (three arrays: reads of one do not wait for copies into another)
+    __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage], stage1[kStage], stage2[kStage];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    if (!paged_work(p, w)) return;
+    const PagedSeq s = paged_seq(p, w.b);
+    const int rows = s.T * p.G, r_tile = w.tile * kRows;
+    if (r_tile >= rows) return;
+    const int r_wave = r_tile + wave * 32 * QB;
+    const bool causal = !SUMI && p.causal;
+    const int k_all = SUMI ? s.n : s.n + s.T;
+    auto sees = [&](int r) { return causal ? s.n + min(r, rows - 1) / p.G + 1 : k_all; };  // packed row r sees keys below it
+    int k_lo, k_hi;
+    paged_part(p, w.split, sees(r_tile + kRows - 1), kTileKeys, k_lo, k_hi);
+    k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+    const int n_tiles = (k_hi - k_lo + kTileKeys - 1) / kTileKeys;
+    const int n_clean = __builtin_amdgcn_readfirstlane(max(0, min(sees(r_tile), k_hi) - k_lo) / kTileKeys);
+
+    const Source<D> src(p, s, w.b, w.hk, k_hi, lane);
+    auto stage = [&](int i) __attribute__((always_inline)) { return (lds_u8 *)(i == 0 ? stage0 : i == 1 ? stage1 : stage2); };
+    // this wave's 16 of the 64 keys of tile i
+    auto issue = [&](int i, int page, lds_u8 *to) __attribute__((always_inline)) {
+        src.issue(k_lo + i * kTileKeys + wave * 16, page, to + wave * 16 * R::kPitch, to + kValues + wave * 16 * R::kPitch);
+    };
+    auto page_of = [&](int i) __attribute__((always_inline)) { return src.page_of(k_lo + i * kTileKeys + wave * 16); };
+    int page = 0;
+    if (n_tiles > 0) {
+        issue(0, page_of(0), stage(0));
+        if (n_tiles > 1) issue(1, page_of(1), stage(1));
+        page = page_of(2);
+    }
+
+    Rows<D> at;
+    at.init(lane);
+    State<D, QB> st;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int r = min(r_wave + qb * 32 + l32, rows - 1);
+        const int64_t row = s.row0 + r / p.G;
+        st.start(p, qb, row, w.hk * p.G + r % p.G, hf);
+        if (SUMI && w.split == 0) st.own(p, qb, row, w.hk, hf);
+    }
+    if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + kRows, rows));
+
+    // all copies issued so far have landed, everywhere
+    auto meet = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if (n_clean > 0) {
+        f32x16 S0[QB], S1[QB];
+        bf16x8 P[QB][2];
+        // Sc: this block's logits, values at v_cur; Sn: the next block's, from k_next
+        auto step = [&](f32x16 (&Sc)[QB], lds_u8 *v_cur, const lds_u8 *k_next, f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
+            st.reference(Sc);
+            st.logits(read_k<D>(at, k_next), Sn);
+            st.weights(Sc, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, v_cur + g * 16 * R::kPitch), P, g);
+        };
+        meet();  // (tile 1 as well)
+        st.logits(read_k<D>(at, stage(0)), S0);
+        auto tile = [&](int t, lds_u8 *prev, lds_u8 *cur, lds_u8 *next) __attribute__((always_inline)) {
+            step(S0, cur + kValues, cur + 32 * R::kPitch, S1);
+            meet();  // tile t + 1 is here, and nobody reads the stage of tile t - 1 any more
+            if (t + 2 < n_tiles) {
+                issue(t + 2, page, prev);
+                page = page_of(t + 3);
+            }
+            step(S1, cur + kValues + 32 * R::kPitch, next, S0);  // (behind the last tile S0 is not used)
+        };
+        for (int t = 0; t < n_clean;) {
+            tile(t, stage(2), stage(0), stage(1));
+            if (++t == n_clean) break;
+            tile(t, stage(0), stage(1), stage(2));
+            if (++t == n_clean) break;
+            tile(t, stage(1), stage(2), stage(0));
+            ++t;
+        }
+    }
+    // tiles that not every row sees whole
+    int top[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) top[qb] = min(sees(r_wave + qb * 32 + l32), k_hi);
+    const int wave_hi = min(sees(r_wave + 32 * QB - 1), k_hi);
+#pragma unroll 1
+    for (int t = n_clean; t < n_tiles; ++t) {
+        meet();
+        if (t + 2 < n_tiles) {
+            issue(t + 2, page, stage((t + 2) % 3));
+            page = page_of(t + 3);
+        }
+        lds_u8 *cur = stage(t % 3);
+#pragma unroll 1
+        for (int blk = 0; blk < 2; ++blk) {
+            const int k0 = k_lo + t * kTileKeys + blk * 32;
+            if (k0 >= wave_hi) break;
+            f32x16 S[QB];
+            bf16x8 P[QB][2];
+            st.logits(read_k<D>(at, cur + blk * 32 * R::kPitch), S);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) hide(S[qb], k0, hf, top[qb]);
+            st.reference(S);
+            st.weights(S, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add_masked(read_v<D>(at, cur + kValues + (blk * 32 + g * 16) * R::kPitch), P, g, k0 + g * 16, hf, top);
+        }
+    }
+
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int r = r_wave + qb * 32 + l32;
+        const float l = st.l[qb] + other_half(st.l[qb]);
+        if (r >= rows) continue;
+        const int64_t row = s.row0 + r / p.G, rh = row * p.H + w.hk * p.G + r % p.G;
+        if (p.n_split > 1) {
+            float *po = p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D + 4 * hf;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(f32x4 *)(po + 32 * db + 8 * g) =
+                        f32x4{st.O[qb][db][4 * g], st.O[qb][db][4 * g + 1], st.O[qb][db][4 * g + 2], st.O[qb][db][4 * g + 3]};
+            if (hf == 0) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{st.m[qb] * st.c[qb], l};
+            continue;
+        }
+        const float inv = 1.f / l;
+        __bf16 *op = (__bf16 *)(p.o + row * p.ld_o) + (int64_t)(w.hk * p.G + r % p.G) * D + 4 * hf;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                bf16x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = (__bf16)(st.O[qb][db][4 * g + e] * inv);
+                *(bf16x4 *)(op + 32 * db + 8 * g) = x;
+            }
+        if (hf == 0 && p.lse) p.lse[rh] = st.m[qb] * st.c[qb] + __builtin_amdgcn_logf(l);
+    }
+}
+
+// ---- few rows ------------------------------------------------------------------------------------
+template <int D, bool SUMI>
+__global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
+{
+    using R = Rows<D>;
+    constexpr int kStage = 2 * 32 * R::kPitch, kLoads = 4 * R::kLoads;  // a wave's
+    __shared__ __attribute__((aligned(1024))) uint8_t stage0[4 * kStage], stage1[4 * kStage];
+    __shared__ float ref[4][32], denom[4][32];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    if (!paged_work(p, w)) return;
+    const PagedSeq s = paged_seq(p, w.b);
+    const int rows = s.T * p.G, r_tile = w.tile * 32;
+    if (r_tile >= rows) return;
+    const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
+    const int64_t row = s.row0 + t;
+    const bool causal = !SUMI && p.causal;
+    const int k_all = SUMI ? s.n : s.n + s.T;
+    const int lim = causal ? s.n + t + 1 : k_all, lim_lo = causal ? s.n + r_tile / p.G + 1 : k_all;
+    const int k_end = causal ? s.n + min(r_tile + 31, rows - 1) / p.G + 1 : k_all;
+    int k_lo, k_hi;
+    paged_part(p, w.split, k_end, 128, k_lo, k_hi);
+    k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+    const int n_blk = (k_hi - k_lo + 31) / 32, mine = n_blk > wave ? (n_blk - wave + 3) / 4 : 0;  // blocks wave, wave + 4, ...
+
+    const Source<D> src(p, s, w.b, w.hk, k_hi, lane);
+    lds_u8 *const at0 = (lds_u8 *)stage0 + wave * kStage, *const at1 = (lds_u8 *)stage1 + wave * kStage;
+    auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
+        const int k0 = k_lo + (i * 4 + wave) * 32;
+        const int p0 = src.page_of(k0), p1 = src.page_of(k0 + 16);
+        src.issue(k0, p0, to, to + 32 * R::kPitch);
+        src.issue(k0 + 16, p1, to + 16 * R::kPitch, to + 48 * R::kPitch);
+    };
+    if (mine > 0) issue(0, at0);
+    if (mine > 1) issue(1, at1);
+
+    Rows<D> at;
+    at.init(lane);
+    State<D, 1> st;
+    st.start(p, 0, row, h, hf);
+    if (SUMI && w.split == 0 && wave == 0) st.own(p, 0, row, w.hk, hf);
+    if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + 32, rows));
+
+    auto block = [&](int i, lds_u8 *keys) __attribute__((always_inline)) {
+        // (the rows and stores above were issued later than the first copies: until they are done, this waits for more than it has to)
+        static_assert(kLoads == 16 || kLoads == 8, "vmcnt immediates");
+        if (i + 1 < mine) {
+            if constexpr (kLoads == 16) asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        lds_u8 *const values = keys + 32 * R::kPitch;
+        const int k0 = k_lo + (i * 4 + wave) * 32;
+        f32x16 S[1];
+        bf16x8 P[1][2];
+        st.logits(read_k<D>(at, keys), S);
+        if (k0 + 32 <= min(lim_lo, k_hi)) {
+            st.reference(S);
+            st.weights(S, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, values + g * 16 * R::kPitch), P, g);
+        } else {
+            const int top[1] = {min(lim, k_hi)};
+            hide(S[0], k0, hf, top[0]);
+            st.reference(S);
+            st.weights(S, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add_masked(read_v<D>(at, values + g * 16 * R::kPitch), P, g, k0 + g * 16, hf, top);
+        }
+        // its place has been read
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + 2 < mine) issue(i + 2, keys);
+    };
+#pragma unroll 1
+    for (int i = 0; i < mine; i += 2) {
+        block(i, at0);
+        if (i + 1 < mine) block(i + 1, at1);
+    }
+
+    // join the waves: denominators and outputs in units of the largest reference
+    const float l = st.l[0] + other_half(st.l[0]);
+    if (hf == 0) ref[wave][l32] = st.m[0], denom[wave][l32] = l;
+    __syncthreads();
+    const float m = fmaxf(fmaxf(ref[0][l32], ref[1][l32]), fmaxf(ref[2][l32], ref[3][l32]));
+    const float mine_w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.m[0] - m) * st.c[0]);
+    float *joined = (float *)stage0 + wave * 32 * D;  // (all copies have arrived and been read)
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : st.O[0][db][4 * g + e] * mine_w;
+            // (16-byte piece c of row r at slot c ^ r % 8: lanes of neighbouring rows write to different banks)
+            *(f32x4 *)(joined + l32 * D + (((8 * db + 2 * g + hf) ^ (l32 & 7)) * 4)) = x;
+        }
+    float total = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) total += denom[j][l32] == 0.f ? 0.f : denom[j][l32] * __builtin_amdgcn_exp2f((ref[j][l32] - m) * st.c[0]);
+    __syncthreads();
+    if (wave == 0 && hf == 0) denom[0][l32] = total;  // (read by all above, before the barrier)
+    __syncthreads();
+    if (wave == 0 && hf == 0 && r_tile + l32 < rows) {
+        const int64_t rh = row * p.H + h;
+        if (p.n_split > 1) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{m * st.c[0], total};
+        else if (p.lse) p.lse[rh] = m * st.c[0] + __builtin_amdgcn_logf(total);
+    }
+    constexpr int C = D / 4;
+    const int n_rows = min(32, rows - r_tile);
+    for (int i = threadIdx.x; i < n_rows * C; i += 256) {
+        const int rr = i / C, c = i % C, tt = (r_tile + rr) / p.G, hh = w.hk * p.G + (r_tile + rr) % p.G;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x += *(const f32x4 *)((const float *)stage0 + j * 32 * D + rr * D + ((c ^ (rr & 7)) * 4));
+        const int64_t rh = (s.row0 + tt) * p.H + hh;
+        if (p.n_split > 1) {
+            *(f32x4 *)(p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D + c * 4) = x;
+        } else {
+            const float inv = 1.f / denom[0][rr];
+            bf16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(x[e] * inv);
+            *(bf16x4 *)((__bf16 *)(p.o + (s.row0 + tt) * p.ld_o) + (int64_t)hh * D + c * 4) = y;
+        }
+    }
+}
+
+template <int D, bool SUMI>
+hipError_t launch(PagedArgs p, hipStream_t s)
+{
+    const int64_t rows = (int64_t)p.m_max * p.G;
+    void (*kernel)(PagedArgs) = attn_paged_tile_kernel<D, 2, SUMI>;
+    int tile = 256;
+    if (rows <= kPagedFewRows) kernel = attn_paged_few_kernel<D, SUMI>, tile = 32;
+    else if (rows <= 128) kernel = attn_paged_tile_kernel<D, 1, SUMI>, tile = 128;
+    p.n_tiles = (int)((rows + tile - 1) / tile);
+    hipLaunchKernelGGL(kernel, dim3(paged_grid(p)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_paged_bf16(const PagedArgs &a, hipStream_t s)
+{
+    if (a.d == 64) return a.sumi ? launch<64, true>(a, s) : launch<64, false>(a, s);
+    return a.sumi ? launch<128, true>(a, s) : launch<128, false>(a, s);
+}
+
+}  // namespace climber

@@ -374,9 +374,8 @@ void launch_mass(const PagedArgs &p, float *part, hipStream_t s)
 
 }  // namespace
 
-hipError_t launch_attn_paged_f32(const PagedArgs &a, bool bf16, hipStream_t s)
+hipError_t launch_attn_paged_f32(const PagedArgs &a, hipStream_t s)
 {
-    if (bf16) return a.d == 64 ? launch<__bf16, 64>(a, s) : launch<__bf16, 128>(a, s);
     return a.d <= 32 ? launch<float, 32>(a, s) : a.d <= 64 ? launch<float, 64>(a, s) : launch<float, 128>(a, s);
 }
 

@@ -105,7 +105,10 @@ static __device__ __forceinline__ float paged_row_scale(const PagedArgs &p, int6
     return p.scale_log2e / p.tau[sc * p.n_beh + bh];
 }
 
-hipError_t launch_attn_paged_f32(const PagedArgs &a, bool bf16, hipStream_t s);
+constexpr int kPagedFewRows = 32;  // bf16: most packed rows of a sequence and cache head that go to the kernel for few rows
+
+hipError_t launch_attn_paged_bf16(const PagedArgs &a, hipStream_t s);
+hipError_t launch_attn_paged_f32(const PagedArgs &a, hipStream_t s);
 hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_paged_mass_f32(const PagedArgs &a, bool bf16, float *part, hipStream_t s);
 

@@ -119,7 +119,7 @@ int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_
     if (!sumi && cfg->sub_len != 0) return CLIMBER_ERR_UNSUPPORTED;
     const int64_t elem = (int64_t)elem_of(cfg), wide = cfg->d_model, kv_wide = (int64_t)kv->n_kv_heads * cfg->d_head;
     if (ld_q < wide || ld_o < wide || ld_kv < kv_wide) return CLIMBER_ERR_SHAPE;
-    const int64_t most = (int64_t)1 << 40;
+    const int64_t most = (int64_t)1 << 24;  // (16 rows are addressed by 32 bits)
     if (ld_q > most || ld_kv > most || ld_o > most) return CLIMBER_ERR_RANGE;
     if (!tau || !off) return CLIMBER_ERR_NULL;
     e = check_pointers(kv);
@@ -182,7 +182,7 @@ int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_
     a.part_ml = (float *)(ws + w.part_ml);
     a.lse = kv->mass ? (float *)(ws + w.lse) : nullptr;
     const hipStream_t s = (hipStream_t)stream;
-    e = rt(launch_attn_paged_f32(a, bf16, s));
+    e = rt(bf16 ? launch_attn_paged_bf16(a, s) : launch_attn_paged_f32(a, s));
     if (e) return e;
     if (a.n_split > 1) e = rt(launch_paged_combine(a, bf16, s));
     if (e || !kv->mass || kv->max_len == 0) return e;
