@@ -21,7 +21,7 @@ LIB = os.path.join(HERE, "libclimber.so")
 NATIVE = os.path.join(HERE, "_native" + EXTENSION_SUFFIXES[0])
 SOURCES = ["climber_api.hip", "attn_bf16.hip", "attn_wave_bf16.hip", "attn_split_bf16.hip", "attn_bias_bf16.hip", "attn_f32.hip", "attn_tile_f32.hip", "kv_cache.hip", "stack.hip",
            "gemm_bf16.hip", "gemm_small_bf16.hip", "gemm_resident_bf16.hip", "layer_tail_bf16.hip", "layer_head_bf16.hip", "rowwise.hip", "hist_fused_bf16.hip", "check.hip", "bgf.hip", "bgf_front_bf16.hip",
-           "paged_api.hip", "attn_paged_f32.hip", "attn_paged_bf16.hip", "paged_evict.hip"]
+           "paged_api.hip", "attn_paged_f32.hip", "attn_paged_bf16.hip", "paged_mass_bf16.hip", "paged_evict.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -16,16 +16,6 @@ constexpr int kKeys = 32;              // keys of a tile
 constexpr float kNoRef = -1.0e30f;     // "no reference yet", below any finite logit
 
 static __device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4 *)p; }
-static __device__ __forceinline__ f32x4 load4(const __bf16 *p)
-{
-    const uint2 u = *(const uint2 *)p;
-    f32x4 x;
-    x[0] = __uint_as_float(u.x << 16);
-    x[1] = __uint_as_float(u.x & 0xffff0000u);
-    x[2] = __uint_as_float(u.y << 16);
-    x[3] = __uint_as_float(u.y & 0xffff0000u);
-    return x;
-}
 static __device__ __forceinline__ void store4(float *p, f32x4 x) { *(f32x4 *)p = x; }
 static __device__ __forceinline__ void store4(__bf16 *p, f32x4 x)
 {
@@ -36,14 +26,14 @@ static __device__ __forceinline__ void store4(__bf16 *p, f32x4 x)
 static __device__ __forceinline__ float half_max(float x) { return fmaxf(x, __shfl_xor(x, 32, 64)); }
 
 // 32 keys (rows pointed to by key_ptr) into LDS, pitch DP + 4 floats, zeros beyond d
-template <typename E, int DP, int NT, typename Ptr>
+template <int DP, int NT, typename Ptr>
 static __device__ __forceinline__ void load_tile(float *to, int d, Ptr key_ptr)
 {
     constexpr int C = DP / 4;
     for (int i = threadIdx.x; i < kKeys * C; i += NT) {
         const int r = i / C, c = (i % C) * 4;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        if (c < d) x = load4((const E *)key_ptr(r) + c);
+        if (c < d) x = load4((const float *)key_ptr(r) + c);
         *(f32x4 *)(to + r * (DP + 4) + c) = x;
     }
 }
@@ -51,7 +41,7 @@ static __device__ __forceinline__ void load_tile(float *to, int d, Ptr key_ptr)
 // The transposed problem, as in the bf16 kernels: S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x2_f32.  A lane owns one packed
 // row (lane % 32), its probabilities leave the accumulator as the operand of the value product (step r of it takes the keys of
 // accumulator register r).  The sum over the dimensions is taken in an order that lets a lane read four of them at once.
-template <typename E, int DP, int NW, bool SUMI>
+template <int DP, int NW, bool SUMI>
 __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs p)
 {
     constexpr int kPitch = DP + 4, NB = DP / 32;
@@ -88,7 +78,7 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
     }
 
     f32x4 q[DP / 8];
-    const E *qp = (const E *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
+    const float *qp = (const float *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
 #pragma unroll
     for (int i = 0; i < DP / 8; ++i) q[i] = 8 * i + 4 * hf < p.d ? load4(qp + 8 * i + 4 * hf) : f32x4{0.f, 0.f, 0.f, 0.f};
     const float c = paged_row_scale(p, row);
@@ -99,7 +89,7 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
     if (SUMI && w.split == 0) {  // the row's own key and value: the first member of its softmax
-        const E *kp = (const E *)(p.k + row * p.ld_kv) + (int64_t)w.hk * p.d, *vp = (const E *)(p.v + row * p.ld_kv) + (int64_t)w.hk * p.d;
+        const float *kp = (const float *)(p.k + row * p.ld_kv) + (int64_t)w.hk * p.d, *vp = (const float *)(p.v + row * p.ld_kv) + (int64_t)w.hk * p.d;
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < DP / 8; ++i)
@@ -131,8 +121,8 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
             };
         };
         __syncthreads();
-        load_tile<E, DP, NW * 64>(tk, p.d, ptr(p.k_pages, p.k));
-        load_tile<E, DP, NW * 64>(tv, p.d, ptr(p.v_pages, p.v));
+        load_tile<DP, NW * 64>(tk, p.d, ptr(p.k_pages, p.k));
+        load_tile<DP, NW * 64>(tv, p.d, ptr(p.v_pages, p.v));
         __syncthreads();
         if (r_wave >= rows || k0 >= lim_hi) continue;  // (no row here, or none that sees a key of the tile)
         f32x16 S;
@@ -222,14 +212,14 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
         return;
     }
     const float inv = 1.f / l;
-    E *op = (E *)(p.o + row * p.ld_o) + (int64_t)h * p.d;
+    float *op = (float *)(p.o + row * p.ld_o) + (int64_t)h * p.d;
 #pragma unroll
     for (int db = 0; db < NB; ++db)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
             if (32 * db + 8 * g + 4 * hf < p.d)
                 store4(op + 32 * db + 8 * g + 4 * hf, f32x4{O[db][4 * g] * inv, O[db][4 * g + 1] * inv, O[db][4 * g + 2] * inv, O[db][4 * g + 3] * inv});
-    if (hf == 0 && p.lse) p.lse[rh] = m * c + __builtin_amdgcn_logf(l);
+    if (hf == 0 && p.lse) p.lse[rh] = float2{c, m * c + __builtin_amdgcn_logf(l)};
 }
 
 // Partial results of the parts of the keys, joined: a wave per row and head.
@@ -267,13 +257,13 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedArgs p)
         for (int e = 0; e < 4; ++e) acc[e] *= inv;
         store4((E *)(p.o + row * p.ld_o) + (int64_t)h * p.d + c, acc);
     }
-    if (lane == 0 && p.lse) p.lse[rh] = M + __builtin_amdgcn_logf(L);
+    if (lane == 0 && p.lse) p.lse[rh] = float2{paged_row_scale(p, row), M + __builtin_amdgcn_logf(L)};
 }
 
 // Attention weights per cached token.  One workgroup: 32 keys of one (sequence, cache head), which stay in registers; its waves
 // take the packed rows in turn, p = exp2(s c - lse) again from the logits, and each lane adds up those of its keys.  The sums of a
 // cache head go to part[b][hk][slot], without atomics: a second kernel adds the heads up in their order.
-template <typename E, int DP>
+template <int DP>
 __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, float *part)
 {
     constexpr int kPitch = DP + 4;
@@ -284,7 +274,7 @@ __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, floa
     const PagedSeq s = paged_seq(p, b);
     const int keys = p.sumi ? s.n : s.n + s.T, k0 = tile * kKeys, rows = s.T * p.G;
     if (k0 >= keys || rows == 0) return;
-    load_tile<E, DP, 256>(tk, p.d, [&](int i) {
+    load_tile<DP, 256>(tk, p.d, [&](int i) {
         const int j = min(k0 + i, keys - 1);
         if (j >= s.n) return p.k + (s.row0 + j - s.n) * p.ld_kv + (int64_t)hk * p.row_bytes;
         return (const uint8_t *)p.k_pages + paged_row(p, paged_page(p, b, j), hk, j);
@@ -299,7 +289,7 @@ __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, floa
         const int r = min(r0 + l32, rows - 1), t = r / p.G, h = hk * p.G + r % p.G;
         const int64_t row = s.row0 + t;
         const int lim = r0 + l32 >= rows ? 0 : causal ? s.n + t + 1 : keys;
-        const E *qp = (const E *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
+        const float *qp = (const float *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
         f32x16 S;
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[i] = 0.f;
@@ -310,7 +300,7 @@ __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, floa
 #pragma unroll
             for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[e], S, 0, 0, 0);
         }
-        const float c = paged_row_scale(p, row), lse = p.lse[row * p.H + h];
+        const float c = p.lse[row * p.H + h].x, lse = p.lse[row * p.H + h].y;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const float w = __builtin_amdgcn_exp2f(fmaf(S[i], c, -lse));
@@ -330,7 +320,7 @@ __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, floa
             (sums[0][threadIdx.x] + sums[1][threadIdx.x]) + (sums[2][threadIdx.x] + sums[3][threadIdx.x]);
 }
 
-__global__ __launch_bounds__(256) void paged_mass_add_kernel(const PagedArgs p, const float *part)
+__global__ __launch_bounds__(256) void paged_mass_add_kernel(const PagedArgs p, const float *part, int n_parts)
 {
     const int per = (p.max_len + 255) / 256, b = blockIdx.x / per, j = (blockIdx.x % per) * 256 + threadIdx.x;
     const PagedSeq s = paged_seq(p, b);
@@ -338,12 +328,12 @@ __global__ __launch_bounds__(256) void paged_mass_add_kernel(const PagedArgs p, 
     const int raw = p.table[(int64_t)b * p.table_ld + (j >> p.page_shift)];
     if (raw < 0 || raw >= p.n_pages) return;
     float x = 0.f;
-    for (int h = 0; h < p.Hkv; ++h) x += part[((int64_t)b * p.Hkv + h) * p.max_len + j];
+    for (int i = 0; i < n_parts; ++i) x += part[((int64_t)b * n_parts + i) * p.max_len + j];
     float *to = p.mass + ((int64_t)raw << p.page_shift) + (j & ((1 << p.page_shift) - 1));
     *to = j < s.n ? *to + x : x;  // a new token has none yet, whatever its slot holds
 }
 
-template <typename E, int DP>
+template <int DP>
 hipError_t launch(const PagedArgs &a, hipStream_t s)
 {
     PagedArgs p = a;
@@ -353,7 +343,7 @@ hipError_t launch(const PagedArgs &a, hipStream_t s)
         constexpr int NW = decltype(nw)::value;
         constexpr bool SUMI = decltype(sumi)::value;
         p.n_tiles = (int)((rows + NW * 32 - 1) / (NW * 32));
-        hipLaunchKernelGGL((attn_paged_f32_kernel<E, DP, NW, SUMI>), dim3(paged_grid(p)), dim3(NW * 64), lds, s, p);
+        hipLaunchKernelGGL((attn_paged_f32_kernel<DP, NW, SUMI>), dim3(paged_grid(p)), dim3(NW * 64), lds, s, p);
     };
     if (rows <= 32) {
         if (a.sumi) go(std::integral_constant<int, 1>{}, std::true_type{});
@@ -365,18 +355,18 @@ hipError_t launch(const PagedArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-template <typename E, int DP>
+template <int DP>
 void launch_mass(const PagedArgs &p, float *part, hipStream_t s)
 {
     const int64_t tiles = (p.max_len + kKeys - 1) / kKeys;
-    hipLaunchKernelGGL((paged_mass_kernel<E, DP>), dim3((unsigned)(tiles * p.n_seqs * p.Hkv)), dim3(256), 0, s, p, part);
+    hipLaunchKernelGGL((paged_mass_kernel<DP>), dim3((unsigned)(tiles * p.n_seqs * p.Hkv)), dim3(256), 0, s, p, part);
 }
 
 }  // namespace
 
 hipError_t launch_attn_paged_f32(const PagedArgs &a, hipStream_t s)
 {
-    return a.d <= 32 ? launch<float, 32>(a, s) : a.d <= 64 ? launch<float, 64>(a, s) : launch<float, 128>(a, s);
+    return a.d <= 32 ? launch<32>(a, s) : a.d <= 64 ? launch<64>(a, s) : launch<128>(a, s);
 }
 
 hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s)
@@ -387,19 +377,17 @@ hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t launch_paged_mass_f32(const PagedArgs &a, bool bf16, float *part, hipStream_t s)
+hipError_t launch_paged_mass_f32(const PagedArgs &a, float *part, hipStream_t s)
 {
-    if (bf16) {
-        if (a.d == 64) launch_mass<__bf16, 64>(a, part, s);
-        else launch_mass<__bf16, 128>(a, part, s);
-    } else {
-        if (a.d <= 32) launch_mass<float, 32>(a, part, s);
-        else if (a.d <= 64) launch_mass<float, 64>(a, part, s);
-        else launch_mass<float, 128>(a, part, s);
-    }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_mass_add_kernel, dim3((unsigned)((a.max_len + 255) / 256 * a.n_seqs)), dim3(256), 0, s, a, part);
+    if (a.d <= 32) launch_mass<32>(a, part, s);
+    else if (a.d <= 64) launch_mass<64>(a, part, s);
+    else launch_mass<128>(a, part, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_mass_add(const PagedArgs &a, const float *part, int n_parts, hipStream_t s)
+{
+    hipLaunchKernelGGL(paged_mass_add_kernel, dim3((unsigned)((a.max_len + 255) / 256 * a.n_seqs)), dim3(256), 0, s, a, part, n_parts);
     return hipGetLastError();
 }
 

@@ -21,13 +21,14 @@ struct PagedArgs {
     uint8_t *o;
     int n_seqs, n_pages, page_shift, table_ld, max_len;
     int H, Hkv, G, d, row_bytes;  // row_bytes: of one key of one head
+    uint32_t G_inv;               // ceil(2^32 / G): r / G is umulhi(r, G_inv) or one less (r, G < 2^26; G > 1)
     int n_scen, n_beh, m_total, m_max;
     int causal, sumi;
     float scale_log2e;
     // work split: tiles of packed rows, parts of the keys
     int n_tiles, n_split, bh_major;
     float *part_o, *part_ml;  // [n_split][m_total H][d], [n_split][m_total H][2] (n_split > 1)
-    float *lse;               // [m_total H], log2 units, or nullptr: not wanted
+    float2 *lse;              // [m_total H] {scale, log of the sum of the exponentials} of a row's softmax, log2 units, or nullptr: not wanted
 };
 
 struct PagedSeq {
@@ -110,7 +111,18 @@ constexpr int kPagedFewRows = 32;  // bf16: most packed rows of a sequence and c
 hipError_t launch_attn_paged_bf16(const PagedArgs &a, hipStream_t s);
 hipError_t launch_attn_paged_f32(const PagedArgs &a, hipStream_t s);
 hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s);
-hipError_t launch_paged_mass_f32(const PagedArgs &a, bool bf16, float *part, hipStream_t s);
+// Attention weights per cached token, in two steps: sums over the rows of one cache head into part[n_seqs][parts][max_len], the parts
+// of a sequence being its cache heads (bf16: times paged_mass_parts), and those added up into the masses.
+hipError_t launch_paged_mass_f32(const PagedArgs &a, float *part, hipStream_t s);
+hipError_t launch_paged_mass_bf16(const PagedArgs &a, float *part, int row_parts, hipStream_t s);
+hipError_t launch_paged_mass_add(const PagedArgs &a, const float *part, int n_parts, hipStream_t s);
+constexpr int kMassKeys = 256;  // bf16: keys of a workgroup
+// bf16: parts of a cache head's rows, so that a launch has a workgroup per CU or more, of 256 rows or more
+static inline int paged_mass_parts(int64_t n_seqs, int64_t Hkv, int64_t max_len, int64_t rows)
+{
+    const int64_t groups = n_seqs * Hkv * ((max_len + kMassKeys - 1) / kMassKeys), most = (rows + 255) / 256, want = groups > 0 ? 512 / groups : 1;
+    return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
+}
 
 struct EvictArgs {
     uint8_t *k_pages, *v_pages;

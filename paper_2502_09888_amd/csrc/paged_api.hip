@@ -73,8 +73,9 @@ Layout layout_of(const climber_config *cfg, const climber_paged_kv *kv, int32_t 
     w.part_o = 0;
     w.part_ml = w.part_o + up(part_rows * cfg->d_head * 4);
     w.lse = w.part_ml + up(part_rows * 8);
-    w.mass = w.lse + (kv->mass ? up((size_t)m_total * cfg->n_heads * 4) : 0);
-    w.bytes = w.mass + (kv->mass ? up((size_t)kv->n_seqs * kv->n_kv_heads * kv->max_len * 4) : 0);
+    w.mass = w.lse + (kv->mass ? up((size_t)m_total * cfg->n_heads * 8) : 0);
+    // (more than one part of the rows: at most 512 workgroups' sums)
+    w.bytes = w.mass + (kv->mass ? up(((size_t)kv->n_seqs * kv->n_kv_heads * kv->max_len + 512 * kMassKeys) * 4) : 0);
     return w;
 }
 
@@ -168,6 +169,7 @@ int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_
     a.H = cfg->n_heads;
     a.Hkv = kv->n_kv_heads;
     a.G = cfg->n_heads / kv->n_kv_heads;
+    a.G_inv = (uint32_t)((((uint64_t)1 << 32) + a.G - 1) / a.G);
     a.d = cfg->d_head;
     a.row_bytes = (int)(cfg->d_head * elem);
     a.n_scen = cfg->n_scen;
@@ -180,13 +182,16 @@ int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_
     a.n_split = n_split;
     a.part_o = (float *)(ws + w.part_o);
     a.part_ml = (float *)(ws + w.part_ml);
-    a.lse = kv->mass ? (float *)(ws + w.lse) : nullptr;
+    a.lse = kv->mass ? (float2 *)(ws + w.lse) : nullptr;
     const hipStream_t s = (hipStream_t)stream;
     e = rt(bf16 ? launch_attn_paged_bf16(a, s) : launch_attn_paged_f32(a, s));
     if (e) return e;
     if (a.n_split > 1) e = rt(launch_paged_combine(a, bf16, s));
     if (e || !kv->mass || kv->max_len == 0) return e;
-    return rt(launch_paged_mass_f32(a, bf16, (float *)(ws + w.mass), s));
+    float *part = (float *)(ws + w.mass);
+    const int row_parts = bf16 ? paged_mass_parts(kv->n_seqs, kv->n_kv_heads, kv->max_len, (int64_t)m_max * a.G) : 1;
+    e = rt(bf16 ? launch_paged_mass_bf16(a, part, row_parts, s) : launch_paged_mass_f32(a, part, s));
+    return e ? e : rt(launch_paged_mass_add(a, part, kv->n_kv_heads * row_parts, s));
 }
 
 }  // namespace

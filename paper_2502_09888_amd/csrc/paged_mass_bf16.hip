@@ -1,0 +1,145 @@
+// Attention weights per token of the paged history cache, bf16 (gfx950): how much of all softmaxes of a call falls on each cached token,
+// sum over rows and query heads of p = exp2(s c - lse) with the logits made again (Eq. (3) of Climber, arXiv 2502.09888).
+//
+// One workgroup = 256 keys of one (sequence, cache head) and a part of its packed rows.  A wave keeps the fragments of its 64 keys
+// in registers and adds up 64 sums a lane; the rows pass by in LDS, 64 at a time in a ring of two stages.  No atomics: sums are made in the
+// order of the rows, then of the lanes, and a second kernel adds up cache heads and parts in theirs.  Bound by the exponentials
+// (16 cycles of a SIMD each 64, of 24 that a logit costs beside the 16 of its products at d_head 128).
+#include "paged_bf16.h"
+
+namespace climber {
+namespace {
+
+using namespace paged;
+
+constexpr int kRowsStage = 64;
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void paged_mass_bf16_kernel(const PagedArgs p, float *part)
+{
+    using R = Rows<D>;
+    constexpr int kStage = kRowsStage * R::kPitch, kLoads = kStage / 1024 / 4;  // (a wave's)
+    __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage], stage1[kStage];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    if (!paged_work(p, w)) return;
+    const PagedSeq s = paged_seq(p, w.b);
+    const int keys = p.sumi ? s.n : s.n + s.T, k_tile = w.tile * kMassKeys, k0 = k_tile + wave * 64, rows = s.T * p.G;
+    if (k_tile >= keys || rows == 0) return;
+    const bool causal = !p.sumi && p.causal;
+    // this part's rows, from the first one that sees a key of the tile
+    const int first = causal ? max(0, k_tile - s.n) * p.G : 0, per = ((rows + p.n_split - 1) / p.n_split + kRowsStage - 1) / kRowsStage * kRowsStage;
+    const int r_lo = max(w.split * per, first / kRowsStage * kRowsStage), r_hi = min((w.split + 1) * per, rows);
+    const int n_stages = __builtin_amdgcn_readfirstlane(max(0, r_hi - r_lo + kRowsStage - 1) / kRowsStage);
+
+    auto token_of = [&](int r) __attribute__((always_inline)) {  // r / G
+        const int t = (int)__umulhi((unsigned)r, p.G_inv);
+        return p.G == 1 ? r : t - (t * p.G > r);
+    };
+    auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int at = (wave * kLoads + j) * R::kPerLoad + lane / R::kPieces, r = min(r_lo + i * kRowsStage + at, rows - 1), t = token_of(r);
+            const int c = (lane % R::kPieces) ^ R::f(at);
+            copy16((glb_u8 *)(p.q + (s.row0 + t) * p.ld_q + (int64_t)(w.hk * p.G + r - t * p.G) * R::kPitch + c * 16), to + (wave * kLoads + j) * 1024);
+        }
+    };
+    float2 next[2];
+    auto stats = [&](int i) __attribute__((always_inline)) {  // the stage's rows of this lane: scale and denominator
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            const int r = min(r_lo + i * kRowsStage + blk * 32 + l32, rows - 1), t = token_of(r);
+            next[blk] = p.lse[(s.row0 + t) * p.H + w.hk * p.G + r - t * p.G];
+        }
+    };
+    if (n_stages > 0) {
+        issue(0, (lds_u8 *)stage0);
+        stats(0);
+    }
+    KFrags<D> k[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+        const int j = min(k0 + kb * 32 + l32, keys - 1);
+        const uint8_t *from = j < s.n ? p.k_pages + paged_row(p, paged_page(p, w.b, j), w.hk, j)
+                                      : p.k + (s.row0 + j - s.n) * p.ld_kv + (int64_t)w.hk * R::kPitch;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) k[kb].a[i] = *(const bf16x8 *)(from + i * 32 + hf * 16);
+    }
+    Rows<D> at;
+    at.init(lane);
+    f32x16 sum[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[kb][i] = 0.f;
+
+    auto stage = [&](int i, lds_u8 *cur, lds_u8 *other) __attribute__((always_inline)) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const float2 now[2] = {next[0], next[1]};
+        if (i + 1 < n_stages) {
+            issue(i + 1, other);
+            stats(i + 1);
+        }
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            const int r0 = r_lo + i * kRowsStage + blk * 32;
+            if (r0 >= r_hi) break;
+            const KFrags<D> q = read_k<D>(at, cur + blk * 32 * R::kPitch);
+            f32x16 S[2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) S[kb][e] = 0.f;
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e) S[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb].a[e], q.a[e], S[kb], 0, 0, 0);
+            }
+            const float c = now[blk].x, lse = now[blk].y;
+            if (r0 + 32 <= rows && (!causal || k0 + 63 <= s.n + __builtin_amdgcn_readfirstlane(token_of(r0)))) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sum[kb][e] += __builtin_amdgcn_exp2f(fmaf(S[kb][e], c, -lse));
+            } else {
+                const int lim = r0 + l32 >= rows ? 0 : causal ? s.n + token_of(r0 + l32) + 1 : keys;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float x = __builtin_amdgcn_exp2f(fmaf(S[kb][e], c, -lse));
+                        if (k0 + kb * 32 + 8 * (e >> 2) + 4 * hf + (e & 3) < lim) sum[kb][e] += x;
+                    }
+            }
+        }
+    };
+    for (int i = 0; i < n_stages; i += 2) {
+        stage(i, (lds_u8 *)stage0, (lds_u8 *)stage1);
+        if (i + 1 < n_stages) stage(i + 1, (lds_u8 *)stage1, (lds_u8 *)stage0);
+    }
+    // over the 32 lanes that have other rows of the same keys
+    float *to = part + (((int64_t)w.b * p.Hkv + w.hk) * p.n_split + w.split) * p.max_len;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            float x = row_sum16(sum[kb][e]);
+            x += __shfl_xor(x, 16, 64);
+            const int j = k0 + kb * 32 + 8 * (e >> 2) + 4 * hf + (e & 3);
+            if (l32 == 0 && j < keys) to[j] = x;
+        }
+}
+
+}  // namespace
+
+hipError_t launch_paged_mass_bf16(const PagedArgs &a, float *part, int row_parts, hipStream_t s)
+{
+    PagedArgs p = a;
+    p.n_split = row_parts;
+    p.n_tiles = (a.max_len + kMassKeys - 1) / kMassKeys;
+    if (a.d == 64) hipLaunchKernelGGL(paged_mass_bf16_kernel<64>, dim3(paged_grid(p)), dim3(256), 0, s, p, part);
+    else hipLaunchKernelGGL(paged_mass_bf16_kernel<128>, dim3(paged_grid(p)), dim3(256), 0, s, p, part);
+    return hipGetLastError();
+}
+
+}  // namespace climber
