@@ -196,58 +196,65 @@ struct State {
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) O[qb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(v.a[db]), P[qb][g], O[qb][db], 0, 0, 0);
     }
-    // The same for keys of which some rows do not see all: a row must not meet the values of keys that it does not see, not even with
-    // probability 0, where they are infinite or no numbers.  Those take part as zeros, and the rows that do see one get it by a
-    // count of such values.  k: the first key; top: the lane's rows see keys below it.
-    __device__ __forceinline__ void add_masked(VFrags<D> v, const bf16x8 (&P)[QB][2], int g, int k, int hf, const int (&top)[QB])
-    {
-        uint32_t odd = 0;
+};
+
+// A row must not meet the values of keys that it does not see, not even with probability 0, where they are infinite or no numbers.
+// In tiles that some rows do not see whole such values become zeros in LDS (ROWS value rows at `rows`, landed, by the wave that
+// copied them), and at the end put_odd adds them to the outputs of the rows that do see them.
+static __device__ __forceinline__ uint32_t odd_halves(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+template <int BYTES>
+static __device__ __forceinline__ bool clear_odd(lds_u8 *rows, int lane)
+{
+    uint32_t odd = 0;
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+    for (int i = 0; i < BYTES / 1024; ++i) {
+        auto *at = (__attribute__((address_space(3))) u32x4 *)(rows + i * 1024 + lane * 16);
+        u32x4 x = *at;
+        uint32_t any = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) odd |= (v.a[db][i] & 0x7f807f80u) + 0x00800080u;  // (all exponent bits set: a carry)
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64((odd & 0x80008000u) != 0) == 0, 1)) {
-            add(v, P, g);
-            return;
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t h = odd_halves(x[e]);
+            any |= h;
+            x[e] &= ~((h >> 15) * 0xffffu);
         }
-        // 0: the others; 1, 2: infinities of a sign, and what is no number counts as both
+        if (any) *at = x;
+        odd |= any;
+    }
+    return __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+}
+// (a wave; its outputs, or partial ones, of packed rows r0 .. r1 - 1 are written; `sees(r)` as in the kernels)
+template <int D, typename Sees>
+static __device__ __forceinline__ void put_odd(const PagedArgs &p, const PagedSeq &s, const PagedWork &w, int k_lo, int k_hi, int r0, int r1,
+                                               Sees sees)
+{
+    const int lane = threadIdx.x & 63;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind) {
-            const float put = kind == 1 ? INFINITY : -INFINITY;
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db) {
-                u32x4 is;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    asm volatile("" : "+v"(v.a[db][i]));  // (nothing of this is worth a register outside the loop)
-                    auto half = [&](uint32_t u) {
-                        const bool odd_one = (u & 0x7f80u) == 0x7f80u;
-                        return kind == 0 ? (odd_one ? 0u : u) : odd_one && ((u & 0x7fu) != 0 || (int)(u >> 15) == kind - 1) ? 0x3f80u : 0u;
-                    };
-                    is[i] = half(v.a[db][i] & 0xffffu) | half(v.a[db][i] >> 16) << 16;
-                }
-#pragma unroll
-                for (int qb = 0; qb < QB; ++qb) {
-                    if (kind == 0) {
-                        O[qb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(is), P[qb][g], O[qb][db], 0, 0, 0);
-                        continue;
-                    }
-                    bf16x8 seen;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) seen[e] = (__bf16)(k + 8 * (e >> 2) + 4 * hf + (e & 3) < top[qb] ? 1.f : 0.f);
-                    f32x16 n;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) n[i] = 0.f;
-                    n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(is), seen, n, 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (n[i] > 0.f) O[qb][db][i] += put;
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+    for (int j = k_lo; j < k_hi; ++j) {
+        const uint8_t *v = j < s.n ? p.v_pages + paged_row(p, paged_page(p, w.b, j), w.hk, j) : p.v + (s.row0 + j - s.n) * p.ld_kv + (int64_t)w.hk * 2 * D;
+        const uint32_t x = lane < D / 2 ? *(const uint32_t *)(v + lane * 4) : 0, odd = odd_halves(x);
+        if (__builtin_amdgcn_ballot_w64(odd != 0) == 0) continue;
+        const float lo = odd & 0x8000u ? __uint_as_float(x << 16) : 0.f, hi = odd >> 31 ? __uint_as_float(x & 0xffff0000u) : 0.f;
+#pragma unroll 1
+        for (int r = r0; r < r1; ++r) {
+            if (j >= sees(r) || !odd) continue;
+            const int64_t row = s.row0 + r / p.G, rh = row * p.H + w.hk * p.G + r % p.G;
+            auto load = [](const uint32_t *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+            auto store = [](uint32_t *at, uint32_t y) { __hip_atomic_store(at, y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+            if (p.n_split > 1) {
+                uint32_t *at = (uint32_t *)(p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D) + 2 * lane;
+                store(at, __float_as_uint(__uint_as_float(load(at)) + lo));
+                store(at + 1, __float_as_uint(__uint_as_float(load(at + 1)) + hi));
+            } else {
+                uint32_t *at = (uint32_t *)(p.o + row * p.ld_o + (int64_t)(w.hk * p.G + r % p.G) * 2 * D) + lane;
+                const uint32_t y = load(at);
+                const float a = __uint_as_float(y << 16) + lo, b = __uint_as_float(y & 0xffff0000u) + hi;
+                store(at, (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16);
             }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (the next key's come on top)
         }
     }
-};
+}
 
 static __device__ __forceinline__ void hide(f32x16 &S, int k, int hf, int top)
 {
@@ -286,6 +293,7 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
     constexpr int kRows = 128 * QB, kValues = kTileKeys * R::kPitch, kStage = 2 * kValues;  // keys, then values
     // (three arrays: reads of one do not wait for copies into another)
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage], stage1[kStage], stage2[kStage];
+    __shared__ int odd_seen[4];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
     if (!paged_work(p, w)) return;
@@ -370,8 +378,12 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) top[qb] = min(sees(r_wave + qb * 32 + l32), k_hi);
     const int wave_hi = min(sees(r_wave + 32 * QB - 1), k_hi);
+    bool odd = false;
 #pragma unroll 1
     for (int t = n_clean; t < n_tiles; ++t) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        odd |= clear_odd<16 * R::kPitch>(stage(t % 3) + kValues + wave * 16 * R::kPitch, lane);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         meet();
         if (t + 2 < n_tiles) {
             issue(t + 2, page, stage((t + 2) % 3));
@@ -390,7 +402,7 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
             st.reference(S);
             st.weights(S, P);
 #pragma unroll
-            for (int g = 0; g < 2; ++g) st.add_masked(read_v<D>(at, cur + kValues + (blk * 32 + g * 16) * R::kPitch), P, g, k0 + g * 16, hf, top);
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, cur + kValues + (blk * 32 + g * 16) * R::kPitch), P, g);
         }
     }
 
@@ -424,6 +436,10 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
             }
         if (hf == 0 && p.lse) p.lse[rh] = float2{st.c[qb], st.m[qb] * st.c[qb] + __builtin_amdgcn_logf(l)};
     }
+    if (lane == 0) odd_seen[wave] = odd;
+    __syncthreads();
+    if (__builtin_expect(odd_seen[0] | odd_seen[1] | odd_seen[2] | odd_seen[3], 0))
+        put_odd<D>(p, s, w, k_lo + n_clean * kTileKeys, k_hi, r_wave, min(r_wave + 32 * QB, rows), sees);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------
@@ -434,6 +450,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     constexpr int kStage = 2 * 32 * R::kPitch, kLoads = 4 * R::kLoads;  // a wave's
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[4 * kStage], stage1[4 * kStage];
     __shared__ float ref[4][32], denom[4][32];
+    __shared__ int odd_seen[4];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
     if (!paged_work(p, w)) return;
@@ -444,10 +461,10 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     const int64_t row = s.row0 + t;
     const bool causal = !SUMI && p.causal;
     const int k_all = SUMI ? s.n : s.n + s.T;
-    const int lim = causal ? s.n + t + 1 : k_all, lim_lo = causal ? s.n + r_tile / p.G + 1 : k_all;
-    const int k_end = causal ? s.n + min(r_tile + 31, rows - 1) / p.G + 1 : k_all;
+    auto sees = [&](int i) { return causal ? s.n + min(i, rows - 1) / p.G + 1 : k_all; };  // packed row i sees keys below it
+    const int lim = sees(r), lim_lo = sees(r_tile);
     int k_lo, k_hi;
-    paged_part(p, w.split, k_end, 128, k_lo, k_hi);
+    paged_part(p, w.split, sees(r_tile + 31), 128, k_lo, k_hi);
     k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
     const int n_blk = (k_hi - k_lo + 31) / 32, mine = n_blk > wave ? (n_blk - wave + 3) / 4 : 0;  // blocks wave, wave + 4, ...
 
@@ -469,6 +486,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     if (SUMI && w.split == 0 && wave == 0) st.own(p, 0, row, w.hk, hf);
     if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + 32, rows));
 
+    bool odd = false;
     auto block = [&](int i, lds_u8 *keys) __attribute__((always_inline)) {
         // (the rows and stores above were issued later than the first copies: until they are done, this waits for more than it has to)
         static_assert(kLoads == 16 || kLoads == 8, "vmcnt immediates");
@@ -489,12 +507,13 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
 #pragma unroll
             for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, values + g * 16 * R::kPitch), P, g);
         } else {
-            const int top[1] = {min(lim, k_hi)};
-            hide(S[0], k0, hf, top[0]);
+            odd |= clear_odd<32 * R::kPitch>(values, lane);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            hide(S[0], k0, hf, min(lim, k_hi));
             st.reference(S);
             st.weights(S, P);
 #pragma unroll
-            for (int g = 0; g < 2; ++g) st.add_masked(read_v<D>(at, values + g * 16 * R::kPitch), P, g, k0 + g * 16, hf, top);
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, values + g * 16 * R::kPitch), P, g);
         }
         // its place has been read
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -509,6 +528,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     // join the waves: denominators and outputs in units of the largest reference
     const float l = st.l[0] + other_half(st.l[0]);
     if (hf == 0) ref[wave][l32] = st.m[0], denom[wave][l32] = l;
+    if (lane == 0) odd_seen[wave] = odd;
     __syncthreads();
     const float m = fmaxf(fmaxf(ref[0][l32], ref[1][l32]), fmaxf(ref[2][l32], ref[3][l32]));
     const float mine_w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.m[0] - m) * st.c[0]);
@@ -551,6 +571,11 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
             for (int e = 0; e < 4; ++e) y[e] = (__bf16)(x[e] * inv);
             *(bf16x4 *)((__bf16 *)(p.o + (s.row0 + tt) * p.ld_o) + (int64_t)hh * D + c * 4) = y;
         }
+    }
+    if (__builtin_expect(odd_seen[0] | odd_seen[1] | odd_seen[2] | odd_seen[3], 0)) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all waves' outputs are written
+        __syncthreads();
+        if (wave == 0) put_odd<D>(p, s, w, k_lo + max(0, min(lim_lo, k_hi) - k_lo) / 32 * 32, k_hi, r_tile, min(r_tile + 32, rows), sees);
     }
 }
 

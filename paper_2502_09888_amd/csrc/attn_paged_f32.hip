@@ -222,35 +222,52 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
     if (hf == 0 && p.lse) p.lse[rh] = float2{c, m * c + __builtin_amdgcn_logf(l)};
 }
 
-// Partial results of the parts of the keys, joined: a wave per row and head.
-template <typename E>
+// Partial results of the parts of the keys, joined.  32 lanes have a row's dimensions; GROUPS such groups share its parts, and 8 / GROUPS
+// rows x heads are a workgroup's (64 parts of 32 rows x heads: 65 us with a wave for each, which takes one part after the other, 5 with 8 groups).
+template <typename E, int GROUPS>
 __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedArgs p)
 {
-    const int64_t all = (int64_t)p.m_total * p.H, rh = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (rh >= all) return;
-    const int64_t row = rh / p.H;
-    if (row < max(p.off[0], 0) || row >= p.off[p.n_seqs]) return;  // a row of no sequence stays as it is
+    __shared__ f32x4 sums[8][32];
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, g = group % GROUPS, c = lane * 4;
+    const int64_t all = (int64_t)p.m_total * p.H, rh = (int64_t)blockIdx.x * (8 / GROUPS) + group / GROUPS, row = rh / p.H;
     const int h = (int)(rh % p.H);
-    float M = -INFINITY;
-    for (int i = 0; i < p.n_split; ++i) {
-        const float2 ml = *(const float2 *)(p.part_ml + (i * all + rh) * 2);
-        if (ml.y != 0.f) M = fmaxf(M, ml.x);
-    }
-    float L = 0.f;
+    const bool mine = rh < all && row >= max(p.off[0], 0) && row < p.off[p.n_seqs];  // a row of no sequence stays as it is
+    float M = -INFINITY, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    const int c = lane * 4;
-    for (int i = 0; i < p.n_split; ++i) {
-        const float2 ml = *(const float2 *)(p.part_ml + (i * all + rh) * 2);
-        if (ml.y == 0.f) continue;  // (no key of the part is seen)
-        const float w = __builtin_amdgcn_exp2f(ml.x - M);
-        L += w * ml.y;
-        if (c < p.d) {
-            const f32x4 x = *(const f32x4 *)(p.part_o + (i * all + rh) * p.d + c);
+    if (mine) {
+        auto part = [&](int i) { return *(const float2 *)(p.part_ml + (i * all + rh) * 2); };
+        for (int i = lane; i < p.n_split; i += 32) {
+            const float2 ml = part(i);
+            if (ml.y != 0.f) M = fmaxf(M, ml.x);  // (0: no key of the part is seen)
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] += w * x[e];
+        for (int o = 1; o < 32; o *= 2) M = fmaxf(M, __shfl_xor(M, o, 64));
+        for (int i = lane; i < p.n_split; i += 32) {
+            const float2 ml = part(i);
+            if (ml.y != 0.f) L += ml.y * __builtin_amdgcn_exp2f(ml.x - M);
+        }
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) L += __shfl_xor(L, o, 64);
+#pragma unroll 4
+        for (int i = g; i < p.n_split; i += GROUPS) {
+            const float2 ml = part(i);
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            if (c < p.d) x = *(const f32x4 *)(p.part_o + (i * all + rh) * p.d + c);
+            const float w = __builtin_amdgcn_exp2f(ml.x - M);
+            if (ml.y != 0.f) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += w * x[e];
+            }
         }
     }
+    if constexpr (GROUPS > 1) {
+        sums[group][lane] = acc;
+        __syncthreads();
+        if (g != 0) return;
+#pragma unroll
+        for (int i = 1; i < GROUPS; ++i) acc += sums[group + i][lane];
+    }
+    if (!mine) return;
     const float inv = 1.f / L;
     if (c < p.d) {
 #pragma unroll
@@ -371,9 +388,15 @@ hipError_t launch_attn_paged_f32(const PagedArgs &a, hipStream_t s)
 
 hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s)
 {
-    const unsigned blocks = (unsigned)(((int64_t)a.m_total * a.H + 3) / 4);
-    if (bf16) hipLaunchKernelGGL(paged_combine_kernel<__bf16>, dim3(blocks), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(paged_combine_kernel<float>, dim3(blocks), dim3(256), 0, s, a);
+    const int64_t all = (int64_t)a.m_total * a.H;
+    auto go = [&](auto groups) {
+        constexpr int GROUPS = decltype(groups)::value;
+        const dim3 grid((unsigned)((all * GROUPS + 7) / 8));
+        if (bf16) hipLaunchKernelGGL((paged_combine_kernel<__bf16, GROUPS>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((paged_combine_kernel<float, GROUPS>), grid, dim3(256), 0, s, a);
+    };
+    if (a.n_split <= 4) go(std::integral_constant<int, 1>{});
+    else go(std::integral_constant<int, 8>{});
     return hipGetLastError();
 }
 
