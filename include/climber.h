@@ -299,7 +299,7 @@ int climber_attn_sumi_paged(const climber_config *cfg, const float *tau_layer, c
  * not NULL, move with their token; `rank` is only read.  Slots from the new length on keep what they held.
  * len_out: dev int32 [n_seqs], the new lengths (may be kv->len).  src: dev int32 [n_seqs][table_ld * page_size] or NULL: for each slot below
  * the new length the slot that its token had before, -1 from there on.  A caller with more data per token moves it by src.
- * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _BUFSIZE, _UNSUPPORTED (d_head), _RUNTIME. */
+ * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _BUFSIZE, _UNSUPPORTED (d_head; max_len over 2^22), _RUNTIME. */
 int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, const float *rank, const int32_t *budget,
                         const int32_t *keep_from, int32_t *len_out, int32_t *src, void *workspace, size_t ws_bytes, void *stream);
 

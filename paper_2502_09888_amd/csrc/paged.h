@@ -124,6 +124,10 @@ static inline int paged_mass_parts(int64_t n_seqs, int64_t Hkv, int64_t max_len,
     return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
 }
 
+// Tokens of a workgroup where a sequence may be too long for one, and the integers that it leaves for the others.
+constexpr int kEvictOne = 16384, kEvictSegment = 4096, kEvictSegInts = 4 * 2048 + 8, kEvictMostSegments = 1025;
+static inline int64_t evict_segments(int64_t max_len) { return max_len <= kEvictOne ? 0 : (max_len + kEvictSegment - 1) / kEvictSegment + 1; }
+
 struct EvictArgs {
     uint8_t *k_pages, *v_pages;
     float *mass;
@@ -131,11 +135,13 @@ struct EvictArgs {
     int32_t *stamp;
     const int32_t *table, *len, *budget, *keep_from;
     int32_t *len_out, *src;
-    int n_seqs, n_pages, page_shift, table_ld, max_len, Hkv, row_bytes;
-    uint32_t *keys;          // workspace [n_seqs][max_len]
-    uint64_t *first;         // workspace [n_seqs][ceil(max_len / 64)]: bit set: ranks before all others
-    int32_t *holes, *movers; // workspace [n_seqs][max_len / 2 + 1]
-    int32_t *n_moves;        // workspace [n_seqs]
+    int n_seqs, n_pages, page_shift, table_ld, max_len, Hkv, row_bytes, segments;
+    // workspace
+    int32_t *holes, *movers;   // [n_seqs][max_len / 2 + 1]
+    int32_t *n_moves;          // [n_seqs]
+    uint32_t *keys;            // [n_seqs][max_len]                  (segments > 0, as what follows)
+    uint64_t *first;           // [n_seqs][segments][64]: bit set: ranks before all others
+    int32_t *hists, *state;    // [n_seqs][segments][kEvictSegInts], [n_seqs][8]
 };
 hipError_t launch_paged_evict(const EvictArgs &a, hipStream_t s);
 

@@ -80,18 +80,20 @@ Layout layout_of(const climber_config *cfg, const climber_paged_kv *kv, int32_t 
 }
 
 struct EvictLayout {
-    size_t keys, first, holes, movers, n_moves, bytes;
+    size_t holes, movers, n_moves, keys, first, hists, state, bytes;
 };
 EvictLayout evict_layout(const climber_paged_kv *kv)
 {
     EvictLayout w{};
-    const size_t B = kv->n_seqs, L = kv->max_len;
-    w.keys = 0;
-    w.first = w.keys + up(B * L * 4);
-    w.holes = w.first + up(B * ((L + 63) / 64) * 8);
+    const size_t B = kv->n_seqs, L = kv->max_len, S = evict_segments(kv->max_len);
+    w.holes = 0;
     w.movers = w.holes + up(B * (L / 2 + 1) * 4);
     w.n_moves = w.movers + up(B * (L / 2 + 1) * 4);
-    w.bytes = w.n_moves + up(B * 4);
+    w.keys = w.n_moves + up(B * 4);
+    w.first = w.keys + (S ? up(B * L * 4) : 0);
+    w.hists = w.first + up(B * S * (kEvictSegment / 64) * 8);
+    w.state = w.hists + up(B * S * kEvictSegInts * 4);
+    w.bytes = w.state + up(B * 32);
     return w;
 }
 
@@ -203,7 +205,8 @@ size_t climber_paged_workspace_bytes(const climber_config *cfg, const climber_pa
     if (check_sizes(cfg, kv) != CLIMBER_OK || check_rows(cfg, m_total, m_max) != CLIMBER_OK) return 0;
     // (a smaller call may have more parts: room for as many as one can have)
     const int64_t n = most_parts(kv) * m_total * cfg->n_heads;
-    return std::max(layout_of(cfg, kv, m_total, most_parts(kv) > 1 ? (size_t)std::min(n, kPartRows) : 0).bytes, evict_layout(kv).bytes);
+    return std::max(layout_of(cfg, kv, m_total, most_parts(kv) > 1 ? (size_t)std::min(n, kPartRows) : 0).bytes,
+                    evict_segments(kv->max_len) <= kEvictMostSegments ? evict_layout(kv).bytes : 0);
 }
 
 int climber_attn_history_paged(const climber_config *cfg, const float *tau_layer, const climber_paged_kv *kv, const void *q, int64_t ld_q,
@@ -232,6 +235,7 @@ int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, c
     if (e) return e;
     if (!budget || !len_out || (!rank && !kv->mass) || (keep_from && !kv->stamp)) return CLIMBER_ERR_NULL;
     if (!aligned(rank, 4) || !aligned(budget, 4) || !aligned(keep_from, 4) || !aligned(len_out, 4) || !aligned(src, 4)) return CLIMBER_ERR_ALIGN;
+    if (evict_segments(kv->max_len) > kEvictMostSegments) return CLIMBER_ERR_UNSUPPORTED;
     const EvictLayout w = evict_layout(kv);
     if (!workspace) return CLIMBER_ERR_NULL;
     if (!aligned(workspace, 256)) return CLIMBER_ERR_ALIGN;
@@ -256,11 +260,14 @@ int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, c
     a.max_len = kv->max_len;
     a.Hkv = kv->n_kv_heads;
     a.row_bytes = (int)(cfg->d_head * elem_of(cfg));
-    a.keys = (uint32_t *)(ws + w.keys);
-    a.first = (uint64_t *)(ws + w.first);
+    a.segments = (int)evict_segments(kv->max_len);
     a.holes = (int32_t *)(ws + w.holes);
     a.movers = (int32_t *)(ws + w.movers);
     a.n_moves = (int32_t *)(ws + w.n_moves);
+    a.keys = (uint32_t *)(ws + w.keys);
+    a.first = (uint64_t *)(ws + w.first);
+    a.hists = (int32_t *)(ws + w.hists);
+    a.state = (int32_t *)(ws + w.state);
     return rt(launch_paged_evict(a, (hipStream_t)stream));
 }
 

@@ -317,7 +317,8 @@ def test_evict_ties_and_odd_ranks():
     evict(case, [0, 1, 1, 1, 1, 1, 1], rank=rank, mass=False, stamp=False, src=False)
 
 
-@pytest.mark.parametrize("n,budget", [(2047, 1000), (5000, 4999), (20011, 7), (20011, 13000)])
+@pytest.mark.parametrize("n,budget", [(1024, 512), (1025, 1024), (2047, 1000), (4096, 1), (5000, 4999), (16384, 8192),
+                                      (16385, 16384), (20011, 7), (20011, 4096), (20011, 13000), (33000, 16000)])
 def test_evict_long(n, budget):
     case = Case([n, 3], [1, 1], H=1, Hkv=1, d=4, dtype="f32", page=64, sumi=True, seed=34)
     evict(case, [budget, 1])
