@@ -25,6 +25,7 @@ using namespace paged;
 
 constexpr float kNoRef = -1.0e30f;  // "no reference yet", below any finite logit
 constexpr float kSlack = 8.0f;      // log2 units that a logit may exceed the reference by
+constexpr float kFar = 0x1p100f;    // a denominator over it: the reference was too low, see attn_paged_tile_kernel
 
 // What a workgroup knows of its sequence, and the copies of 16 keys and values into LDS.
 template <int D>
@@ -87,6 +88,18 @@ struct Source {
     }
 };
 
+// 8 dimensions of a row as a lane reads or writes them (16 bytes: the first 8 of 16 in the lower half-wave) <-> as the accumulator has
+// them (4 and 4: the first 4 of each 8 in the lower half-wave)
+static __device__ __forceinline__ void swap_pieces(u32x4 &x)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x[i], x[2 + i], false, false);
+        x[i] = r[0];
+        x[2 + i] = r[1];
+    }
+}
+
 // The softmax state of a wave's QB x 32 packed rows.
 template <int D, int QB>
 struct State {
@@ -111,7 +124,7 @@ struct State {
     __device__ __forceinline__ void own(const PagedArgs &p, int qb, int64_t row, int hk, int hf)
     {
         const __bf16 *kp = (const __bf16 *)(p.k + row * p.ld_kv) + (int64_t)hk * D + 8 * hf;
-        const __bf16 *vp = (const __bf16 *)(p.v + row * p.ld_kv) + (int64_t)hk * D + 4 * hf;
+        const __bf16 *vp = (const __bf16 *)(p.v + row * p.ld_kv) + (int64_t)hk * D + 8 * hf;
         float dot = 0.f;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
@@ -126,10 +139,14 @@ struct State {
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const bf16x4 v = *(const bf16x4 *)(vp + 32 * db + 8 * g);
+            for (int g = 0; g < 4; g += 2) {
+                u32x4 v = *(const u32x4 *)(vp + 32 * db + 8 * g);
+                swap_pieces(v);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) O[qb][db][4 * g + e] = (float)v[e];
+                for (int e = 0; e < 4; ++e) {
+                    O[qb][db][4 * g + 2 * e] = __uint_as_float(v[e] << 16);
+                    O[qb][db][4 * g + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+                }
             }
     }
     __device__ __forceinline__ void logits(const KFrags<D> &k, f32x16 (&S)[QB]) const
@@ -143,8 +160,8 @@ struct State {
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) S[qb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.a[s], q[qb][s], S[qb], 0, 0, 0);
     }
-    // S: logits of 32 keys, -inf where masked.  The reference moves where a logit exceeds it by far.
-    __device__ __forceinline__ void reference(const f32x16 (&S)[QB])
+    // S: logits of 32 keys, -inf where masked.  The reference of the rows that may moves where a logit exceeds it by far.
+    __device__ __forceinline__ void reference(const f32x16 (&S)[QB], const bool (&may)[QB])
     {
         float v[QB];
         bool need[QB], any = false;
@@ -154,7 +171,7 @@ struct State {
 #pragma unroll
             for (int i = 2; i < 16; i += 2) x = fmaxf(fmaxf(x, S[qb][i]), S[qb][i + 1]);
             v[qb] = half_max(x);
-            need[qb] = (v[qb] - m[qb]) * c[qb] > kSlack;
+            need[qb] = may[qb] && (v[qb] - m[qb]) * c[qb] > kSlack;
             any |= need[qb];
         }
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(any) != 0, 0)) {
@@ -169,6 +186,13 @@ struct State {
                     for (int i = 0; i < 16; ++i) O[qb][db][i] *= alpha;
             }
         }
+    }
+    __device__ __forceinline__ void reference(const f32x16 (&S)[QB])
+    {
+        bool may[QB];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) may[qb] = true;
+        reference(S, may);
     }
     // P: the operand of the value product
     __device__ __forceinline__ void weights(const f32x16 (&S)[QB], bf16x8 (&P)[QB][2])
@@ -293,7 +317,7 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
     constexpr int kRows = 128 * QB, kValues = kTileKeys * R::kPitch, kStage = 2 * kValues;  // keys, then values
     // (three arrays: reads of one do not wait for copies into another)
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage], stage1[kStage], stage2[kStage];
-    __shared__ int odd_seen[4];
+    __shared__ int flags[4];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
     if (!paged_work(p, w)) return;
@@ -327,13 +351,16 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
     Rows<D> at;
     at.init(lane);
     State<D, QB> st;
+    auto start = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int r = min(r_wave + qb * 32 + l32, rows - 1);
-        const int64_t row = s.row0 + r / p.G;
-        st.start(p, qb, row, w.hk * p.G + r % p.G, hf);
-        if (SUMI && w.split == 0) st.own(p, qb, row, w.hk, hf);
-    }
+        for (int qb = 0; qb < QB; ++qb) {
+            const int r = min(r_wave + qb * 32 + l32, rows - 1);
+            const int64_t row = s.row0 + r / p.G;
+            st.start(p, qb, row, w.hk * p.G + r % p.G, hf);
+            if (SUMI && w.split == 0) st.own(p, qb, row, w.hk, hf);
+        }
+    };
+    start();
     if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + kRows, rows));
 
     // all copies issued so far have landed, everywhere
@@ -347,7 +374,6 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
         bf16x8 P[QB][2];
         // Sc: this block's logits, values at v_cur; Sn: the next block's, from k_next
         auto step = [&](f32x16 (&Sc)[QB], lds_u8 *v_cur, const lds_u8 *k_next, f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
-            st.reference(Sc);
             st.logits(read_k<D>(at, k_next), Sn);
             st.weights(Sc, P);
 #pragma unroll
@@ -355,6 +381,7 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
         };
         meet();  // (tile 1 as well)
         st.logits(read_k<D>(at, stage(0)), S0);
+        st.reference(S0);
         auto tile = [&](int t, lds_u8 *prev, lds_u8 *cur, lds_u8 *next) __attribute__((always_inline)) {
             step(S0, cur + kValues, cur + 32 * R::kPitch, S1);
             meet();  // tile t + 1 is here, and nobody reads the stage of tile t - 1 any more
@@ -378,41 +405,73 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) top[qb] = min(sees(r_wave + qb * 32 + l32), k_hi);
     const int wave_hi = min(sees(r_wave + 32 * QB - 1), k_hi);
-    bool odd = false;
-#pragma unroll 1
-    for (int t = n_clean; t < n_tiles; ++t) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        odd |= clear_odd<16 * R::kPitch>(stage(t % 3) + kValues + wave * 16 * R::kPitch, lane);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        meet();
-        if (t + 2 < n_tiles) {
-            issue(t + 2, page, stage((t + 2) % 3));
-            page = page_of(t + 3);
-        }
-        lds_u8 *cur = stage(t % 3);
-#pragma unroll 1
-        for (int blk = 0; blk < 2; ++blk) {
-            const int k0 = k_lo + t * kTileKeys + blk * 32;
-            if (k0 >= wave_hi) break;
-            f32x16 S[QB];
-            bf16x8 P[QB][2];
-            st.logits(read_k<D>(at, cur + blk * 32 * R::kPitch), S);
+    bool odd = false, far[QB];
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) hide(S[qb], k0, hf, top[qb]);
-            st.reference(S);
-            st.weights(S, P);
+    for (int qb = 0; qb < QB; ++qb) far[qb] = false;
+    int from = n_clean;
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+#pragma unroll 1
+        for (int t = from; t < n_tiles; ++t) {
+            if (t >= n_clean) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                odd |= clear_odd<16 * R::kPitch>(stage(t % 3) + kValues + wave * 16 * R::kPitch, lane);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+            meet();
+            if (t + 2 < n_tiles) {
+                issue(t + 2, page, stage((t + 2) % 3));
+                page = page_of(t + 3);
+            }
+            lds_u8 *cur = stage(t % 3);
+#pragma unroll 1
+            for (int blk = 0; blk < 2; ++blk) {
+                const int k0 = k_lo + t * kTileKeys + blk * 32;
+                if (k0 >= wave_hi) break;
+                f32x16 S[QB];
+                bf16x8 P[QB][2];
+                st.logits(read_k<D>(at, cur + blk * 32 * R::kPitch), S);
 #pragma unroll
-            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, cur + kValues + (blk * 32 + g * 16) * R::kPitch), P, g);
+                for (int qb = 0; qb < QB; ++qb) hide(S[qb], k0, hf, top[qb]);
+                bool may[QB];
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) may[qb] = t >= n_clean || t + blk == 0 || far[qb];
+                st.reference(S, may);
+                st.weights(S, P);
+#pragma unroll
+                for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, cur + kValues + (blk * 32 + g * 16) * R::kPitch), P, g);
+            }
         }
+        if (again || n_clean == 0) break;
+        // Weights far above the reference of the first block: all of it again, block by block.  The reference of the rows that have them may
+        // move then; the others' results are made in the same way again, and do not depend on their neighbours.
+        bool some = false;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            far[qb] = !(st.l[qb] + other_half(st.l[qb]) < kFar);
+            some |= far[qb];
+        }
+        const int wave_far = __builtin_amdgcn_ballot_w64(some) != 0;
+        if (lane == 0) flags[wave] = wave_far;
+        __syncthreads();
+        const bool any = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+        __syncthreads();
+        if (__builtin_expect(!any, 1)) break;
+        start();
+        odd = false;
+        from = 0;
+        issue(0, page_of(0), stage(0));
+        if (n_tiles > 1) issue(1, page_of(1), stage(1));
+        page = page_of(2);
     }
 
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
         const int r = r_wave + qb * 32 + l32;
         const float l = st.l[qb] + other_half(st.l[qb]);
-        if (r >= rows) continue;
-        const int64_t row = s.row0 + r / p.G, rh = row * p.H + w.hk * p.G + r % p.G;
+        const int64_t row = s.row0 + r / p.G, rh = row * p.H + w.hk * p.G + r % p.G;  // (r >= rows: not stored)
         if (p.n_split > 1) {
+            if (r >= rows) continue;
             float *po = p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D + 4 * hf;
 #pragma unroll
             for (int db = 0; db < D / 32; ++db)
@@ -424,21 +483,23 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
             continue;
         }
         const float inv = 1.f / l;
-        __bf16 *op = (__bf16 *)(p.o + row * p.ld_o) + (int64_t)(w.hk * p.G + r % p.G) * D + 4 * hf;
+        __bf16 *op = (__bf16 *)(p.o + row * p.ld_o) + (int64_t)(w.hk * p.G + r % p.G) * D + 8 * hf;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                bf16x4 x;
+            for (int g = 0; g < 4; g += 2) {
+                bf16x8 x;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = (__bf16)(st.O[qb][db][4 * g + e] * inv);
-                *(bf16x4 *)(op + 32 * db + 8 * g) = x;
+                for (int e = 0; e < 8; ++e) x[e] = (__bf16)(st.O[qb][db][4 * g + e] * inv);
+                u32x4 y = __builtin_bit_cast(u32x4, x);
+                swap_pieces(y);
+                if (r < rows) *(u32x4 *)(op + 32 * db + 8 * g) = y;
             }
-        if (hf == 0 && p.lse) p.lse[rh] = float2{st.c[qb], st.m[qb] * st.c[qb] + __builtin_amdgcn_logf(l)};
+        if (hf == 0 && p.lse && r < rows) p.lse[rh] = float2{st.c[qb], st.m[qb] * st.c[qb] + __builtin_amdgcn_logf(l)};
     }
-    if (lane == 0) odd_seen[wave] = odd;
+    if (lane == 0) flags[wave] = odd;
     __syncthreads();
-    if (__builtin_expect(odd_seen[0] | odd_seen[1] | odd_seen[2] | odd_seen[3], 0))
+    if (__builtin_expect(flags[0] | flags[1] | flags[2] | flags[3], 0))
         put_odd<D>(p, s, w, k_lo + n_clean * kTileKeys, k_hi, r_wave, min(r_wave + 32 * QB, rows), sees);
 }
 
