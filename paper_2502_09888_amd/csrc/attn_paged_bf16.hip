@@ -27,29 +27,31 @@ constexpr float kNoRef = -1.0e30f;  // "no reference yet", below any finite logi
 constexpr float kSlack = 8.0f;      // log2 units that a logit may exceed the reference by
 constexpr float kFar = 0x1p100f;    // a denominator over it: the reference was too low, see attn_paged_tile_kernel
 
-// What a workgroup knows of its sequence, and the copies of 16 keys and values into LDS.
-template <int D>
+// What a wave knows of its sequence, and its copies of keys and values into LDS: LOADS times 1 KiB of the rows of 16 keys, from the
+// FIRST-th on.
+template <int D, int LOADS>
 struct Source {
+    using R = Rows<D>;
     const PagedArgs &p;
     PagedSeq s;
-    int b, hk, k_hi, lane;
-    uint32_t page_off[Rows<D>::kLoads], row_off[Rows<D>::kLoads];  // of this lane's piece, per load: rows of a page, rows of the call
-    const uint8_t *k_new, *v_new;                                  // row 0 of the call's rows of this sequence and head
+    int b, hk, k_hi, lane, first;
+    uint32_t page_off[LOADS], row_off[LOADS];  // of this lane's piece, per load: in rows of a page, in rows of the call
+    const uint8_t *k_new, *v_new;              // row 0 of the call's rows of this sequence and head
 
-    __device__ __forceinline__ Source(const PagedArgs &p_, const PagedSeq &s_, int b_, int hk_, int k_hi_, int lane_)
-        : p(p_), s(s_), b(b_), hk(hk_), k_hi(k_hi_), lane(lane_)
+    __device__ __forceinline__ Source(const PagedArgs &p_, const PagedSeq &s_, int b_, int hk_, int k_hi_, int lane_, int first_)
+        : p(p_), s(s_), b(b_), hk(hk_), k_hi(k_hi_), lane(lane_), first(first_)
     {
-        using R = Rows<D>;
 #pragma unroll
-        for (int i = 0; i < R::kLoads; ++i) {
-            const int r = i * R::kPerLoad + lane / R::kPieces, c = (lane % R::kPieces) ^ R::f(r);
-            page_off[i] = r * R::kPitch + c * 16;
-            row_off[i] = (uint32_t)r * (uint32_t)p.ld_kv + c * 16;
+        for (int i = 0; i < LOADS; ++i) {
+            page_off[i] = row(i) * R::kPitch + piece(i);
+            row_off[i] = (uint32_t)row(i) * (uint32_t)p.ld_kv + piece(i);
         }
         const int64_t at = s.row0 * p.ld_kv + (int64_t)hk * R::kPitch;
         k_new = p.k + at;
         v_new = p.v + at;
     }
+    __device__ __forceinline__ int row(int i) const { return (first + i) * R::kPerLoad + lane / R::kPieces; }
+    __device__ __forceinline__ int piece(int i) const { return ((lane % R::kPieces) ^ R::f(row(i))) * 16; }
     // the page of keys g .. g + 15 (a multiple of 16: they lie in one page), or of the last key, which stands for those behind it
     __device__ __forceinline__ int page_of(int g) const
     {
@@ -57,29 +59,28 @@ struct Source {
         const const_i32 *t = (const const_i32 *)(p.table + (int64_t)b * p.table_ld);
         return min(max(t[__builtin_amdgcn_readfirstlane(slot >> p.page_shift)], 0), p.n_pages - 1);
     }
-    // keys g .. g + 15 to LDS rows at to_k, to_v (wave-uniform)
+    // of keys g .. g + 15 to LDS at to_k, to_v (wave-uniform)
     __device__ __forceinline__ void issue(int g, int page, lds_u8 *to_k, lds_u8 *to_v) const
     {
-        using R = Rows<D>;
         if (g + 16 <= min(s.n, k_hi)) {
             const int64_t at = paged_row(p, page, hk, g);
 #pragma unroll
-            for (int i = 0; i < R::kLoads; ++i) {
+            for (int i = 0; i < LOADS; ++i) {
                 copy16((glb_u8 *)(p.k_pages + at) + page_off[i], to_k + i * 1024);
                 copy16((glb_u8 *)(p.v_pages + at) + page_off[i], to_v + i * 1024);
             }
         } else if (g >= s.n && g + 16 <= k_hi) {
             const int64_t at = (g - s.n) * p.ld_kv;
 #pragma unroll
-            for (int i = 0; i < R::kLoads; ++i) {
+            for (int i = 0; i < LOADS; ++i) {
                 copy16((glb_u8 *)(k_new + at) + row_off[i], to_k + i * 1024);
                 copy16((glb_u8 *)(v_new + at) + row_off[i], to_v + i * 1024);
             }
         } else {  // cached and new ones, or fewer than 16: the last key again in the places behind it
 #pragma unroll
-            for (int i = 0; i < R::kLoads; ++i) {
-                const int r = i * R::kPerLoad + lane / R::kPieces, j = min(g + r, k_hi - 1), c = ((lane % R::kPieces) ^ R::f(r)) * 16;
-                const int64_t cached = paged_row(p, page, hk, j) + c, fresh = (int64_t)(j - s.n) * p.ld_kv + c;
+            for (int i = 0; i < LOADS; ++i) {
+                const int j = min(g + row(i), k_hi - 1);
+                const int64_t cached = paged_row(p, page, hk, j) + piece(i), fresh = (int64_t)(j - s.n) * p.ld_kv + piece(i);
                 const bool old = j < s.n;
                 copy16((glb_u8 *)(old ? p.k_pages + cached : k_new + fresh), to_k + i * 1024);
                 copy16((glb_u8 *)(old ? p.v_pages + cached : v_new + fresh), to_v + i * 1024);
@@ -304,19 +305,18 @@ static __device__ __forceinline__ void store_new(const PagedArgs &p, const Paged
 }
 
 // ---- tiles ---------------------------------------------------------------------------------------
-constexpr int kTileKeys = 64;
-
-// 4 waves of QB x 32 packed rows over a ring of three stages of 64 keys.  The keys that every row of the tile sees go through a
-// pipeline over blocks of 32: while the exponentials of block j are made, the matrix pipe has the logits of block j + 1.  The rest (the diagonal of the causal mask, the end of the keys) block by block.
-// D = 128, QB = 2: one wave per SIMD with its 512 registers; each fragment serves 64 rows, without which LDS reads (16 KiB per 32 keys and
-// wave) take as long as the products.
+// 4 waves of QB x 32 packed rows over a ring of four stages of 32 keys.  Keys that every row of the tile sees go through a pipeline: while
+// the exponentials of a block are made, the matrix pipe has the logits of the next one, and two more are on their way.  The rest (the diagonal
+// of the causal mask, the end of the keys) block by block.  Two waves per SIMD, so 256 registers: QB = 2 at D = 64; at D = 128, where
+// outputs and queries of 64 rows would be 192 of them, QB = 1.
 template <int D, int QB, bool SUMI>
-__global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_tile_kernel(const PagedArgs p)
+__global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs p)
 {
     using R = Rows<D>;
-    constexpr int kRows = 128 * QB, kValues = kTileKeys * R::kPitch, kStage = 2 * kValues;  // keys, then values
-    // (three arrays: reads of one do not wait for copies into another)
-    __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage], stage1[kStage], stage2[kStage];
+    constexpr int kRows = 128 * QB, kValues = 32 * R::kPitch, kStage = 2 * kValues;  // keys, then values
+    constexpr int kShare = 8 * R::kPitch, kCopies = kShare / 1024;                   // a wave's part of either; copies of it
+    // (four arrays: reads of one do not wait for copies into another)
+    __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage], stage1[kStage], stage2[kStage], stage3[kStage];
     __shared__ int flags[4];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
@@ -329,24 +329,25 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
     const int k_all = SUMI ? s.n : s.n + s.T;
     auto sees = [&](int r) { return causal ? s.n + min(r, rows - 1) / p.G + 1 : k_all; };  // packed row r sees keys below it
     int k_lo, k_hi;
-    paged_part(p, w.split, sees(r_tile + kRows - 1), kTileKeys, k_lo, k_hi);
+    paged_part(p, w.split, sees(r_tile + kRows - 1), 32, k_lo, k_hi);
     k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
-    const int n_tiles = (k_hi - k_lo + kTileKeys - 1) / kTileKeys;
-    const int n_clean = __builtin_amdgcn_readfirstlane(max(0, min(sees(r_tile), k_hi) - k_lo) / kTileKeys);
+    const int n_blocks = (k_hi - k_lo + 31) / 32, n_clean = __builtin_amdgcn_readfirstlane(max(0, min(sees(r_tile), k_hi) - k_lo) / 32);
 
-    const Source<D> src(p, s, w.b, w.hk, k_hi, lane);
-    auto stage = [&](int i) __attribute__((always_inline)) { return (lds_u8 *)(i == 0 ? stage0 : i == 1 ? stage1 : stage2); };
-    // this wave's 16 of the 64 keys of tile i
+    const Source<D, kCopies> src(p, s, w.b, w.hk, k_hi, lane, (wave & 1) * kCopies);
+    auto stage = [&](int i) __attribute__((always_inline)) { return (lds_u8 *)(i == 0 ? stage0 : i == 1 ? stage1 : i == 2 ? stage2 : stage3); };
+    // this wave's 8 of the 32 keys of block i
     auto issue = [&](int i, int page, lds_u8 *to) __attribute__((always_inline)) {
-        src.issue(k_lo + i * kTileKeys + wave * 16, page, to + wave * 16 * R::kPitch, to + kValues + wave * 16 * R::kPitch);
+        src.issue(k_lo + i * 32 + (wave >> 1) * 16, page, to + wave * kShare, to + kValues + wave * kShare);
     };
-    auto page_of = [&](int i) __attribute__((always_inline)) { return src.page_of(k_lo + i * kTileKeys + wave * 16); };
+    auto page_of = [&](int i) __attribute__((always_inline)) { return src.page_of(k_lo + i * 32 + (wave >> 1) * 16); };
     int page = 0;
-    if (n_tiles > 0) {
-        issue(0, page_of(0), stage(0));
-        if (n_tiles > 1) issue(1, page_of(1), stage(1));
-        page = page_of(2);
-    }
+    auto issue_first = [&]() __attribute__((always_inline)) {
+        if (n_blocks > 0) issue(0, page_of(0), stage(0));
+        if (n_blocks > 1) issue(1, page_of(1), stage(1));
+        if (n_blocks > 2) issue(2, page_of(2), stage(2));
+        if (n_blocks > 3) page = page_of(3);
+    };
+    issue_first();
 
     Rows<D> at;
     at.init(lane);
@@ -363,44 +364,49 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
     start();
     if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + kRows, rows));
 
-    // all copies issued so far have landed, everywhere
+    // this wave's copies have landed but for those of `later` blocks, the last ones issued
+    auto landed = [&](int later) __attribute__((always_inline)) {
+        static_assert(kCopies == 1 || kCopies == 2, "vmcnt immediates");
+        if (later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kCopies) : "memory");
+        else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
     auto meet = [&]() __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
     if (n_clean > 0) {
         f32x16 S0[QB], S1[QB];
         bf16x8 P[QB][2];
-        // Sc: this block's logits, values at v_cur; Sn: the next block's, from k_next
-        auto step = [&](f32x16 (&Sc)[QB], lds_u8 *v_cur, const lds_u8 *k_next, f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
-            st.logits(read_k<D>(at, k_next), Sn);
-            st.weights(Sc, P);
-#pragma unroll
-            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, v_cur + g * 16 * R::kPitch), P, g);
-        };
-        meet();  // (tile 1 as well)
+        landed(min(n_blocks - 1, 2));
+        meet();
         st.logits(read_k<D>(at, stage(0)), S0);
         st.reference(S0);
-        auto tile = [&](int t, lds_u8 *prev, lds_u8 *cur, lds_u8 *next) __attribute__((always_inline)) {
-            step(S0, cur + kValues, cur + 32 * R::kPitch, S1);
-            meet();  // tile t + 1 is here, and nobody reads the stage of tile t - 1 any more
-            if (t + 2 < n_tiles) {
-                issue(t + 2, page, prev);
-                page = page_of(t + 3);
+        // block j: its logits in Sc, values in cur; the next one's keys in next; prev is free
+        auto step = [&](int j, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB], lds_u8 *prev, lds_u8 *cur, lds_u8 *next) __attribute__((always_inline)) {
+            landed(min(1, n_blocks - 2 - j));
+            meet();  // block j + 1 is here, and nobody reads block j - 1 any more
+            if (j + 3 < n_blocks) {
+                issue(j + 3, page, prev);
+                page = page_of(j + 4);
             }
-            step(S1, cur + kValues + 32 * R::kPitch, next, S0);  // (behind the last tile S0 is not used)
+            st.logits(read_k<D>(at, next), Sn);  // (behind the last block: not used)
+            st.weights(Sc, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, cur + kValues + g * 16 * R::kPitch), P, g);
         };
-        for (int t = 0; t < n_clean;) {
-            tile(t, stage(2), stage(0), stage(1));
-            if (++t == n_clean) break;
-            tile(t, stage(0), stage(1), stage(2));
-            if (++t == n_clean) break;
-            tile(t, stage(1), stage(2), stage(0));
-            ++t;
+        for (int j = 0; j < n_clean;) {
+            step(j, S0, S1, stage(3), stage(0), stage(1));
+            if (++j == n_clean) break;
+            step(j, S1, S0, stage(0), stage(1), stage(2));
+            if (++j == n_clean) break;
+            step(j, S0, S1, stage(1), stage(2), stage(3));
+            if (++j == n_clean) break;
+            step(j, S1, S0, stage(2), stage(3), stage(0));
+            ++j;
         }
     }
-    // tiles that not every row sees whole
+    // blocks that not every row sees whole
     int top[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) top[qb] = min(sees(r_wave + qb * 32 + l32), k_hi);
@@ -412,35 +418,33 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
 #pragma unroll 1
     for (bool again = false;; again = true) {
 #pragma unroll 1
-        for (int t = from; t < n_tiles; ++t) {
-            if (t >= n_clean) {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                odd |= clear_odd<16 * R::kPitch>(stage(t % 3) + kValues + wave * 16 * R::kPitch, lane);
+        for (int j = from; j < n_blocks; ++j) {
+            lds_u8 *cur = stage(j & 3);
+            landed(min(2, n_blocks - 1 - j));
+            if (j >= n_clean) {
+                odd |= clear_odd<kShare>(cur + kValues + wave * kShare, lane);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
             meet();
-            if (t + 2 < n_tiles) {
-                issue(t + 2, page, stage((t + 2) % 3));
-                page = page_of(t + 3);
+            if (j + 3 < n_blocks) {
+                issue(j + 3, page, stage((j + 3) & 3));
+                page = page_of(j + 4);
             }
-            lds_u8 *cur = stage(t % 3);
-#pragma unroll 1
-            for (int blk = 0; blk < 2; ++blk) {
-                const int k0 = k_lo + t * kTileKeys + blk * 32;
-                if (k0 >= wave_hi) break;
-                f32x16 S[QB];
-                bf16x8 P[QB][2];
-                st.logits(read_k<D>(at, cur + blk * 32 * R::kPitch), S);
+            const int k0 = k_lo + j * 32;
+            if (k0 >= wave_hi) continue;
+            f32x16 S[QB];
+            bf16x8 P[QB][2];
+            bool may[QB];
+            st.logits(read_k<D>(at, cur), S);
 #pragma unroll
-                for (int qb = 0; qb < QB; ++qb) hide(S[qb], k0, hf, top[qb]);
-                bool may[QB];
-#pragma unroll
-                for (int qb = 0; qb < QB; ++qb) may[qb] = t >= n_clean || t + blk == 0 || far[qb];
-                st.reference(S, may);
-                st.weights(S, P);
-#pragma unroll
-                for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, cur + kValues + (blk * 32 + g * 16) * R::kPitch), P, g);
+            for (int qb = 0; qb < QB; ++qb) {
+                hide(S[qb], k0, hf, top[qb]);
+                may[qb] = j >= n_clean || j == 0 || far[qb];
             }
+            st.reference(S, may);
+            st.weights(S, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, cur + kValues + g * 16 * R::kPitch), P, g);
         }
         if (again || n_clean == 0) break;
         // Weights far above the reference of the first block: all of it again, block by block.  The reference of the rows that have them may
@@ -460,9 +464,7 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
         start();
         odd = false;
         from = 0;
-        issue(0, page_of(0), stage(0));
-        if (n_tiles > 1) issue(1, page_of(1), stage(1));
-        page = page_of(2);
+        issue_first();
     }
 
 #pragma unroll
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(256, D == 128 && QB == 2 ? 1 : 2) void attn_paged_t
     if (lane == 0) flags[wave] = odd;
     __syncthreads();
     if (__builtin_expect(flags[0] | flags[1] | flags[2] | flags[3], 0))
-        put_odd<D>(p, s, w, k_lo + n_clean * kTileKeys, k_hi, r_wave, min(r_wave + 32 * QB, rows), sees);
+        put_odd<D>(p, s, w, k_lo + n_clean * 32, k_hi, r_wave, min(r_wave + 32 * QB, rows), sees);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------
@@ -529,7 +531,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
     const int n_blk = (k_hi - k_lo + 31) / 32, mine = n_blk > wave ? (n_blk - wave + 3) / 4 : 0;  // blocks wave, wave + 4, ...
 
-    const Source<D> src(p, s, w.b, w.hk, k_hi, lane);
+    const Source<D, R::kLoads> src(p, s, w.b, w.hk, k_hi, lane, 0);
     lds_u8 *const at0 = (lds_u8 *)stage0 + wave * kStage, *const at1 = (lds_u8 *)stage1 + wave * kStage;
     auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
         const int k0 = k_lo + (i * 4 + wave) * 32;
@@ -644,8 +646,9 @@ template <int D, bool SUMI>
 hipError_t launch(PagedArgs p, hipStream_t s)
 {
     const int64_t rows = (int64_t)p.m_max * p.G;
-    void (*kernel)(PagedArgs) = attn_paged_tile_kernel<D, 2, SUMI>;
-    int tile = 256;
+    constexpr int QB = D == 64 ? 2 : 1;
+    void (*kernel)(PagedArgs) = attn_paged_tile_kernel<D, QB, SUMI>;
+    int tile = 128 * QB;
     if (rows <= kPagedFewRows) kernel = attn_paged_few_kernel<D, SUMI>, tile = 32;
     else if (rows <= 128) kernel = attn_paged_tile_kernel<D, 1, SUMI>, tile = 128;
     p.n_tiles = (int)((rows + tile - 1) / tile);
