@@ -27,6 +27,14 @@ constexpr float kNoRef = -1.0e30f;  // "no reference yet", below any finite logi
 constexpr float kSlack = 8.0f;      // log2 units that a logit may exceed the reference by
 constexpr float kFar = 0x1p100f;    // a denominator over it: the reference was too low, see attn_paged_tile_kernel
 
+// a pointer that is the same in all lanes, in scalar registers
+static __device__ __forceinline__ const uint8_t *uniform(const uint8_t *p)
+{
+    const uint64_t a = (uint64_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return (const uint8_t *)(((uint64_t)hi << 32) | lo);
+}
+
 // What a wave knows of its sequence, and its copies of keys and values into LDS: LOADS times 1 KiB of the rows of 16 keys, from the
 // FIRST-th on.
 template <int D, int LOADS>
@@ -34,56 +42,62 @@ struct Source {
     using R = Rows<D>;
     const PagedArgs &p;
     PagedSeq s;
-    int b, hk, k_hi, lane, first;
+    int hk, k_hi, cached, lane, first;         // cached: keys below it are in pages (and below k_hi)
     uint32_t page_off[LOADS], row_off[LOADS];  // of this lane's piece, per load: in rows of a page, in rows of the call
-    const uint8_t *k_new, *v_new;              // row 0 of the call's rows of this sequence and head
+    const uint8_t *k_page, *k_new;             // the head's keys of page 0; of the sequence's first row of the call
+    int64_t to_v_page, to_v_new, page_bytes;   // from a key to its value; from a page to the next
+    const int32_t *table;
 
-    __device__ __forceinline__ Source(const PagedArgs &p_, const PagedSeq &s_, int b_, int hk_, int k_hi_, int lane_, int first_)
-        : p(p_), s(s_), b(b_), hk(hk_), k_hi(k_hi_), lane(lane_), first(first_)
+    __device__ __forceinline__ Source(const PagedArgs &p_, const PagedSeq &s_, int b, int hk_, int k_hi_, int lane_, int first_)
+        : p(p_), s(s_), hk(hk_), k_hi(k_hi_), cached(min(s_.n, k_hi_)), lane(lane_), first(first_)
     {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             page_off[i] = row(i) * R::kPitch + piece(i);
             row_off[i] = (uint32_t)row(i) * (uint32_t)p.ld_kv + piece(i);
         }
-        const int64_t at = s.row0 * p.ld_kv + (int64_t)hk * R::kPitch;
-        k_new = p.k + at;
-        v_new = p.v + at;
+        const int64_t in_page = ((int64_t)hk << p.page_shift) * R::kPitch, at = s.row0 * p.ld_kv + (int64_t)hk * R::kPitch;
+        page_bytes = ((int64_t)p.Hkv << p.page_shift) * R::kPitch;
+        k_page = uniform(p.k_pages + in_page);
+        k_new = uniform(p.k + at);
+        to_v_page = p.v_pages - p.k_pages;
+        to_v_new = p.v - p.k;
+        table = p.table + (int64_t)b * p.table_ld;
     }
     __device__ __forceinline__ int row(int i) const { return (first + i) * R::kPerLoad + lane / R::kPieces; }
     __device__ __forceinline__ int piece(int i) const { return ((lane % R::kPieces) ^ R::f(row(i))) * 16; }
-    // the page of keys g .. g + 15 (a multiple of 16: they lie in one page), or of the last key, which stands for those behind it
-    __device__ __forceinline__ int page_of(int g) const
+    // of key g (groups of 16 lie in one page), or of the last cached key, which stands for those behind it
+    __device__ __forceinline__ int page_number(int g) const
     {
-        const int slot = max(0, min(min(g, k_hi - 1), s.n - 1));
-        const const_i32 *t = (const const_i32 *)(p.table + (int64_t)b * p.table_ld);
-        return min(max(t[__builtin_amdgcn_readfirstlane(slot >> p.page_shift)], 0), p.n_pages - 1);
+        return min(max(table[max(min(g, cached - 1), 0) >> p.page_shift], 0), p.n_pages - 1);
     }
-    // of keys g .. g + 15 to LDS at to_k, to_v (wave-uniform)
+    // of keys g .. g + 15, which lie in `page`, to LDS at to_k, to_v (wave-uniform)
     __device__ __forceinline__ void issue(int g, int page, lds_u8 *to_k, lds_u8 *to_v) const
     {
-        if (g + 16 <= min(s.n, k_hi)) {
-            const int64_t at = paged_row(p, page, hk, g);
+        const int in_page = (1 << p.page_shift) - 1;
+        if (g + 16 <= cached) {
+            const uint8_t *k = uniform(k_page + page * page_bytes + (g & in_page) * R::kPitch), *v = uniform(k + to_v_page);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                copy16((glb_u8 *)(p.k_pages + at) + page_off[i], to_k + i * 1024);
-                copy16((glb_u8 *)(p.v_pages + at) + page_off[i], to_v + i * 1024);
+                copy16((glb_u8 *)k + page_off[i], to_k + i * 1024);
+                copy16((glb_u8 *)v + page_off[i], to_v + i * 1024);
             }
         } else if (g >= s.n && g + 16 <= k_hi) {
-            const int64_t at = (g - s.n) * p.ld_kv;
+            const uint8_t *k = uniform(k_new + (g - s.n) * p.ld_kv), *v = uniform(k + to_v_new);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
-                copy16((glb_u8 *)(k_new + at) + row_off[i], to_k + i * 1024);
-                copy16((glb_u8 *)(v_new + at) + row_off[i], to_v + i * 1024);
+                copy16((glb_u8 *)k + row_off[i], to_k + i * 1024);
+                copy16((glb_u8 *)v + row_off[i], to_v + i * 1024);
             }
         } else {  // cached and new ones, or fewer than 16: the last key again in the places behind it
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
                 const int j = min(g + row(i), k_hi - 1);
-                const int64_t cached = paged_row(p, page, hk, j) + piece(i), fresh = (int64_t)(j - s.n) * p.ld_kv + piece(i);
                 const bool old = j < s.n;
-                copy16((glb_u8 *)(old ? p.k_pages + cached : k_new + fresh), to_k + i * 1024);
-                copy16((glb_u8 *)(old ? p.v_pages + cached : v_new + fresh), to_v + i * 1024);
+                const uint8_t *cached_k = k_page + page * page_bytes + (j & in_page) * R::kPitch + piece(i), *new_k = k_new + (j - s.n) * p.ld_kv + piece(i);
+                const uint8_t *cached_v = cached_k + to_v_page, *new_v = new_k + to_v_new;
+                copy16((glb_u8 *)(old ? cached_k : new_k), to_k + i * 1024);
+                copy16((glb_u8 *)(old ? cached_v : new_v), to_v + i * 1024);
             }
         }
     }
@@ -179,7 +193,7 @@ struct State {
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
                 const float alpha = need[qb] ? __builtin_amdgcn_exp2f((m[qb] - v[qb]) * c[qb]) : 1.f;
-                m[qb] = need[qb] ? v[qb] : m[qb];
+                if (need[qb]) m[qb] = v[qb];
                 l[qb] *= alpha;
 #pragma unroll
                 for (int db = 0; db < D / 32; ++db)
@@ -195,23 +209,26 @@ struct State {
         for (int qb = 0; qb < QB; ++qb) may[qb] = true;
         reference(S, may);
     }
-    // P: the operand of the value product
-    __device__ __forceinline__ void weights(const f32x16 (&S)[QB], bf16x8 (&P)[QB][2])
+    // P: the operand of the value product for 16 of the 32 keys
+    __device__ __forceinline__ void weights(const f32x16 (&S)[QB], bf16x8 (&P)[QB][2], int g)
     {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             const float sub = m[qb] * c[qb];
             float sum = 0.f;
 #pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(S[qb][8 * g + e], c[qb], -sub));
-                    sum += x;
-                    P[qb][g][e] = (__bf16)x;
-                }
+            for (int e = 0; e < 8; ++e) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(S[qb][8 * g + e], c[qb], -sub));
+                sum += x;
+                P[qb][g][e] = (__bf16)x;
+            }
             l[qb] += sum;
         }
+    }
+    __device__ __forceinline__ void weights(const f32x16 (&S)[QB], bf16x8 (&P)[QB][2])
+    {
+        weights(S, P, 0);
+        weights(S, P, 1);
     }
     // 16 keys' values
     __device__ __forceinline__ void add(const VFrags<D> &v, const bf16x8 (&P)[QB][2], int g)
@@ -336,16 +353,19 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
     const Source<D, kCopies> src(p, s, w.b, w.hk, k_hi, lane, (wave & 1) * kCopies);
     auto stage = [&](int i) __attribute__((always_inline)) { return (lds_u8 *)(i == 0 ? stage0 : i == 1 ? stage1 : i == 2 ? stage2 : stage3); };
     // this wave's 8 of the 32 keys of block i
-    auto issue = [&](int i, int page, lds_u8 *to) __attribute__((always_inline)) {
-        src.issue(k_lo + i * 32 + (wave >> 1) * 16, page, to + wave * kShare, to + kValues + wave * kShare);
+    const int k_mine = k_lo + (wave >> 1) * 16;
+    int pages = 0, pages_next = 0;  // page numbers of 64 of the wave's groups of 16 keys, one in each lane, and of the 64 after them
+    auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
+        if ((i & 63) == 0) {
+            pages = i == 0 ? src.page_number(k_mine + lane * 32) : pages_next;
+            pages_next = src.page_number(k_mine + (i + 64 + lane) * 32);
+        }
+        src.issue(k_mine + i * 32, __builtin_amdgcn_readlane(pages, i & 63), to + wave * kShare, to + kValues + wave * kShare);
     };
-    auto page_of = [&](int i) __attribute__((always_inline)) { return src.page_of(k_lo + i * 32 + (wave >> 1) * 16); };
-    int page = 0;
     auto issue_first = [&]() __attribute__((always_inline)) {
-        if (n_blocks > 0) issue(0, page_of(0), stage(0));
-        if (n_blocks > 1) issue(1, page_of(1), stage(1));
-        if (n_blocks > 2) issue(2, page_of(2), stage(2));
-        if (n_blocks > 3) page = page_of(3);
+        if (n_blocks > 0) issue(0, stage(0));
+        if (n_blocks > 1) issue(1, stage(1));
+        if (n_blocks > 2) issue(2, stage(2));
     };
     issue_first();
 
@@ -386,14 +406,15 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         auto step = [&](int j, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB], lds_u8 *prev, lds_u8 *cur, lds_u8 *next) __attribute__((always_inline)) {
             landed(min(1, n_blocks - 2 - j));
             meet();  // block j + 1 is here, and nobody reads block j - 1 any more
-            if (j + 3 < n_blocks) {
-                issue(j + 3, page, prev);
-                page = page_of(j + 4);
-            }
-            st.logits(read_k<D>(at, next), Sn);  // (behind the last block: not used)
+            if (j + 3 < n_blocks) issue(j + 3, prev);
+            const KFrags<D> k = read_k<D>(at, next);
+            __builtin_amdgcn_sched_barrier(0);
+            st.logits(k, Sn);  // (behind the last block: not used)
             st.weights(Sc, P);
-#pragma unroll
-            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, cur + kValues + g * 16 * R::kPitch), P, g);
+            const VFrags<D> v0 = read_v<D>(at, cur + kValues), v1 = read_v<D>(at, cur + kValues + 16 * R::kPitch);
+            __builtin_amdgcn_sched_barrier(0x40f);
+            st.add(v0, P, 0);
+            st.add(v1, P, 1);
         };
         for (int j = 0; j < n_clean;) {
             step(j, S0, S1, stage(3), stage(0), stage(1));
@@ -426,10 +447,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             }
             meet();
-            if (j + 3 < n_blocks) {
-                issue(j + 3, page, stage((j + 3) & 3));
-                page = page_of(j + 4);
-            }
+            if (j + 3 < n_blocks) issue(j + 3, stage((j + 3) & 3));
             const int k0 = k_lo + j * 32;
             if (k0 >= wave_hi) continue;
             f32x16 S[QB];
@@ -533,11 +551,17 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
 
     const Source<D, R::kLoads> src(p, s, w.b, w.hk, k_hi, lane, 0);
     lds_u8 *const at0 = (lds_u8 *)stage0 + wave * kStage, *const at1 = (lds_u8 *)stage1 + wave * kStage;
+    // groups of 16 keys: blocks wave, wave + 4, ... of 32; the lower 32 lanes look up the first groups of 32 blocks, the upper the second
+    const int k_mine = k_lo + wave * 32 - (lane >> 5) * (32 * 128 - 16);
+    int pages = 0, pages_next = 0;
     auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
+        if ((i & 31) == 0) {
+            pages = i == 0 ? src.page_number(k_mine + lane * 128) : pages_next;
+            pages_next = src.page_number(k_mine + (i + 32 + lane) * 128);
+        }
         const int k0 = k_lo + (i * 4 + wave) * 32;
-        const int p0 = src.page_of(k0), p1 = src.page_of(k0 + 16);
-        src.issue(k0, p0, to, to + 32 * R::kPitch);
-        src.issue(k0 + 16, p1, to + 16 * R::kPitch, to + 48 * R::kPitch);
+        src.issue(k0, __builtin_amdgcn_readlane(pages, i & 31), to, to + 32 * R::kPitch);
+        src.issue(k0 + 16, __builtin_amdgcn_readlane(pages, 32 + (i & 31)), to + 16 * R::kPitch, to + 48 * R::kPitch);
     };
     if (mine > 0) issue(0, at0);
     if (mine > 1) issue(1, at1);
