@@ -122,28 +122,44 @@ struct State {
     f32x16 O[QB][D / 32];
     float c[QB], m[QB], l[QB];  // scale; reference (raw logit); this half-wave's share of the denominator
 
-    __device__ __forceinline__ void start(const PagedArgs &p, int qb, int64_t row, int h, int hf)
+    // A row's inputs are requested together, and made use of later: all of them are on their way before the first is waited for.
+    struct Row {
+        u32x4 k[D / 16], v[D / 16];
+        int at;  // its temperature's place
+    };
+    template <bool OWN>
+    __device__ __forceinline__ void request(const PagedArgs &p, int qb, int64_t row, int h, int hk, int hf, Row &in)
     {
-        const __bf16 *qp = (const __bf16 *)(p.q + row * p.ld_q) + (int64_t)h * D + 8 * hf;
+        const int sc = p.scen[row], bh = p.beh[row];
+        const u32x4 *qp = (const u32x4 *)(p.q + row * p.ld_q + (int64_t)h * (2 * D)) + hf;
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) q[qb][s] = *(const bf16x8 *)(qp + 16 * s);
-        c[qb] = paged_row_scale(p, row);
+        for (int s = 0; s < D / 16; ++s) q[qb][s] = __builtin_bit_cast(bf16x8, qp[2 * s]);
+        if (OWN) {
+            const u32x4 *kp = (const u32x4 *)(p.k + row * p.ld_kv + (int64_t)hk * (2 * D)) + hf, *vp = (const u32x4 *)(p.v + row * p.ld_kv + (int64_t)hk * (2 * D)) + hf;
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                in.k[s] = kp[2 * s];
+                in.v[s] = vp[2 * s];
+            }
+        }
+        in.at = min(max(sc, 0), p.n_scen - 1) * p.n_beh + min(max(bh, 0), p.n_beh - 1);
+    }
+    // OWN: the row's own key and value are the first member of its softmax (candidates, one part of the keys)
+    template <bool OWN>
+    __device__ __forceinline__ void start(const PagedArgs &p, int qb, int hf, const Row &in, bool own)
+    {
+        c[qb] = p.scale_log2e / p.tau[in.at];
         m[qb] = kNoRef;
         l[qb] = 0.f;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) O[qb][db][i] = 0.f;
-    }
-    // the row's own key and value as the first member of the softmax (candidates)
-    __device__ __forceinline__ void own(const PagedArgs &p, int qb, int64_t row, int hk, int hf)
-    {
-        const __bf16 *kp = (const __bf16 *)(p.k + row * p.ld_kv) + (int64_t)hk * D + 8 * hf;
-        const __bf16 *vp = (const __bf16 *)(p.v + row * p.ld_kv) + (int64_t)hk * D + 8 * hf;
+        if (!OWN || !own) return;
         float dot = 0.f;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            const bf16x8 k = *(const bf16x8 *)(kp + 16 * s);
+            const bf16x8 k = __builtin_bit_cast(bf16x8, in.k[s]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot += (float)q[qb][s][e] * (float)k[e];
         }
@@ -152,17 +168,15 @@ struct State {
         m[qb] = dot;
         if (dot != dot) l[qb] = dot, m[qb] = kNoRef;  // (a logit that is no number makes the row none)
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+        for (int s = 0; s < D / 16; ++s) {
+            u32x4 v = in.v[s];
+            swap_pieces(v);
 #pragma unroll
-            for (int g = 0; g < 4; g += 2) {
-                u32x4 v = *(const u32x4 *)(vp + 32 * db + 8 * g);
-                swap_pieces(v);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    O[qb][db][4 * g + 2 * e] = __uint_as_float(v[e] << 16);
-                    O[qb][db][4 * g + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
-                }
+            for (int e = 0; e < 4; ++e) {
+                O[qb][s / 2][8 * (s & 1) + 2 * e] = __uint_as_float(v[e] << 16);
+                O[qb][s / 2][8 * (s & 1) + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
             }
+        }
     }
     __device__ __forceinline__ void logits(const KFrags<D> &k, f32x16 (&S)[QB]) const
     {
@@ -354,34 +368,32 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
     auto stage = [&](int i) __attribute__((always_inline)) { return (lds_u8 *)(i == 0 ? stage0 : i == 1 ? stage1 : i == 2 ? stage2 : stage3); };
     // this wave's 8 of the 32 keys of block i
     const int k_mine = k_lo + (wave >> 1) * 16;
-    int pages = 0, pages_next = 0;  // page numbers of 64 of the wave's groups of 16 keys, one in each lane, and of the 64 after them
+    // page numbers of 64 of the wave's groups of 16 keys, one in each lane, and of the 64 after them
+    const int first_pages = src.page_number(k_mine + lane * 32), next_pages = src.page_number(k_mine + (64 + lane) * 32);
+    int pages = first_pages, pages_next = next_pages;
     auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
-        if ((i & 63) == 0) {
-            pages = i == 0 ? src.page_number(k_mine + lane * 32) : pages_next;
+        if ((i & 63) == 0 && i > 0) {
+            pages = pages_next;
             pages_next = src.page_number(k_mine + (i + 64 + lane) * 32);
         }
         src.issue(k_mine + i * 32, __builtin_amdgcn_readlane(pages, i & 63), to + wave * kShare, to + kValues + wave * kShare);
     };
-    auto issue_first = [&]() __attribute__((always_inline)) {
-        if (n_blocks > 0) issue(0, stage(0));
-        if (n_blocks > 1) issue(1, stage(1));
-        if (n_blocks > 2) issue(2, stage(2));
-    };
-    issue_first();
-
     Rows<D> at;
     at.init(lane);
     State<D, QB> st;
     auto start = [&]() __attribute__((always_inline)) {
+        typename State<D, QB>::Row in[QB];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             const int r = min(r_wave + qb * 32 + l32, rows - 1);
-            const int64_t row = s.row0 + r / p.G;
-            st.start(p, qb, row, w.hk * p.G + r % p.G, hf);
-            if (SUMI && w.split == 0) st.own(p, qb, row, w.hk, hf);
+            st.template request<SUMI>(p, qb, s.row0 + r / p.G, w.hk * p.G + r % p.G, w.hk, hf, in[qb]);
         }
+        if (n_blocks > 0) issue(0, stage(0));
+        if (n_blocks > 1) issue(1, stage(1));
+        if (n_blocks > 2) issue(2, stage(2));
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) st.template start<SUMI>(p, qb, hf, in[qb], w.split == 0);
     };
-    start();
     if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + kRows, rows));
 
     // this wave's copies have landed but for those of `later` blocks, the last ones issued
@@ -395,39 +407,6 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    if (n_clean > 0) {
-        f32x16 S0[QB], S1[QB];
-        bf16x8 P[QB][2];
-        landed(min(n_blocks - 1, 2));
-        meet();
-        st.logits(read_k<D>(at, stage(0)), S0);
-        st.reference(S0);
-        // block j: its logits in Sc, values in cur; the next one's keys in next; prev is free
-        auto step = [&](int j, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB], lds_u8 *prev, lds_u8 *cur, lds_u8 *next) __attribute__((always_inline)) {
-            landed(min(1, n_blocks - 2 - j));
-            meet();  // block j + 1 is here, and nobody reads block j - 1 any more
-            if (j + 3 < n_blocks) issue(j + 3, prev);
-            const KFrags<D> k = read_k<D>(at, next);
-            __builtin_amdgcn_sched_barrier(0);
-            st.logits(k, Sn);  // (behind the last block: not used)
-            st.weights(Sc, P);
-            const VFrags<D> v0 = read_v<D>(at, cur + kValues), v1 = read_v<D>(at, cur + kValues + 16 * R::kPitch);
-            __builtin_amdgcn_sched_barrier(0x40f);
-            st.add(v0, P, 0);
-            st.add(v1, P, 1);
-        };
-        for (int j = 0; j < n_clean;) {
-            step(j, S0, S1, stage(3), stage(0), stage(1));
-            if (++j == n_clean) break;
-            step(j, S1, S0, stage(0), stage(1), stage(2));
-            if (++j == n_clean) break;
-            step(j, S0, S1, stage(1), stage(2), stage(3));
-            if (++j == n_clean) break;
-            step(j, S1, S0, stage(2), stage(3), stage(0));
-            ++j;
-        }
-    }
-    // blocks that not every row sees whole
     int top[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) top[qb] = min(sees(r_wave + qb * 32 + l32), k_hi);
@@ -435,11 +414,44 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
     bool odd = false, far[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) far[qb] = false;
-    int from = n_clean;
 #pragma unroll 1
     for (bool again = false;; again = true) {
+        start();
+        if (!again && n_clean > 0) {
+            f32x16 S0[QB], S1[QB];
+            bf16x8 P[QB][2];
+            landed(min(n_blocks - 1, 2));
+            meet();
+            st.logits(read_k<D>(at, stage(0)), S0);
+            st.reference(S0);
+            // block j: its logits in Sc, values in cur; the next one's keys in next; prev is free
+            auto step = [&](int j, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB], lds_u8 *prev, lds_u8 *cur, lds_u8 *next) __attribute__((always_inline)) {
+                landed(min(1, n_blocks - 2 - j));
+                meet();  // block j + 1 is here, and nobody reads block j - 1 any more
+                if (j + 3 < n_blocks) issue(j + 3, prev);
+                const KFrags<D> k = read_k<D>(at, next);
+                __builtin_amdgcn_sched_barrier(0);
+                st.logits(k, Sn);  // (behind the last block: not used)
+                st.weights(Sc, P);
+                const VFrags<D> v0 = read_v<D>(at, cur + kValues), v1 = read_v<D>(at, cur + kValues + 16 * R::kPitch);
+                __builtin_amdgcn_sched_barrier(0x40f);
+                st.add(v0, P, 0);
+                st.add(v1, P, 1);
+            };
+            for (int j = 0; j < n_clean;) {
+                step(j, S0, S1, stage(3), stage(0), stage(1));
+                if (++j == n_clean) break;
+                step(j, S1, S0, stage(0), stage(1), stage(2));
+                if (++j == n_clean) break;
+                step(j, S0, S1, stage(1), stage(2), stage(3));
+                if (++j == n_clean) break;
+                step(j, S1, S0, stage(2), stage(3), stage(0));
+                ++j;
+            }
+        }
+        // blocks that not every row sees whole
 #pragma unroll 1
-        for (int j = from; j < n_blocks; ++j) {
+        for (int j = again ? 0 : n_clean; j < n_blocks; ++j) {
             lds_u8 *cur = stage(j & 3);
             landed(min(2, n_blocks - 1 - j));
             if (j >= n_clean) {
@@ -479,10 +491,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         const bool any = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
         __syncthreads();
         if (__builtin_expect(!any, 1)) break;
-        start();
+        pages = first_pages, pages_next = next_pages;
         odd = false;
-        from = 0;
-        issue_first();
     }
 
 #pragma unroll
@@ -553,24 +563,26 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     lds_u8 *const at0 = (lds_u8 *)stage0 + wave * kStage, *const at1 = (lds_u8 *)stage1 + wave * kStage;
     // groups of 16 keys: blocks wave, wave + 4, ... of 32; the lower 32 lanes look up the first groups of 32 blocks, the upper the second
     const int k_mine = k_lo + wave * 32 - (lane >> 5) * (32 * 128 - 16);
-    int pages = 0, pages_next = 0;
+    int pages = src.page_number(k_mine + lane * 128), pages_next = src.page_number(k_mine + (32 + lane) * 128);
     auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
-        if ((i & 31) == 0) {
-            pages = i == 0 ? src.page_number(k_mine + lane * 128) : pages_next;
+        if ((i & 31) == 0 && i > 0) {
+            pages = pages_next;
             pages_next = src.page_number(k_mine + (i + 32 + lane) * 128);
         }
         const int k0 = k_lo + (i * 4 + wave) * 32;
         src.issue(k0, __builtin_amdgcn_readlane(pages, i & 31), to, to + 32 * R::kPitch);
         src.issue(k0 + 16, __builtin_amdgcn_readlane(pages, 32 + (i & 31)), to + 16 * R::kPitch, to + 48 * R::kPitch);
     };
-    if (mine > 0) issue(0, at0);
-    if (mine > 1) issue(1, at1);
-
     Rows<D> at;
     at.init(lane);
     State<D, 1> st;
-    st.start(p, 0, row, h, hf);
-    if (SUMI && w.split == 0 && wave == 0) st.own(p, 0, row, w.hk, hf);
+    {
+        typename State<D, 1>::Row in;
+        st.template request<SUMI>(p, 0, row, h, w.hk, hf, in);
+        if (mine > 0) issue(0, at0);
+        if (mine > 1) issue(1, at1);
+        st.template start<SUMI>(p, 0, hf, in, w.split == 0 && wave == 0);
+    }
     if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + 32, rows));
 
     bool odd = false;
