@@ -414,9 +414,11 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
     bool odd = false, far[QB];
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) far[qb] = false;
+    // (one copy of the start's code at D = 128, where a second makes the loop spill; two at D = 64, where one costs the loop 5 %)
+    if constexpr (D == 64) start();
 #pragma unroll 1
     for (bool again = false;; again = true) {
-        start();
+        if constexpr (D != 64) start();
         if (!again && n_clean > 0) {
             f32x16 S0[QB], S1[QB];
             bf16x8 P[QB][2];
@@ -431,8 +433,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
                 if (j + 3 < n_blocks) issue(j + 3, prev);
                 const KFrags<D> k = read_k<D>(at, next);
                 __builtin_amdgcn_sched_barrier(0);
+                st.weights(Sc, P, 0);
+                __builtin_amdgcn_sched_barrier(0);
                 st.logits(k, Sn);  // (behind the last block: not used)
-                st.weights(Sc, P);
+                st.weights(Sc, P, 1);
                 const VFrags<D> v0 = read_v<D>(at, cur + kValues), v1 = read_v<D>(at, cur + kValues + 16 * R::kPitch);
                 __builtin_amdgcn_sched_barrier(0x40f);
                 st.add(v0, P, 0);
@@ -493,6 +497,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         if (__builtin_expect(!any, 1)) break;
         pages = first_pages, pages_next = next_pages;
         odd = false;
+        if constexpr (D == 64) start();
     }
 
 #pragma unroll
@@ -585,6 +590,15 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     }
     if (!SUMI && w.split == 0) store_new<D>(p, s, w.b, w.hk, r_tile, min(r_tile + 32, rows));
 
+    // logits for the weights per token
+    float *const logits = p.logits ? p.logits + (((int64_t)w.b * p.Hkv + w.hk) * (p.m_max * p.G) + r_tile + l32) * p.logits_ld + 4 * hf : nullptr;
+    auto keep = [&](const f32x16 &S, int k0) __attribute__((always_inline)) {
+        if (logits && r_tile + l32 < rows) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *(f32x4 *)(logits + k0 + 8 * g) = f32x4{S[4 * g] * st.c[0], S[4 * g + 1] * st.c[0], S[4 * g + 2] * st.c[0], S[4 * g + 3] * st.c[0]};
+        }
+    };
     bool odd = false;
     auto block = [&](int i, lds_u8 *keys) __attribute__((always_inline)) {
         // (the rows and stores above were issued later than the first copies: until they are done, this waits for more than it has to)
@@ -601,6 +615,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
         bf16x8 P[1][2];
         st.logits(read_k<D>(at, keys), S);
         if (k0 + 32 <= min(lim_lo, k_hi)) {
+            keep(S[0], k0);
             st.reference(S);
             st.weights(S, P);
 #pragma unroll
@@ -609,6 +624,7 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
             odd |= clear_odd<32 * R::kPitch>(values, lane);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             hide(S[0], k0, hf, min(lim, k_hi));
+            keep(S[0], k0);
             st.reference(S);
             st.weights(S, P);
 #pragma unroll

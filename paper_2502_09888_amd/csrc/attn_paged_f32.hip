@@ -350,6 +350,29 @@ __global__ __launch_bounds__(256) void paged_mass_add_kernel(const PagedArgs p, 
     *to = j < s.n ? *to + x : x;  // a new token has none yet, whatever its slot holds
 }
 
+// The same from logits that the attention of few rows has left: a thread per token, cache heads and rows in their order.
+__global__ __launch_bounds__(256) void paged_mass_few_kernel(const PagedArgs p)
+{
+    const int per = (p.max_len + 255) / 256, b = blockIdx.x / per, j = (blockIdx.x % per) * 256 + threadIdx.x;
+    const PagedSeq s = paged_seq(p, b);
+    if (s.T == 0 || j >= (p.sumi ? s.n : s.n + s.T)) return;
+    const int raw = p.table[(int64_t)b * p.table_ld + (j >> p.page_shift)];
+    if (raw < 0 || raw >= p.n_pages) return;
+    float x = 0.f;
+    const int rows = s.T * p.G;
+    for (int hk = 0; hk < p.Hkv; ++hk) {
+        const float *logits = p.logits + ((int64_t)b * p.Hkv + hk) * (p.m_max * p.G) * p.logits_ld + j;
+        float at[kMassFewRows];
+#pragma unroll
+        for (int r = 0; r < kMassFewRows; ++r) at[r] = r < rows ? logits[(int64_t)r * p.logits_ld] : -INFINITY;
+#pragma unroll
+        for (int r = 0; r < kMassFewRows; ++r)
+            if (r < rows) x += __builtin_amdgcn_exp2f(at[r] - p.lse[(s.row0 + r / p.G) * p.H + hk * p.G + r % p.G].y);
+    }
+    float *to = p.mass + ((int64_t)raw << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+    *to = j < s.n ? *to + x : x;
+}
+
 template <int DP>
 hipError_t launch(const PagedArgs &a, hipStream_t s)
 {
@@ -405,6 +428,12 @@ hipError_t launch_paged_mass_f32(const PagedArgs &a, float *part, hipStream_t s)
     if (a.d <= 32) launch_mass<32>(a, part, s);
     else if (a.d <= 64) launch_mass<64>(a, part, s);
     else launch_mass<128>(a, part, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_mass_few(const PagedArgs &a, hipStream_t s)
+{
+    hipLaunchKernelGGL(paged_mass_few_kernel, dim3((unsigned)((a.max_len + 255) / 256 * a.n_seqs)), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 

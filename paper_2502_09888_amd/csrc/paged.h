@@ -28,6 +28,8 @@ struct PagedArgs {
     // work split: tiles of packed rows, parts of the keys
     int n_tiles, n_split, bh_major;
     float *part_o, *part_ml;  // [n_split][m_total H][d], [n_split][m_total H][2] (n_split > 1)
+    float *logits;            // few rows: [n_seqs Hkv][m_max G][logits_ld] logits in log2 units for paged_mass_few, or nullptr
+    int logits_ld;
     float2 *lse;              // [m_total H] {scale, log of the sum of the exponentials} of a row's softmax, log2 units, or nullptr: not wanted
 };
 
@@ -115,12 +117,17 @@ hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s);
 // of a sequence being its cache heads (bf16: times paged_mass_parts), and those added up into the masses.
 hipError_t launch_paged_mass_f32(const PagedArgs &a, float *part, hipStream_t s);
 hipError_t launch_paged_mass_bf16(const PagedArgs &a, float *part, int row_parts, hipStream_t s);
+// ... in one step for at most kMassFewRows packed rows of a sequence and cache head, whose attention has left its logits: keys are not
+// read again
+constexpr int kMassFewRows = 8;
+hipError_t launch_paged_mass_few(const PagedArgs &a, hipStream_t s);
 hipError_t launch_paged_mass_add(const PagedArgs &a, const float *part, int n_parts, hipStream_t s);
-constexpr int kMassKeys = 256;  // bf16: keys of a workgroup
-// bf16: parts of a cache head's rows, so that a launch has a workgroup per CU or more, of 256 rows or more
+constexpr int kMassKeys = 256, kMassGroups = 2048;  // bf16: keys of a workgroup; workgroups of a launch that parts of the rows bring it to
+// bf16: parts of a cache head's rows, of 256 rows or more (us of two cases of ragged lengths with 512, 1024, 2048, 4096 workgroups:
+// 184, 183, 181, 191 and 210, 196, 194, 203)
 static inline int paged_mass_parts(int64_t n_seqs, int64_t Hkv, int64_t max_len, int64_t rows)
 {
-    const int64_t groups = n_seqs * Hkv * ((max_len + kMassKeys - 1) / kMassKeys), most = (rows + 255) / 256, want = groups > 0 ? 512 / groups : 1;
+    const int64_t groups = n_seqs * Hkv * ((max_len + kMassKeys - 1) / kMassKeys), most = (rows + 255) / 256, want = groups > 0 ? kMassGroups / groups : 1;
     return (int)(want < 1 || most < 1 ? 1 : want < most ? want : most);
 }
 

@@ -63,6 +63,8 @@ int parts(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total
     return (int)std::max<int64_t>(1, std::min(std::min(512 / groups, room), most_parts(kv)));
 }
 
+size_t logits_pitch(const climber_paged_kv *kv) { return ((size_t)kv->max_len + 31) / 32 * 32; }
+
 struct Layout {  // of the workspace
     size_t part_o, part_ml, lse, mass, bytes;
 };
@@ -73,9 +75,14 @@ Layout layout_of(const climber_config *cfg, const climber_paged_kv *kv, int32_t 
     w.part_o = 0;
     w.part_ml = w.part_o + up(part_rows * cfg->d_head * 4);
     w.lse = w.part_ml + up(part_rows * 8);
-    w.mass = w.lse + (kv->mass ? up((size_t)m_total * cfg->n_heads * 8) : 0);
-    // (more than one part of the rows: at most 512 workgroups' sums)
-    w.bytes = w.mass + (kv->mass ? up(((size_t)kv->n_seqs * kv->n_kv_heads * kv->max_len + 512 * kMassKeys) * 4) : 0);
+    w.mass = w.bytes = w.lse + (kv->mass ? up((size_t)m_total * cfg->n_heads * 8) : 0);
+    if (kv->mass) {
+        // sums of the rows' parts (more than one: of at most kMassGroups workgroups), or the logits of few rows (a call may have fewer rows
+        // than it is asked for here)
+        const size_t groups = (size_t)kv->n_seqs * kv->n_kv_heads, G = cfg->n_heads / kv->n_kv_heads;
+        const size_t few = cfg->dtype == CLIMBER_BF16 ? kMassFewRows / G * G * logits_pitch(kv) : 0;
+        w.bytes += up(std::max(groups * kv->max_len + (size_t)kMassGroups * kMassKeys, groups * few) * 4);
+    }
     return w;
 }
 
@@ -185,12 +192,18 @@ int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_
     a.part_o = (float *)(ws + w.part_o);
     a.part_ml = (float *)(ws + w.part_ml);
     a.lse = kv->mass ? (float2 *)(ws + w.lse) : nullptr;
+    float *part = (float *)(ws + w.mass);
+    const bool few = bf16 && kv->mass && (int64_t)m_max * a.G <= kMassFewRows;
+    if (few) {
+        a.logits = part;
+        a.logits_ld = (int)logits_pitch(kv);
+    }
     const hipStream_t s = (hipStream_t)stream;
     e = rt(bf16 ? launch_attn_paged_bf16(a, s) : launch_attn_paged_f32(a, s));
     if (e) return e;
     if (a.n_split > 1) e = rt(launch_paged_combine(a, bf16, s));
     if (e || !kv->mass || kv->max_len == 0) return e;
-    float *part = (float *)(ws + w.mass);
+    if (few) return rt(launch_paged_mass_few(a, s));
     const int row_parts = bf16 ? paged_mass_parts(kv->n_seqs, kv->n_kv_heads, kv->max_len, (int64_t)m_max * a.G) : 1;
     e = rt(bf16 ? launch_paged_mass_bf16(a, part, row_parts, s) : launch_paged_mass_f32(a, part, s));
     return e ? e : rt(launch_paged_mass_add(a, part, kv->n_kv_heads * row_parts, s));
