@@ -698,11 +698,10 @@ template <int D, bool SUMI>
 hipError_t launch(PagedArgs p, hipStream_t s)
 {
     const int64_t rows = (int64_t)p.m_max * p.G;
-    constexpr int QB = D == 64 ? 2 : 1;
-    void (*kernel)(PagedArgs) = attn_paged_tile_kernel<D, QB, SUMI>;
-    int tile = 128 * QB;
-    if (rows <= kPagedFewRows) kernel = attn_paged_few_kernel<D, SUMI>, tile = 32;
-    else if (rows <= 128) kernel = attn_paged_tile_kernel<D, 1, SUMI>, tile = 128;
+    const int tile = paged_tile_rows(true, D, rows, (int64_t)p.n_seqs * p.Hkv);
+    void (*kernel)(PagedArgs) = tile == 32 ? attn_paged_few_kernel<D, SUMI> : attn_paged_tile_kernel<D, 1, SUMI>;
+    if constexpr (D == 64)
+        if (tile == 256) kernel = attn_paged_tile_kernel<D, 2, SUMI>;
     p.n_tiles = (int)((rows + tile - 1) / tile);
     hipLaunchKernelGGL(kernel, dim3(paged_grid(p)), dim3(256), 0, s, p);
     return hipGetLastError();

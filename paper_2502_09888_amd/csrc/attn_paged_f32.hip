@@ -38,15 +38,123 @@ static __device__ __forceinline__ void load_tile(float *to, int d, Ptr key_ptr)
     }
 }
 
+// The new tokens of packed rows r0 .. r1 - 1 go into their pages.  (No call reads them from there before this one is done.)
+template <int NT>
+static __device__ __forceinline__ void store_new(const PagedArgs &p, const PagedSeq &s, int b, int hk, int r0, int r1)
+{
+    const int t0 = (r0 + p.G - 1) / p.G, t1 = (r1 + p.G - 1) / p.G, C = p.row_bytes / 16;
+    for (int i = threadIdx.x; i < (t1 - t0) * C; i += NT) {
+        const int t = t0 + i / C, c = (i % C) * 16, slot = s.n + t, page = p.table[(int64_t)b * p.table_ld + (slot >> p.page_shift)];
+        if (page < 0 || page >= p.n_pages) continue;
+        const int64_t to = paged_row(p, page, hk, slot) + c, from = (s.row0 + t) * p.ld_kv + (int64_t)hk * p.row_bytes + c;
+        *(uint4 *)(p.k_pages + to) = *(const uint4 *)(p.k + from);
+        *(uint4 *)(p.v_pages + to) = *(const uint4 *)(p.v + from);
+        if (hk == 0 && c == 0 && p.stamp) p.stamp[((int64_t)page << p.page_shift) + (slot & ((1 << p.page_shift) - 1))] = p.stamp_new[s.row0 + t];
+    }
+}
+
+// a candidate's own key and value: the first member of its softmax
+template <int DP>
+static __device__ __forceinline__ void own_first(const PagedArgs &p, int64_t row, int hk, int hf, const f32x4 (&q)[DP / 8], float &m, float &l,
+                                                 f32x16 (&O)[DP / 32])
+{
+    const float *kp = (const float *)(p.k + row * p.ld_kv) + (int64_t)hk * p.d, *vp = (const float *)(p.v + row * p.ld_kv) + (int64_t)hk * p.d;
+    float dot = 0.f;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i)
+        if (8 * i + 4 * hf < p.d) {
+            const f32x4 x = load4(kp + 8 * i + 4 * hf);
+            dot += q[i][0] * x[0] + q[i][1] * x[1] + q[i][2] * x[2] + q[i][3] * x[3];
+        }
+    m = dot + __shfl_xor(dot, 32, 64);
+    l = hf == 0 ? 1.f : 0.f;
+    if (m != m) l = m, m = kNoRef;  // (a logit that is no number makes the row none)
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            if (32 * db + 8 * g + 4 * hf < p.d) {
+                const f32x4 x = load4(vp + 32 * db + 8 * g + 4 * hf);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[db][4 * g + e] = x[e];
+            }
+}
+
+// 32 keys from k0 on: logits S, values by value(db, i), the operand of step i; the lane's row sees keys below `top`, and all rows of the
+// wave see all keys unless masked
+template <int DP, typename Value>
+static __device__ __forceinline__ void block_softmax(f32x16 &S, float &m, float &l, f32x16 (&O)[DP / 32], float c, int k0, int hf, int top, bool masked,
+                                                     Value value)
+{
+    constexpr int NB = DP / 32;
+    auto key_of = [&](int i) { return k0 + 8 * (i >> 2) + 4 * hf + (i & 3); };
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (key_of(i) >= top) S[i] = -INFINITY;
+    }
+    float mx = S[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
+    mx = fmaxf(half_max(mx), m);
+    const float alpha = __builtin_amdgcn_exp2f((m - mx) * c);
+    m = mx;
+    l *= alpha;
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[db][i] *= alpha;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        S[i] = __builtin_amdgcn_exp2f((S[i] - m) * c);
+        l += S[i];
+    }
+    if (!masked) {
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(value(db, i), S[i], O[db], 0, 0, 0);
+        return;
+    }
+    // A row must not meet the values of keys that it does not see, not even with probability 0, where they are infinite or
+    // no numbers: those take part as zeros, and the rows that do see one get it by a count of such values.
+#pragma unroll
+    for (int db = 0; db < NB; ++db) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float x = value(db, i);
+            const bool fine = fabsf(x) < INFINITY;
+            odd |= !fine;
+            O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(fine ? x : 0.f, S[i], O[db], 0, 0, 0);
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd) == 0, 1)) continue;
+#pragma unroll 1
+        for (int kind = 0; kind < 2; ++kind) {  // infinities of a sign; what is no number counts as both
+            f32x16 n;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) n[i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = value(db, i);
+                const bool is = x != x || x == (kind == 0 ? INFINITY : -INFINITY);
+                n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.f : 0.f, key_of(i) < top ? 1.f : 0.f, n, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (n[i] > 0.f) O[db][i] += kind == 0 ? INFINITY : -INFINITY;
+        }
+    }
+}
+
 // The transposed problem, as in the bf16 kernels: S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x2_f32.  A lane owns one packed
 // row (lane % 32), its probabilities leave the accumulator as the operand of the value product (step r of it takes the keys of
 // accumulator register r).  The sum over the dimensions is taken in an order that lets a lane read four of them at once.
-template <int DP, int NW, bool SUMI>
-__global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs p)
+template <int DP, bool SUMI>
+__global__ __launch_bounds__(256) void attn_paged_f32_kernel(const PagedArgs p)
 {
-    constexpr int kPitch = DP + 4, NB = DP / 32;
-    extern __shared__ __attribute__((aligned(16))) float lds[];
-    float *tk = lds, *tv = lds + kKeys * kPitch;
+    constexpr int kPitch = DP + 4, NB = DP / 32, NW = 4;
+    __shared__ __attribute__((aligned(16))) float tk[kKeys * kPitch], tv[kKeys * kPitch];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
     if (!paged_work(p, w)) return;
@@ -64,18 +172,7 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
     int k_lo, k_hi;
     paged_part(p, w.split, k_end, kKeys, k_lo, k_hi);
 
-    if (!SUMI && w.split == 0) {  // the tile's new tokens go into their pages (no call reads them from there before this one is done)
-        const int t0 = (r_tile + p.G - 1) / p.G, t1 = (min(r_tile + NW * 32, rows) + p.G - 1) / p.G, C = p.row_bytes / 8;
-        for (int i = threadIdx.x; i < (t1 - t0) * C; i += NW * 64) {
-            const int tt = t0 + i / C, c = (i % C) * 8, slot = s.n + tt;
-            const int raw = p.table[(int64_t)w.b * p.table_ld + (slot >> p.page_shift)];
-            if (raw < 0 || raw >= p.n_pages) continue;
-            const int64_t at = paged_row(p, raw, w.hk, slot) + c, from = (s.row0 + tt) * p.ld_kv + (int64_t)w.hk * p.row_bytes + c;
-            *(uint2 *)(p.k_pages + at) = *(const uint2 *)(p.k + from);
-            *(uint2 *)(p.v_pages + at) = *(const uint2 *)(p.v + from);
-            if (w.hk == 0 && c == 0 && p.stamp) p.stamp[((int64_t)raw << p.page_shift) + (slot & ((1 << p.page_shift) - 1))] = p.stamp_new[s.row0 + tt];
-        }
-    }
+    if (!SUMI && w.split == 0) store_new<NW * 64>(p, s, w.b, w.hk, r_tile, min(r_tile + NW * 32, rows));
 
     f32x4 q[DP / 8];
     const float *qp = (const float *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
@@ -88,28 +185,7 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
     for (int db = 0; db < NB; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
-    if (SUMI && w.split == 0) {  // the row's own key and value: the first member of its softmax
-        const float *kp = (const float *)(p.k + row * p.ld_kv) + (int64_t)w.hk * p.d, *vp = (const float *)(p.v + row * p.ld_kv) + (int64_t)w.hk * p.d;
-        float dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < DP / 8; ++i)
-            if (8 * i + 4 * hf < p.d) {
-                const f32x4 x = load4(kp + 8 * i + 4 * hf);
-                dot += q[i][0] * x[0] + q[i][1] * x[1] + q[i][2] * x[2] + q[i][3] * x[3];
-            }
-        m = dot + __shfl_xor(dot, 32, 64);
-        l = hf == 0 ? 1.f : 0.f;
-        if (m != m) l = m, m = kNoRef;  // (a logit that is no number makes the row none)
-#pragma unroll
-        for (int db = 0; db < NB; ++db)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                if (32 * db + 8 * g + 4 * hf < p.d) {
-                    const f32x4 x = load4(vp + 32 * db + 8 * g + 4 * hf);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) O[db][4 * g + e] = x[e];
-                }
-    }
+    if (SUMI && w.split == 0) own_first<DP>(p, row, w.hk, hf, q, m, l, O);
 
     for (int k0 = k_lo; k0 < k_hi; k0 += kKeys) {
         // keys behind the last one are read as the last one, and masked
@@ -134,67 +210,8 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
 #pragma unroll
             for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], q[i][e], S, 0, 0, 0);
         }
-        const int top = min(lim, k_hi);
-        const bool masked = k0 + kKeys > min(lim_lo, k_hi);
-        auto key_of = [&](int i) { return k0 + 8 * (i >> 2) + 4 * hf + (i & 3); };
-        if (masked) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (key_of(i) >= top) S[i] = -INFINITY;
-        }
-        float mx = S[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i]);
-        mx = fmaxf(half_max(mx), m);
-        const float alpha = __builtin_amdgcn_exp2f((m - mx) * c);
-        m = mx;
-        l *= alpha;
-#pragma unroll
-        for (int db = 0; db < NB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) O[db][i] *= alpha;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            S[i] = __builtin_amdgcn_exp2f((S[i] - m) * c);
-            l += S[i];
-        }
-        if (!masked) {
-#pragma unroll
-            for (int db = 0; db < NB; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(tv[(8 * (i >> 2) + 4 * hf + (i & 3)) * kPitch + 32 * db + l32], S[i], O[db], 0, 0, 0);
-        } else {
-            // A row must not meet the values of keys that it does not see, not even with probability 0, where they are infinite or
-            // no numbers: those take part as zeros, and the rows that do see one get it by a count of such values.
-#pragma unroll
-            for (int db = 0; db < NB; ++db) {
-                bool odd = false;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x = tv[(8 * (i >> 2) + 4 * hf + (i & 3)) * kPitch + 32 * db + l32];
-                    const bool fine = fabsf(x) < INFINITY;
-                    odd |= !fine;
-                    O[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(fine ? x : 0.f, S[i], O[db], 0, 0, 0);
-                }
-                if (__builtin_amdgcn_ballot_w64(odd) == 0) continue;
-                for (int kind = 0; kind < 3; ++kind) {
-                    f32x16 n;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) n[i] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float x = tv[(8 * (i >> 2) + 4 * hf + (i & 3)) * kPitch + 32 * db + l32];
-                        const bool is = kind == 0 ? x == INFINITY : kind == 1 ? x == -INFINITY : x != x;
-                        n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.f : 0.f, key_of(i) < top ? 1.f : 0.f, n, 0, 0, 0);
-                    }
-                    const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (n[i] > 0.f) O[db][i] += add;
-                }
-            }
-        }
+        block_softmax<DP>(S, m, l, O, c, k0, hf, min(lim, k_hi), k0 + kKeys > min(lim_lo, k_hi),
+                          [&](int db, int i) { return tv[(8 * (i >> 2) + 4 * hf + (i & 3)) * kPitch + 32 * db + l32]; });
     }
 
     if (r_wave + l32 >= rows) return;
@@ -220,6 +237,124 @@ __global__ __launch_bounds__(NW * 64) void attn_paged_f32_kernel(const PagedArgs
             if (32 * db + 8 * g + 4 * hf < p.d)
                 store4(op + 32 * db + 8 * g + 4 * hf, f32x4{O[db][4 * g] * inv, O[db][4 * g + 1] * inv, O[db][4 * g + 2] * inv, O[db][4 * g + 3] * inv});
     if (hf == 0 && p.lse) p.lse[rh] = float2{c, m * c + __builtin_amdgcn_logf(l)};
+}
+
+// The same without LDS tiles, for few rows: the waves of a workgroup have the same 32 packed rows and take blocks of 32 keys in turn, whose
+// keys and values come straight from memory as operands, all requested before the first is used; their results are joined at
+// the end.  Such a call is bound by its chain of loads: 64 cached tokens of one user 13.6 us with one wave after the other tile.
+template <int DP, bool SUMI>
+__global__ __launch_bounds__(256) void attn_paged_few_f32_kernel(const PagedArgs p)
+{
+    constexpr int NB = DP / 32;
+    __shared__ __attribute__((aligned(16))) float joined[4][32 * DP];
+    __shared__ float ref[4][32], denom[4][32];
+    __shared__ const uint8_t *value_row[4][32];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    if (!paged_work(p, w)) return;
+    const PagedSeq s = paged_seq(p, w.b);
+    const int rows = s.T * p.G, r_tile = w.tile * 32;
+    if (r_tile >= rows) return;
+    const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
+    const int64_t row = s.row0 + t;
+    const bool causal = !SUMI && p.causal;
+    auto sees = [&](int i) { return SUMI ? s.n : s.n + (causal ? min(i, rows - 1) / p.G + 1 : s.T); };  // packed row i sees keys below it
+    const int lim = sees(r), lim_lo = sees(r_tile);
+    int k_lo, k_hi;
+    paged_part(p, w.split, sees(r_tile + 31), kKeys, k_lo, k_hi);
+    const int n_blk = (k_hi - k_lo + kKeys - 1) / kKeys;
+
+    // a block's operands: key row l32, dimensions 8 i + 4 hf + e; values of key 8 (i / 4) + 4 hf + i % 4, dimension 32 db + l32
+    f32x4 k[DP / 8];
+    float v[NB][16];
+    auto request = [&](int blk) __attribute__((always_inline)) {
+        const int j = min(k_lo + blk * kKeys + l32, k_hi - 1);  // keys behind the last one: that one again, and masked
+        const bool old = j < s.n;
+        const int64_t cached = paged_row(p, old ? paged_page(p, w.b, j) : 0, w.hk, j), fresh = (s.row0 + j - s.n) * p.ld_kv + (int64_t)w.hk * p.row_bytes;
+        const uint8_t *at_k = old ? p.k_pages + cached : p.k + fresh, *at_v = old ? p.v_pages + cached : p.v + fresh;
+        if (hf == 0) value_row[wave][l32] = at_v;  // (read by the same wave: LDS keeps its order)
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) k[i] = 8 * i + 4 * hf < p.d ? load4((const float *)at_k + 8 * i + 4 * hf) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float *from = (const float *)value_row[wave][8 * (i >> 2) + 4 * hf + (i & 3)];
+#pragma unroll
+            for (int db = 0; db < NB; ++db) v[db][i] = 32 * db + l32 < p.d ? from[32 * db + l32] : 0.f;
+        }
+    };
+    f32x4 q[DP / 8];
+    const float *qp = (const float *)(p.q + row * p.ld_q) + (int64_t)h * p.d;
+#pragma unroll
+    for (int i = 0; i < DP / 8; ++i) q[i] = 8 * i + 4 * hf < p.d ? load4(qp + 8 * i + 4 * hf) : f32x4{0.f, 0.f, 0.f, 0.f};
+    const float c = paged_row_scale(p, row);
+    if (wave < n_blk) request(wave);
+    if (!SUMI && w.split == 0) store_new<256>(p, s, w.b, w.hk, r_tile, min(r_tile + 32, rows));
+    float m = kNoRef, l = 0.f;
+    f32x16 O[NB];
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
+    if (SUMI && w.split == 0 && wave == 0) own_first<DP>(p, row, w.hk, hf, q, m, l, O);
+
+    for (int blk = wave; blk < n_blk; blk += 4) {
+        const int k0 = k_lo + blk * kKeys;
+        f32x16 S;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i][e], q[i][e], S, 0, 0, 0);
+        block_softmax<DP>(S, m, l, O, c, k0, hf, min(lim, k_hi), k0 + kKeys > min(lim_lo, k_hi), [&](int db, int i) { return v[db][i]; });
+        if (blk + 4 < n_blk) request(blk + 4);
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (hf == 0) ref[wave][l32] = m, denom[wave][l32] = l;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(ref[0][l32], ref[1][l32]), fmaxf(ref[2][l32], ref[3][l32]));
+    const float mine = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
+#pragma unroll
+    for (int db = 0; db < NB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : O[db][4 * g + e] * mine;
+            *(f32x4 *)(joined[wave] + l32 * DP + (((8 * db + 2 * g + hf) ^ (l32 & 7)) * 4)) = x;  // (pieces permuted: no conflicts)
+        }
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) total += denom[i][l32] == 0.f ? 0.f : denom[i][l32] * __builtin_amdgcn_exp2f((ref[i][l32] - top) * c);
+    __syncthreads();
+    if (wave == 0 && hf == 0) {
+        denom[0][l32] = total;
+        if (r_tile + l32 < rows) {
+            const int64_t rh = row * p.H + h;
+            if (p.n_split > 1) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{top * c, total};
+            else if (p.lse) p.lse[rh] = float2{c, top * c + __builtin_amdgcn_logf(total)};
+        }
+    }
+    __syncthreads();
+    constexpr int C = DP / 4;
+    const int n_rows = min(32, rows - r_tile);
+    for (int i = threadIdx.x; i < n_rows * C; i += 256) {
+        const int rr = i / C, cc = i % C, tt = (r_tile + rr) / p.G, hh = w.hk * p.G + (r_tile + rr) % p.G;
+        if (cc * 4 >= p.d) continue;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x += *(const f32x4 *)(joined[j] + rr * DP + ((cc ^ (rr & 7)) * 4));
+        const int64_t rh = (s.row0 + tt) * p.H + hh;
+        if (p.n_split > 1) {
+            *(f32x4 *)(p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * p.d + cc * 4) = x;
+        } else {
+            const float inv = 1.f / denom[0][rr];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] *= inv;
+            store4((float *)(p.o + (s.row0 + tt) * p.ld_o) + (int64_t)hh * p.d + cc * 4, x);
+        }
+    }
 }
 
 // Partial results of the parts of the keys, joined.  32 lanes have a row's dimensions; GROUPS such groups share its parts, and 8 / GROUPS
@@ -378,20 +513,12 @@ hipError_t launch(const PagedArgs &a, hipStream_t s)
 {
     PagedArgs p = a;
     const int64_t rows = (int64_t)a.m_max * a.G;
-    const size_t lds = 2 * kKeys * (DP + 4) * sizeof(float);
-    auto go = [&](auto nw, auto sumi) {
-        constexpr int NW = decltype(nw)::value;
-        constexpr bool SUMI = decltype(sumi)::value;
-        p.n_tiles = (int)((rows + NW * 32 - 1) / (NW * 32));
-        hipLaunchKernelGGL((attn_paged_f32_kernel<DP, NW, SUMI>), dim3(paged_grid(p)), dim3(NW * 64), lds, s, p);
-    };
-    if (rows <= 32) {
-        if (a.sumi) go(std::integral_constant<int, 1>{}, std::true_type{});
-        else go(std::integral_constant<int, 1>{}, std::false_type{});
-    } else {
-        if (a.sumi) go(std::integral_constant<int, 4>{}, std::true_type{});
-        else go(std::integral_constant<int, 4>{}, std::false_type{});
-    }
+    const int tile = paged_tile_rows(false, a.d, rows, (int64_t)a.n_seqs * a.Hkv);
+    p.n_tiles = (int)((rows + tile - 1) / tile);
+    void (*kernel)(PagedArgs) = a.sumi ? attn_paged_few_f32_kernel<DP, true> : attn_paged_few_f32_kernel<DP, false>;
+    if constexpr (DP <= 64)
+        if (tile == 128) kernel = a.sumi ? attn_paged_f32_kernel<DP, true> : attn_paged_f32_kernel<DP, false>;
+    hipLaunchKernelGGL(kernel, dim3(paged_grid(p)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

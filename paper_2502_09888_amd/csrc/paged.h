@@ -108,7 +108,15 @@ static __device__ __forceinline__ float paged_row_scale(const PagedArgs &p, int6
     return p.scale_log2e / p.tau[sc * p.n_beh + bh];
 }
 
-constexpr int kPagedFewRows = 32;  // bf16: most packed rows of a sequence and cache head that go to the kernel for few rows
+// Packed rows of a workgroup, 32: the kernels for few rows, whose waves share out keys.  bf16: where a sequence and cache head has no
+// more of them.  fp32, which has no use for more rows per operand than 32: also where tiles of 128 rows are fewer than 96 (us few /
+// tiles at d_head 64: 48 of them 36 / 46, 128 of them 91 / 75), and above d_head 64, where tiles would leave one wave per SIMD (788 / 1020
+// for chunks of 1000 of 8 users on 1000).
+static inline int paged_tile_rows(bool bf16, int d, int64_t rows, int64_t groups)
+{
+    if (rows <= 32 || (!bf16 && (d > 64 || (rows + 127) / 128 * groups < 96))) return 32;
+    return bf16 && d == 64 && rows > 128 ? 256 : 128;
+}
 
 hipError_t launch_attn_paged_bf16(const PagedArgs &a, hipStream_t s);
 hipError_t launch_attn_paged_f32(const PagedArgs &a, hipStream_t s);

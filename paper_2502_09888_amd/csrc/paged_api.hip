@@ -58,7 +58,8 @@ int64_t most_parts(const climber_paged_kv *kv) { return std::max<int64_t>(1, kv-
 int parts(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total, int32_t m_max)
 {
     const int64_t rows = (int64_t)m_max * (cfg->n_heads / kv->n_kv_heads);
-    const int64_t groups = std::max<int64_t>(1, (rows <= 32 ? 1 : (rows + 127) / 128) * kv->n_seqs * kv->n_kv_heads);
+    const int64_t heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged_tile_rows(cfg->dtype == CLIMBER_BF16, cfg->d_head, rows, heads);
+    const int64_t groups = std::max<int64_t>(1, (rows + tile - 1) / tile * heads);
     const int64_t room = kPartRows / std::max<int64_t>(1, (int64_t)m_total * cfg->n_heads);
     return (int)std::max<int64_t>(1, std::min(std::min(512 / groups, room), most_parts(kv)));
 }
