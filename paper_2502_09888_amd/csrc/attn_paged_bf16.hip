@@ -351,8 +351,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
     __shared__ int flags[4];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
-    if (!paged_work(p, w)) return;
-    const PagedSeq s = paged_seq(p, w.b);
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
     const int rows = s.T * p.G, r_tile = w.tile * kRows;
     if (r_tile >= rows) return;
     const int r_wave = r_tile + wave * 32 * QB;
@@ -549,8 +549,8 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     __shared__ int odd_seen[4];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
-    if (!paged_work(p, w)) return;
-    const PagedSeq s = paged_seq(p, w.b);
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
     const int rows = s.T * p.G, r_tile = w.tile * 32;
     if (r_tile >= rows) return;
     const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;

@@ -157,8 +157,8 @@ __global__ __launch_bounds__(256) void attn_paged_f32_kernel(const PagedArgs p)
     __shared__ __attribute__((aligned(16))) float tk[kKeys * kPitch], tv[kKeys * kPitch];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
-    if (!paged_work(p, w)) return;
-    const PagedSeq s = paged_seq(p, w.b);
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
     const int rows = s.T * p.G, r_tile = w.tile * NW * 32;
     if (r_tile >= rows) return;
     const int r_wave = r_tile + wave * 32, r = min(r_wave + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
@@ -251,8 +251,8 @@ __global__ __launch_bounds__(256) void attn_paged_few_f32_kernel(const PagedArgs
     __shared__ const uint8_t *value_row[4][32];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
-    if (!paged_work(p, w)) return;
-    const PagedSeq s = paged_seq(p, w.b);
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
     const int rows = s.T * p.G, r_tile = w.tile * 32;
     if (r_tile >= rows) return;
     const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;

@@ -26,7 +26,7 @@ struct PagedArgs {
     int causal, sumi;
     float scale_log2e;
     // work split: tiles of packed rows, parts of the keys
-    int n_tiles, n_split, bh_major;
+    int n_tiles, n_split, bh_major, by_work;
     float *part_o, *part_ml;  // [n_split][m_total H][d], [n_split][m_total H][2] (n_split > 1)
     float *logits;            // few rows: [n_seqs Hkv][m_max G][logits_ld] logits in log2 units for paged_mass_few, or nullptr
     int logits_ld;
@@ -64,10 +64,12 @@ static __device__ __forceinline__ int64_t paged_row(const PagedArgs &p, int page
 // Workgroup -> (sequence, cache head), tile, part of the keys.  Tiles of one head read the same keys: they follow each other on one XCD
 // (workgroups are dealt to the eight in turn), where there are heads enough to have each XCD work; the last tiles, which see the
 // most keys under the causal mask, first.
+// With by_work the sequences of each 64 take their turns in the order of their work (each wave ranks them, one in a lane): lengths differ,
+// and a long one that is begun last would be waited for.
 struct PagedWork {
     int b, hk, tile, split;
 };
-static __device__ __forceinline__ bool paged_work(const PagedArgs &p, PagedWork &w)
+static __device__ __forceinline__ bool paged_work(const PagedArgs &p, PagedWork &w, PagedSeq &s)
 {
     const int per = p.n_tiles * p.n_split, n_bh = p.n_seqs * p.Hkv;
     int bh, in;
@@ -84,12 +86,35 @@ static __device__ __forceinline__ bool paged_work(const PagedArgs &p, PagedWork 
     w.hk = bh % p.Hkv;
     w.tile = p.n_tiles - 1 - in / p.n_split;
     w.split = in % p.n_split;
+    if (!p.by_work) {
+        s = paged_seq(p, w.b);
+        return true;
+    }
+    const int lane = threadIdx.x & 63, b0 = w.b & ~63, n = min(p.n_seqs - b0, 64);
+    const PagedSeq mine = paged_seq(p, b0 + min(lane, n - 1));
+    // (work in 26 bits, and the lane: no two alike)
+    const uint32_t work = lane < n ? (__float_as_uint((float)mine.T * (float)(mine.n + mine.T)) & ~63u) | (uint32_t)(63 - lane) : 0;
+    int at = w.b - b0;
+    if (__builtin_amdgcn_ballot_w64(lane < n && (work >> 6) != (__builtin_amdgcn_readfirstlane(work) >> 6)) != 0) {
+        int rank = 0;
+        for (int j0 = 0; j0 < n; j0 += 16)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) rank += (uint32_t)__builtin_amdgcn_readlane(work, j0 + j) > work;
+        at = __ffsll((unsigned long long)__builtin_amdgcn_ballot_w64(lane < n && rank == at)) - 1;
+    }
+    at = __builtin_amdgcn_readfirstlane(at);
+    w.b = b0 + at;
+    s.n = __builtin_amdgcn_readlane(mine.n, at);
+    s.T = __builtin_amdgcn_readlane(mine.T, at);
+    s.row0 = __builtin_amdgcn_readlane((int)mine.row0, at);
     return true;
 }
 static inline unsigned paged_grid(PagedArgs &p)
 {
     const int64_t bh = (int64_t)p.n_seqs * p.Hkv;
     p.bh_major = bh % 8 == 0 || bh >= 64;
+    const int64_t all = bh * p.n_tiles * p.n_split;
+    p.by_work = p.n_seqs > 1 && all >= 512 && all < 4096;
     return (unsigned)((p.bh_major ? (bh + 7) / 8 * 8 : bh) * p.n_tiles * p.n_split);
 }
 

@@ -15,15 +15,15 @@ using namespace paged;
 constexpr int kRowsStage = 64;
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void paged_mass_bf16_kernel(const PagedArgs p, float *part)
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_mass_bf16_kernel(const PagedArgs p, float *part)
 {
     using R = Rows<D>;
     constexpr int kStage = kRowsStage * R::kPitch, kLoads = kStage / 1024 / 4;  // (a wave's)
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage], stage1[kStage];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
-    if (!paged_work(p, w)) return;
-    const PagedSeq s = paged_seq(p, w.b);
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
     const int keys = p.sumi ? s.n : s.n + s.T, k_tile = w.tile * kMassKeys, k0 = k_tile + wave * 64, rows = s.T * p.G;
     if (k_tile >= keys || rows == 0) return;
     const bool causal = !p.sumi && p.causal;
@@ -36,25 +36,55 @@ __global__ __launch_bounds__(256, 2) void paged_mass_bf16_kernel(const PagedArgs
         const int t = (int)__umulhi((unsigned)r, p.G_inv);
         return p.G == 1 ? r : t - (t * p.G > r);
     };
-    auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
+    // Where a row lies: of its query (this lane's piece, for each copy), and of its statistics.  From stage to stage they move by 64 rows, which
+    // is next_t tokens and next_h heads; rows behind the last are read as the last.
+    const int next_t = kRowsStage / p.G, next_h = kRowsStage % p.G;
+    int head[kLoads], stat_head[2];
+    const uint8_t *from[kLoads];
+    const float2 *stat[2];
+    auto place = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const int at = (wave * kLoads + j) * R::kPerLoad + lane / R::kPieces, r = min(r_lo + i * kRowsStage + at, rows - 1), t = token_of(r);
-            const int c = (lane % R::kPieces) ^ R::f(at);
-            copy16((glb_u8 *)(p.q + (s.row0 + t) * p.ld_q + (int64_t)(w.hk * p.G + r - t * p.G) * R::kPitch + c * 16), to + (wave * kLoads + j) * 1024);
+            const int in = (wave * kLoads + j) * R::kPerLoad + lane / R::kPieces, r = min(r0 + in, rows - 1), t = token_of(r);
+            const int c = (lane % R::kPieces) ^ R::f(in);
+            head[j] = r - t * p.G;
+            from[j] = p.q + (s.row0 + t) * p.ld_q + (int64_t)(w.hk * p.G + head[j]) * R::kPitch + c * 16;
+        }
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            const int r = min(r0 + blk * 32 + l32, rows - 1), t = token_of(r);
+            stat_head[blk] = r - t * p.G;
+            stat[blk] = p.lse + (s.row0 + t) * p.H + w.hk * p.G + stat_head[blk];
+        }
+    };
+    const int64_t q_step = next_t * p.ld_q + next_h * R::kPitch, q_wrap = p.ld_q - p.G * R::kPitch;
+    const int stat_step = next_t * p.H + next_h, stat_wrap = p.H - p.G;
+    auto advance = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            head[j] += next_h;
+            const bool over = head[j] >= p.G;
+            head[j] -= over ? p.G : 0;
+            from[j] += q_step + (over ? q_wrap : 0);
+        }
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) {
+            stat_head[blk] += next_h;
+            const bool over = stat_head[blk] >= p.G;
+            stat_head[blk] -= over ? p.G : 0;
+            stat[blk] += stat_step + (over ? stat_wrap : 0);
         }
     };
     float2 next[2];
-    auto stats = [&](int i) __attribute__((always_inline)) {  // the stage's rows of this lane: scale and denominator
+    auto issue = [&](lds_u8 *to) __attribute__((always_inline)) {
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            const int r = min(r_lo + i * kRowsStage + blk * 32 + l32, rows - 1), t = token_of(r);
-            next[blk] = p.lse[(s.row0 + t) * p.H + w.hk * p.G + r - t * p.G];
-        }
+        for (int j = 0; j < kLoads; ++j) copy16((glb_u8 *)from[j], to + (wave * kLoads + j) * 1024);
+#pragma unroll
+        for (int blk = 0; blk < 2; ++blk) next[blk] = *stat[blk];
     };
     if (n_stages > 0) {
-        issue(0, (lds_u8 *)stage0);
-        stats(0);
+        place(r_lo);
+        issue((lds_u8 *)stage0);
     }
     KFrags<D> k[2];
 #pragma unroll
@@ -65,6 +95,11 @@ __global__ __launch_bounds__(256, 2) void paged_mass_bf16_kernel(const PagedArgs
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) k[kb].a[i] = *(const bf16x8 *)(from + i * 32 + hf * 16);
     }
+    // (they have arrived: else every use in the loop would wait for whatever was requested last)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(k[kb].a[i]));
     Rows<D> at;
     at.init(lane);
     f32x16 sum[2];
@@ -77,10 +112,13 @@ __global__ __launch_bounds__(256, 2) void paged_mass_bf16_kernel(const PagedArgs
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        const float2 now[2] = {next[0], next[1]};
+        float2 now[2] = {next[0], next[1]};
+        asm volatile("" : "+v"(now[0].x), "+v"(now[0].y), "+v"(now[1].x), "+v"(now[1].y));
         if (i + 1 < n_stages) {
-            issue(i + 1, other);
-            stats(i + 1);
+            const int r1 = r_lo + (i + 1) * kRowsStage;
+            if (r1 + kRowsStage <= rows) advance();
+            else place(r1);
+            issue(other);
         }
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk) {
@@ -96,21 +134,22 @@ __global__ __launch_bounds__(256, 2) void paged_mass_bf16_kernel(const PagedArgs
                 for (int e = 0; e < D / 16; ++e) S[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[kb].a[e], q.a[e], S[kb], 0, 0, 0);
             }
             const float c = now[blk].x, lse = now[blk].y;
-            if (r0 + 32 <= rows && (!causal || k0 + 63 <= s.n + __builtin_amdgcn_readfirstlane(token_of(r0)))) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) S[kb][e] = __builtin_amdgcn_exp2f(fmaf(S[kb][e], c, -lse));
+            if (r0 + 32 > rows || (causal && k0 + 63 > s.n + __builtin_amdgcn_readfirstlane(token_of(r0)))) {
+                const int lim = (r0 + l32 >= rows ? 0 : causal ? s.n + token_of(r0 + l32) + 1 : keys) - k0 - 4 * hf;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) sum[kb][e] += __builtin_amdgcn_exp2f(fmaf(S[kb][e], c, -lse));
-            } else {
-                const int lim = r0 + l32 >= rows ? 0 : causal ? s.n + token_of(r0 + l32) + 1 : keys;
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float x = __builtin_amdgcn_exp2f(fmaf(S[kb][e], c, -lse));
-                        if (k0 + kb * 32 + 8 * (e >> 2) + 4 * hf + (e & 3) < lim) sum[kb][e] += x;
-                    }
+                    for (int e = 0; e < 16; ++e)
+                        if (kb * 32 + 8 * (e >> 2) + (e & 3) >= lim) S[kb][e] = 0.f;
             }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[kb][e] += S[kb][e];
         }
     };
     for (int i = 0; i < n_stages; i += 2) {
