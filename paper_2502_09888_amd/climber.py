@@ -164,7 +164,9 @@ def _load_native(lib):
         current = None, None
     native.bind(*(C.cast(f, C.c_void_p).value for f in (lib.climber_attn_history, lib.climber_attn_sumi, lib.climber_attn_history_bias,
                                                         lib.climber_attn_sumi_bias)),
-                Config, RelBias, *current)
+                Config, RelBias, *current,
+                *(C.cast(f, C.c_void_p).value for f in (lib.climber_attn_history_paged, lib.climber_attn_sumi_paged, lib.climber_paged_evict)),
+                PagedKV)
     _native = native
     return native
 
@@ -451,27 +453,40 @@ def climber_attn_history_paged(cfg: Config, tau_layer, kv: PagedKV, q, k, v, off
                                workspace, stream=None) -> None:
     """Append a chunk of new behaviours to the paged cache and attend from them.  q, k, v, o: row r is [r] of the tensor (row pitches are
     taken from it, so that columns of one projection's output can be passed as they are)."""
-    d, dk = cfg.d_model, kv.n_kv_heads * cfg.d_head
-    _ok(load_library().climber_attn_history_paged(
-        C.byref(cfg), _ptr(tau_layer), C.byref(kv), _ptr(q), _pitch(q, d), _ptr(k), _ptr(v), _same_pitch(k, v, dk), _ptr(off), m_total, m_max,
-        _ptr(scen), _ptr(beh), _ptr(stamp), _ptr(o), _pitch(o, d), _ptr(workspace), _nbytes(workspace), _stream(stream)),
-        "climber_attn_history_paged")
+    code = (_native or _load_native(load_library())).attn_history_paged(cfg, tau_layer, kv, q, k, v, off, m_total, m_max, scen, beh, stamp, o,
+                                                                        workspace, stream)
+    if code is None:
+        d, dk = cfg.d_model, kv.n_kv_heads * cfg.d_head
+        code = load_library().climber_attn_history_paged(
+            C.byref(cfg), _ptr(tau_layer), C.byref(kv), _ptr(q), _pitch(q, d), _ptr(k), _ptr(v), _same_pitch(k, v, dk), _ptr(off), m_total, m_max,
+            _ptr(scen), _ptr(beh), _ptr(stamp), _ptr(o), _pitch(o, d), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_attn_history_paged")
 
 
 def climber_attn_sumi_paged(cfg: Config, tau_layer, kv: PagedKV, q_c, k_c, v_c, cand_off, m_total: int, m_max: int, cand_scen, cand_beh,
                             o_c, workspace, stream=None) -> None:
     """Candidates against the paged cache (rows as in climber_attn_history_paged)."""
-    d, dk = cfg.d_model, kv.n_kv_heads * cfg.d_head
-    _ok(load_library().climber_attn_sumi_paged(
-        C.byref(cfg), _ptr(tau_layer), C.byref(kv), _ptr(q_c), _pitch(q_c, d), _ptr(k_c), _ptr(v_c), _same_pitch(k_c, v_c, dk), _ptr(cand_off),
-        m_total, m_max, _ptr(cand_scen), _ptr(cand_beh), _ptr(o_c), _pitch(o_c, d), _ptr(workspace), _nbytes(workspace), _stream(stream)),
-        "climber_attn_sumi_paged")
+    code = (_native or _load_native(load_library())).attn_sumi_paged(cfg, tau_layer, kv, q_c, k_c, v_c, cand_off, m_total, m_max, cand_scen,
+                                                                     cand_beh, o_c, workspace, stream)
+    if code is None:
+        d, dk = cfg.d_model, kv.n_kv_heads * cfg.d_head
+        code = load_library().climber_attn_sumi_paged(
+            C.byref(cfg), _ptr(tau_layer), C.byref(kv), _ptr(q_c), _pitch(q_c, d), _ptr(k_c), _ptr(v_c), _same_pitch(k_c, v_c, dk),
+            _ptr(cand_off), m_total, m_max, _ptr(cand_scen), _ptr(cand_beh), _ptr(o_c), _pitch(o_c, d), _ptr(workspace), _nbytes(workspace),
+            _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_attn_sumi_paged")
 
 
 def climber_paged_evict(cfg: Config, kv: PagedKV, rank, budget, keep_from, len_out, src, workspace, stream=None) -> None:
     """Cut every sequence of the paged cache to its budget, least weight first."""
-    _ok(load_library().climber_paged_evict(C.byref(cfg), C.byref(kv), _ptr(rank), _ptr(budget), _ptr(keep_from), _ptr(len_out), _ptr(src),
-                                           _ptr(workspace), _nbytes(workspace), _stream(stream)), "climber_paged_evict")
+    code = (_native or _load_native(load_library())).paged_evict(cfg, kv, rank, budget, keep_from, len_out, src, workspace, stream)
+    if code is None:
+        code = load_library().climber_paged_evict(C.byref(cfg), C.byref(kv), _ptr(rank), _ptr(budget), _ptr(keep_from), _ptr(len_out), _ptr(src),
+                                                  _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_paged_evict")
 
 
 def climber_check_paged(cfg: Config, kv: PagedKV, off, m_total: int, m_max: int, appends: bool, status, stream=None) -> None:
