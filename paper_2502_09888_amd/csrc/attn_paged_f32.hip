@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void attn_paged_f32_kernel(const PagedArgs p)
 // keys and values come straight from memory as operands, all requested before the first is used; their results are joined at
 // the end.  Such a call is bound by its chain of loads: 64 cached tokens of one user 13.6 us with one wave after the other tile.
 template <int DP, bool SUMI>
-__global__ __launch_bounds__(256) void attn_paged_few_f32_kernel(const PagedArgs p)
+__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_paged_few_f32_kernel(const PagedArgs p)
 {
     constexpr int NB = DP / 32;
     __shared__ __attribute__((aligned(16))) float joined[4][32 * DP];

@@ -259,12 +259,14 @@ __global__ __launch_bounds__(kThreads) void evict_step_kernel(const EvictArgs p)
     } else {
         // sums over the segments: this thread's two bins of the last pass's histogram, and the tokens with a stamp that counts
         int n_first = 0;
-        for (int g = 0; g < s.segs; ++g) n_first += base[(int64_t)g * kEvictSegInts + 4 * kBins];
+        for (int g = lane; g < s.segs; g += 64) n_first += base[(int64_t)g * kEvictSegInts + 4 * kBins];
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) n_first += __shfl_xor(n_first, o, 64);
         const bool among_first = n_first >= s.keep;
         const int last = STEP == 1 ? (among_first ? 1 : 0) : STEP;  // which of the four
         const int bin = kBins - 1 - 2 * tid;
         int high = 0, low = 0;
-#pragma unroll 4
+#pragma unroll 16  // (requested together: other workgroups wrote them, far away)
         for (int g = 0; g < s.segs; ++g) {
             const int2 x = *(const int2 *)(base + (int64_t)g * kEvictSegInts + last * kBins + bin - 1);
             low += x.x;
@@ -315,7 +317,11 @@ __global__ __launch_bounds__(kThreads) void evict_step_kernel(const EvictArgs p)
             for (int g = wave; g < s.segs; g += kWaves) {
                 const int32_t *seg = base + (int64_t)g * kEvictSegInts;
                 int above = 0;
-                for (int i = pick + 1 + lane; i < 1024; i += 64) above += seg[3 * kBins + i];
+#pragma unroll
+                for (int i = 0; i < 1024; i += 64) {
+                    const int x = seg[3 * kBins + i + lane];
+                    above += i + lane > pick ? x : 0;
+                }
 #pragma unroll
                 for (int o = 1; o < 64; o *= 2) above += __shfl_xor(above, o, 64);
                 if (lane == 0) {
@@ -324,20 +330,25 @@ __global__ __launch_bounds__(kThreads) void evict_step_kernel(const EvictArgs p)
                 }
             }
             __syncthreads();
-            if (tid == 0) {
-                int equal = 0, holes = 0, movers = 0, all = 0;
-                for (int g = 0; g < s.segs; ++g) {
-                    if (g == s.mine) total[0] = equal, total[1] = g < s.low ? holes : movers;
-                    const int kept = hist[1][g] + min(hist[0][g], max(0, need - equal));
-                    equal += hist[0][g];
-                    if (g < s.low) {
-                        holes += min(kEvictSegment, s.keep - g * kEvictSegment) - kept;
-                        all = holes;
-                    } else {
-                        movers += kept;
+            if (wave == 0) {  // (64 segments at a time)
+                int equal = 0, holes = 0, movers = 0;  // before them
+                auto sum = [&](int x) {                // of the lanes up to this one
+#pragma unroll
+                    for (int o = 1; o < 64; o *= 2) {
+                        const int y = __shfl_up(x, o, 64);
+                        if (lane >= o) x += y;
                     }
+                    return x;
+                };
+                for (int g0 = 0; g0 < s.segs; g0 += 64) {
+                    const int g = g0 + lane, eq = g < s.segs ? hist[0][g] : 0, eq_to = equal + sum(eq);
+                    const int kept = g < s.segs ? hist[1][g] + min(eq, max(0, need - (eq_to - eq))) : 0;
+                    const int hole = g < s.low ? min(kEvictSegment, s.keep - g * kEvictSegment) - kept : 0, mover = g < s.low ? 0 : kept;
+                    const int hole_to = holes + sum(hole), mover_to = movers + sum(mover);
+                    if (g == s.mine) total[0] = eq_to - eq, total[1] = g < s.low ? hole_to - hole : mover_to - mover;
+                    equal = __shfl(eq_to, 63, 64), holes = __shfl(hole_to, 63, 64), movers = __shfl(mover_to, 63, 64);
                 }
-                if (s.mine == 0) p.n_moves[b] = all;
+                if (s.mine == 0 && lane == 0) p.n_moves[b] = holes;
             }
             int equal = 0;
 #pragma unroll
@@ -379,20 +390,22 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictArgs p, int 
     const int32_t *holes = p.holes + (int64_t)b * (p.max_len / 2 + 1), *movers = p.movers + (int64_t)b * (p.max_len / 2 + 1);
     const int32_t *table = p.table + (int64_t)b * p.table_ld;
     const int C = p.row_bytes / 16, in_page = (1 << p.page_shift) - 1;
-    const int64_t items = (int64_t)n * p.Hkv * C;
-    for (int64_t i = (int64_t)part * 256 + threadIdx.x; i < items; i += (int64_t)per_seq * 256) {
-        const int c = (int)(i % C), h = (int)(i / C % p.Hkv), m = (int)(i / C / p.Hkv), to = holes[m], from = movers[m];
-        const int tp = table[to >> p.page_shift], fp = min(max(table[from >> p.page_shift], 0), p.n_pages - 1);
-        if (h == 0 && c == 0 && p.segments > 0 && p.src) p.src[(int64_t)b * (p.table_ld << p.page_shift) + to] = from;
-        if (tp < 0 || tp >= p.n_pages) continue;
-        const int64_t t = ((((int64_t)tp * p.Hkv + h) << p.page_shift) + (to & in_page)) * p.row_bytes + c * 16;
-        const int64_t f = ((((int64_t)fp * p.Hkv + h) << p.page_shift) + (from & in_page)) * p.row_bytes + c * 16;
-        *(uint4 *)(p.k_pages + t) = *(const uint4 *)(p.k_pages + f);
-        *(uint4 *)(p.v_pages + t) = *(const uint4 *)(p.v_pages + f);
-        if (h == 0 && c == 0) {
-            const int64_t ts = ((int64_t)tp << p.page_shift) + (to & in_page), fs = ((int64_t)fp << p.page_shift) + (from & in_page);
-            if (p.mass) p.mass[ts] = p.mass[fs];
-            if (p.stamp) p.stamp[ts] = p.stamp[fs];
+    const int pieces = p.Hkv * C, together = max(1, 256 / pieces);  // 16 bytes of a head of a token each; tokens that a workgroup moves at once
+    for (int m0 = part * together; m0 < n; m0 += per_seq * together) {
+        for (int x = threadIdx.x; x < min(together, n - m0) * pieces; x += 256) {
+            const int m = m0 + x / pieces, c = x % C, h = x / C % p.Hkv, to = holes[m], from = movers[m];
+            const int tp = table[to >> p.page_shift], fp = min(max(table[from >> p.page_shift], 0), p.n_pages - 1);
+            if (h == 0 && c == 0 && p.segments > 0 && p.src) p.src[(int64_t)b * (p.table_ld << p.page_shift) + to] = from;
+            if (tp < 0 || tp >= p.n_pages) continue;
+            const int64_t t = ((((int64_t)tp * p.Hkv + h) << p.page_shift) + (to & in_page)) * p.row_bytes + c * 16;
+            const int64_t f = ((((int64_t)fp * p.Hkv + h) << p.page_shift) + (from & in_page)) * p.row_bytes + c * 16;
+            *(uint4 *)(p.k_pages + t) = *(const uint4 *)(p.k_pages + f);
+            *(uint4 *)(p.v_pages + t) = *(const uint4 *)(p.v_pages + f);
+            if (h == 0 && c == 0) {
+                const int64_t ts = ((int64_t)tp << p.page_shift) + (to & in_page), fs = ((int64_t)fp << p.page_shift) + (from & in_page);
+                if (p.mass) p.mass[ts] = p.mass[fs];
+                if (p.stamp) p.stamp[ts] = p.stamp[fs];
+            }
         }
     }
 }
@@ -413,8 +426,8 @@ hipError_t launch_paged_evict(const EvictArgs &a, hipStream_t s)
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const int64_t items = (int64_t)(a.max_len / 2 + 1) * a.Hkv * (a.row_bytes / 16);  // the most that a sequence can have
-    const int per = (int)std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 4096 / a.n_seqs));
+    const int64_t most = ((int64_t)(a.max_len / 2 + 1) * a.Hkv * (a.row_bytes / 16) + 255) / 256;  // workgroups that a sequence can use
+    const int per = (int)std::max<int64_t>(1, std::min<int64_t>(most, 4096 / a.n_seqs));
     hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(per * a.n_seqs)), dim3(256), 0, s, a, per);
     return hipGetLastError();
 }
