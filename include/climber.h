@@ -244,17 +244,21 @@ int climber_attn_sumi_bias(const climber_config *cfg, const float *tau_layer,
  *               not NULL, both attention calls add to a token's entry its softmax weights in all of the call's
  *               rows and heads (not a candidate's weight on itself); an appended token starts from 0.  Sums are
  *               made in fp32 in an order that only depends on the sizes of the call.  Two calls that add to
- *               the same tokens must not overlap.
+ *               the same tokens must not overlap, and no two sequences of a call may list the same page then.
  *   stamp       dev int32 [n_pages][page_size] or NULL: a number of the caller's per token (its time, its
  *               position), stored by climber_attn_history_paged and kept with its token by climber_paged_evict.
  * page_size: a power of two, 16 .. 4096.  n_kv_heads divides cfg->n_heads: query head h reads cache head
  * h / (n_heads / n_kv_heads).  CLIMBER_BF16: d_head 64 or 128; CLIMBER_F32: d_head <= 128, a multiple of 4.
  * A page may be listed by several sequences (a shared prefix) as long as no call writes into it: an append
- * writes the pages of slots len[b] .. len[b] + rows - 1, an eviction those of slots below the budget.
+ * writes the pages of slots len[b] .. len[b] + rows - 1, an eviction those of slots below the budget, and with
+ * mass every call its entries of all tokens.
  * Contents of slots from len[b] on are never used: they may hold anything, NaN included.
  * Lengths, offsets and page numbers are device memory and cannot be checked on the host: lengths are clamped to
  * max_len, offsets to m_total, page numbers that are read to the pool, and a token whose page number lies outside the
  * pool is not stored.  climber_check_paged reports such values.
+ * Values are added up before they are divided by the sum of their weights: |v| times the tokens that a row sees has to stay below
+ * 2^119, or outputs may be infinite.
+ * A workspace belongs to one call at a time: two calls, or two captured graphs, that may run at once need one each.
  * Rows (q, k, v, o): row r starts r * ld elements behind the pointer and holds its heads one after the other;
  * pointers and row pitches are multiples of 16 bytes; o must not share an element with q, k or v.  Rows of no
  * sequence (behind off[n_seqs]) stay as they are. */
@@ -297,7 +301,7 @@ int climber_attn_sumi_paged(const climber_config *cfg, const float *tau_layer, c
  * The cache of a sequence is a set: kept tokens of slots below the new length stay where they are, and the places of evicted tokens
  * among them are filled, in ascending order, with the kept tokens of the slots behind.  k, v, and mass and stamp where they are
  * not NULL, move with their token; `rank` is only read.  Slots from the new length on keep what they held.
- * len_out: dev int32 [n_seqs], the new lengths (may be kv->len).  src: dev int32 [n_seqs][table_ld * page_size] or NULL: for each slot below
+ * len_out: dev int32 [n_seqs], the new lengths (may be kv->len, or budget).  src: dev int32 [n_seqs][table_ld * page_size] or NULL: for each slot below
  * the new length the slot that its token had before, -1 from there on.  A caller with more data per token moves it by src.
  * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _BUFSIZE, _UNSUPPORTED (d_head; max_len over 2^22), _RUNTIME. */
 int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, const float *rank, const int32_t *budget,

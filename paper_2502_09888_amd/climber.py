@@ -57,6 +57,7 @@ class PagedKV(C.Structure):
     """Mirror of ``climber_paged_kv`` (device pointers).  Build with ``paged_kv(...)``."""
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "mass", "stamp", "page_table", "len")] + \
                [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "n_seqs", "table_ld", "max_len")]
+    _device = None  # the CUDA device of its tensors, if it was made from tensors
 
 
 class _Weights(C.Structure):
@@ -420,9 +421,23 @@ def paged_kv(k, v, page_table, len, max_len: int, mass=None, stamp=None) -> Page
     n_seqs, table_ld = page_table.shape
     if v.shape != k.shape or len.numel() != n_seqs or any(t is not None and t.numel() != n_pages * page_size for t in (mass, stamp)):
         raise ValueError("k, v, page_table, len, mass and stamp are not of one cache")
+    if any(t is not None and t.device != k.device for t in (v, page_table, len, mass, stamp)):
+        raise ValueError("k, v, page_table, len, mass and stamp are not on one device")
     kv = PagedKV(_ptr(k), _ptr(v), _ptr(mass), _ptr(stamp), _ptr(page_table), _ptr(len), n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len)
     kv._keep = (k, v, mass, stamp, page_table, len)
+    if k.is_cuda:
+        kv._device = k.device.index
     return kv
+
+
+def _on_device(kv: PagedKV, stream) -> None:
+    """A call without a stream goes to the current device's, a call with one to its device: that has to be the cache's."""
+    at = kv._device
+    if at is None or isinstance(stream, int):
+        return
+    import torch
+    if at != (torch.cuda.current_device() if stream is None else getattr(stream, "device_index", at)):
+        raise ValueError("the paged cache is on another device than the stream")
 
 
 def climber_paged_workspace_bytes(cfg: Config, kv: PagedKV, m_total: int, m_max: int) -> int:
@@ -453,6 +468,7 @@ def climber_attn_history_paged(cfg: Config, tau_layer, kv: PagedKV, q, k, v, off
                                workspace, stream=None) -> None:
     """Append a chunk of new behaviours to the paged cache and attend from them.  q, k, v, o: row r is [r] of the tensor (row pitches are
     taken from it, so that columns of one projection's output can be passed as they are)."""
+    _on_device(kv, stream)
     code = (_native or _load_native(load_library())).attn_history_paged(cfg, tau_layer, kv, q, k, v, off, m_total, m_max, scen, beh, stamp, o,
                                                                         workspace, stream)
     if code is None:
@@ -467,6 +483,7 @@ def climber_attn_history_paged(cfg: Config, tau_layer, kv: PagedKV, q, k, v, off
 def climber_attn_sumi_paged(cfg: Config, tau_layer, kv: PagedKV, q_c, k_c, v_c, cand_off, m_total: int, m_max: int, cand_scen, cand_beh,
                             o_c, workspace, stream=None) -> None:
     """Candidates against the paged cache (rows as in climber_attn_history_paged)."""
+    _on_device(kv, stream)
     code = (_native or _load_native(load_library())).attn_sumi_paged(cfg, tau_layer, kv, q_c, k_c, v_c, cand_off, m_total, m_max, cand_scen,
                                                                      cand_beh, o_c, workspace, stream)
     if code is None:
@@ -481,6 +498,7 @@ def climber_attn_sumi_paged(cfg: Config, tau_layer, kv: PagedKV, q_c, k_c, v_c, 
 
 def climber_paged_evict(cfg: Config, kv: PagedKV, rank, budget, keep_from, len_out, src, workspace, stream=None) -> None:
     """Cut every sequence of the paged cache to its budget, least weight first."""
+    _on_device(kv, stream)
     code = (_native or _load_native(load_library())).paged_evict(cfg, kv, rank, budget, keep_from, len_out, src, workspace, stream)
     if code is None:
         code = load_library().climber_paged_evict(C.byref(cfg), C.byref(kv), _ptr(rank), _ptr(budget), _ptr(keep_from), _ptr(len_out), _ptr(src),

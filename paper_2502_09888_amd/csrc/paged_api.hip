@@ -30,7 +30,10 @@ int check_sizes(const climber_config *cfg, const climber_paged_kv *kv)
     if (kv->max_len < 0 || kv->max_len > (int64_t)kv->table_ld * kv->page_size) return CLIMBER_ERR_RANGE;
     // slots of a table row, rows of a launch and tokens of the pool are counted in 32 bits
     if ((int64_t)kv->table_ld * kv->page_size >= (int64_t)1 << 30 || (int64_t)kv->n_pages * kv->page_size >= (int64_t)1 << 31) return CLIMBER_ERR_RANGE;
-    if ((int64_t)kv->n_seqs * kv->n_kv_heads * std::max<int64_t>(1, kv->max_len / 32) >= (int64_t)1 << 31) return CLIMBER_ERR_RANGE;
+    // a launch has less than 2^32 threads: 256 for 256 tokens of a sequence and cache head (attention weights), 1024 for 4096 of a sequence
+    // (eviction)
+    if ((int64_t)kv->n_seqs * kv->n_kv_heads * (((int64_t)kv->max_len + 511) / 256 * 256) >= (int64_t)1 << 32) return CLIMBER_ERR_RANGE;
+    if (kv->n_seqs * std::max<int64_t>(1, evict_segments(kv->max_len)) >= (int64_t)1 << 22) return CLIMBER_ERR_RANGE;
     return CLIMBER_OK;
 }
 
@@ -49,6 +52,7 @@ int check_pointers(const climber_paged_kv *kv)
     return CLIMBER_OK;
 }
 
+constexpr int64_t kMostGroups = 1 << 24;  // workgroups of 256 threads of a launch
 constexpr int64_t kPartRows = 1 << 16;  // rows x heads x parts that a call's partial results have room for at most
 
 // Parts have 128 keys at least, beyond 16 parts 256: few keys are soon done, many parts take long to join (us with 256 / 128 / this: 128
@@ -149,13 +153,16 @@ int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_
         overlap(o, ld_o * elem, wide * elem, q, ld_q * elem, wide * elem, m_total))
         return CLIMBER_ERR_UNSUPPORTED;
     const int n_split = parts(cfg, kv, m_total, m_max);
+    const bool bf16 = cfg->dtype == CLIMBER_BF16;
+    const int64_t G = cfg->n_heads / kv->n_kv_heads, heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged_tile_rows(bf16, cfg->d_head, m_max * G, heads);
+    if ((m_max * G + tile - 1) / tile * (heads + 7) * n_split >= kMostGroups) return CLIMBER_ERR_RANGE;
+    if (kv->mass && !bf16 && heads * ((kv->max_len + 31) / 32) >= kMostGroups) return CLIMBER_ERR_RANGE;
     const Layout w = layout_of(cfg, kv, m_total, n_split > 1 ? (size_t)n_split * m_total * cfg->n_heads : 0);
     if (w.bytes > 0 && !workspace) return CLIMBER_ERR_NULL;
     if (!aligned(workspace, 256)) return CLIMBER_ERR_ALIGN;
     if (ws_bytes < w.bytes) return CLIMBER_ERR_BUFSIZE;
 
     uint8_t *ws = (uint8_t *)workspace;
-    const bool bf16 = cfg->dtype == CLIMBER_BF16;
     PagedArgs a{};
     a.k_pages = (uint8_t *)kv->k;
     a.v_pages = (uint8_t *)kv->v;

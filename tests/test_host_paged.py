@@ -154,3 +154,100 @@ def test_row_pitches_come_from_the_tensors():
             P.paged_kv(*args, 64)
     with pytest.raises(ValueError):
         P.paged_kv(pages, pages, table, n, 64, mass=torch.zeros(10, 8))
+
+
+def test_launches_that_would_be_too_large():
+    # a launch has fewer than 2^32 threads: 2^24 workgroups of 256, of 1024 for an eviction
+    c = cfg()
+    lib = P.load_library()
+    assert attend(cache=kv(n_seqs=1 << 20)) == RANGE      # 2^20 sequences x 2 heads x 2304 (2048 and up to 256 more) tokens: 1.1 x 2^32
+    assert attend(cache=kv(n_seqs=1 << 22, max_len=16)) == RANGE
+    assert attend(cache=kv(n_seqs=1 << 16), m_total=1 << 18, m_max=1 << 17) == RANGE   # rows of 2^16 sequences with 2^17 each
+    assert P.climber_paged_workspace_bytes(c, kv(n_seqs=1 << 22, max_len=16), 4, 4) == 0
+    cache = kv(n_seqs=1 << 13, max_len=1 << 21, table_ld=1 << 15, n_kv_heads=1)
+    assert lib.climber_paged_evict(C.byref(c), C.byref(cache), FAKE, FAKE, None, FAKE, None, FAKE, 1 << 40, None) == RANGE
+    f32 = cfg(dtype=P.F32)
+    assert attend(f32, kv(n_seqs=1 << 16, max_len=1 << 12, table_ld=64, mass=FAKE)) == RANGE
+    assert attend(f32, kv(n_seqs=1 << 12, max_len=1 << 12, table_ld=64, mass=FAKE)) == BUFSIZE
+
+
+def test_caches_and_streams_of_other_devices(monkeypatch):
+    torch = pytest.importorskip("torch")
+    pages, table, n = torch.zeros(10, 2, 16, 64), torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        P.paged_kv(pages, pages, table.to("meta"), n, 64)
+    cache = kv()
+    cache._device = 1                                   # a cache of cuda:1 while cuda:0 is the current device
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    other = type("Stream", (), {"cuda_stream": 5, "device_index": 0})()
+    for stream in (None, other):
+        with pytest.raises(ValueError):
+            P.climber_attn_history_paged(cfg(), FAKE, cache, FAKE, FAKE, FAKE, FAKE, 4, 4, FAKE, FAKE, None, FAKE, None, stream)
+        with pytest.raises(ValueError):
+            P.climber_attn_sumi_paged(cfg(), FAKE, cache, FAKE, FAKE, FAKE, FAKE, 4, 4, FAKE, FAKE, FAKE, None, stream)
+        with pytest.raises(ValueError):
+            P.climber_paged_evict(cfg(), cache, FAKE, FAKE, None, FAKE, None, None, stream)
+    other.device_index = 1                              # its own device: the call goes on, and stops at its arguments
+    with pytest.raises(P.ClimberError) as e:
+        P.climber_paged_evict(cfg(), cache, FAKE, None, None, FAKE, None, None, other)
+    assert e.value.code == NULL
+
+
+@pytest.mark.parametrize("name", ["climber_attn_history_paged", "climber_attn_sumi_paged", "climber_paged_evict"])
+def test_native_binding_passes_every_argument_in_its_place(name, monkeypatch):
+    # the binding's entry point is replaced by one that records what arrives; what it does not convert goes to ctypes, which does or refuses
+    torch = pytest.importorskip("torch")
+    from paper_2502_09888_amd import _native, climber as mod
+    lib = P.load_library()
+    real, args = getattr(lib, name), getattr(lib, name).argtypes
+    seen = []
+    structs = [hasattr(t, "_type_") and hasattr(t._type_, "_fields_") for t in args]
+
+    def record(*a):
+        seen.append([C.string_at(x, C.sizeof(t._type_)) if s else x for x, t, s in zip(a, args, structs)])
+        return -5
+    call = C.CFUNCTYPE(C.c_int, *(C.c_void_p if s else t for t, s in zip(args, structs)))(record)
+
+    def bind(which):
+        def address(n):
+            return C.cast(call if n == which else getattr(lib, n), C.c_void_p).value
+        _native.bind(*(address(n) for n in ("climber_attn_history", "climber_attn_sumi", "climber_attn_history_bias", "climber_attn_sumi_bias")),
+                     P.Config, P.RelBias, torch.cuda.current_device, torch._C._cuda_getCurrentRawStream,
+                     *(address(n) for n in ("climber_attn_history_paged", "climber_attn_sumi_paged", "climber_paged_evict")), PagedKV)
+    c, cache = cfg(), kv()
+    rows = torch.zeros(6, 12 * 64, dtype=torch.bfloat16)                        # one projection's output: 8 + 2 + 2 heads
+    q, k, v = rows[:, :512], rows[:, 512:640], rows[:, 640:].unflatten(1, (2, 64))
+    o, t, ws = torch.zeros(6, 8, 64, dtype=torch.bfloat16), [torch.zeros(4) for _ in range(8)], torch.zeros(300, dtype=torch.uint8)
+    raw = [C.string_at(C.byref(x), C.sizeof(x)) for x in (c, cache)]
+    ptr = [x.data_ptr() for x in t]
+    if name == "climber_paged_evict":
+        given = [c, cache, t[0], t[1], None, t[2], FAKE, ws]
+        arrives = [*raw, ptr[0], ptr[1], None, ptr[2], FAKE, ws.data_ptr(), 300]
+    elif name == "climber_attn_sumi_paged":
+        given = [c, t[0], cache, q, k, v, t[1], 70000, 2**31 - 1, t[2], t[3], o, ws]
+        arrives = [raw[0], ptr[0], raw[1], q.data_ptr(), 768, k.data_ptr(), v.data_ptr(), 768, ptr[1], 70000, 2**31 - 1, ptr[2], ptr[3],
+                   o.data_ptr(), 512, ws.data_ptr(), 300]
+    else:
+        given = [c, t[0], cache, FAKE, q[:1, :128], k[1:2], t[1], 1, 1, t[2], t[3], t[4], o, None]
+        arrives = [raw[0], ptr[0], raw[1], FAKE, 512, q.data_ptr(), k[1:2].data_ptr(), 128, ptr[1], 1, 1, ptr[2], ptr[3], ptr[4], o.data_ptr(), 512,
+                   None, 0]
+    try:
+        bind(name)
+        for stream, handle in ((0x55AA, 0x55AA), (type("S", (), {"cuda_stream": 77})(), 77), (0, None)):
+            with pytest.raises(P.ClimberError) as e:
+                getattr(P, name)(*given, stream=stream)
+            assert e.value.code == -5 and seen.pop() == arrives + [handle]
+        for at in range(len(given)):
+            bad = list(given)
+            bad[at] = type("Wrong", (), {})()
+            with pytest.raises((AttributeError, TypeError, C.ArgumentError)):
+                getattr(P, name)(*bad, stream=0)
+        if name == "climber_attn_sumi_paged":           # rows that no pitch describes
+            for at, bad in ((3, rows.t()), (4, rows.view(6, 12, 64).transpose(1, 2)), (5, torch.zeros(6, 128)), (11, rows[:, ::2])):
+                wrong = list(given)
+                wrong[at] = bad
+                with pytest.raises(ValueError):
+                    getattr(P, name)(*wrong, stream=0)
+        assert not seen and mod._native is _native and real.argtypes == args
+    finally:
+        bind(None)
