@@ -53,7 +53,9 @@ int check_pointers(const climber_paged_kv *kv)
 }
 
 constexpr int64_t kMostGroups = 1 << 24;  // workgroups of 256 threads of a launch
-constexpr int64_t kPartRows = 1 << 16;  // rows x heads x parts that a call's partial results have room for at most
+// Rows x heads x parts that a call's partial results have room for at most.  They are written and read again, which pays off where a
+// part is long (us of four users with 512 candidates on 2000 with room for them / without 48 / 31, of twelve on up to 20000 166 / 399).
+int64_t part_rows(const climber_paged_kv *kv) { return std::min<int64_t>(4, std::max<int64_t>(1, kv->max_len / 4096)) << 16; }
 
 // Parts have 128 keys at least, beyond 16 parts 256: few keys are soon done, many parts take long to join (us with 256 / 128 / this: 128
 // candidates on 1000 tokens 16.5 / 13.3 / 13.3, one token on 8000 19.2 / 22.6 / 19.2).
@@ -62,13 +64,16 @@ int64_t most_parts(const climber_paged_kv *kv)
     return std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(16, kv->max_len / 128), kv->max_len / 256));
 }
 
-// Parts of the keys, so that a launch has two workgroups per CU.
+// Parts of the keys, so that a launch has two workgroups per CU; in bf16, whose parts cost less beside their keys' work, two that are
+// expected to have rows (three ragged sessions on up to 4000 96 / 66 us).
 int parts(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total, int32_t m_max)
 {
+    const bool bf16 = cfg->dtype == CLIMBER_BF16;
     const int64_t rows = (int64_t)m_max * (cfg->n_heads / kv->n_kv_heads);
-    const int64_t heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged_tile_rows(cfg->dtype == CLIMBER_BF16, cfg->d_head, rows, heads);
-    const int64_t groups = std::max<int64_t>(1, (rows + tile - 1) / tile * heads);
-    const int64_t room = kPartRows / std::max<int64_t>(1, (int64_t)m_total * cfg->n_heads);
+    const int64_t heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged_tile_rows(bf16, cfg->d_head, rows, heads);
+    const double with_rows = bf16 ? (double)m_total / ((double)kv->n_seqs * std::max(1, m_max)) : 1.0;
+    const int64_t groups = std::max<int64_t>(1, (int64_t)(std::min(1.0, with_rows) * (double)((rows + tile - 1) / tile * heads)));
+    const int64_t room = part_rows(kv) / std::max<int64_t>(1, (int64_t)m_total * cfg->n_heads);
     return (int)std::max<int64_t>(1, std::min(std::min(512 / groups, room), most_parts(kv)));
 }
 
@@ -230,7 +235,7 @@ size_t climber_paged_workspace_bytes(const climber_config *cfg, const climber_pa
     if (check_sizes(cfg, kv) != CLIMBER_OK || check_rows(cfg, m_total, m_max) != CLIMBER_OK) return 0;
     // (a smaller call may have more parts: room for as many as one can have)
     const int64_t n = most_parts(kv) * m_total * cfg->n_heads;
-    return std::max(layout_of(cfg, kv, m_total, most_parts(kv) > 1 ? (size_t)std::min(n, kPartRows) : 0).bytes,
+    return std::max(layout_of(cfg, kv, m_total, most_parts(kv) > 1 ? (size_t)std::min(n, part_rows(kv)) : 0).bytes,
                     evict_segments(kv->max_len) <= kEvictMostSegments ? evict_layout(kv).bytes : 0);
 }
 
