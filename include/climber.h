@@ -308,7 +308,8 @@ int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, c
                         const int32_t *keep_from, int32_t *len_out, int32_t *src, void *workspace, size_t ws_bytes, void *stream);
 
 /* climber_check_inputs for a paged cache: one small kernel that reads page_table, len and, if not NULL, off against the rules
- * above for a call of m_total rows that stores them (appends != 0) or does not, and ORs CLIMBER_BAD_* bits into *status. */
+ * above for a call of m_total rows that stores them (appends != 0) or does not, and ORs CLIMBER_BAD_* bits into *status.  Offsets
+ * that end before m_total are in order: the rows behind belong to no sequence. */
 #define CLIMBER_BAD_PAGE 32 /* a page number of a token outside [0, n_pages) */
 #define CLIMBER_BAD_LEN 64  /* a length below 0, or over max_len after the call */
 int climber_check_paged(const climber_config *cfg, const climber_paged_kv *kv, const int32_t *off, int32_t m_total, int32_t m_max,

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(256) void check_paged_kernel(const int32_t *table, 
     int64_t rows = 0;
     if (off) {
         const int lo = off[b], hi = off[b + 1];
-        if (hi < lo || lo < 0 || (b == 0 && lo != 0) || hi > m_total || (b == n_seqs - 1 && hi != m_total)) bad |= CLIMBER_BAD_OFFSETS;
+        if (hi < lo || lo < 0 || (b == 0 && lo != 0) || hi > m_total) bad |= CLIMBER_BAD_OFFSETS;
         rows = (int64_t)hi - lo;
         if (rows > m_max) bad |= CLIMBER_BAD_M_MAX;
     }

@@ -16,7 +16,6 @@ typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef const __attribute__((address_space(1))) uint8_t glb_u8;
-typedef const __attribute__((address_space(4))) int32_t const_i32;  // read by scalar loads
 
 static __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
 static __device__ __forceinline__ float half_max(float x)

@@ -148,3 +148,15 @@ def test_new_lengths_in_place_of_the_budget(n):
     torch.cuda.synchronize()
     assert out.tolist() == budget.tolist() == [n // 3, 5]
     assert same_bits(dev.k, other.k) and same_bits(dev.v, other.v) and same_bits(dev.mass, other.mass)
+
+
+def test_check_allows_rows_of_no_sequence():
+    case = Case([30, 0, 7], [4, 0, 2], seed=57, tail=5)
+    dev = Device(case)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    for appends in (True, False):
+        dev.P.climber_check_paged(dev.cfg, dev.kv, dev.off, case.m, dev.m_max, appends, status)
+    assert status.item() == 0
+    dev.off[3] = case.m + 1
+    dev.P.climber_check_paged(dev.cfg, dev.kv, dev.off, case.m, dev.m_max, False, status)
+    assert status.item() == dev.P.BAD_OFFSETS | dev.P.BAD_M_MAX
