@@ -421,6 +421,10 @@ def paged_kv(k, v, page_table, len, max_len: int, mass=None, stamp=None) -> Page
     n_seqs, table_ld = page_table.shape
     if v.shape != k.shape or len.numel() != n_seqs or any(t is not None and t.numel() != n_pages * page_size for t in (mass, stamp)):
         raise ValueError("k, v, page_table, len, mass and stamp are not of one cache")
+    kinds = [str(t.dtype)[6:] for t in (k, v, page_table, len, mass, stamp) if t is not None]  # (without "torch.")
+    if kinds != [kinds[0]] * 2 + ["int32"] * 2 + ["float32"] * (mass is not None) + ["int32"] * (stamp is not None) or \
+            kinds[0] not in ("bfloat16", "float32"):
+        raise ValueError("k, v are bfloat16 or float32, page_table, len and stamp int32, mass float32")
     if any(t is not None and t.device != k.device for t in (v, page_table, len, mass, stamp)):
         raise ValueError("k, v, page_table, len, mass and stamp are not on one device")
     kv = PagedKV(_ptr(k), _ptr(v), _ptr(mass), _ptr(stamp), _ptr(page_table), _ptr(len), n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len)

@@ -251,3 +251,17 @@ def test_native_binding_passes_every_argument_in_its_place(name, monkeypatch):
         assert not seen and mod._native is _native and real.argtypes == args
     finally:
         bind(None)
+
+
+def test_a_cache_of_other_types_is_none():
+    torch = pytest.importorskip("torch")
+    parts = dict(k=torch.zeros(10, 2, 16, 64), v=torch.zeros(10, 2, 16, 64), page_table=torch.zeros(3, 4, dtype=torch.int32),
+                 len=torch.zeros(3, dtype=torch.int32), mass=torch.zeros(10, 16), stamp=torch.zeros(10, 16, dtype=torch.int32))
+    P.paged_kv(**parts, max_len=64)
+    P.paged_kv(**{**parts, "k": parts["k"].bfloat16(), "v": parts["v"].bfloat16(), "mass": None}, max_len=64)
+    for name, to in (("k", torch.bfloat16), ("v", torch.float64), ("page_table", torch.int64), ("len", torch.int64), ("mass", torch.float64),
+                     ("stamp", torch.float32)):
+        with pytest.raises(ValueError):
+            P.paged_kv(**{**parts, name: parts[name].to(to)}, max_len=64)
+    with pytest.raises(ValueError):
+        P.paged_kv(**{**parts, "k": parts["k"].half(), "v": parts["v"].half()}, max_len=64)
