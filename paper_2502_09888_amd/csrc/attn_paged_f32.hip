@@ -363,42 +363,54 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_paged_few_f32_kern
 
 // Partial results of the parts of the keys, joined.  32 lanes have a row's dimensions; GROUPS such groups share its parts, and 8 / GROUPS
 // rows x heads are a workgroup's (64 parts of 32 rows x heads: 65 us with a wave for each, which takes one part after the other, 5 with 8 groups).
+// A launch as short as this is bound by its trips to memory: whatever a thread can need is requested at once, before it is known to be needed.
 template <typename E, int GROUPS>
 __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedArgs p)
 {
+    constexpr int kFirst = GROUPS > 1 ? 8 : 4;  // parts of a group requested at once
     __shared__ f32x4 sums[8][32];
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, g = group % GROUPS, c = lane * 4;
     const int64_t all = (int64_t)p.m_total * p.H, rh = (int64_t)blockIdx.x * (8 / GROUPS) + group / GROUPS, row = rh / p.H;
     const int h = (int)(rh % p.H);
-    const bool mine = rh < all && row >= max(p.off[0], 0) && row < p.off[p.n_seqs];  // a row of no sequence stays as it is
     float M = -INFINITY, L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (mine) {
+    if (rh < all) {
         auto part = [&](int i) { return *(const float2 *)(p.part_ml + (i * all + rh) * 2); };
+        auto sum = [&](int i) { return c < p.d ? *(const f32x4 *)(p.part_o + (i * all + rh) * p.d + c) : f32x4{0.f, 0.f, 0.f, 0.f}; };
+        f32x4 x[kFirst];
+        float2 ml[kFirst];
+#pragma unroll
+        for (int k = 0; k < kFirst; ++k)
+            if (g + k * GROUPS < p.n_split) {
+                ml[k] = part(g + k * GROUPS);
+                x[k] = sum(g + k * GROUPS);
+            }
         for (int i = lane; i < p.n_split; i += 32) {
-            const float2 ml = part(i);
-            if (ml.y != 0.f) M = fmaxf(M, ml.x);  // (0: no key of the part is seen)
+            const float2 y = part(i);
+            if (y.y != 0.f) M = fmaxf(M, y.x);  // (0: no key of the part is seen)
         }
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) M = fmaxf(M, __shfl_xor(M, o, 64));
         for (int i = lane; i < p.n_split; i += 32) {
-            const float2 ml = part(i);
-            if (ml.y != 0.f) L += ml.y * __builtin_amdgcn_exp2f(ml.x - M);
+            const float2 y = part(i);
+            if (y.y != 0.f) L += y.y * __builtin_amdgcn_exp2f(y.x - M);
         }
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) L += __shfl_xor(L, o, 64);
-#pragma unroll 4
-        for (int i = g; i < p.n_split; i += GROUPS) {
-            const float2 ml = part(i);
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
-            if (c < p.d) x = *(const f32x4 *)(p.part_o + (i * all + rh) * p.d + c);
-            const float w = __builtin_amdgcn_exp2f(ml.x - M);
-            if (ml.y != 0.f) {
+        auto add = [&](float2 y, f32x4 o) {
+            const float w = __builtin_amdgcn_exp2f(y.x - M);
+            if (y.y != 0.f) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += w * x[e];
+                for (int e = 0; e < 4; ++e) acc[e] += w * o[e];
             }
-        }
+        };
+#pragma unroll
+        for (int k = 0; k < kFirst; ++k)
+            if (g + k * GROUPS < p.n_split) add(ml[k], x[k]);
+#pragma unroll 4
+        for (int i = g + kFirst * GROUPS; i < p.n_split; i += GROUPS) add(part(i), sum(i));
     }
+    const bool mine = rh < all && row >= max(p.off[0], 0) && row < p.off[p.n_seqs];  // a row of no sequence stays as it is
     if constexpr (GROUPS > 1) {
         sums[group][lane] = acc;
         __syncthreads();
@@ -478,13 +490,14 @@ __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, floa
 
 __global__ __launch_bounds__(256) void paged_mass_add_kernel(const PagedArgs p, const float *part, int n_parts)
 {
-    const int per = (p.max_len + 255) / 256, b = blockIdx.x / per, j = (blockIdx.x % per) * 256 + threadIdx.x;
-    const PagedSeq s = paged_seq(p, b);
-    if (s.T == 0 || j >= (p.sumi ? s.n : s.n + s.T)) return;
+    const int per = (p.max_len + 255) / 256, b = blockIdx.x / per, j = min((int)(blockIdx.x % per) * 256 + (int)threadIdx.x, p.max_len - 1);
     const int raw = p.table[(int64_t)b * p.table_ld + (j >> p.page_shift)];
-    if (raw < 0 || raw >= p.n_pages) return;
-    float x = 0.f;
+    float x = 0.f;  // (of no meaning where the sequence has no such token; requested before its length is known)
+#pragma unroll 8
     for (int i = 0; i < n_parts; ++i) x += part[((int64_t)b * n_parts + i) * p.max_len + j];
+    const PagedSeq s = paged_seq(p, b);
+    if (s.T == 0 || j >= (p.sumi ? s.n : s.n + s.T) || j != (int)(blockIdx.x % per) * 256 + (int)threadIdx.x) return;
+    if (raw < 0 || raw >= p.n_pages) return;
     float *to = p.mass + ((int64_t)raw << p.page_shift) + (j & ((1 << p.page_shift) - 1));
     *to = j < s.n ? *to + x : x;  // a new token has none yet, whatever its slot holds
 }
