@@ -3,6 +3,7 @@
 #include "../../include/climber.h"
 
 #include <algorithm>
+#include <cmath>
 
 #include "internal.h"
 #include "paged.h"
@@ -53,28 +54,29 @@ int check_pointers(const climber_paged_kv *kv)
 }
 
 constexpr int64_t kMostGroups = 1 << 24;  // workgroups of 256 threads of a launch
-// Rows x heads x parts that a call's partial results have room for at most.  They are written and read again, which pays off where a
-// part is long (us of four users with 512 candidates on 2000 with room for them / without 48 / 31, of twelve on up to 20000 166 / 399).
+// Rows x heads x parts that a call's partial results have room for at most, and parts.
 int64_t part_rows(const climber_paged_kv *kv) { return std::min<int64_t>(4, std::max<int64_t>(1, kv->max_len / 4096)) << 16; }
+int64_t most_parts(const climber_paged_kv *kv) { return std::min<int64_t>(512, std::max<int64_t>(1, kv->max_len / 32)); }
 
-// Parts have 128 keys at least, beyond 16 parts 256: few keys are soon done, many parts take long to join (us with 256 / 128 / this: 128
-// candidates on 1000 tokens 16.5 / 13.3 / 13.3, one token on 8000 19.2 / 22.6 / 19.2).
-int64_t most_parts(const climber_paged_kv *kv)
-{
-    return std::max<int64_t>(1, std::max<int64_t>(std::min<int64_t>(16, kv->max_len / 128), kv->max_len / 256));
-}
-
-// Parts of the keys, so that a launch has two workgroups per CU; in bf16, whose parts cost less beside their keys' work, two that are
-// expected to have rows (three ragged sessions on up to 4000 96 / 66 us).
+// Parts of the keys: up to two workgroups per CU (in bf16, whose parts cost less beside their keys' work, two that are expected to have
+// rows), and as many as are worth it.  In us, fitted to sweeps: a workgroup needs per_key for each key and d_head's unit; a join is a launch of 3.5,
+// and each part costs it 0.1 and its rows, written and read again.  One / chosen parts: 128 candidates of one user on 1000 16 / 13, three
+// sessions on up to 4000 96 / 66, candidates of twelve users on up to 20000 400 / 166, one fp32 row on 1000 22 / 15; parts / one where the rows are
+// many and the keys few: 18 prompts of up to 268 31 / 18, eight of up to 700 35 / 28.
 int parts(const climber_config *cfg, const climber_paged_kv *kv, int32_t m_total, int32_t m_max)
 {
     const bool bf16 = cfg->dtype == CLIMBER_BF16;
-    const int64_t rows = (int64_t)m_max * (cfg->n_heads / kv->n_kv_heads);
+    const int64_t rows = (int64_t)m_max * (cfg->n_heads / kv->n_kv_heads), out = std::max<int64_t>(1, (int64_t)m_total * cfg->n_heads);
     const int64_t heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged_tile_rows(bf16, cfg->d_head, rows, heads);
     const double with_rows = bf16 ? (double)m_total / ((double)kv->n_seqs * std::max(1, m_max)) : 1.0;
     const int64_t groups = std::max<int64_t>(1, (int64_t)(std::min(1.0, with_rows) * (double)((rows + tile - 1) / tile * heads)));
-    const int64_t room = part_rows(kv) / std::max<int64_t>(1, (int64_t)m_total * cfg->n_heads);
-    return (int)std::max<int64_t>(1, std::min(std::min(512 / groups, room), most_parts(kv)));
+    const int64_t unit = bf16 && tile == 32 ? 128 : 32;  // keys that a workgroup takes at once
+    const int64_t most = std::min(std::min(512 / groups, part_rows(kv) / out), std::min(most_parts(kv), kv->max_len / unit));
+    if (most < 2) return 1;
+    const double per_key = bf16 ? (tile == 32 ? 9e-5 : tile == 128 ? 2e-4 : 3.5e-4) : tile == 32 ? 3.5e-4 : 9e-4;
+    const double one = per_key * cfg->d_head * kv->max_len, each = 0.1 + 8.0 * cfg->d_head * (double)out / 2.5e6;
+    const int64_t n = std::min<int64_t>(most, (int64_t)(std::sqrt(one / each) + 0.5));
+    return n > 1 && one / (double)n + 3.5 + each * (double)n < one ? (int)n : 1;
 }
 
 size_t logits_pitch(const climber_paged_kv *kv) { return ((size_t)kv->max_len + 31) / 32 * 32; }
