@@ -150,10 +150,11 @@ static __device__ __forceinline__ void block_softmax(f32x16 &S, float &m, float 
 // The transposed problem, as in the bf16 kernels: S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x2_f32.  A lane owns one packed
 // row (lane % 32), its probabilities leave the accumulator as the operand of the value product (step r of it takes the keys of
 // accumulator register r).  The sum over the dimensions is taken in an order that lets a lane read four of them at once.  Four waves
-// with 32 rows each share the keys of a stage.  Chunks of 1000 behaviours of eight users on 1000, 8 heads of 64: 367 us, 67 TFLOP/s (a library
-// product reaches 155), with one stage and a barrier on either side of it; bound by the two in turn.
+// with 32 rows each share the keys of a stage.  Chunks of 1000 behaviours of eight users on 1000, 8 heads of 64: 315 us, 79 TFLOP/s (a library
+// product reaches 155; 370 us with keys requested when their turn comes); 256 candidates of each of 16 users on 1000 97 us (120 with registers
+// for one workgroup per CU).
 template <int DP, bool SUMI>
-__global__ __launch_bounds__(256) void attn_paged_f32_kernel(const PagedArgs p)
+__global__ __launch_bounds__(256, 2) void attn_paged_f32_kernel(const PagedArgs p)
 {
     constexpr int kPitch = DP + 4, NB = DP / 32, NW = 4;
     __shared__ __attribute__((aligned(16))) float tk[kKeys * kPitch], tv[kKeys * kPitch];
@@ -189,19 +190,31 @@ __global__ __launch_bounds__(256) void attn_paged_f32_kernel(const PagedArgs p)
         for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
     if (SUMI && w.split == 0) own_first<DP>(p, row, w.hk, hf, q, m, l, O);
 
+    // The next keys are on their way, in registers, while these are worked on.
+    constexpr int C = DP / 4, kMine = kKeys * C / 256;
+    f32x4 next_k[kMine], next_v[kMine];
+    auto request = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < kMine; ++u) {
+            const int i = threadIdx.x + u * 256, j = min(k0 + i / C, k_hi - 1), x = (i % C) * 4;  // keys behind the last one: that one again, and masked
+            const bool old = j < s.n;
+            const int64_t cached = old ? paged_row(p, paged_page(p, w.b, j), w.hk, j) : 0, fresh = (s.row0 + j - s.n) * p.ld_kv + (int64_t)w.hk * p.row_bytes;
+            const float *from_k = (const float *)(old ? p.k_pages + cached : p.k + fresh), *from_v = (const float *)(old ? p.v_pages + cached : p.v + fresh);
+            next_k[u] = x < p.d ? load4(from_k + x) : f32x4{0.f, 0.f, 0.f, 0.f};
+            next_v[u] = x < p.d ? load4(from_v + x) : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    if (k_lo < k_hi) request(k_lo);
     for (int k0 = k_lo; k0 < k_hi; k0 += kKeys) {
-        // keys behind the last one are read as the last one, and masked
-        auto ptr = [&](const uint8_t *pages, const uint8_t *fresh) {
-            return [&, pages, fresh](int i) {
-                const int j = min(k0 + i, k_hi - 1);
-                if (j < s.n) return pages + paged_row(p, paged_page(p, w.b, j), w.hk, j);
-                return fresh + (s.row0 + j - s.n) * p.ld_kv + (int64_t)w.hk * p.row_bytes;
-            };
-        };
         __syncthreads();
-        load_tile<DP, NW * 64>(tk, p.d, ptr(p.k_pages, p.k));
-        load_tile<DP, NW * 64>(tv, p.d, ptr(p.v_pages, p.v));
+#pragma unroll
+        for (int u = 0; u < kMine; ++u) {
+            const int i = threadIdx.x + u * 256, to = i / C * kPitch + i % C * 4;
+            *(f32x4 *)(tk + to) = next_k[u];
+            *(f32x4 *)(tv + to) = next_v[u];
+        }
         __syncthreads();
+        if (k0 + kKeys < k_hi) request(k0 + kKeys);
         if (r_wave >= rows || k0 >= lim_hi) continue;  // (no row here, or none that sees a key of the tile)
         f32x16 S;
 #pragma unroll

@@ -135,7 +135,7 @@ static __device__ __forceinline__ float paged_row_scale(const PagedArgs &p, int6
 
 // Packed rows of a workgroup.  32: the kernels for few rows, whose waves share out keys.  bf16: where a sequence and cache head has no
 // more of them.  fp32, which has no use for more rows per operand than 32: also where tiles of 128 rows are fewer than 96 (us few /
-// tiles at d_head 64: 48 of them 30 / 46, 128 of them 76 / 75, 256 of them 156 / 143), and above d_head 64, where tiles would leave one wave
+// tiles at d_head 64: 48 of them 30 / 46, 128 of them 76 / 70, 256 of them 156 / 127), and above d_head 64, where tiles would leave one wave
 // per SIMD (788 / 1020 for chunks of 1000 of 8 users on 1000).  256 at d_head 64 in bf16: 108 / 123 with 128 for 512 candidates of
 // each of 64 users on 1024.
 static inline int paged_tile_rows(bool bf16, int d, int64_t rows, int64_t groups)
