@@ -315,6 +315,8 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_paged_few_f32_kern
         for (int i = 0; i < 16; ++i) O[db][i] = 0.f;
     if (SUMI && w.split == 0 && wave == 0) own_first<DP>(p, row, w.hk, hf, q, m, l, O);
 
+    // logits for the weights per token
+    float *const logits = p.logits ? p.logits + (((int64_t)w.b * p.Hkv + w.hk) * (p.m_max * p.G) + r_tile + l32) * p.logits_ld + 4 * hf : nullptr;
     for (int blk = wave; blk < n_blk; blk += 4) {
         const int k0 = k_lo + blk * kKeys;
         f32x16 S;
@@ -324,6 +326,15 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_paged_few_f32_kern
         for (int i = 0; i < DP / 8; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) S = __builtin_amdgcn_mfma_f32_32x32x2f32(k[i][e], q[i][e], S, 0, 0, 0);
+        if (logits && r_tile + l32 < rows) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = k0 + 8 * g + 4 * hf + e < min(lim, k_hi) ? S[4 * g + e] * c : -INFINITY;
+                *(f32x4 *)(logits + k0 + 8 * g) = x;
+            }
+        }
         block_softmax<DP>(S, m, l, O, c, k0, hf, min(lim, k_hi), k0 + kKeys > min(lim_lo, k_hi), [&](int db, int i) { return v[db][i]; });
         if (blk + 4 < n_blk) request(blk + 4);
     }

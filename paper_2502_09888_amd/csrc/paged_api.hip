@@ -96,7 +96,7 @@ Layout layout_of(const climber_config *cfg, const climber_paged_kv *kv, int32_t 
         // sums of the rows' parts (more than one: of at most kMassGroups workgroups), or the logits of few rows (a call may have fewer rows
         // than it is asked for here)
         const size_t groups = (size_t)kv->n_seqs * kv->n_kv_heads, G = cfg->n_heads / kv->n_kv_heads;
-        const size_t few = cfg->dtype == CLIMBER_BF16 ? kMassFewRows / G * G * logits_pitch(kv) : 0;
+        const size_t few = kMassFewRows / G * G * logits_pitch(kv);
         w.bytes += up(std::max(groups * kv->max_len + (size_t)kMassGroups * kMassKeys, groups * few) * 4);
     }
     return w;
@@ -212,7 +212,7 @@ int attn_paged(const climber_config *cfg, const float *tau, const climber_paged_
     a.part_ml = (float *)(ws + w.part_ml);
     a.lse = kv->mass ? (float2 *)(ws + w.lse) : nullptr;
     float *part = (float *)(ws + w.mass);
-    const bool few = bf16 && kv->mass && (int64_t)m_max * a.G <= kMassFewRows;
+    const bool few = kv->mass && (int64_t)m_max * a.G <= kMassFewRows;
     if (few) {
         a.logits = part;
         a.logits_ld = (int)logits_pitch(kv);
