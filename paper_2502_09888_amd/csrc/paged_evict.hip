@@ -38,15 +38,22 @@ static __device__ __forceinline__ int64_t token_at(const EvictArgs &p, int b, in
     return ((int64_t)page << p.page_shift) + (slot & ((1 << p.page_shift) - 1));
 }
 
+// inclusive sum over the lanes, by DPP: row_shr 1, 2, 4, 8, then each row's last lane to the rows behind it
+static __device__ __forceinline__ int sum_to_me(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 and 47 of the rows before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31
+    return x;
+}
+
 // exclusive sum over the threads of a workgroup, in their order (one barrier; `room` is free again after the next one)
 static __device__ __forceinline__ int before_me(int x, int *room, int lane, int wave)
 {
-    int sum = x;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int y = __shfl_up(sum, o, 64);
-        if (lane >= o) sum += y;
-    }
+    const int sum = sum_to_me(x);
     if (lane == 63) room[wave] = sum;
     __syncthreads();
     int at = sum - x;
@@ -55,20 +62,20 @@ static __device__ __forceinline__ int before_me(int x, int *room, int lane, int 
     return at;
 }
 
-// The bin in which the need-th largest lies (bins counted from the highest down; this thread has two) -> chosen = {bin, how many of it};
-// ends without a barrier.
+// The bin in which the need-th largest lies (bins counted from the highest down; this thread has two) -> chosen = {bin, how many of it, of
+// how many}; ends without a barrier.
 static __device__ __forceinline__ void choose(int high, int low, int need, int *room, int *chosen, int tid)
 {
     const int at = before_me(high + low, room, tid & 63, tid >> 6), bin = kBins - 1 - 2 * tid;
-    if (at < need && need <= at + high) chosen[0] = bin, chosen[1] = need - at;
-    else if (at + high < need && need <= at + high + low) chosen[0] = bin - 1, chosen[1] = need - at - high;
+    if (at < need && need <= at + high) chosen[0] = bin, chosen[1] = need - at, chosen[2] = high;
+    else if (at + high < need && need <= at + high + low) chosen[0] = bin - 1, chosen[1] = need - at - high, chosen[2] = low;
 }
 
 // ---- one workgroup per sequence, K words of 64 tokens a wave ---------------------------------------
 template <int K>
 __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs p)
 {
-    __shared__ int hist[3][kBins], room[3][kWaves], count[4][kWaves], chosen[3][2], movers_lds[K * kThreads / 2];
+    __shared__ int hist[3][kBins], room[3][kWaves], count[4][kWaves], chosen[3][3], movers_lds[K * kThreads / 2];
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = min(max(p.len[b], 0), p.max_len), keep = min(max(p.budget[b], 0), n);
     const int limit = p.keep_from ? p.keep_from[b] : 0;
@@ -126,7 +133,10 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs 
         prefix |= (uint32_t)chosen[pass][0] << kShift[pass];
         known |= (uint32_t)kMask[pass] << kShift[pass];
         need = chosen[pass][1];
+        if (need == chosen[pass][2]) break;  // all of the bin: no matter what their other bits are
     }
+#pragma unroll
+    for (int j = 0; j < K; ++j) key[j] &= known;
     int equal = 0;
 #pragma unroll
     for (int j = 0; j < K; ++j) equal += __popcll(__builtin_amdgcn_ballot_w64(contested[j] && key[j] == prefix));
@@ -203,7 +213,7 @@ static __device__ __forceinline__ Segment segment_of(const EvictArgs &p, int b, 
 template <int STEP>
 __global__ __launch_bounds__(kThreads) void evict_step_kernel(const EvictArgs p)
 {
-    __shared__ int hist[2][kBins], room[3][kWaves], count[2][kWaves], chosen[2], total[2];
+    __shared__ int hist[2][kBins], room[3][kWaves], count[2][kWaves], chosen[3], total[2];
     const int b = blockIdx.x / p.segments, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // (len_out may be len: step 3 writes it, and takes what step 0 read)
     int32_t *state = p.state + (int64_t)b * 8;  // len; bits chosen by step 1, 2; of how many of those that have them the last one is kept
@@ -333,19 +343,11 @@ __global__ __launch_bounds__(kThreads) void evict_step_kernel(const EvictArgs p)
             __syncthreads();
             if (wave == 0) {  // (64 segments at a time)
                 int equal = 0, holes = 0, movers = 0;  // before them
-                auto sum = [&](int x) {                // of the lanes up to this one
-#pragma unroll
-                    for (int o = 1; o < 64; o *= 2) {
-                        const int y = __shfl_up(x, o, 64);
-                        if (lane >= o) x += y;
-                    }
-                    return x;
-                };
                 for (int g0 = 0; g0 < s.segs; g0 += 64) {
-                    const int g = g0 + lane, eq = g < s.segs ? hist[0][g] : 0, eq_to = equal + sum(eq);
+                    const int g = g0 + lane, eq = g < s.segs ? hist[0][g] : 0, eq_to = equal + sum_to_me(eq);
                     const int kept = g < s.segs ? hist[1][g] + min(eq, max(0, need - (eq_to - eq))) : 0;
                     const int hole = g < s.low ? min(kEvictSegment, s.keep - g * kEvictSegment) - kept : 0, mover = g < s.low ? 0 : kept;
-                    const int hole_to = holes + sum(hole), mover_to = movers + sum(mover);
+                    const int hole_to = holes + sum_to_me(hole), mover_to = movers + sum_to_me(mover);
                     if (g == s.mine) total[0] = eq_to - eq, total[1] = g < s.low ? hole_to - hole : mover_to - mover;
                     equal = __shfl(eq_to, 63, 64), holes = __shfl(hole_to, 63, 64), movers = __shfl(mover_to, 63, 64);
                 }
