@@ -93,15 +93,14 @@ __global__ __launch_bounds__(kThreads) void evict_select_kernel(const EvictArgs 
     uint32_t key[K];
     uint64_t first[K];
     int n_first = 0;
-    if (keep < n && keep > 0) {
 #pragma unroll
-        for (int j = 0; j < K; ++j) {
-            const int i = i0 + 64 * j;
-            const int64_t at = token_at(p, b, min(i, n - 1));
-            key[j] = order_bits(p.rank[at]);
-            first[j] = __builtin_amdgcn_ballot_w64(i < n && p.keep_from && p.stamp[at] >= limit);
-            n_first += __popcll(first[j]);
-        }
+    for (int j = 0; j < K; ++j) {  // (what lies behind the last token is read, before the length is known, and not used)
+        const int i = i0 + 64 * j;
+        const int64_t at = token_at(p, b, max(min(i, p.max_len - 1), 0));
+        key[j] = order_bits(p.rank[at]);
+        const int32_t stamp = p.keep_from ? p.stamp[at] : 0;
+        first[j] = __builtin_amdgcn_ballot_w64(i < n && p.keep_from && stamp >= limit);
+        n_first += __popcll(first[j]);
     }
     for (int i = tid; i < 3 * kBins; i += kThreads) hist[0][i] = 0;
     if (lane == 0) count[0][wave] = n_first;
