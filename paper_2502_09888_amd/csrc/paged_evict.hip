@@ -9,8 +9,8 @@
 // tokens that the cut lies in (those with a stamp that counts, or the others); of the tokens that equal it the first are kept.
 // Up to 16384 tokens a sequence: one workgroup each, whose threads keep their keys.  Longer ones: a workgroup per 4096 tokens, in four
 // launches (a pass each needs the histograms of all; one workgroup for 98765 tokens took 380 us).  Then the move, 16 bytes a
-// thread, bound by memory.  98765 tokens of 8 heads of 128 cut to 50000: 44 us for all five launches, of which the move 25; 64 sequences of up
-// to 4096 cut to 2048: 31 to 34 us, the selection 12 of them, bound by the barriers of its three passes.
+// thread, bound by memory.  98765 tokens of 8 heads of 128 cut to 50000: 43 us for all five launches, of which the move 25; 64 sequences of up
+// to 4096 cut to 2048: 28 us, the selection 9 of them, bound by its trips to memory and the barriers of its passes.
 #include "paged.h"
 
 #include <algorithm>
