@@ -408,7 +408,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
+    // (with this wave's reads of a stage done: behind the barrier others copy into it)
     auto meet = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -463,10 +465,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         for (int j = again ? 0 : n_clean; j < n_blocks; ++j) {
             lds_u8 *cur = stage(j & 3);
             landed(min(2, n_blocks - 1 - j));
-            if (j >= n_clean) {
-                odd |= clear_odd<kShare>(cur + kValues + wave * kShare, lane);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            }
+            if (j >= n_clean) odd |= clear_odd<kShare>(cur + kValues + wave * kShare, lane);
             meet();
             if (j + 3 < n_blocks) issue(j + 3, stage((j + 3) & 3));
             const int k0 = k_lo + j * 32;

@@ -114,7 +114,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_mass_bf16_kernel(c
         for (int i = 0; i < 16; ++i) sum[kb][i] = 0.f;
 
     auto stage = [&](int i, lds_u8 *cur, lds_u8 *other) __attribute__((always_inline)) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // this stage's copies have landed, and this wave's reads of the stage before, which is filled again behind the barrier, are done
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         float2 now[2] = {next[0], next[1]};

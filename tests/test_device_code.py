@@ -58,6 +58,20 @@ def test_bias_attention_waits_for_its_lds_reads_before_a_ring_stage_is_filled_ag
     assert seen > 0
 
 
+def test_paged_rings_wait_for_their_lds_reads_before_a_stage_is_filled_again(kernels):
+    # Behind a barrier the stage that was read before it is filled again: right before it, on the way that leads to it whichever wait for
+    # copies was taken, a wave waits for its own reads, wherever the compiler puts the products that use them.
+    seen = {}
+    for name, code in kernels.items():
+        kind = re.search(r"attn_paged_tile_kernelILi\d+ELi\dELb[01]E|paged_mass_bf16_kernelILi\d+E", name)
+        for i, ins in enumerate(code if kind else ()):
+            if ins == "s_barrier":
+                seen[kind.group(0)] = seen.get(kind.group(0), 0) + 1
+                before = next(x for x in reversed(code[:i]) if x.startswith(("s_waitcnt", "s_cbranch", "s_branch", "s_barrier", "ds_", "global_load_lds")))
+                assert re.match(r"s_waitcnt .*lgkmcnt\(0\)", before), (name, i, before)
+    assert len(seen) == 8 and min(seen.values()) >= 2
+
+
 def test_inline_assembly_of_several_instructions_keeps_its_inputs():
     # an output that an earlier instruction writes may share its register with an input that a later one reads, where the compiler knows
     # both to have one value, unless it is marked as an early clobber
