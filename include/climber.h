@@ -247,6 +247,8 @@ int climber_attn_sumi_bias(const climber_config *cfg, const float *tau_layer,
  *               the same tokens must not overlap, and no two sequences of a call may list the same page then.
  *   stamp       dev int32 [n_pages][page_size] or NULL: a number of the caller's per token (its time, its
  *               position), stored by climber_attn_history_paged and kept with its token by climber_paged_evict.
+ *   d_head, elem_bytes  host: elements of a head's key or value in the pages, and bytes of one.  A call whose cfg has others is refused
+ *               (CLIMBER_ERR_SHAPE): it would read and write beyond the pool.  0: not stated, and not checked.
  * page_size: a power of two, 16 .. 4096.  n_kv_heads divides cfg->n_heads: query head h reads cache head
  * h / (n_heads / n_kv_heads).  CLIMBER_BF16: d_head 64 or 128; CLIMBER_F32: d_head <= 128, a multiple of 4.
  * A page may be listed by several sequences (a shared prefix) as long as no call writes into it: an append
@@ -268,6 +270,7 @@ typedef struct climber_paged_kv {
     int32_t *stamp;
     const int32_t *page_table, *len;
     int32_t n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len;
+    int32_t d_head, elem_bytes;
 } climber_paged_kv;
 
 /* Bytes of scratch that any call on this cache needs for up to m_total rows, at most m_max per sequence (0, 0: eviction only).

@@ -56,7 +56,7 @@ class BgfWeights(C.Structure):
 class PagedKV(C.Structure):
     """Mirror of ``climber_paged_kv`` (device pointers).  Build with ``paged_kv(...)``."""
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "mass", "stamp", "page_table", "len")] + \
-               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "n_seqs", "table_ld", "max_len")]
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "n_seqs", "table_ld", "max_len", "d_head", "elem_bytes")]
     _device = None  # the CUDA device of its tensors, if it was made from tensors
 
 
@@ -417,7 +417,7 @@ def paged_kv(k, v, page_table, len, max_len: int, mass=None, stamp=None) -> Page
     for t in (k, v, page_table, len, mass, stamp):
         if t is not None and not t.is_contiguous():
             raise ValueError("a paged cache is described by contiguous tensors")
-    n_pages, n_kv_heads, page_size, _ = k.shape
+    n_pages, n_kv_heads, page_size, d_head = k.shape
     n_seqs, table_ld = page_table.shape
     if v.shape != k.shape or len.numel() != n_seqs or any(t is not None and t.numel() != n_pages * page_size for t in (mass, stamp)):
         raise ValueError("k, v, page_table, len, mass and stamp are not of one cache")
@@ -427,7 +427,8 @@ def paged_kv(k, v, page_table, len, max_len: int, mass=None, stamp=None) -> Page
         raise ValueError("k, v are bfloat16 or float32, page_table, len and stamp int32, mass float32")
     if any(t is not None and t.device != k.device for t in (v, page_table, len, mass, stamp)):
         raise ValueError("k, v, page_table, len, mass and stamp are not on one device")
-    kv = PagedKV(_ptr(k), _ptr(v), _ptr(mass), _ptr(stamp), _ptr(page_table), _ptr(len), n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len)
+    kv = PagedKV(_ptr(k), _ptr(v), _ptr(mass), _ptr(stamp), _ptr(page_table), _ptr(len), n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len,
+                 d_head, k.element_size())
     kv._keep = (k, v, mass, stamp, page_table, len)
     if k.is_cuda:
         kv._device = k.device.index

@@ -27,6 +27,7 @@ int check_sizes(const climber_config *cfg, const climber_paged_kv *kv)
         return CLIMBER_ERR_UNSUPPORTED;
     if (kv->n_pages < 1 || kv->n_seqs < 1 || kv->table_ld < 1 || kv->n_kv_heads < 1 || cfg->n_heads % kv->n_kv_heads != 0 || kv->page_size < 1)
         return CLIMBER_ERR_SHAPE;
+    if ((kv->d_head != 0 && kv->d_head != cfg->d_head) || (kv->elem_bytes != 0 && kv->elem_bytes != (int32_t)elem_of(cfg))) return CLIMBER_ERR_SHAPE;
     if (kv->page_size < 16 || kv->page_size > 4096 || (kv->page_size & (kv->page_size - 1)) != 0) return CLIMBER_ERR_ALIGN;
     if (kv->max_len < 0 || kv->max_len > (int64_t)kv->table_ld * kv->page_size) return CLIMBER_ERR_RANGE;
     // slots of a table row, rows of a launch and tokens of the pool are counted in 32 bits
