@@ -57,7 +57,7 @@ class PagedKV(C.Structure):
     """Mirror of ``climber_paged_kv`` (device pointers).  Build with ``paged_kv(...)``."""
     _fields_ = [(n, C.c_void_p) for n in ("k", "v", "mass", "stamp", "page_table", "len")] + \
                [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "n_seqs", "table_ld", "max_len", "d_head", "elem_bytes")]
-    _device = None  # the CUDA device of its tensors, if it was made from tensors
+    _device = None  # the CUDA device of its tensors (-1: they are in host memory that is not pinned), if it was made from tensors
 
 
 class _Weights(C.Structure):
@@ -432,12 +432,16 @@ def paged_kv(k, v, page_table, len, max_len: int, mass=None, stamp=None) -> Page
     kv._keep = (k, v, mass, stamp, page_table, len)
     if k.is_cuda:
         kv._device = k.device.index
+    elif not all(t is None or t.is_pinned() for t in kv._keep):
+        kv._device = -1
     return kv
 
 
 def _on_device(kv: PagedKV, stream) -> None:
     """A call without a stream goes to the current device's, a call with one to its device: that has to be the cache's."""
     at = kv._device
+    if at == -1:
+        raise ValueError("the paged cache is in host memory that no kernel can reach")
     if at is None or isinstance(stream, int):
         return
     import torch
@@ -514,5 +518,6 @@ def climber_paged_evict(cfg: Config, kv: PagedKV, rank, budget, keep_from, len_o
 
 def climber_check_paged(cfg: Config, kv: PagedKV, off, m_total: int, m_max: int, appends: bool, status, stream=None) -> None:
     """Device-side check of page numbers / lengths / offsets; ORs BAD_* bits into status (int32 tensor)."""
+    _on_device(kv, stream)
     _ok(load_library().climber_check_paged(C.byref(cfg), C.byref(kv), _ptr(off), m_total, m_max, int(appends), _ptr(status), _stream(stream)),
         "climber_check_paged")

@@ -45,3 +45,21 @@ def test_a_description_without_them_is_taken_as_it_is():
         assert SHAPE not in every_call(c, kv)
     kv.elem_bytes = 2
     assert SHAPE not in every_call(cfg(), kv) and every_call(cfg(dtype=P.F32), kv) == [SHAPE] * 4 + [0]
+
+
+def test_a_cache_in_host_memory_reaches_no_kernel(monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    pages = torch.zeros(10, 2, 16, 64, dtype=torch.bfloat16)
+    kv = P.paged_kv(pages, pages.clone(), torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), 64, mass=torch.zeros(10, 16))
+    c = cfg()
+    assert P.climber_paged_workspace_bytes(c, kv, 4, 4) > 0       # (needs no device)
+    for stream in (None, 0, 5):                                    # (no workspace, no status: nothing would be launched anyway)
+        with pytest.raises(ValueError):
+            P.climber_attn_history_paged(c, FAKE, kv, FAKE, FAKE, FAKE, FAKE, 4, 4, FAKE, FAKE, None, FAKE, None, stream)
+        with pytest.raises(ValueError):
+            P.climber_attn_sumi_paged(c, FAKE, kv, FAKE, FAKE, FAKE, FAKE, 4, 4, FAKE, FAKE, FAKE, None, stream)
+        with pytest.raises(ValueError):
+            P.climber_paged_evict(c, kv, None, FAKE, None, FAKE, None, None, stream)
+        with pytest.raises(ValueError):
+            P.climber_check_paged(c, kv, FAKE, 4, 4, True, None, stream)
