@@ -459,6 +459,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
                 step(j, S1, S0, stage(2), stage(3), stage(0));
                 ++j;
             }
+            // (now, and at the end: in the blocks to come the reference may move by more than 2^126, which makes zeros of the sums so far)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) far[qb] = !(st.l[qb] + other_half(st.l[qb]) < kFar);
         }
         // blocks that not every row sees whole
 #pragma unroll 1
@@ -496,7 +499,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
             for (int db = 0; db < D / 32; ++db)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) nothing = fmaf(st.O[qb][db][i], 0.f, nothing);
-            far[qb] = !(st.l[qb] + other_half(st.l[qb]) < kFar) || !(nothing + other_half(nothing) == 0.f);
+            far[qb] |= !(st.l[qb] + other_half(st.l[qb]) < kFar) || !(nothing + other_half(nothing) == 0.f);
             some |= far[qb];
         }
         const int wave_far = __builtin_amdgcn_ballot_w64(some) != 0;

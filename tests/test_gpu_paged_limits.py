@@ -1,0 +1,64 @@
+"""The paged history cache at its limits: full caches, logits and values at the ends of their ranges, long parts and many segments (against
+definitions in 64 bits)."""
+import math
+
+import pytest
+import torch
+
+from paged_ref import HALF_BF16, HALF_F32, Case, Device
+from test_gpu_paged import check, same_bits
+
+pytestmark = pytest.mark.gpu
+
+
+def attention(case, b, sees):
+    """Rows of sequence b over the keys that they see (bool [rows, keys]: cached ones, then the call's own): o, its bound, weights [keys] and
+    theirs, in 64 bits.  The bounds are those of Case.expect."""
+    n, t, G, d = case.cached[b], case.chunk[b], case.H // case.Hkv, case.d
+    r = slice(int(case.off[b]), int(case.off[b]) + t)
+    ks, vs = torch.cat([case.rows(case.k, b, n), case.kn[r]]).double(), torch.cat([case.rows(case.v, b, n), case.vn[r]]).double()
+    nobody = ~sees.any(0)
+    ks[nobody], vs[nobody] = 0, 0
+    c = (case.scale / case.tau.double()[case.scen[r].long(), case.beh[r].long()])[:, None]
+    o, tol = torch.zeros(t, case.H, d, dtype=torch.float64), torch.zeros(t, case.H, d, dtype=torch.float64)
+    w, wtol = torch.zeros(n + t, dtype=torch.float64), torch.zeros(n + t, dtype=torch.float64)
+    bf16 = HALF_BF16 if case.dtype == "bf16" else 0
+    for h in range(case.H):
+        q, k, v = case.q[r, h].double(), ks[:, h // G], vs[:, h // G]
+        p = torch.softmax(torch.where(sees, (q @ k.t()) * c, -math.inf), dim=1)
+        worst = torch.where(sees, (q.abs() @ k.abs().t()) * c, 0.0).amax(1, keepdim=True)
+        rel = 2 * (d + 4) * HALF_F32 * worst + (n + t + 12) * HALF_F32
+        a = p @ v.abs()
+        o[:, h] = p @ v
+        tol[:, h] = a * (rel + bf16) * 1.01
+        tol[:, h] += (o[:, h].abs() + tol[:, h]) * (bf16 or HALF_F32)
+        w += p.sum(0)
+        wtol += t * 2.0 ** -126 + (p * (rel + (t * G + 40) * HALF_F32)).sum(0) * 1.01
+    return o, tol, w, wtol
+
+
+def visible(case, b, most=None):
+    """Keys that the rows of sequence b see: the cached ones and their own, or up to their own, no more than `most`."""
+    n, t = case.cached[b], case.chunk[b]
+    key, row = torch.arange(n + t), torch.arange(t)[:, None]
+    new = key - n == row if case.sumi else key - n <= row if case.causal else key - n < t
+    return ((key < n) | new) & (key < (n + t if most is None else most))
+
+
+def near(got, o, tol):
+    off = (got - o).abs() - tol
+    assert torch.isfinite(got).all() and off.max() <= 0, f"max over the bound {off.max():.3e}, error {(got - o).abs().max():.3e}"
+
+
+@pytest.mark.parametrize("late", [1.0, 40.0], ids=["even", "late"])
+@pytest.mark.parametrize("cached,rows,d", [(8500, 1, 64), (8500, 1, 128), (4300, 33, 64), (4300, 130, 64), (4300, 33, 128)])
+def test_long_sequences_in_one_part(cached, rows, d, late):
+    # So many sequences and heads that keys are not shared out, and one of the sequences long: its page numbers are fetched 64 at a
+    # time, the third time too.  `late`: the last keys' weights exceed the first ones' by more than 2^100, so that tiles run twice.
+    n_seqs = 64 if rows == 1 else 33
+    case = Case([cached] + [b % 5 for b in range(1, n_seqs)], [rows] * n_seqs, H=8, Hkv=8, d=d, seed=74)
+    slot = torch.arange(cached - 100, cached)
+    case.k[case.table[0].long()[slot // 16], :, slot % 16] *= late
+    dev = Device(case, mass=True)
+    dev.attend()
+    check(case, dev)
