@@ -257,7 +257,8 @@ int climber_attn_sumi_bias(const climber_config *cfg, const float *tau_layer,
  * Contents of slots from len[b] on are never used: they may hold anything, NaN included.
  * Lengths, offsets and page numbers are device memory and cannot be checked on the host: lengths are clamped to
  * max_len, offsets to m_total, page numbers that are read to the pool, and a token whose page number lies outside the
- * pool is not stored.  climber_check_paged reports such values.
+ * pool is not stored.  Nor are new tokens from slot max_len on: no row sees them, theirs attend to what the cache then holds, and cached tokens
+ * stay.  climber_check_paged reports such values.
  * Values are added up before they are divided by the sum of their weights: |v| times the tokens that a row sees has to stay below
  * 2^119, or outputs may be infinite.
  * A workspace belongs to one call at a time: two calls, or two captured graphs, that may run at once need one each.

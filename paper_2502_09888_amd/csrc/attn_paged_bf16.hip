@@ -331,7 +331,9 @@ static __device__ __forceinline__ void store_new(const PagedArgs &p, const Paged
     constexpr int C = D / 8;
     const int t0 = (r0 + p.G - 1) / p.G, t1 = (r1 + p.G - 1) / p.G;
     for (int i = threadIdx.x; i < (t1 - t0) * C; i += 256) {
-        const int t = t0 + i / C, c = (i % C) * 16, slot = s.n + t, page = p.table[(int64_t)b * p.table_ld + (slot >> p.page_shift)];
+        const int t = t0 + i / C, c = (i % C) * 16, slot = s.n + t;
+        if (slot >= p.max_len) break;
+        const int page = p.table[(int64_t)b * p.table_ld + (slot >> p.page_shift)];
         if (page < 0 || page >= p.n_pages) continue;
         const int64_t to = paged_row(p, page, hk, slot) + c, from = (s.row0 + t) * p.ld_kv + (int64_t)hk * (2 * D) + c;
         *(uint4 *)(p.k_pages + to) = *(const uint4 *)(p.k + from);
@@ -362,8 +364,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
     if (r_tile >= rows) return;
     const int r_wave = r_tile + wave * 32 * QB;
     const bool causal = !SUMI && p.causal;
-    const int k_all = SUMI ? s.n : s.n + s.T;
-    auto sees = [&](int r) { return causal ? s.n + min(r, rows - 1) / p.G + 1 : k_all; };  // packed row r sees keys below it
+    const int k_all = SUMI ? s.n : paged_keys(p, s);
+    auto sees = [&](int r) { return causal ? min(s.n + min(r, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row r sees keys below it
     int k_lo, k_hi;
     paged_part(p, w.split, sees(r_tile + kRows - 1), 32, k_lo, k_hi);
     k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
@@ -552,8 +554,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
 }
 
 // ---- few rows ------------------------------------------------------------------------------------
+// (workgroups of a CU: as many as there is LDS for)
 template <int D, bool SUMI>
-__global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_paged_few_kernel(const PagedArgs p)
 {
     using R = Rows<D>;
     constexpr int kStage = 2 * 32 * R::kPitch, kLoads = 4 * R::kLoads;  // a wave's
@@ -569,8 +572,8 @@ __global__ __launch_bounds__(256) void attn_paged_few_kernel(const PagedArgs p)
     const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
     const int64_t row = s.row0 + t;
     const bool causal = !SUMI && p.causal;
-    const int k_all = SUMI ? s.n : s.n + s.T;
-    auto sees = [&](int i) { return causal ? s.n + min(i, rows - 1) / p.G + 1 : k_all; };  // packed row i sees keys below it
+    const int k_all = SUMI ? s.n : paged_keys(p, s);
+    auto sees = [&](int i) { return causal ? min(s.n + min(i, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row i sees keys below it
     const int lim = sees(r), lim_lo = sees(r_tile);
     int k_lo, k_hi;
     paged_part(p, w.split, sees(r_tile + 31), 128, k_lo, k_hi);

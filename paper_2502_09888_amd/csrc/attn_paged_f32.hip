@@ -44,7 +44,9 @@ static __device__ __forceinline__ void store_new(const PagedArgs &p, const Paged
 {
     const int t0 = (r0 + p.G - 1) / p.G, t1 = (r1 + p.G - 1) / p.G, C = p.row_bytes / 16;
     for (int i = threadIdx.x; i < (t1 - t0) * C; i += NT) {
-        const int t = t0 + i / C, c = (i % C) * 16, slot = s.n + t, page = p.table[(int64_t)b * p.table_ld + (slot >> p.page_shift)];
+        const int t = t0 + i / C, c = (i % C) * 16, slot = s.n + t;
+        if (slot >= p.max_len) break;
+        const int page = p.table[(int64_t)b * p.table_ld + (slot >> p.page_shift)];
         if (page < 0 || page >= p.n_pages) continue;
         const int64_t to = paged_row(p, page, hk, slot) + c, from = (s.row0 + t) * p.ld_kv + (int64_t)hk * p.row_bytes + c;
         *(uint4 *)(p.k_pages + to) = *(const uint4 *)(p.k + from);
@@ -167,11 +169,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_f32_kernel(const PagedArgs 
     const int r_wave = r_tile + wave * 32, r = min(r_wave + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
     const int64_t row = s.row0 + t;
     const bool causal = !SUMI && p.causal;
-    const int k_all = SUMI ? s.n : s.n + s.T;
-    // this lane's row sees keys below lim; the tile's and the wave's bounds
-    const int lim = causal ? s.n + t + 1 : k_all;
-    const int t_tile = min(r_tile + NW * 32 - 1, rows - 1) / p.G, k_end = causal ? s.n + t_tile + 1 : k_all;
-    const int lim_lo = causal ? s.n + min(r_wave, rows - 1) / p.G + 1 : k_all, lim_hi = causal ? s.n + min(r_wave + 31, rows - 1) / p.G + 1 : k_all;
+    const int k_all = SUMI ? s.n : paged_keys(p, s);
+    auto sees = [&](int i) { return causal ? min(s.n + min(i, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row i sees keys below it
+    // this lane's row's, the tile's and the wave's bounds
+    const int lim = sees(r), k_end = sees(r_tile + NW * 32 - 1), lim_lo = sees(r_wave), lim_hi = sees(r_wave + 31);
     int k_lo, k_hi;
     paged_part(p, w.split, k_end, kKeys, k_lo, k_hi);
 
@@ -275,7 +276,8 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_paged_few_f32_kern
     const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
     const int64_t row = s.row0 + t;
     const bool causal = !SUMI && p.causal;
-    auto sees = [&](int i) { return SUMI ? s.n : s.n + (causal ? min(i, rows - 1) / p.G + 1 : s.T); };  // packed row i sees keys below it
+    const int k_all = SUMI ? s.n : paged_keys(p, s);
+    auto sees = [&](int i) { return causal ? min(s.n + min(i, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row i sees keys below it
     const int lim = sees(r), lim_lo = sees(r_tile);
     int k_lo, k_hi;
     paged_part(p, w.split, sees(r_tile + 31), kKeys, k_lo, k_hi);
@@ -464,7 +466,7 @@ __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, floa
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = threadIdx.x >> 6;
     const int tiles = (p.max_len + kKeys - 1) / kKeys, tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / p.Hkv, hk = bh % p.Hkv;
     const PagedSeq s = paged_seq(p, b);
-    const int keys = p.sumi ? s.n : s.n + s.T, k0 = tile * kKeys, rows = s.T * p.G;
+    const int keys = paged_keys(p, s), k0 = tile * kKeys, rows = s.T * p.G;
     if (k0 >= keys || rows == 0) return;
     load_tile<DP, 256>(tk, p.d, [&](int i) {
         const int j = min(k0 + i, keys - 1);
@@ -520,7 +522,7 @@ __global__ __launch_bounds__(256) void paged_mass_add_kernel(const PagedArgs p, 
 #pragma unroll 8
     for (int i = 0; i < n_parts; ++i) x += part[((int64_t)b * n_parts + i) * p.max_len + j];
     const PagedSeq s = paged_seq(p, b);
-    if (s.T == 0 || j >= (p.sumi ? s.n : s.n + s.T) || j != (int)(blockIdx.x % per) * 256 + (int)threadIdx.x) return;
+    if (s.T == 0 || j >= paged_keys(p, s) || j != (int)(blockIdx.x % per) * 256 + (int)threadIdx.x) return;
     if (raw < 0 || raw >= p.n_pages) return;
     float *to = p.mass + ((int64_t)raw << p.page_shift) + (j & ((1 << p.page_shift) - 1));
     *to = j < s.n ? *to + x : x;  // a new token has none yet, whatever its slot holds
@@ -531,7 +533,7 @@ __global__ __launch_bounds__(256) void paged_mass_few_kernel(const PagedArgs p)
 {
     const int per = (p.max_len + 255) / 256, b = blockIdx.x / per, j = (blockIdx.x % per) * 256 + threadIdx.x;
     const PagedSeq s = paged_seq(p, b);
-    if (s.T == 0 || j >= (p.sumi ? s.n : s.n + s.T)) return;
+    if (s.T == 0 || j >= paged_keys(p, s)) return;
     const int raw = p.table[(int64_t)b * p.table_ld + (j >> p.page_shift)];
     if (raw < 0 || raw >= p.n_pages) return;
     float x = 0.f;

@@ -38,17 +38,19 @@ struct PagedSeq {
     int64_t row0;  // first row
 };
 
-// Lengths and offsets live in device memory: whatever they hold, nothing is read or written outside the arrays.
+// Lengths and offsets live in device memory: whatever they hold, nothing is read or written outside the arrays.  New tokens that a sequence of
+// max_len tokens has no room for are not stored, and no row sees them.
 static __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs &p, int b)
 {
     PagedSeq s;
     const int r0 = min(max(p.off[b], 0), p.m_total);
     s.T = min(min(max(p.off[b + 1] - r0, 0), p.m_total - r0), p.m_max);
-    if (!p.sumi) s.T = min(s.T, p.max_len);
-    s.n = min(max(p.len[b], 0), p.sumi ? p.max_len : p.max_len - s.T);
+    s.n = min(max(p.len[b], 0), p.max_len);
     s.row0 = r0;
     return s;
 }
+// keys of a sequence: the cached tokens, then the new ones that have a slot
+static __device__ __forceinline__ int paged_keys(const PagedArgs &p, const PagedSeq &s) { return p.sumi ? s.n : min(s.n + s.T, p.max_len); }
 
 static __device__ __forceinline__ int paged_page(const PagedArgs &p, int b, int slot)
 {

@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_mass_bf16_kernel(c
     PagedWork w;
     PagedSeq s;
     if (!paged_work(p, w, s)) return;
-    const int keys = p.sumi ? s.n : s.n + s.T, k_tile = w.tile * kMassKeys, k0 = k_tile + wave * 64, rows = s.T * p.G;
+    const int keys = paged_keys(p, s), k_tile = w.tile * kMassKeys, k0 = k_tile + wave * 64, rows = s.T * p.G;
     if (k_tile >= keys || rows == 0) return;
     const bool causal = !p.sumi && p.causal;
     // this part's rows, from the first one that sees a key of the tile

@@ -50,6 +50,47 @@ def near(got, o, tol):
     assert torch.isfinite(got).all() and off.max() <= 0, f"max over the bound {off.max():.3e}, error {(got - o).abs().max():.3e}"
 
 
+FULL = {
+    # (cached, chunk, capacity, query heads, cache heads)
+    "decode": ([64, 63, 20], [1, 3, 2], 64, 4, 2),
+    "few rows": ([60, 20, 64, 0], [6, 5, 3, 2], 64, 4, 2),
+    "chunks": ([40, 20, 64, 0], [70, 5, 33, 80], 64, 4, 2),
+    "many": ([40, 64, 5] * 4, [41, 40, 33] * 4, 64, 8, 8),
+    "parts": ([1000], [40], 1010, 2, 1),
+}
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "whole"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 32), ("f32", 128)])
+@pytest.mark.parametrize("name", FULL)
+def test_tokens_that_a_full_cache_has_no_room_for(name, dtype, d, causal):
+    # They are not stored and nobody sees them; what the cache holds already stays, and their rows attend to what it holds then.
+    cached, chunk, most, H, Hkv = FULL[name]
+    case = Case(cached, chunk, H=H, Hkv=Hkv, d=d, dtype=dtype, causal=causal, seed=70, tail=2)
+    dev = Device(case, mass=True, stamp=True, max_len=most)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    dev.P.climber_check_paged(dev.cfg, dev.kv, dev.off, case.m, dev.m_max, True, status)
+    assert status.item() == dev.P.BAD_LEN
+    dev.attend()
+    got = dev.out()
+    assert (got[sum(chunk):] == 77.0).all()
+    k, v, mass, stamp = case.k.clone(), case.v.clone(), case.mass.double().clone(), case.stamp.clone()
+    bound = torch.zeros_like(mass)
+    for b, (n, t) in enumerate(zip(cached, chunk)):
+        r0 = int(case.off[b])
+        o, tol, w, wtol = attention(case, b, visible(case, b, most))
+        near(got[r0:r0 + t], o, tol)
+        for j in range(min(n + t, most)):
+            pg, s = case.at(b, j)
+            if j >= n:
+                k[pg, :, s], v[pg, :, s], stamp[pg, s] = case.kn[r0 + j - n], case.vn[r0 + j - n], case.stamp_new[r0 + j - n]
+            mass[pg, s] = (mass[pg, s] if j < n else 0.0) + w[j]
+            bound[pg, s] = wtol[j] + mass[pg, s] * 2.0 ** -23
+    assert same_bits(dev.k, k) and same_bits(dev.v, v) and torch.equal(dev.stamp.cpu(), stamp)
+    got = dev.mass.double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(mass)) and ((got - mass).abs().nan_to_num() <= bound).all()
+
+
 @pytest.mark.parametrize("late", [1.0, 40.0], ids=["even", "late"])
 @pytest.mark.parametrize("cached,rows,d", [(8500, 1, 64), (8500, 1, 128), (4300, 33, 64), (4300, 130, 64), (4300, 33, 128)])
 def test_long_sequences_in_one_part(cached, rows, d, late):
