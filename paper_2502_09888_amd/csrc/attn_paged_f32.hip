@@ -423,13 +423,16 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedArgs p)
         }
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) L += __shfl_xor(L, o, 64);
+        // A part's mean, no larger than its values, by its share of all weights: the parts' sums may pass the largest number together.
+        const float inv = 1.f / L;
         auto add = [&](float2 y, f32x4 o) {
-            const float w = __builtin_amdgcn_exp2f(y.x - M);
             if (y.y != 0.f) {
+                const float share = y.y * __builtin_amdgcn_exp2f(y.x - M) * inv, mean = 1.f / y.y;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += w * o[e];
+                for (int e = 0; e < 4; ++e) acc[e] += share * (o[e] * mean);
             }
         };
+        if (L == 0.f) acc[0] = acc[1] = acc[2] = acc[3] = NAN;  // (all logits -inf)
 #pragma unroll
         for (int k = 0; k < kFirst; ++k)
             if (g + k * GROUPS < p.n_split) add(ml[k], x[k]);
@@ -445,12 +448,7 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedArgs p)
         for (int i = 1; i < GROUPS; ++i) acc += sums[group + i][lane];
     }
     if (!mine) return;
-    const float inv = 1.f / L;
-    if (c < p.d) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] *= inv;
-        store4((E *)(p.o + row * p.ld_o) + (int64_t)h * p.d + c, acc);
-    }
+    if (c < p.d) store4((E *)(p.o + row * p.ld_o) + (int64_t)h * p.d + c, acc);
     if (lane == 0 && p.lse) p.lse[rh] = float2{paged_row_scale(p, row), M + __builtin_amdgcn_logf(L)};
 }
 

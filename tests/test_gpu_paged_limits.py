@@ -91,6 +91,32 @@ def test_tokens_that_a_full_cache_has_no_room_for(name, dtype, d, causal):
     assert torch.equal(torch.isnan(got), torch.isnan(mass)) and ((got - mass).abs().nan_to_num() <= bound).all()
 
 
+@pytest.mark.parametrize("d,rows", [(64, 100), (64, 200), (128, 100)])
+def test_parts_whose_sums_pass_the_largest_number_together(d, rows):
+    # One user's chunk on 4096 tokens: parts of the keys.  All values are 2^99 (times the tokens 2^111), the weights of most keys 2^19 times those of the
+    # first 32 of a part, which are its reference: its sums are near 2^126, finite, and those of all parts are not.  Where parts begin is not
+    # known here: every distance is tried.
+    case = Case([4096], [rows], H=1, Hkv=1, d=d, page=64, causal=False, scale=1.0, seed=71)
+    case.tau.fill_(1.0)
+    for x in (case.q, case.k, case.kn):
+        x[torch.isfinite(x)] = 0
+    case.q[..., 0] = 1
+    case.v[torch.isfinite(case.v)] = 2.0 ** 99
+    case.vn.fill_(2.0 ** 99)
+    dev = Device(case)
+    slot = torch.arange(4096)
+    page = case.table[0].long()[slot // 64]
+    for distance in range(2, 40):
+        low = slot // 32 % distance == 0
+        case.k[page, 0, slot % 64, 0] = torch.where(low, 0.0, 13.1875).to(case.dt)
+        dev.k.copy_(case.k)
+        dev.o.fill_(0)
+        dev.attend()
+        got = dev.out()
+        # equal values: their mean, but for the rounding of each weight and of the output
+        assert ((got / 2.0 ** 99 - 1).abs() <= 2 * HALF_BF16 * 1.01).all(), (distance, got.min(), got.max())
+
+
 @pytest.mark.parametrize("late", [1.0, 40.0], ids=["even", "late"])
 @pytest.mark.parametrize("cached,rows,d", [(8500, 1, 64), (8500, 1, 128), (4300, 33, 64), (4300, 130, 64), (4300, 33, 128)])
 def test_long_sequences_in_one_part(cached, rows, d, late):
