@@ -171,10 +171,12 @@ struct State {
         dot += other_half(dot);
         l[qb] = hf == 0 ? 1.f : 0.f;
         m[qb] = dot;
+        const bool none = dot == -INFINITY;           // (has no part in it)
+        if (none) l[qb] = 0.f, m[qb] = kNoRef;
         if (dot != dot) l[qb] = dot, m[qb] = kNoRef;  // (a logit that is no number makes the row none)
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            u32x4 v = in.v[s];
+            u32x4 v = none ? u32x4{0, 0, 0, 0} : in.v[s];
             swap_pieces(v);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {

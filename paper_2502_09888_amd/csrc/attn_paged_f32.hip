@@ -71,6 +71,10 @@ static __device__ __forceinline__ void own_first(const PagedArgs &p, int64_t row
     m = dot + __shfl_xor(dot, 32, 64);
     l = hf == 0 ? 1.f : 0.f;
     if (m != m) l = m, m = kNoRef;  // (a logit that is no number makes the row none)
+    if (m == -INFINITY) {           // (one of -inf has no part in it)
+        l = 0.f, m = kNoRef;
+        return;
+    }
 #pragma unroll
     for (int db = 0; db < DP / 32; ++db)
 #pragma unroll

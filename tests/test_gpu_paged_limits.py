@@ -117,6 +117,30 @@ def test_parts_whose_sums_pass_the_largest_number_together(d, rows):
         assert ((got / 2.0 ** 99 - 1).abs() <= 2 * HALF_BF16 * 1.01).all(), (distance, got.min(), got.max())
 
 
+@pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("cached,chunk", [([200], [3]), ([200], [100]), ([200, 40] * 6, [70, 7] * 6), ([3000], [50])],
+                         ids=["few rows", "chunks", "many", "parts"])
+def test_logits_of_minus_infinity_take_no_part(cached, chunk, dtype, d, sumi):
+    # the first 40 cached tokens' and every third new token's
+    H = 8 if len(cached) == 12 else 4
+    case = Case(cached, chunk, H=H, Hkv=H if H == 8 else 2, d=d, dtype=dtype, sumi=sumi, seed=73)
+    case.q[..., 0] = case.q[..., 0].abs() + 0.5
+    case.kn[::3, :, 0] = -math.inf
+    for b, n in enumerate(cached):
+        for j in range(min(n, 40) if n > 40 else 5):
+            pg, s = case.at(b, j)
+            case.k[pg, :, s, 0] = -math.inf
+    dev = Device(case)
+    dev.attend()
+    got = dev.out()
+    for b in range(len(cached)):
+        r = slice(int(case.off[b]), int(case.off[b + 1]))
+        alive = torch.cat([case.rows(case.k, b, cached[b]), case.kn[r]])[:, 0, 0] > -math.inf
+        o, tol, _, _ = attention(case, b, visible(case, b) & alive)
+        near(got[r], o, tol)
+
+
 @pytest.mark.parametrize("late", [1.0, 40.0], ids=["even", "late"])
 @pytest.mark.parametrize("cached,rows,d", [(8500, 1, 64), (8500, 1, 128), (4300, 33, 64), (4300, 130, 64), (4300, 33, 128)])
 def test_long_sequences_in_one_part(cached, rows, d, late):
