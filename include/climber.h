@@ -260,7 +260,8 @@ int climber_attn_sumi_bias(const climber_config *cfg, const float *tau_layer,
  * pool is not stored.  Nor are new tokens from slot max_len on: no row sees them, theirs attend to what the cache then holds, and cached tokens
  * stay.  climber_check_paged reports such values.
  * Values are added up before they are divided by the sum of their weights: |v| times the tokens that a row sees has to stay below
- * 2^119, or outputs may be infinite.
+ * 2^119, or outputs may be infinite.  Logits (qk_scale <q, k> / tau) have to stay below 10^7 in magnitude, where a step of fp32 is 1, or
+ * rows may be no numbers; <q, k> itself may be any finite fp32 number.
  * A workspace belongs to one call at a time: two calls, or two captured graphs, that may run at once need one each.
  * Rows (q, k, v, o): row r starts r * ld elements behind the pointer and holds its heads one after the other;
  * pointers and row pitches are multiples of 16 bytes; o must not share an element with q, k or v.  Rows of no

@@ -28,7 +28,9 @@ namespace {
 
 using namespace paged;
 
-constexpr float kNoRef = -1.0e30f;  // "no reference yet", below any finite logit
+// "no reference yet", as a raw logit: no finite one is below it once scaled by c, and c times it is finite (a hidden key's weight is
+// exp2(-inf - c m))
+static __device__ __forceinline__ float no_ref(float c) { return -3.4028e38f * __builtin_amdgcn_rcpf(fmaxf(c, 1.f)); }
 constexpr float kSlack = 8.0f;      // log2 units that a logit may exceed the reference by
 constexpr float kFar = 0x1p100f;    // a denominator over it: the reference was too low, see attn_paged_tile_kernel
 
@@ -154,7 +156,8 @@ struct State {
     __device__ __forceinline__ void start(const PagedArgs &p, int qb, int hf, const Row &in, bool own)
     {
         c[qb] = p.scale_log2e / p.tau[in.at];
-        m[qb] = kNoRef;
+        const float none_yet = no_ref(c[qb]);
+        m[qb] = none_yet;
         l[qb] = 0.f;
 #pragma unroll
         for (int db = 0; db < D / 32; ++db)
@@ -172,8 +175,8 @@ struct State {
         l[qb] = hf == 0 ? 1.f : 0.f;
         m[qb] = dot;
         const bool none = dot == -INFINITY;           // (has no part in it)
-        if (none) l[qb] = 0.f, m[qb] = kNoRef;
-        if (dot != dot) l[qb] = dot, m[qb] = kNoRef;  // (a logit that is no number makes the row none)
+        if (none) l[qb] = 0.f, m[qb] = none_yet;
+        if (dot != dot) l[qb] = dot, m[qb] = none_yet;  // (a logit that is no number makes the row none)
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
             u32x4 v = none ? u32x4{0, 0, 0, 0} : in.v[s];

@@ -13,7 +13,7 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
 
 constexpr int kKeys = 32;              // keys of a tile
-constexpr float kNoRef = -1.0e30f;     // "no reference yet", below any finite logit
+constexpr float kNoRef = -3.40282347e38f;  // "no reference yet": no finite logit is below it
 
 static __device__ __forceinline__ f32x4 load4(const float *p) { return *(const f32x4 *)p; }
 static __device__ __forceinline__ void store4(float *p, f32x4 x) { *(f32x4 *)p = x; }

@@ -118,6 +118,20 @@ def test_parts_whose_sums_pass_the_largest_number_together(d, rows):
 
 
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("cached,chunk", [([0, 5, 150], [1, 2, 3]), ([150, 40, 1], [90, 140, 1]), ([40] * 12, [70] * 12), ([3000], [1]), ([3000], [50])],
+                         ids=["few rows", "chunks", "many", "parts of few", "parts"])
+def test_products_far_below_zero_with_ordinary_logits(cached, chunk, dtype, d, sumi):
+    # <q, k> of -1e34 to -1e35, with a scale that makes logits of some hundreds of it
+    H = 8 if len(cached) == 12 else 4
+    case = Case(cached, chunk, H=H, Hkv=H if H == 8 else 2, d=d, dtype=dtype, sumi=sumi, std=2.0 ** 55, scale=d ** -0.5 * 2.0 ** -104, seed=72)
+    case.q, case.k, case.kn = case.q.abs(), -case.k.abs(), -case.kn.abs()
+    dev = Device(case, mass=True)
+    dev.attend()
+    check(case, dev)
+
+
+@pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 64)])
 @pytest.mark.parametrize("cached,chunk", [([200], [3]), ([200], [100]), ([200, 40] * 6, [70, 7] * 6), ([3000], [50])],
                          ids=["few rows", "chunks", "many", "parts"])
