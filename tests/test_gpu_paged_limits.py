@@ -167,3 +167,48 @@ def test_long_sequences_in_one_part(cached, rows, d, late):
     dev = Device(case, mass=True)
     dev.attend()
     check(case, dev)
+
+
+@pytest.mark.parametrize("budget,recent", [(270000, 0), (270000, 20000), (299999, 0), (5, 0), (265000, 290000)])
+def test_eviction_from_more_than_64_segments(budget, recent):
+    # ranks of four values, the cut inside equal ones
+    import paper_2502_09888_amd as P
+    n, page = [300000, 5000], 64
+    g = torch.Generator().manual_seed(75)
+    need = [-(-x // page) for x in n]
+    order = torch.randperm(sum(need), generator=g).int()
+    table = torch.full((2, need[0]), -1, dtype=torch.int32)
+    table[0], table[1, :need[1]] = order[:need[0]], order[need[0]:]
+    k = torch.randn(sum(need), 1, page, 4, generator=g)
+    rank = torch.randint(0, 4, (sum(need), page), generator=g).float()
+    stamp = torch.zeros(sum(need), page, dtype=torch.int32)
+    for b in range(2):
+        stamp[table[b, :need[b]].long()] = torch.arange(need[b] * page, dtype=torch.int32).view(-1, page)
+    at = [(table[b, :need[b]].long()[:, None] * page + torch.arange(page)).flatten()[:n[b]] for b in range(2)]   # places in the pool, by slot
+    kd, rd, sd, td, length = k.cuda(), rank.cuda(), stamp.cuda(), table.cuda(), torch.tensor(n, dtype=torch.int32, device="cuda:0")
+    vd = -kd
+    cfg = P.Config(n_heads=1, d_head=4, n_scen=1, n_beh=1, dtype=P.F32)
+    kv = P.paged_kv(kd, vd, td, length, n[0], mass=rd, stamp=sd)
+    ws = torch.empty(P.climber_paged_workspace_bytes(cfg, kv, 0, 0), dtype=torch.uint8, device="cuda:0")
+    src = torch.full((2, need[0] * page), -9, dtype=torch.int32, device="cuda:0")
+    budgets, keep_from = [budget, 2500], [x - recent for x in n]
+    P.climber_paged_evict(cfg, kv, None, torch.tensor(budgets, dtype=torch.int32, device="cuda:0"),
+                          torch.tensor(keep_from, dtype=torch.int32, device="cuda:0") if recent else None, length, src, ws)
+    torch.cuda.synchronize()
+    assert length.tolist() == budgets
+    want_k, want_rank, want_stamp = (x.clone().view(-1, *x.shape[3:]) if x.dim() == 4 else x.clone().view(-1) for x in (k, rank, stamp))
+    for b in range(2):
+        r, slot = rank.view(-1)[at[b]].double(), torch.arange(n[b])
+        r = r + 10.0 * (slot >= keep_from[b]) if recent else r
+        kept = torch.zeros(n[b], dtype=torch.bool)
+        kept[torch.sort(r, descending=True, stable=True).indices[:budgets[b]]] = True
+        front = slot < budgets[b]
+        hole, mover = slot[front & ~kept], slot[kept & ~front]
+        moved = slot[:budgets[b]].clone()
+        moved[hole] = mover
+        assert torch.equal(src[b, :budgets[b]].cpu(), moved.int()) and (src[b, budgets[b]:] == -1).all()
+        for want, was in ((want_k, k), (want_rank, rank), (want_stamp, stamp)):
+            was = was.view(want.shape)
+            want[at[b][hole]] = was[at[b][mover]]
+    assert same_bits(kd, want_k.view(k.shape)) and same_bits(vd, -want_k.view(k.shape))
+    assert same_bits(rd, want_rank.view(rank.shape)) and same_bits(sd, want_stamp.view(stamp.shape))
