@@ -16,9 +16,10 @@
 // sequence and cache head, so that nothing is shared): the waves of a workgroup take different keys, each through a ring of its own and
 // without a barrier, and their results are joined at the end; bound by reading the cache once.
 //
-// Measured: three whole histories of up to 6000 tokens, 32 heads, d_head 128: 424 us, 980 TFLOP/s, where a library product of random
-// matrices reaches 1230 to 1270 on this card and of zeros 1740: its power is the limit, and the exponentials draw on it as well.  One
-// token of each of 64 sequences of 500 to 4000: 108 us for 581 MB, 5.4 TB/s.
+// Measured: three whole histories of up to 6000 tokens, 32 heads, d_head 128: 439 to 454 us from run to run, 915 to 945 TFLOP/s, and 525 us in
+// a row of 22 calls, where the clock is at 1.8 GHz; the matrix pipe is busy in 43 % of the cycles.  A library product of random matrices reaches
+// 1230 to 1270 TFLOP/s on this card and of zeros 1740: power is part of the limit.  One token of each of 64 sequences of 500 to
+// 4000: 108 us for 581 MB, 5.4 TB/s.
 #include "paged_bf16.h"
 
 #include <type_traits>

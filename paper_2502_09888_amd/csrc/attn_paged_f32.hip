@@ -156,9 +156,10 @@ static __device__ __forceinline__ void block_softmax(f32x16 &S, float &m, float 
 // The transposed problem, as in the bf16 kernels: S^T = K Q^T and O^T = V^T P^T with v_mfma_f32_32x32x2_f32.  A lane owns one packed
 // row (lane % 32), its probabilities leave the accumulator as the operand of the value product (step r of it takes the keys of
 // accumulator register r).  The sum over the dimensions is taken in an order that lets a lane read four of them at once.  Four waves
-// with 32 rows each share the keys of a stage.  Chunks of 1000 behaviours of eight users on 1000, 8 heads of 64: 315 us, 79 TFLOP/s (a library
-// product reaches 155; 370 us with keys requested when their turn comes); 256 candidates of each of 16 users on 1000 97 us (120 with registers
-// for one workgroup per CU).
+// with 32 rows each share the keys of a stage.  Chunks of 1000 behaviours of eight users on 1000, 8 heads of 64: 327 us, 75 TFLOP/s (a library
+// product reaches 155; with keys requested when their turn comes a sixth more time); 256 candidates of each of 16 users on 1000 102 us,
+// 82 TFLOP/s (a quarter more time with registers for one workgroup per CU).  There are two barriers for each 32 keys, and a page number's trip
+// to memory in front of each request.
 template <int DP, bool SUMI>
 __global__ __launch_bounds__(256, 2) void attn_paged_f32_kernel(const PagedArgs p)
 {
@@ -458,7 +459,8 @@ __global__ __launch_bounds__(256) void paged_combine_kernel(const PagedArgs p)
 
 // Attention weights per cached token.  One workgroup: 32 keys of one (sequence, cache head), which stay in registers; its waves
 // take the packed rows in turn, p = exp2(s c - lse) again from the logits, and each lane adds up those of its keys.  The sums of a
-// cache head go to part[b][hk][slot], without atomics: a second kernel adds the heads up in their order.
+// cache head go to part[b][hk][slot], without atomics: a second kernel adds the heads up in their order.  Chunks of 1000 behaviours of eight users on
+// 1000, 8 heads of 64: 178 us of a call's 505, 69 TFLOP/s; queries come straight from memory, a block's when its turn comes.
 template <int DP>
 __global__ __launch_bounds__(256) void paged_mass_kernel(const PagedArgs p, float *part)
 {

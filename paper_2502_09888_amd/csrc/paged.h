@@ -115,6 +115,10 @@ static inline unsigned paged_grid(PagedArgs &p)
 {
     const int64_t bh = (int64_t)p.n_seqs * p.Hkv;
     p.bh_major = bh % 8 == 0 || bh >= 64;
+    // By work: us with / without for a token of each of 64 users 107 / 117, ragged scoring of 16 users 154 / 175, sessions of eight 171 / 177 (weights
+    // and all).  Where lengths are spread evenly over a factor of eight it also loses: scoring of 16 users 127 / 119, a token of each of 300
+    // 81 / 73.  Fewer workgroups all run at once (256 of scoring 51 / 51, 128 38 / 41), more have small shares, and the ranks cost more than they give (4096 of
+    // scoring 268 / 255, 8000 of single tokens 173 / 144).
     const int64_t all = bh * p.n_tiles * p.n_split;
     p.by_work = p.n_seqs > 1 && all >= 512 && all < 4096;
     return (unsigned)((p.bh_major ? (bh + 7) / 8 * 8 : bh) * p.n_tiles * p.n_split);
@@ -154,7 +158,9 @@ hipError_t launch_paged_combine(const PagedArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_paged_mass_f32(const PagedArgs &a, float *part, hipStream_t s);
 hipError_t launch_paged_mass_bf16(const PagedArgs &a, float *part, int row_parts, hipStream_t s);
 // ... in one step for at most kMassFewRows packed rows of a sequence and cache head, whose attention has left its logits: keys are not
-// read again
+// read again.  us this way / with logits made again, chunks of 64 users on 500 to 4000, heads of 128: 4 rows 139 / 208, 8 rows 147 / 210; one long
+// cache, 4 rows 72 / 98; fp32, 16 users, 4 rows 36 / 60.  With room for 16 rows 4 take 145, 8 take 154 and 16 171 / 212; for 32 rows 163, 173, 189 and
+// 32 220 / 215.
 constexpr int kMassFewRows = 8;
 hipError_t launch_paged_mass_few(const PagedArgs &a, hipStream_t s);
 hipError_t launch_paged_mass_add(const PagedArgs &a, const float *part, int n_parts, hipStream_t s);
