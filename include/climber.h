@@ -320,6 +320,40 @@ int climber_paged_evict(const climber_config *cfg, const climber_paged_kv *kv, c
 int climber_check_paged(const climber_config *cfg, const climber_paged_kv *kv, const int32_t *off, int32_t m_total, int32_t m_max,
                         int32_t appends, int32_t *status, void *stream);
 
+/* ---- paged history cache in 8 bits --------------------------------------------------------------
+ * The same cache at half the memory and half the traffic: keys and values are held as e4m3 numbers (4 exponent bits, 3 mantissa bits,
+ * largest 448) with a power of two for each block of 16 tokens and cache head:
+ *   kv.k, kv.v        dev [n_pages][n_kv_heads][page_size][d_head], one byte each (kv.elem_bytes 1, or 0: not stated), 16-byte aligned
+ *   k_scale, v_scale  dev [n_pages][n_kv_heads][page_size / 16], one byte s each: the block's elements stand for e4m3 * 2^(s - 127)
+ * and everything else as in climber_paged_kv.  CLIMBER_BF16 with d_head 64 or 128 (rows of a call are bf16); kv.mass must be NULL.
+ * A block's scale is the least s >= 10 with which every finite element of its tokens is at most 448 * 2^(s - 127) in magnitude; elements
+ * are rounded to the nearest e4m3 number, ties to even, and infinities and NaN become NaN.  A token that joins a block raises the scale
+ * where it has to: the block's older elements are then rounded once more.  A scale never falls while its block has tokens; the first token of a block
+ * (slot a multiple of 16) starts it anew.  Elements of keys and values have to stay below 2^127 in magnitude, and scales that the caller
+ * writes between 10 and 247.
+ * Two sequences of a call may list the same page as long as no call writes it; the append writes to the blocks of slots len[b] .. len[b] + rows - 1
+ * whole, the older tokens of the first one among them.  Eviction does not take this cache; climber_check_paged takes &kv8->kv. */
+typedef struct climber_paged_kv8 {
+    climber_paged_kv kv;
+    uint8_t *k_scale, *v_scale;
+} climber_paged_kv8;
+
+/* Bytes of scratch for up to m_total rows, at most m_max per sequence.  0 on an invalid argument. */
+size_t climber_paged8_workspace_bytes(const climber_config *cfg, const climber_paged_kv8 *kv8, int32_t m_total, int32_t m_max);
+
+/* climber_attn_history_paged: cached tokens as the cache holds them before the call, the chunk's own as they are brought; then the
+ * chunk is rounded and stored.  Errors as there (_UNSUPPORTED also: not CLIMBER_BF16, mass). */
+int climber_attn_history_paged8(const climber_config *cfg, const float *tau_layer, const climber_paged_kv8 *kv8, const void *q,
+                                int64_t ld_q, const void *k, const void *v, int64_t ld_kv, const int32_t *off, int32_t m_total,
+                                int32_t m_max, const int32_t *scen, const int32_t *beh, const int32_t *stamp, void *o,
+                                int64_t ld_o, void *workspace, size_t ws_bytes, void *stream);
+
+/* climber_attn_sumi_paged over the cache in 8 bits. */
+int climber_attn_sumi_paged8(const climber_config *cfg, const float *tau_layer, const climber_paged_kv8 *kv8, const void *q_c,
+                             int64_t ld_q, const void *k_c, const void *v_c, int64_t ld_kv, const int32_t *cand_off,
+                             int32_t m_total, int32_t m_max, const int32_t *cand_scen, const int32_t *cand_beh, void *o_c,
+                             int64_t ld_o, void *workspace, size_t ws_bytes, void *stream);
+
 /* ---- debug check of device-resident inputs -----------------------------------------------------
  * Eq. (3) divides a row's logits by tau[scen][beh]: the ids must lie inside the table and the entry
  * must be finite and > 0.  Ids, offsets and the table live in device memory, so the compute calls

@@ -10,6 +10,7 @@ from .climber import (BAD_BEH, BAD_LEN, BAD_M_MAX, BAD_OFFSETS, BAD_PAGE, BAD_SC
                       climber_kv_cache_destroy, climber_kv_cache_rows, climber_layer_forward, climber_pack_weights,
                       climber_packed_weights_bytes, PagedKV, paged_kv, climber_attn_history_paged, climber_attn_sumi_paged,
                       climber_check_paged, climber_paged_evict, climber_paged_workspace_bytes,
+                      PagedKV8, paged_kv8, climber_attn_history_paged8, climber_attn_sumi_paged8, climber_paged8_workspace_bytes,
                       climber_strerror, climber_sumi_forward, climber_sumi_score, climber_sumi_score_static, climber_workspace_bytes, library_path,
                       load_library)
 

@@ -60,6 +60,12 @@ class PagedKV(C.Structure):
     _device = None  # the CUDA device of its tensors (-1: they are in host memory that is not pinned), if it was made from tensors
 
 
+class PagedKV8(C.Structure):
+    """Mirror of ``climber_paged_kv8`` (device pointers).  Build with ``paged_kv8(...)``; its ``kv`` goes to ``climber_check_paged``."""
+    _fields_ = [("kv", PagedKV), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+    _device = None  # as PagedKV's
+
+
 class _Weights(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("layers", C.POINTER(LayerWeights)), ("packed", C.c_void_p)]
 
@@ -145,6 +151,13 @@ def load_library():
     lib.climber_paged_evict.argtypes = [cfgp, pkv, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.climber_check_paged.restype = C.c_int
     lib.climber_check_paged.argtypes = [cfgp, pkv, vp, i32, i32, i32, vp, vp]
+    pkv8 = C.POINTER(PagedKV8)
+    lib.climber_paged8_workspace_bytes.restype = sz
+    lib.climber_paged8_workspace_bytes.argtypes = [cfgp, pkv8, i32, i32]
+    lib.climber_attn_history_paged8.restype = C.c_int
+    lib.climber_attn_history_paged8.argtypes = [cfgp, vp, pkv8, vp, i64, vp, vp, i64, vp, i32, i32, vp, vp, vp, vp, i64, vp, sz, vp]
+    lib.climber_attn_sumi_paged8.restype = C.c_int
+    lib.climber_attn_sumi_paged8.argtypes = [cfgp, vp, pkv8, vp, i64, vp, vp, i64, vp, i32, i32, vp, vp, vp, i64, vp, sz, vp]
     try:
         _load_native(lib)
     except ImportError:  # the host's calls do without; an attention call raises it
@@ -167,7 +180,7 @@ def _load_native(lib):
                                                         lib.climber_attn_sumi_bias)),
                 Config, RelBias, *current,
                 *(C.cast(f, C.c_void_p).value for f in (lib.climber_attn_history_paged, lib.climber_attn_sumi_paged, lib.climber_paged_evict)),
-                PagedKV)
+                PagedKV, *(C.cast(f, C.c_void_p).value for f in (lib.climber_attn_history_paged8, lib.climber_attn_sumi_paged8)), PagedKV8)
     _native = native
     return native
 
@@ -521,3 +534,67 @@ def climber_check_paged(cfg: Config, kv: PagedKV, off, m_total: int, m_max: int,
     _on_device(kv, stream)
     _ok(load_library().climber_check_paged(C.byref(cfg), C.byref(kv), _ptr(off), m_total, m_max, int(appends), _ptr(status), _stream(stream)),
         "climber_check_paged")
+
+
+def paged_kv8(k, v, k_scale, v_scale, page_table, len, max_len: int, stamp=None) -> PagedKV8:
+    """climber_paged_kv8 from contiguous device tensors: k, v float8_e4m3fn or uint8 [n_pages, n_kv_heads, page_size, d_head]; k_scale, v_scale uint8
+    (or float8_e8m0fnu) [n_pages, n_kv_heads, page_size / 16]; the others as in paged_kv."""
+    tensors = [t for t in (k, v, k_scale, v_scale, page_table, len, stamp) if t is not None]
+    for t in tensors:
+        if not t.is_contiguous():
+            raise ValueError("a paged cache is described by contiguous tensors")
+    n_pages, n_kv_heads, page_size, d_head = k.shape
+    n_seqs, table_ld = page_table.shape
+    blocks = (n_pages, n_kv_heads, page_size // 16)
+    if v.shape != k.shape or tuple(k_scale.shape) != blocks or tuple(v_scale.shape) != blocks or len.numel() != n_seqs or \
+            (stamp is not None and stamp.numel() != n_pages * page_size):
+        raise ValueError("k, v, k_scale, v_scale, page_table, len and stamp are not of one cache")
+    kinds = [str(t.dtype)[6:] for t in tensors]  # (without "torch.")
+    if any(x not in ("float8_e4m3fn", "uint8") for x in kinds[:2]) or any(x not in ("uint8", "float8_e8m0fnu") for x in kinds[2:4]) or \
+            any(x != "int32" for x in kinds[4:]):
+        raise ValueError("k, v are float8_e4m3fn or uint8, k_scale and v_scale uint8 or float8_e8m0fnu, page_table, len and stamp int32")
+    if any(t.device != k.device for t in tensors):
+        raise ValueError("k, v, k_scale, v_scale, page_table, len and stamp are not on one device")
+    kv = PagedKV8(PagedKV(_ptr(k), _ptr(v), None, _ptr(stamp), _ptr(page_table), _ptr(len), n_pages, page_size, n_kv_heads, n_seqs, table_ld, max_len,
+                          d_head, 1), _ptr(k_scale), _ptr(v_scale))
+    kv._keep = tensors
+    if k.is_cuda:
+        kv._device = k.device.index
+    elif not all(t.is_pinned() for t in tensors):
+        kv._device = -1
+    return kv
+
+
+def climber_paged8_workspace_bytes(cfg: Config, kv8: PagedKV8, m_total: int, m_max: int) -> int:
+    return int(load_library().climber_paged8_workspace_bytes(C.byref(cfg), C.byref(kv8), m_total, m_max))
+
+
+def climber_attn_history_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q, k, v, off, m_total: int, m_max: int, scen, beh, stamp, o,
+                                workspace, stream=None) -> None:
+    """climber_attn_history_paged on a cache in 8 bits."""
+    _on_device(kv8, stream)
+    code = (_native or _load_native(load_library())).attn_history_paged8(cfg, tau_layer, kv8, q, k, v, off, m_total, m_max, scen, beh, stamp, o,
+                                                                         workspace, stream)
+    if code is None:
+        d, dk = cfg.d_model, kv8.kv.n_kv_heads * cfg.d_head
+        code = load_library().climber_attn_history_paged8(
+            C.byref(cfg), _ptr(tau_layer), C.byref(kv8), _ptr(q), _pitch(q, d), _ptr(k), _ptr(v), _same_pitch(k, v, dk), _ptr(off), m_total, m_max,
+            _ptr(scen), _ptr(beh), _ptr(stamp), _ptr(o), _pitch(o, d), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_attn_history_paged8")
+
+
+def climber_attn_sumi_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q_c, k_c, v_c, cand_off, m_total: int, m_max: int, cand_scen, cand_beh,
+                             o_c, workspace, stream=None) -> None:
+    """climber_attn_sumi_paged on a cache in 8 bits."""
+    _on_device(kv8, stream)
+    code = (_native or _load_native(load_library())).attn_sumi_paged8(cfg, tau_layer, kv8, q_c, k_c, v_c, cand_off, m_total, m_max, cand_scen,
+                                                                      cand_beh, o_c, workspace, stream)
+    if code is None:
+        d, dk = cfg.d_model, kv8.kv.n_kv_heads * cfg.d_head
+        code = load_library().climber_attn_sumi_paged8(
+            C.byref(cfg), _ptr(tau_layer), C.byref(kv8), _ptr(q_c), _pitch(q_c, d), _ptr(k_c), _ptr(v_c), _same_pitch(k_c, v_c, dk),
+            _ptr(cand_off), m_total, m_max, _ptr(cand_scen), _ptr(cand_beh), _ptr(o_c), _pitch(o_c, d), _ptr(workspace), _nbytes(workspace),
+            _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_attn_sumi_paged8")

@@ -1,0 +1,387 @@
+// Attention over the paged history cache in 8 bits (gfx950): rows of the call in bf16, cached keys and values in e4m3 with a power of two
+// for each 16 tokens and cache head (Eq. (3) of Climber, arXiv 2502.09888; the mask of Sec. 3.2 for candidates).
+//
+// The mathematics are those of the bf16 paged attention (transposed problem, a lane owns a packed row, one pass over the keys).  An e4m3 value
+// times a power of two is a bf16 number exactly, so that v_cvt_scalef32_pk_bf16_fp8, which multiplies on its way, makes the operands of the bf16
+// matrix instructions and nothing is lost behind the cache's own rounding.  (Products of 8-bit operands would round queries and
+// probabilities to four bits.)  Every row sees all cached tokens of its sequence; masks only concern the call's own rows, which
+// are seen as they were brought.
+#include "paged8.h"
+#include "paged_state_bf16.h"
+
+namespace climber {
+namespace {
+
+using namespace paged;
+
+typedef int i32x2 __attribute__((__vector_size__(8)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+
+// 4 codes as bf16 numbers, times `scale` (a power of two)
+static __device__ __forceinline__ u32x2 wide4(uint32_t codes, float scale)
+{
+    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true);
+    return u32x2{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
+}
+static __device__ __forceinline__ u32x4 wide8(u32x2 codes, float scale)
+{
+    const u32x2 a = wide4(codes.x, scale), b = wide4(codes.y, scale);
+    return u32x4{a.x, a.y, b.x, b.y};
+}
+static __device__ __forceinline__ float scale_of(uint32_t stored) { return __uint_as_float((stored & 255u) << 23); }
+
+// Rows of D codes in LDS: 16-byte piece c of row r at slot c ^ f(r).  f takes 16 consecutive rows (key fragments: 16 lanes read one piece
+// each) to 16 places of the 64 banks, and so it does two pieces of rows r, r + 1, r + 2, r + 3, r + 8, ... r + 11 (value fragments).
+template <int D>
+struct Rows8 {
+    static constexpr int kPieces = D / 16, kPerLoad = 64 / kPieces, kLoads = 16 / kPerLoad;  // (of 16 rows)
+    static __device__ __forceinline__ int f(int r)
+    {
+        return D == 128 ? ((r >> 2) & 1) | (r & 2) | ((r >> 1) & 4) : ((r >> 2) & 1) | ((r >> 2) & 2);
+    }
+    uint32_t k_at[D / 32], v_at[D / 32];
+    __device__ __forceinline__ void init(int lane)
+    {
+        const int l32 = lane & 31, hf = lane >> 5, G = lane >> 4, i16 = lane & 15;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) k_at[j] = l32 * D + ((2 * j + hf) ^ f(l32)) * 16;
+        // transpose reads: a group of 16 lanes names 8 rows of 16 codes, each by two lanes, and each lane gets the 8 codes of one column
+        const int j = i16 >> 1, r = 8 * (j >> 2) + 4 * (G >> 1) + (j & 3);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) v_at[db] = r * D + ((2 * db + (G & 1)) ^ f(r)) * 16 + 8 * (i16 & 1);
+    }
+};
+
+// A wave's copies of the codes of 16 cached keys and their values (one page's) into LDS.
+template <int D>
+struct Source8 {
+    using R = Rows8<D>;
+    const Paged8Args &p;
+    int hk, cached;              // keys below `cached` are read
+    uint32_t at[R::kLoads];
+    const uint8_t *k_page;
+    int64_t to_v, page_bytes;
+    const int32_t *table;
+
+    __device__ __forceinline__ Source8(const Paged8Args &p_, int b, int hk_, int cached_, int lane) : p(p_), hk(hk_), cached(cached_)
+    {
+#pragma unroll
+        for (int i = 0; i < R::kLoads; ++i) {
+            const int row = i * R::kPerLoad + lane / R::kPieces;
+            at[i] = row * D + ((lane % R::kPieces) ^ R::f(row)) * 16;
+        }
+        page_bytes = ((int64_t)p.Hkv << p.page_shift) * D;
+        k_page = uniform(p.k_pages + ((int64_t)hk << p.page_shift) * D);
+        to_v = p.v_pages - p.k_pages;
+        table = p.table + (int64_t)b * p.table_ld;
+    }
+    // of key g, or of the last cached key, which stands for those behind it
+    __device__ __forceinline__ int page_number(int g) const { return min(max(table[max(min(g, cached - 1), 0) >> p.page_shift], 0), p.n_pages - 1); }
+    // the scales of the 16 keys from g on: of keys in the low byte, of values in the next
+    __device__ __forceinline__ uint32_t scales(int g, int page) const
+    {
+        const int64_t i = (((int64_t)page * p.Hkv + hk) << (p.page_shift - 4)) + ((max(min(g, cached - 1), 0) & ((1 << p.page_shift) - 1)) >> 4);
+        return p.k_scale[i] | (uint32_t)p.v_scale[i] << 8;
+    }
+    __device__ __forceinline__ void issue(int g, int page, lds_u8 *to_k, lds_u8 *to_v_lds) const
+    {
+        // (a group behind the cached keys: the place in the page is one of the page's, whatever it holds)
+        const uint8_t *k = uniform(k_page + page * page_bytes + (g & ((1 << p.page_shift) - 1)) * D), *v = uniform(k + to_v);
+#pragma unroll
+        for (int i = 0; i < R::kLoads; ++i) {
+            copy16((glb_u8 *)k + at[i], to_k + i * 1024);
+            copy16((glb_u8 *)v + at[i], to_v_lds + i * 1024);
+        }
+    }
+};
+
+// Key fragments of 32 rows of codes; `scale` is that of this lane's row.
+template <int D>
+static __device__ __forceinline__ KFrags<D> read_k8(const Rows8<D> &w, const lds_u8 *base, float scale)
+{
+    KFrags<D> f;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        const u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)(base + w.k_at[j]);
+        f.a[2 * j] = frag(wide8(u32x2{x.x, x.y}, scale));
+        f.a[2 * j + 1] = frag(wide8(u32x2{x.z, x.w}, scale));
+    }
+    return f;
+}
+// Value fragments of 16 rows of codes.  `keep`: bits of the codes that stay (8 keys of this lane).
+template <int D>
+static __device__ __forceinline__ VFrags<D> read_v8(const Rows8<D> &w, lds_u8 *base, float scale, u32x2 keep)
+{
+    VFrags<D> f;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+        const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(base + w.v_at[db])));
+        f.a[db] = wide8(x & keep, scale);
+    }
+    return f;
+}
+// the first n of 4 bytes (n from below 0 to above 4)
+static __device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : (1u << (8 * max(n, 0))) - 1u; }
+
+// Fragments of 32 bf16 key rows in the order of a wide state.
+template <int D>
+static __device__ __forceinline__ KFrags<D> read_k_wide(const lds_u8 *base, int lane)
+{
+    using R = Rows<D>;
+    const int l32 = lane & 31, hf = lane >> 5;
+    KFrags<D> f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+        f.a[s] = *(const __attribute__((address_space(3))) bf16x8 *)(base + l32 * R::kPitch + ((4 * (s >> 1) + 2 * hf + (s & 1)) ^ R::f(l32)) * 16);
+    return f;
+}
+
+// ---- few rows ------------------------------------------------------------------------------------
+// 32 packed rows; the waves of a workgroup take different blocks of 32 keys, each through a ring of its own, and are joined at the end.
+template <int D, bool SUMI>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_paged8_few_kernel(const Paged8Args p)
+{
+    constexpr int kStage = 2 * 32 * D, kLoads = 4 * Rows8<D>::kLoads;  // a wave's, of a block of 32 keys
+    __shared__ __attribute__((aligned(1024))) uint8_t stage0[4 * kStage], stage1[4 * kStage], stage2[4 * kStage], stage3[4 * kStage];
+    __shared__ JoinRoom joined;
+    __shared__ int odd_seen[4];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
+    const int rows = s.T * p.G, r_tile = w.tile * 32;
+    if (r_tile >= rows) return;
+    const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
+    const int64_t row = s.row0 + t;
+    const bool causal = !SUMI && p.causal;
+    const int k_all = SUMI ? s.n : paged_keys(p, s);
+    auto sees = [&](int i) { return causal ? min(s.n + min(i, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row i sees keys below it
+    int k_lo, k_hi;
+    paged_part(p, w.split, sees(r_tile + 31), 128, k_lo, k_hi);
+    k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+    const int c_lo = min(k_lo, s.n), c_hi = min(k_hi, s.n);            // the cached ones
+    const int n_blk = (c_hi - c_lo + 31) / 32, mine = n_blk > wave ? (n_blk - wave + 3) / 4 : 0;  // blocks wave, wave + 4, ...
+
+    const Source8<D> src(p, w.b, w.hk, c_hi, lane);
+    auto stage = [&](int i) __attribute__((always_inline)) {
+        return (lds_u8 *)((i & 3) == 0 ? stage0 : (i & 3) == 1 ? stage1 : (i & 3) == 2 ? stage2 : stage3) + wave * kStage;
+    };
+    // page numbers of 32 blocks: the lower 32 lanes have those of the first 16 keys, the upper those of the others; of the 32 after them
+    const int k_mine = c_lo + wave * 32 - (lane >> 5) * (32 * 128 - 16);
+    int pages = src.page_number(k_mine + lane * 128), pages_next = src.page_number(k_mine + (32 + lane) * 128);
+    uint32_t scales = src.scales(k_mine + lane * 128, pages), scales_next = scales;
+    auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
+        if ((i & 31) == 0 && i > 0) {
+            pages = pages_next;
+            pages_next = src.page_number(k_mine + (i + 32 + lane) * 128);
+        }
+        const int k0 = c_lo + (i * 4 + wave) * 32;
+        src.issue(k0, __builtin_amdgcn_readlane(pages, i & 31), to, to + 32 * D);
+        src.issue(k0 + 16, __builtin_amdgcn_readlane(pages, 32 + (i & 31)), to + 16 * D, to + 48 * D);
+    };
+    Rows8<D> at;
+    at.init(lane);
+    State<D, 1, true> st;
+    {
+        typename State<D, 1, true>::Row in;
+        st.template request<SUMI>(p, 0, row, h, w.hk, hf, in);
+        if (mine > 0) issue(0, stage(0));
+        if (mine > 1) issue(1, stage(1));
+        if (mine > 2) issue(2, stage(2));
+        st.template start<SUMI>(p, 0, hf, in, w.split == 0 && wave == 0);
+    }
+    auto block = [&](int i, lds_u8 *keys, lds_u8 *free) __attribute__((always_inline)) {
+        // (rows, page numbers and scales were asked for among the copies: this waits for more than it has to, never for less)
+        const int later = min(mine - 1 - i, 2);
+        if (later == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+        else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (i + 3 < mine) issue(i + 3, free);
+        if ((i & 31) == 0 && i > 0) scales = scales_next;
+        if ((i & 31) == 16) scales_next = src.scales(k_mine + ((i & ~31) + 32 + lane) * 128, pages_next);
+        const uint32_t s0 = __builtin_amdgcn_readlane(scales, i & 31), s1 = __builtin_amdgcn_readlane(scales, 32 + (i & 31));
+        const int k0 = c_lo + (i * 4 + wave) * 32;
+        f32x16 S[1];
+        bf16x8 P[1][2];
+        st.logits(read_k8<D>(at, keys, scale_of(l32 < 16 ? s0 : s1)), S);
+        const bool whole = k0 + 32 <= c_hi;
+        if (!whole) hide(S[0], k0, hf, c_hi);
+        st.reference(S);
+        st.weights(S, P);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int left = c_hi - (k0 + 16 * g + 4 * hf);  // (codes of hidden keys may be no numbers)
+            st.add(read_v8<D>(at, keys + 32 * D + g * 16 * D, scale_of((g ? s1 : s0) >> 8), u32x2{first_bytes(left), first_bytes(left - 8)}), P, g);
+        }
+        // its place has been read
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+#pragma unroll 1
+    for (int i = 0; i < mine; i += 4) {
+        block(i, stage(0), stage(3));
+        if (i + 1 < mine) block(i + 1, stage(1), stage(0));
+        if (i + 2 < mine) block(i + 2, stage(2), stage(1));
+        if (i + 3 < mine) block(i + 3, stage(3), stage(2));
+    }
+
+    bool odd = false;
+    int n_lo = 0;
+    if constexpr (!SUMI) {
+        // the call's own rows: blocks of 32 from the part's first one on
+        n_lo = max(k_lo - s.n, 0);
+        const int n_hi = max(k_hi - s.n, 0), n_new = (n_hi - n_lo + 31) / 32;
+        PagedSeq own = s;
+        own.n = 0;
+        const Source<D, Rows<D>::kLoads> rows_src(p, own, w.b, w.hk, n_hi, lane, 0);
+        Rows<D> vat;
+        vat.init(lane);
+        const int lim = sees(r) - s.n, lim_lo = sees(r_tile) - s.n;
+#pragma unroll 1
+        for (int i = wave; i < n_new; i += 4) {
+            const int k0 = n_lo + i * 32;
+            lds_u8 *const keys = stage(0), *const values = stage(1);
+            rows_src.issue(k0, 0, keys, values);
+            rows_src.issue(k0 + 16, 0, keys + 16 * Rows<D>::kPitch, values + 16 * Rows<D>::kPitch);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            f32x16 S[1];
+            bf16x8 P[1][2];
+            st.logits(read_k_wide<D>(keys, lane), S);
+            if (k0 + 32 > min(lim_lo, n_hi)) {
+                odd |= clear_odd<32 * Rows<D>::kPitch>(values, lane);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                hide(S[0], k0, hf, min(lim, n_hi));
+            }
+            st.reference(S);
+            st.weights(S, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(vat, values + g * 16 * Rows<D>::kPitch), P, g);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    }
+    if (lane == 0) odd_seen[wave] = odd;
+    // (each wave's outputs in units of its reference take the 2 x kStage bytes of two waves' places; all waves are done with theirs at the first barrier)
+    join_few<D, true>(p, s, w, st, joined, [&](int j) { return (float *)(j < 2 ? stage0 : stage1) + (j & 1) * 32 * D; }, row, h, r_tile, rows);
+    if constexpr (!SUMI) {
+        if (__builtin_expect(odd_seen[0] | odd_seen[1] | odd_seen[2] | odd_seen[3], 0)) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all waves' outputs are written
+            __syncthreads();
+            const int from = s.n + n_lo, clean = max(0, min(sees(r_tile), k_hi) - from) / 32 * 32;
+            if (wave == 0) put_odd<D>(p, s, w, from + clean, k_hi, r_tile, min(r_tile + 32, rows), sees);
+        }
+    }
+}
+
+// ---- new tokens ----------------------------------------------------------------------------------
+// A wave for a block of 16 tokens of a cache head.  The scale is the least with which all of the block's tokens, those that were
+// stored before too, stay within 448 of it; where it grows these are rounded again (by a power of two, so that only what lies near the
+// smallest numbers changes).  Infinities become no numbers.
+static __device__ __forceinline__ uint32_t wave_max(uint32_t x)
+{
+#pragma unroll
+    for (int m = 32; m; m >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, m, 64));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void paged8_store_kernel(const Paged8Args p, int n_blk)
+{
+    constexpr int kLanes = D / 8, kRows = 64 / kLanes, kLoads = 16 / kRows;  // lanes of a row, 8 values each
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t bh = unit / n_blk;
+    if (bh >= (int64_t)p.n_seqs * p.Hkv) return;
+    const int b = (int)(bh / p.Hkv), hk = (int)(bh % p.Hkv);
+    const PagedSeq s = paged_seq(p, b);
+    const int end = min(s.n + s.T, p.max_len), slot0 = ((s.n >> 4) + (int)(unit % n_blk)) * 16;
+    if (slot0 >= end || s.T == 0) return;
+    const int page = p.table[(int64_t)b * p.table_ld + (slot0 >> p.page_shift)];
+    if (page < 0 || page >= p.n_pages) return;
+    const int in = slot0 & ((1 << p.page_shift) - 1), old = min(max(s.n - slot0, 0), 16), n = min(end - slot0, 16);  // tokens [0, old) stay, [old, n) come
+    const int64_t head = (int64_t)page * p.Hkv + hk, to = ((head << p.page_shift) + in) * D, at = (head << (p.page_shift - 4)) + (in >> 4);
+    u32x4 x[2][kLoads];
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int j = i * kRows + lane / kLanes;
+            x[kv][i] = u32x4{0, 0, 0, 0};
+            if (j >= old && j < n)
+                x[kv][i] = *(const u32x4 *)((kv ? p.v : p.k) + (s.row0 + slot0 + j - s.n) * p.ld_kv + (int64_t)hk * (2 * D) + (lane % kLanes) * 16);
+        }
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+        uint8_t *const pages = kv ? p.v_pages : p.k_pages, *const scale = (kv ? p.v_scale : p.k_scale) + at;
+        uint32_t top = 0;  // largest finite magnitude, as bits of a bf16
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = x[kv][i][e] & 0x7fffu, hi = (x[kv][i][e] >> 16) & 0x7fffu;
+                top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+            }
+        top = wave_max(top);
+        // 1.m 2^(e - 127) <= 448 2^s = 1.75 2^(s + 8)
+        const int was = old > 0 ? *scale : 0, mine = max((int)(top >> 7) - 8 + ((top & 127u) > 96u), kLeastScale), now = max(was, mine);
+        if (old > 0 && now > was) {
+            const float down = now - was > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (now - was)) << 23);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int j = i * kRows + lane / kLanes;
+                if (j >= old) continue;
+                u32x2 *const c = (u32x2 *)(pages + to + j * D + (lane % kLanes) * 8);
+                u32x2 y = *c;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(y[e], false), b2 = __builtin_amdgcn_cvt_pk_f32_fp8(y[e], true);
+                    y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(b2[0] * down, b2[1] * down, __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * down, a[1] * down, 0, false), true);
+                }
+                *c = y;
+            }
+        }
+        const float up = __uint_as_float((uint32_t)(254 - now) << 23);  // 2^(127 - now)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int j = i * kRows + lane / kLanes;
+            if (j < old || j >= n) continue;
+            u32x2 y;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint32_t u = x[kv][i][2 * e], v = x[kv][i][2 * e + 1];
+                y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(u << 16) * up, __uint_as_float(u & 0xffff0000u) * up, 0, false);
+                y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(v << 16) * up, __uint_as_float(v & 0xffff0000u) * up, y[e], true);
+            }
+            *(u32x2 *)(pages + to + j * D + (lane % kLanes) * 8) = y;
+        }
+        if (lane == 0 && now != was) *scale = (uint8_t)now;
+    }
+    if (hk == 0 && p.stamp && lane >= old && lane < n) p.stamp[((int64_t)page << p.page_shift) + in + lane] = p.stamp_new[s.row0 + slot0 + lane - s.n];
+}
+
+template <int D, bool SUMI>
+hipError_t launch(Paged8Args p, hipStream_t s)
+{
+    const int64_t rows = (int64_t)p.m_max * p.G;
+    p.n_tiles = (int)((rows + 31) / 32);
+    hipLaunchKernelGGL((attn_paged8_few_kernel<D, SUMI>), dim3(paged_grid(p)), dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t s)
+{
+    if (a.d == 64) return a.sumi ? launch<64, true>(a, s) : launch<64, false>(a, s);
+    return a.sumi ? launch<128, true>(a, s) : launch<128, false>(a, s);
+}
+
+hipError_t launch_paged8_store(const Paged8Args &a, hipStream_t s)
+{
+    const int64_t n_blk = paged8_store_blocks(a.m_max), units = (int64_t)a.n_seqs * a.Hkv * n_blk;
+    const dim3 grid((unsigned)((units + 3) / 4));
+    if (a.d == 64) hipLaunchKernelGGL(paged8_store_kernel<64>, grid, dim3(256), 0, s, a, (int)n_blk);
+    else hipLaunchKernelGGL(paged8_store_kernel<128>, grid, dim3(256), 0, s, a, (int)n_blk);
+    return hipGetLastError();
+}
+
+}  // namespace climber

@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_paged_few_kernel(co
     using R = Rows<D>;
     constexpr int kStage = 2 * 32 * R::kPitch, kLoads = 4 * R::kLoads;  // a wave's
     __shared__ __attribute__((aligned(1024))) uint8_t stage0[4 * kStage], stage1[4 * kStage];
-    __shared__ float ref[4][32], denom[4][32];
+    __shared__ JoinRoom joined;
     __shared__ int odd_seen[4];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     PagedWork w;
@@ -361,53 +361,8 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_paged_few_kernel(co
         if (i + 1 < mine) block(i + 1, at1);
     }
 
-    // join the waves: denominators and outputs in units of the largest reference
-    const float l = st.l[0] + other_half(st.l[0]);
-    if (hf == 0) ref[wave][l32] = st.m[0], denom[wave][l32] = l;
     if (lane == 0) odd_seen[wave] = odd;
-    __syncthreads();
-    const float m = fmaxf(fmaxf(ref[0][l32], ref[1][l32]), fmaxf(ref[2][l32], ref[3][l32]));
-    const float mine_w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.m[0] - m) * st.c[0]);
-    float *joined = (float *)stage0 + wave * 32 * D;  // (all copies have arrived and been read)
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            f32x4 x;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : st.O[0][db][4 * g + e] * mine_w;
-            // (16-byte piece c of row r at slot c ^ r % 8: lanes of neighbouring rows write to different banks)
-            *(f32x4 *)(joined + l32 * D + (((8 * db + 2 * g + hf) ^ (l32 & 7)) * 4)) = x;
-        }
-    float total = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) total += denom[j][l32] == 0.f ? 0.f : denom[j][l32] * __builtin_amdgcn_exp2f((ref[j][l32] - m) * st.c[0]);
-    __syncthreads();
-    if (wave == 0 && hf == 0) denom[0][l32] = total;  // (read by all above, before the barrier)
-    __syncthreads();
-    if (wave == 0 && hf == 0 && r_tile + l32 < rows) {
-        const int64_t rh = row * p.H + h;
-        if (p.n_split > 1) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{m * st.c[0], total};
-        else if (p.lse) p.lse[rh] = float2{st.c[0], m * st.c[0] + __builtin_amdgcn_logf(total)};
-    }
-    constexpr int C = D / 4;
-    const int n_rows = min(32, rows - r_tile);
-    for (int i = threadIdx.x; i < n_rows * C; i += 256) {
-        const int rr = i / C, c = i % C, tt = (r_tile + rr) / p.G, hh = w.hk * p.G + (r_tile + rr) % p.G;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x += *(const f32x4 *)((const float *)stage0 + j * 32 * D + rr * D + ((c ^ (rr & 7)) * 4));
-        const int64_t rh = (s.row0 + tt) * p.H + hh;
-        if (p.n_split > 1) {
-            *(f32x4 *)(p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D + c * 4) = x;
-        } else {
-            const float inv = 1.f / denom[0][rr];
-            bf16x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(x[e] * inv);
-            *(bf16x4 *)((__bf16 *)(p.o + (s.row0 + tt) * p.ld_o) + (int64_t)hh * D + c * 4) = y;
-        }
-    }
+    join_few<D>(p, s, w, st, joined, [&](int j) { return (float *)stage0 + j * 32 * D; }, row, h, r_tile, rows);
     if (__builtin_expect(odd_seen[0] | odd_seen[1] | odd_seen[2] | odd_seen[3], 0)) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all waves' outputs are written
         __syncthreads();

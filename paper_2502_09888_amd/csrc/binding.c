@@ -17,7 +17,9 @@ static __typeof__(&climber_attn_sumi_bias) attn_sumi_bias_fn;
 static __typeof__(&climber_attn_history_paged) attn_history_paged_fn;
 static __typeof__(&climber_attn_sumi_paged) attn_sumi_paged_fn;
 static __typeof__(&climber_paged_evict) paged_evict_fn;
-static PyObject *config_type, *bias_type, *current_device, *raw_stream, *paged_type, *s_data_ptr, *s_cuda_stream, *s_shape, *s_stride, *s_nbytes;
+static __typeof__(&climber_attn_history_paged8) attn_history_paged8_fn;
+static __typeof__(&climber_attn_sumi_paged8) attn_sumi_paged8_fn;
+static PyObject *config_type, *bias_type, *current_device, *raw_stream, *paged_type, *paged8_type, *s_data_ptr, *s_cuda_stream, *s_shape, *s_stride, *s_nbytes;
 
 static int unsigned_of(PyObject *o, void **p) /* takes the reference */
 {
@@ -149,7 +151,7 @@ static int bytes_of(PyObject *o, size_t *n)
 }
 
 /* cfg, tau, kv, q, k, v, off, m_total, m_max, scen, beh[, stamp], o, workspace, stream */
-static PyObject *paged(PyObject *const *a, Py_ssize_t n, int appends)
+static PyObject *paged(PyObject *const *a, Py_ssize_t n, int appends, int bits8)
 {
     if (n != 14 + appends) return elsewhere();
     void *p[14], *s;
@@ -162,14 +164,17 @@ static PyObject *paged(PyObject *const *a, Py_ssize_t n, int appends)
         if (i != 2 && i != 7 && i != 8 && !pointer(a[i], &p[i])) return elsewhere();
     if (!number(a[7], &m_total) || !number(a[8], &m_max) || !bytes_of(a[o + 1], &ws_bytes) || !stream_of(a[n - 1], &s)) return elsewhere();
     if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
-    if (!structure(a[2], paged_type, sizeof(climber_paged_kv), &kv)) return PyBuffer_Release(&cfg), elsewhere();
-    const climber_config *c = cfg.buf;
+    if (bits8 ? !paged8_type || !structure(a[2], paged8_type, sizeof(climber_paged_kv8), &kv) : !structure(a[2], paged_type, sizeof(climber_paged_kv), &kv))
+        return PyBuffer_Release(&cfg), elsewhere();
+    const climber_config *c = cfg.buf; /* (a climber_paged_kv8 begins with its climber_paged_kv) */
     const int64_t wide = c->d_model, kv_wide = (int64_t)((const climber_paged_kv *)kv.buf)->n_kv_heads * c->d_head;
     int code = 0;
     const int ok = pitch(a[3], wide, &ld_q) && pitch(a[4], kv_wide, &ld_kv) && pitch(a[5], ld_kv, &ld_v) && ld_v == ld_kv && pitch(a[o], wide, &ld_o);
     if (ok) {
         Py_BEGIN_ALLOW_THREADS
-        if (appends) code = attn_history_paged_fn(c, p[1], kv.buf, p[3], ld_q, p[4], p[5], ld_kv, p[6], m_total, m_max, p[9], p[10], p[11], p[12], ld_o, p[13], ws_bytes, s);
+        if (bits8 && appends) code = attn_history_paged8_fn(c, p[1], kv.buf, p[3], ld_q, p[4], p[5], ld_kv, p[6], m_total, m_max, p[9], p[10], p[11], p[12], ld_o, p[13], ws_bytes, s);
+        else if (bits8) code = attn_sumi_paged8_fn(c, p[1], kv.buf, p[3], ld_q, p[4], p[5], ld_kv, p[6], m_total, m_max, p[9], p[10], p[11], ld_o, p[12], ws_bytes, s);
+        else if (appends) code = attn_history_paged_fn(c, p[1], kv.buf, p[3], ld_q, p[4], p[5], ld_kv, p[6], m_total, m_max, p[9], p[10], p[11], p[12], ld_o, p[13], ws_bytes, s);
         else code = attn_sumi_paged_fn(c, p[1], kv.buf, p[3], ld_q, p[4], p[5], ld_kv, p[6], m_total, m_max, p[9], p[10], p[11], ld_o, p[12], ws_bytes, s);
         Py_END_ALLOW_THREADS
     }
@@ -178,8 +183,10 @@ static PyObject *paged(PyObject *const *a, Py_ssize_t n, int appends)
     return ok ? PyLong_FromLong(code) : elsewhere();
 }
 
-static PyObject *attn_history_paged(PyObject *m, PyObject *const *a, Py_ssize_t n) { return paged(a, n, 1); }
-static PyObject *attn_sumi_paged(PyObject *m, PyObject *const *a, Py_ssize_t n) { return paged(a, n, 0); }
+static PyObject *attn_history_paged(PyObject *m, PyObject *const *a, Py_ssize_t n) { return paged(a, n, 1, 0); }
+static PyObject *attn_sumi_paged(PyObject *m, PyObject *const *a, Py_ssize_t n) { return paged(a, n, 0, 0); }
+static PyObject *attn_history_paged8(PyObject *m, PyObject *const *a, Py_ssize_t n) { return paged(a, n, 1, 1); }
+static PyObject *attn_sumi_paged8(PyObject *m, PyObject *const *a, Py_ssize_t n) { return paged(a, n, 0, 1); }
 
 /* cfg, kv, rank, budget, keep_from, len_out, src, workspace, stream */
 static PyObject *paged_evict(PyObject *m, PyObject *const *a, Py_ssize_t n)
@@ -203,14 +210,18 @@ static PyObject *paged_evict(PyObject *m, PyObject *const *a, Py_ssize_t n)
 }
 
 /* bind(addresses of the four entry points, Config, RelBias, torch.cuda.current_device, torch's raw current stream
- *      [, addresses of the three on a paged cache, PagedKV]) */
+ *      [, addresses of the three on a paged cache, PagedKV[, of the two on one in 8 bits, PagedKV8]]) */
 static PyObject *bind(PyObject *m, PyObject *args)
 {
-    unsigned long long f[4], g[3] = {0, 0, 0};
-    PyObject *t[5] = {NULL};
-    if (!PyArg_ParseTuple(args, "KKKKO!O!OO|KKKO!", &f[0], &f[1], &f[2], &f[3], &PyType_Type, &t[0], &PyType_Type, &t[1], &t[2], &t[3], &g[0],
-                          &g[1], &g[2], &PyType_Type, &t[4]))
+    unsigned long long f[4], g[5] = {0, 0, 0, 0, 0};
+    PyObject *t[6] = {NULL};
+    if (!PyArg_ParseTuple(args, "KKKKO!O!OO|KKKO!KKO!", &f[0], &f[1], &f[2], &f[3], &PyType_Type, &t[0], &PyType_Type, &t[1], &t[2], &t[3], &g[0],
+                          &g[1], &g[2], &PyType_Type, &t[4], &g[3], &g[4], &PyType_Type, &t[5]))
         return NULL;
+    if (t[5]) {
+        attn_history_paged8_fn = (__typeof__(attn_history_paged8_fn))(uintptr_t)g[3];
+        attn_sumi_paged8_fn = (__typeof__(attn_sumi_paged8_fn))(uintptr_t)g[4];
+    }
     if (t[4]) {
         attn_history_paged_fn = (__typeof__(attn_history_paged_fn))(uintptr_t)g[0];
         attn_sumi_paged_fn = (__typeof__(attn_sumi_paged_fn))(uintptr_t)g[1];
@@ -220,8 +231,8 @@ static PyObject *bind(PyObject *m, PyObject *args)
     attn_sumi_fn = (__typeof__(attn_sumi_fn))(uintptr_t)f[1];
     attn_history_bias_fn = (__typeof__(attn_history_bias_fn))(uintptr_t)f[2];
     attn_sumi_bias_fn = (__typeof__(attn_sumi_bias_fn))(uintptr_t)f[3];
-    PyObject **const to[5] = {&config_type, &bias_type, &current_device, &raw_stream, &paged_type};
-    for (int i = 0; i < 5 && t[i]; ++i) {
+    PyObject **const to[6] = {&config_type, &bias_type, &current_device, &raw_stream, &paged_type, &paged8_type};
+    for (int i = 0; i < 6 && t[i]; ++i) {
         PyObject *was = *to[i];
         *to[i] = Py_NewRef(t[i]);
         Py_XDECREF(was);
@@ -237,6 +248,8 @@ static PyMethodDef methods[] = {
     {"attn_sumi_bias", (PyCFunction)(void (*)(void))attn_sumi_bias, METH_FASTCALL, NULL},
     {"attn_history_paged", (PyCFunction)(void (*)(void))attn_history_paged, METH_FASTCALL, NULL},
     {"attn_sumi_paged", (PyCFunction)(void (*)(void))attn_sumi_paged, METH_FASTCALL, NULL},
+    {"attn_history_paged8", (PyCFunction)(void (*)(void))attn_history_paged8, METH_FASTCALL, NULL},
+    {"attn_sumi_paged8", (PyCFunction)(void (*)(void))attn_sumi_paged8, METH_FASTCALL, NULL},
     {"paged_evict", (PyCFunction)(void (*)(void))paged_evict, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 

@@ -1,0 +1,22 @@
+// The paged history cache in 8 bits: what its kernels are given beside the arguments of a paged call (internal).
+#pragma once
+#include "paged.h"
+
+namespace climber {
+
+constexpr int kScaleBlock = 16, kLeastScale = 10;  // tokens of a scale; the least one, as stored: 2^(10 - 127)
+
+struct Paged8Args : PagedArgs {
+    uint8_t *k_scale, *v_scale;  // [n_pages][Hkv][page / 16]
+};
+
+// packed rows of a workgroup
+static inline int paged8_tile_rows(int d, int64_t rows) { return 32; }
+
+hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t s);
+// The call's new tokens into their pages, behind everything that reads these.
+hipError_t launch_paged8_store(const Paged8Args &a, hipStream_t s);
+// blocks of 16 tokens that a sequence's new tokens can touch
+static inline int64_t paged8_store_blocks(int64_t m_max) { return (m_max + 2 * kScaleBlock - 2) / kScaleBlock; }
+
+}  // namespace climber

@@ -100,8 +100,9 @@ static __device__ __forceinline__ void swap_pieces(u32x4 &x)
     }
 }
 
-// The softmax state of a wave's QB x 32 packed rows.
-template <int D, int QB>
+// The softmax state of a wave's QB x 32 packed rows.  WIDE: product s of the logits takes dimensions 32 (s / 2) + 16 hf + 8 (s % 2) of
+// half-wave hf, so that a lane reads 16 dimensions of a key at once (keys in 8 bits); otherwise 16 s + 8 hf.
+template <int D, int QB, bool WIDE = false>
 struct State {
     bf16x8 q[QB][D / 16];
     f32x16 O[QB][D / 32];
@@ -116,14 +117,16 @@ struct State {
     __device__ __forceinline__ void request(const PagedArgs &p, int qb, int64_t row, int h, int hk, int hf, Row &in)
     {
         const int sc = p.scen[row], bh = p.beh[row];
-        const u32x4 *qp = (const u32x4 *)(p.q + row * p.ld_q + (int64_t)h * (2 * D)) + hf;
+        const int to = WIDE ? 2 * hf : hf;
+        auto piece = [](int s) { return WIDE ? 4 * (s >> 1) + (s & 1) : 2 * s; };
+        const u32x4 *qp = (const u32x4 *)(p.q + row * p.ld_q + (int64_t)h * (2 * D)) + to;
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) q[qb][s] = __builtin_bit_cast(bf16x8, qp[2 * s]);
+        for (int s = 0; s < D / 16; ++s) q[qb][s] = __builtin_bit_cast(bf16x8, qp[piece(s)]);
         if (OWN) {
-            const u32x4 *kp = (const u32x4 *)(p.k + row * p.ld_kv + (int64_t)hk * (2 * D)) + hf, *vp = (const u32x4 *)(p.v + row * p.ld_kv + (int64_t)hk * (2 * D)) + hf;
+            const u32x4 *kp = (const u32x4 *)(p.k + row * p.ld_kv + (int64_t)hk * (2 * D)) + to, *vp = (const u32x4 *)(p.v + row * p.ld_kv + (int64_t)hk * (2 * D)) + hf;
 #pragma unroll
             for (int s = 0; s < D / 16; ++s) {
-                in.k[s] = kp[2 * s];
+                in.k[s] = kp[piece(s)];
                 in.v[s] = vp[2 * s];
             }
         }
@@ -305,6 +308,65 @@ static __device__ __forceinline__ void hide(f32x16 &S, int k, int hf, int top)
 #pragma unroll
     for (int i = 0; i < 16; ++i)
         if (k + 8 * (i >> 2) + 4 * hf + (i & 3) >= top) S[i] = -INFINITY;
+}
+
+// The four waves of a workgroup have had different keys of the same 32 packed rows: their denominators and outputs in units of the largest
+// reference, added up and stored.  room(j): 32 D floats of LDS for wave j (whose copies have arrived and been read).
+struct JoinRoom {
+    float ref[4][32], denom[4][32];
+};
+template <int D, bool WIDE, typename Room>
+static __device__ __forceinline__ void join_few(const PagedArgs &p, const PagedSeq &s, const PagedWork &w, const State<D, 1, WIDE> &st, JoinRoom &j4,
+                                                Room room, int64_t row, int h, int r_tile, int rows)
+{
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    auto &ref = j4.ref;
+    auto &denom = j4.denom;
+    const float l = st.l[0] + other_half(st.l[0]);
+    if (hf == 0) ref[wave][l32] = st.m[0], denom[wave][l32] = l;
+    __syncthreads();
+    const float m = fmaxf(fmaxf(ref[0][l32], ref[1][l32]), fmaxf(ref[2][l32], ref[3][l32]));
+    const float mine_w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f((st.m[0] - m) * st.c[0]);
+    float *joined = room(wave);
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : st.O[0][db][4 * g + e] * mine_w;
+            // (16-byte piece c of row r at slot c ^ r % 8: lanes of neighbouring rows write to different banks)
+            *(f32x4 *)(joined + l32 * D + (((8 * db + 2 * g + hf) ^ (l32 & 7)) * 4)) = x;
+        }
+    float total = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) total += denom[j][l32] == 0.f ? 0.f : denom[j][l32] * __builtin_amdgcn_exp2f((ref[j][l32] - m) * st.c[0]);
+    __syncthreads();
+    if (wave == 0 && hf == 0) denom[0][l32] = total;  // (read by all above, before the barrier)
+    __syncthreads();
+    if (wave == 0 && hf == 0 && r_tile + l32 < rows) {
+        const int64_t rh = row * p.H + h;
+        if (p.n_split > 1) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{m * st.c[0], total};
+        else if (p.lse) p.lse[rh] = float2{st.c[0], m * st.c[0] + __builtin_amdgcn_logf(total)};
+    }
+    constexpr int C = D / 4;
+    const int n_rows = min(32, rows - r_tile);
+    for (int i = threadIdx.x; i < n_rows * C; i += 256) {
+        const int rr = i / C, c = i % C, tt = (r_tile + rr) / p.G, hh = w.hk * p.G + (r_tile + rr) % p.G;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x += *(const f32x4 *)(room(j) + rr * D + ((c ^ (rr & 7)) * 4));
+        const int64_t rh = (s.row0 + tt) * p.H + hh;
+        if (p.n_split > 1) {
+            *(f32x4 *)(p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D + c * 4) = x;
+        } else {
+            const float inv = 1.f / denom[0][rr];
+            bf16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(x[e] * inv);
+            *(bf16x4 *)((__bf16 *)(p.o + (s.row0 + tt) * p.ld_o) + (int64_t)hh * D + c * 4) = y;
+        }
+    }
 }
 
 }  // namespace paged
