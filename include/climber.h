@@ -354,6 +354,62 @@ int climber_attn_sumi_paged8(const climber_config *cfg, const float *tau_layer, 
                              int32_t m_total, int32_t m_max, const int32_t *cand_scen, const int32_t *cand_beh, void *o_c,
                              int64_t ld_o, void *workspace, size_t ws_bytes, void *stream);
 
+/* ---- pages -------------------------------------------------------------------------------------
+ * Who holds which pages of a paged cache.  One pool of page numbers serves any number of caches of the same page_size (the layers of a
+ * stack): the three calls below change the page table, and climber_paged_copy / climber_paged8_copy then do what has to be done in each cache.
+ *   refs        dev int32 [n_pages]: how many entries of the table hold a page, and whatever else the caller counts (a prefix that is
+ *               to stay adds 1); 0: the page is free
+ *   page_table  dev int32 [n_seqs][table_ld], as a climber_paged_kv's
+ *   held        dev int32 [n_seqs]: pages that a sequence holds, its row's first entries
+ *   len         dev int32 [n_seqs]: its tokens, as a climber_paged_kv's: at most held * page_size
+ * Empty: all zeros.  page_size, and the limits of the sizes, as in climber_paged_kv; n_seqs * table_ld below 2^31, n_seqs below 2^24.
+ * Results do not depend on the order in which the device works.  Values are device memory and cannot be checked on the host: whatever
+ * they hold, nothing is read or written outside the arrays, and calls OR what they find into *status (dev int32, not cleared):
+ *   CLIMBER_BAD_PAGE  a page number that is held lies outside the pool (or, compact, is of a page with refs 0)
+ *   CLIMBER_BAD_SEQ   fork: a parent from n_seqs on (the row stays as it is)
+ *   CLIMBER_POOL_FULL extend: not enough free pages, or more than a row of the table has room for
+ * A workspace belongs to one call at a time, and so does a pool.  workspace: climber_pages_workspace_bytes(), 256-byte aligned.
+ * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _BUFSIZE, _RUNTIME. */
+#define CLIMBER_POOL_FULL 128
+#define CLIMBER_BAD_SEQ 256
+typedef struct climber_page_pool {
+    int32_t *refs, *page_table, *held, *len;
+    int32_t n_pages, page_size, n_seqs, table_ld;
+} climber_page_pool;
+
+size_t climber_pages_workspace_bytes(const climber_page_pool *pool); /* 0 on an invalid argument */
+
+/* All rows at once: sequence b becomes what sequence parent[b] was before the call, up to its first keep[b] tokens (parent, keep: dev int32
+ * [n_seqs]; keep NULL: all of them; below 0 counts as 0).  parent[b] = b and nothing cut: the row stays as it is, with the pages
+ * that it holds beyond its tokens.  parent[b] < 0: the sequence becomes empty.  Otherwise the pages that hold the tokens are shared
+ * (held: as many), what the row held before is given up, and entries of it that are held no more become -1.  Branches of a history, beams that take
+ * each other's place, a shared prefix, tokens taken back, users that leave are each one call. */
+int climber_pages_fork(const climber_page_pool *pool, const int32_t *parent, const int32_t *keep, int32_t *status, void *workspace,
+                       size_t ws_bytes, void *stream);
+
+/* Room for rows[b] more tokens of each sequence (dev int32 [n_seqs]; below 1: none), to be called before the append: then the pages of slots
+ * len[b] .. len[b] + rows[b] - 1 are held, and by nobody else.  Free pages are handed out in ascending order, to the sequences
+ * in ascending order: first in the places of shared pages that the new tokens go into, then for new ones.  A shared page that all who hold
+ * it write to in this call (as many sequences as its refs) stays with the last of them.  Where a page was replaced and holds tokens of
+ * the sequence, copies gets (page, its replacement, tokens).  A call that cannot be served whole (CLIMBER_POOL_FULL, CLIMBER_BAD_PAGE) changes nothing.
+ * copies: dev int32 [n_seqs][3]; counts: dev int32 [2]: how many of them there are (those behind stay as they are), and pages in use after the call.
+ * A page that was given up may be handed out again by the next extend: copy before it. */
+int climber_pages_extend(const climber_page_pool *pool, const int32_t *rows, int32_t *copies, int32_t *counts, int32_t *status,
+                         void *workspace, size_t ws_bytes, void *stream);
+
+/* Moves pages so that the pages in use are 0 .. counts[1] - 1: those behind go, in ascending order, to the free ones before.  Table and refs
+ * follow; copies (dev int32 [n_pages / 2][3]) gets (old number, new number, page_size) of each, counts[0] of them. */
+int climber_pages_compact(const climber_page_pool *pool, int32_t *copies, int32_t *counts, int32_t *status, void *workspace,
+                          size_t ws_bytes, void *stream);
+
+/* In a cache: the first copies[i][2] tokens of page copies[i][0] to page copies[i][1], i < min(counts[0], max_copies): keys, values, and
+ * mass, stamp and scales where there are any.  max_copies (host) sizes the launch.  No page may be both read and written, or written twice.
+ * Pages outside the pool are left out.  Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _TAU, _UNSUPPORTED, _RUNTIME. */
+int climber_paged_copy(const climber_config *cfg, const climber_paged_kv *kv, const int32_t *copies, const int32_t *counts,
+                       int32_t max_copies, void *stream);
+int climber_paged8_copy(const climber_config *cfg, const climber_paged_kv8 *kv8, const int32_t *copies, const int32_t *counts,
+                        int32_t max_copies, void *stream);
+
 /* ---- debug check of device-resident inputs -----------------------------------------------------
  * Eq. (3) divides a row's logits by tau[scen][beh]: the ids must lie inside the table and the entry
  * must be finite and > 0.  Ids, offsets and the table live in device memory, so the compute calls

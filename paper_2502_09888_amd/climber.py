@@ -66,6 +66,12 @@ class PagedKV8(C.Structure):
     _device = None  # as PagedKV's
 
 
+class PagePool(C.Structure):
+    """Mirror of ``climber_page_pool`` (device pointers).  Build with ``page_pool(...)``."""
+    _fields_ = [(n, C.c_void_p) for n in ("refs", "page_table", "held", "len")] + [(n, C.c_int32) for n in ("n_pages", "page_size", "n_seqs", "table_ld")]
+    _device = None  # as PagedKV's
+
+
 class _Weights(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("layers", C.POINTER(LayerWeights)), ("packed", C.c_void_p)]
 
@@ -158,6 +164,13 @@ def load_library():
     lib.climber_attn_history_paged8.argtypes = [cfgp, vp, pkv8, vp, i64, vp, vp, i64, vp, i32, i32, vp, vp, vp, vp, i64, vp, sz, vp]
     lib.climber_attn_sumi_paged8.restype = C.c_int
     lib.climber_attn_sumi_paged8.argtypes = [cfgp, vp, pkv8, vp, i64, vp, vp, i64, vp, i32, i32, vp, vp, vp, i64, vp, sz, vp]
+    pool = C.POINTER(PagePool)
+    lib.climber_pages_workspace_bytes.restype = sz
+    lib.climber_pages_workspace_bytes.argtypes = [pool]
+    for name, types in (("climber_pages_fork", [pool, vp, vp, vp, vp, sz, vp]), ("climber_pages_extend", [pool, vp, vp, vp, vp, vp, sz, vp]),
+                        ("climber_pages_compact", [pool, vp, vp, vp, vp, sz, vp]), ("climber_paged_copy", [cfgp, pkv, vp, vp, i32, vp]),
+                        ("climber_paged8_copy", [cfgp, pkv8, vp, vp, i32, vp])):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = C.c_int, types
     try:
         _load_native(lib)
     except ImportError:  # the host's calls do without; an attention call raises it
@@ -286,6 +299,7 @@ def climber_attn_sumi(cfg: Config, tau_layer, cache: KVCache, layer: int, q_c, k
 
 
 BAD_SCEN, BAD_BEH, BAD_TAU, BAD_OFFSETS, BAD_M_MAX, BAD_PAGE, BAD_LEN = 1, 2, 4, 8, 16, 32, 64
+POOL_FULL, BAD_SEQ = 128, 256
 
 
 def climber_check_inputs(cfg: Config, tau_layer, scen, beh, cache: Optional[KVCache], m_total: int,
@@ -598,3 +612,66 @@ def climber_attn_sumi_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q_c, k_c, v_
             _stream(stream))
     if code:
         raise ClimberError(code, "climber_attn_sumi_paged8")
+
+
+def page_pool(refs, page_table, held, len, page_size: int) -> PagePool:
+    """climber_page_pool from contiguous int32 device tensors: refs [n_pages], page_table [n_seqs, table_ld], held, len [n_seqs]."""
+    tensors = (refs, page_table, held, len)
+    if any(not t.is_contiguous() or str(t.dtype) != "torch.int32" for t in tensors):
+        raise ValueError("refs, page_table, held and len are contiguous tensors of int32")
+    n_seqs, table_ld = page_table.shape
+    if held.numel() != n_seqs or len.numel() != n_seqs:
+        raise ValueError("page_table, held and len are not of one pool")
+    if any(t.device != refs.device for t in tensors):
+        raise ValueError("refs, page_table, held and len are not on one device")
+    pool = PagePool(*(_ptr(t) for t in tensors), refs.numel(), page_size, n_seqs, table_ld)
+    pool._keep = tensors
+    if refs.is_cuda:
+        pool._device = refs.device.index
+    elif not all(t.is_pinned() for t in tensors):
+        pool._device = -1
+    return pool
+
+
+def climber_pages_workspace_bytes(pool: PagePool) -> int:
+    return int(load_library().climber_pages_workspace_bytes(C.byref(pool)))
+
+
+def _copies(t, least: int) -> Optional[int]:
+    if t is not None and not isinstance(t, int) and (t.numel() < 3 * least or not t.is_contiguous()):
+        raise ValueError(f"copies needs room for {least} of three numbers")
+    return _ptr(t)
+
+
+def climber_pages_fork(pool: PagePool, parent, keep, status, workspace, stream=None) -> None:
+    """Sequence b becomes what sequence parent[b] was (below 0: empty), up to its first keep[b] tokens; pages are shared."""
+    _on_device(pool, stream)
+    _ok(load_library().climber_pages_fork(C.byref(pool), _ptr(parent), _ptr(keep), _ptr(status), _ptr(workspace), _nbytes(workspace), _stream(stream)),
+        "climber_pages_fork")
+
+
+def climber_pages_extend(pool: PagePool, rows, copies, counts, status, workspace, stream=None) -> None:
+    """Pages for rows[b] more tokens of each sequence; shared pages that they go into are replaced, and copies says by which."""
+    _on_device(pool, stream)
+    _ok(load_library().climber_pages_extend(C.byref(pool), _ptr(rows), _copies(copies, pool.n_seqs), _ptr(counts), _ptr(status), _ptr(workspace),
+                                            _nbytes(workspace), _stream(stream)), "climber_pages_extend")
+
+
+def climber_pages_compact(pool: PagePool, copies, counts, status, workspace, stream=None) -> None:
+    """The pages in use move to the front of the pool; copies says which went where."""
+    _on_device(pool, stream)
+    _ok(load_library().climber_pages_compact(C.byref(pool), _copies(copies, pool.n_pages // 2), _ptr(counts), _ptr(status), _ptr(workspace),
+                                             _nbytes(workspace), _stream(stream)), "climber_pages_compact")
+
+
+def climber_paged_copy(cfg: Config, kv: PagedKV, copies, counts, max_copies: int, stream=None) -> None:
+    """What climber_pages_extend or climber_pages_compact has left to copy, in one paged cache."""
+    _on_device(kv, stream)
+    _ok(load_library().climber_paged_copy(C.byref(cfg), C.byref(kv), _copies(copies, 0), _ptr(counts), max_copies, _stream(stream)), "climber_paged_copy")
+
+
+def climber_paged8_copy(cfg: Config, kv8: PagedKV8, copies, counts, max_copies: int, stream=None) -> None:
+    """climber_paged_copy in a cache in 8 bits."""
+    _on_device(kv8, stream)
+    _ok(load_library().climber_paged8_copy(C.byref(cfg), C.byref(kv8), _copies(copies, 0), _ptr(counts), max_copies, _stream(stream)),
+        "climber_paged8_copy")

@@ -8,14 +8,6 @@ using namespace climber::paged_host;
 
 namespace {
 
-int check_sizes8(const climber_config *cfg, const climber_paged_kv8 *kv8)
-{
-    if (!cfg || !kv8) return CLIMBER_ERR_NULL;
-    const int e = check_sizes(cfg, &kv8->kv, 1);
-    if (e) return e;
-    return cfg->dtype != CLIMBER_BF16 || kv8->kv.mass ? CLIMBER_ERR_UNSUPPORTED : CLIMBER_OK;
-}
-
 int attn_paged8(const Call &c, const climber_paged_kv8 *kv8, void *workspace, size_t ws_bytes, void *stream)
 {
     const climber_config *cfg = c.cfg;

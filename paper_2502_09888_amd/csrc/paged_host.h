@@ -38,6 +38,14 @@ static inline int check_sizes(const climber_config *cfg, const climber_paged_kv 
     return CLIMBER_OK;
 }
 
+static inline int check_sizes8(const climber_config *cfg, const climber_paged_kv8 *kv8)
+{
+    if (!cfg || !kv8) return CLIMBER_ERR_NULL;
+    const int e = check_sizes(cfg, &kv8->kv, 1);
+    if (e) return e;
+    return cfg->dtype != CLIMBER_BF16 || kv8->kv.mass ? CLIMBER_ERR_UNSUPPORTED : CLIMBER_OK;
+}
+
 static inline int check_rows(const climber_config *cfg, int32_t m_total, int32_t m_max)
 {
     if (m_total < 0 || m_max < 0 || m_max > m_total || (m_total > 0 && m_max == 0)) return CLIMBER_ERR_SHAPE;
