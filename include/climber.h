@@ -410,6 +410,41 @@ int climber_paged_copy(const climber_config *cfg, const climber_paged_kv *kv, co
 int climber_paged8_copy(const climber_config *cfg, const climber_paged_kv8 *kv8, const int32_t *copies, const int32_t *counts,
                         int32_t max_copies, void *stream);
 
+/* ---- rotary positions ---------------------------------------------------------------------------
+ * Query and key rows are turned by their positions before they are appended or scored: the products of a query and a key, and with them
+ * the logits of Eq. (3), then depend on the distance of the two.  Pair i of a head's first rot_dims elements, (a, b), becomes
+ *     scale * (a cos t - b sin t, a sin t + b cos t),  t = pos * freq[i]
+ * b: the element behind a (interleaved != 0), or rot_dims / 2 behind it.  Elements from rot_dims on stay as they are.  inverse != 0 turns the other way: with
+ * rows of gradients this is the gradient of the call.  Angles are made in 64 bits, products and sums in 32, rounded once.
+ *   freq  dev fp64 [rot_dims / 2], radians per position; climber_rotary_frequencies makes them on the host. */
+typedef struct climber_rotary_plan {
+    const double *freq;
+    int32_t rot_dims, interleaved, inverse;
+    float scale;
+} climber_rotary_plan;
+
+/* freq[i] (host, rot_dims / 2 of them) = base^(-2 i / rot_dims), for contexts longer than those that a model was made for by a factor:
+ *   CLIMBER_ROTARY_LINEAR  divided by factor
+ *   CLIMBER_ROTARY_BASE    with base * factor^(rot_dims / (rot_dims - 2)): the slowest pair is divided by factor, the fastest stays
+ *   CLIMBER_ROTARY_PARTS   with r = made_for * freq / (2 pi) turns within the length made_for (arXiv 2309.00071, Sec. 3.2): pairs of at least `fast`
+ *                          turns stay, those of at most `slow` are divided by factor, and between them linearly in r; *scale = 0.1 ln(factor) + 1
+ * *scale is 1 otherwise.  What a kind does not use is not looked at.  Errors: CLIMBER_ERR_NULL, _SHAPE, _RANGE, _UNSUPPORTED (kind). */
+#define CLIMBER_ROTARY_PLAIN 0
+#define CLIMBER_ROTARY_LINEAR 1
+#define CLIMBER_ROTARY_BASE 2
+#define CLIMBER_ROTARY_PARTS 3
+int climber_rotary_frequencies(int32_t rot_dims, double base, int32_t kind, double factor, double made_for, double fast,
+                               double slow, double *freq, float *scale);
+
+/* q [m][ld_q] of cfg->n_heads * d_head, k [m][ld_k] of n_kv_heads * d_head (n_kv_heads 0: no k), elements of the config's dtype; pos: dev int32 [m].
+ * Row pitches are free, and so is the alignment; rows of whole 16 bytes are faster.  q_out, k_out: of the same widths; q_out may be q
+ * with the same pitch (turned in place), and k_out k; otherwise what is written must not share an element with anything else.  Uses d_model,
+ * n_heads, d_head and dtype of cfg; any d_head, rot_dims even, 2 .. min(d_head, 512).
+ * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _UNSUPPORTED, _RUNTIME. */
+int climber_rotary(const climber_config *cfg, const climber_rotary_plan *rot, const int32_t *pos, int64_t m, int32_t n_kv_heads,
+                   const void *q, int64_t ld_q, const void *k, int64_t ld_k, void *q_out, int64_t ld_qo, void *k_out, int64_t ld_ko,
+                   void *stream);
+
 /* ---- debug check of device-resident inputs -----------------------------------------------------
  * Eq. (3) divides a row's logits by tau[scen][beh]: the ids must lie inside the table and the entry
  * must be finite and > 0.  Ids, offsets and the table live in device memory, so the compute calls

@@ -13,6 +13,7 @@ from .climber import (BAD_BEH, BAD_LEN, BAD_M_MAX, BAD_OFFSETS, BAD_PAGE, BAD_SC
                       PagedKV8, paged_kv8, climber_attn_history_paged8, climber_attn_sumi_paged8, climber_paged8_workspace_bytes,
                       PagePool, page_pool, climber_pages_workspace_bytes, climber_pages_fork, climber_pages_extend, climber_pages_compact,
                       climber_paged_copy, climber_paged8_copy,
+                      ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS, RotaryPlan, rotary, climber_rotary, climber_rotary_frequencies,
                       climber_strerror, climber_sumi_forward, climber_sumi_score, climber_sumi_score_static, climber_workspace_bytes, library_path,
                       load_library)
 

@@ -72,6 +72,12 @@ class PagePool(C.Structure):
     _device = None  # as PagedKV's
 
 
+class RotaryPlan(C.Structure):
+    """Mirror of ``climber_rotary_plan`` (device pointer).  Build with ``rotary(...)``."""
+    _fields_ = [("freq", C.c_void_p)] + [(n, C.c_int32) for n in ("rot_dims", "interleaved", "inverse")] + [("scale", C.c_float)]
+    _device = None  # as PagedKV's
+
+
 class _Weights(C.Structure):
     _fields_ = [("n_layers", C.c_int32), ("layers", C.POINTER(LayerWeights)), ("packed", C.c_void_p)]
 
@@ -171,6 +177,11 @@ def load_library():
                         ("climber_pages_compact", [pool, vp, vp, vp, vp, sz, vp]), ("climber_paged_copy", [cfgp, pkv, vp, vp, i32, vp]),
                         ("climber_paged8_copy", [cfgp, pkv8, vp, vp, i32, vp])):
         getattr(lib, name).restype, getattr(lib, name).argtypes = C.c_int, types
+    f64 = C.c_double
+    lib.climber_rotary_frequencies.restype = C.c_int
+    lib.climber_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, C.POINTER(f64), C.POINTER(C.c_float)]
+    lib.climber_rotary.restype = C.c_int
+    lib.climber_rotary.argtypes = [cfgp, C.POINTER(RotaryPlan), vp, i64, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
     try:
         _load_native(lib)
     except ImportError:  # the host's calls do without; an attention call raises it
@@ -675,3 +686,40 @@ def climber_paged8_copy(cfg: Config, kv8: PagedKV8, copies, counts, max_copies: 
     _on_device(kv8, stream)
     _ok(load_library().climber_paged8_copy(C.byref(cfg), C.byref(kv8), _copies(copies, 0), _ptr(counts), max_copies, _stream(stream)),
         "climber_paged8_copy")
+
+
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
+
+
+def climber_rotary_frequencies(rot_dims: int, base: float = 10000.0, kind: int = ROTARY_PLAIN, factor: float = 1.0, made_for: float = 0.0,
+                               fast: float = 32.0, slow: float = 1.0):
+    """(radians per position of each pair, what turned values are multiplied by)."""
+    freq, scale = (C.c_double * max(1, rot_dims // 2))(), C.c_float()
+    _ok(load_library().climber_rotary_frequencies(rot_dims, base, kind, factor, made_for, fast, slow, freq, C.byref(scale)),
+        "climber_rotary_frequencies")
+    return list(freq), scale.value
+
+
+def rotary(freq, rot_dims: int, interleaved: bool = False, scale: float = 1.0, inverse: bool = False) -> RotaryPlan:
+    """climber_rotary_plan from a float64 device tensor of rot_dims / 2 frequencies."""
+    if str(freq.dtype) != "torch.float64" or not freq.is_contiguous() or freq.numel() != rot_dims // 2:
+        raise ValueError("freq is a contiguous float64 tensor of rot_dims / 2 elements")
+    plan = RotaryPlan(_ptr(freq), rot_dims, int(interleaved), int(inverse), scale)
+    plan._keep = freq
+    plan._device = freq.device.index if freq.is_cuda else None if freq.is_pinned() else -1
+    return plan
+
+
+def climber_rotary(cfg: Config, rot: RotaryPlan, pos, n_kv_heads: int, q, k, q_out, k_out, stream=None) -> None:
+    """Turn q and k rows by their positions (row r is [r] of the tensors, as many rows as q has; row pitches are taken from them)."""
+    _on_device(rot, stream)
+    m, d, dk = q.shape[0], cfg.d_model, n_kv_heads * cfg.d_head
+    for t, wide in ((q, d), (q_out, d)) + (((k, dk), (k_out, dk)) if n_kv_heads else ()):
+        if t.shape[0] != m or t.numel() != m * wide:
+            raise ValueError("q, k, q_out and k_out have other rows")
+        if str(t.dtype) != ("torch.float32" if cfg.dtype == F32 else "torch.bfloat16"):
+            raise ValueError("q, k, q_out and k_out are of the configuration's type")
+    if str(pos.dtype) != "torch.int32" or not pos.is_contiguous() or pos.numel() != m:
+        raise ValueError("pos is a contiguous int32 tensor with a position for each row")
+    _ok(load_library().climber_rotary(C.byref(cfg), C.byref(rot), _ptr(pos), m, n_kv_heads, _ptr(q), _pitch(q, d), _ptr(k), _pitch(k, dk), _ptr(q_out),
+                                      _pitch(q_out, d), _ptr(k_out), _pitch(k_out, dk), _stream(stream)), "climber_rotary")
