@@ -137,6 +137,334 @@ static __device__ __forceinline__ KFrags<D> read_k_wide(const lds_u8 *base, int 
     return f;
 }
 
+// ---- tiles ---------------------------------------------------------------------------------------
+// 4 waves of QB x 32 packed rows share the keys.  Cached blocks of 32 keys: each wave brings 8 keys and their values as codes, by copies that are
+// four to five blocks ahead, into a place that only it reads; two blocks ahead it makes bf16 rows of its keys, one block ahead of its values, in
+// buffers that all waves take their fragments from.  The codes are widened once for 128 or 256 rows that way.  The call's own rows
+// follow as in the bf16 paged cache, in the same LDS.
+template <int D, int QB, bool SUMI>
+__global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Args p)
+{
+    using R = Rows<D>;
+    constexpr int kRows = 128 * QB, kValues = 32 * R::kPitch;
+    constexpr int kShare = 8 * R::kPitch, kCopies = kShare / 1024;  // own rows: a wave's part of either; copies of it
+    constexpr int kCopies8 = D / 64, kSlot = 16 * D;                // codes: copies of a wave's part of a block, keys and values; their bytes
+    // (arrays of their own: reads of one do not wait for copies into another.)  Codes in 0 .. 3, keys in 4 and 5, values in 6 and 7; own rows: keys
+    // and values of stage i in 2 i and 2 i + 1.
+    __shared__ __attribute__((aligned(1024))) uint8_t a0[kValues], a1[kValues], a2[kValues], a3[kValues], a4[kValues], a5[kValues], a6[kValues], a7[kValues];
+    __shared__ int flags[4];
+    auto room = [&](int i) __attribute__((always_inline)) {
+        return (lds_u8 *)(i == 0 ? a0 : i == 1 ? a1 : i == 2 ? a2 : i == 3 ? a3 : i == 4 ? a4 : i == 5 ? a5 : i == 6 ? a6 : a7);
+    };
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
+    const int rows = s.T * p.G, r_tile = w.tile * kRows;
+    if (r_tile >= rows) return;
+    const int r_wave = r_tile + wave * 32 * QB;
+    const bool causal = !SUMI && p.causal;
+    const int k_all = SUMI ? s.n : paged_keys(p, s);
+    auto sees = [&](int r) { return causal ? min(s.n + min(r, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row r sees keys below it
+    int k_lo, k_hi;
+    paged_part(p, w.split, sees(r_tile + kRows - 1), 32, k_lo, k_hi);
+    k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+    // cached keys: all rows see them
+    const int c_lo = min(k_lo, s.n), c_hi = min(k_hi, s.n), n_blocks = (c_hi - c_lo + 31) / 32, n_whole = (c_hi - c_lo) / 32;
+
+    const int k_mine = c_lo + (wave >> 1) * 16;  // this wave's group of 16 keys of block 0
+    const Source8<D> src(p, w.b, w.hk, c_hi, lane);
+    // page numbers and scales of 64 of the wave's groups, one in each lane, and of the 64 after them
+    const int first_pages = src.page_number(k_mine + lane * 32), next_pages = src.page_number(k_mine + (64 + lane) * 32);
+    const uint32_t first_scales = src.scales(k_mine + lane * 32, first_pages);
+    int pages = first_pages, pages_next = next_pages;
+    uint32_t scales = first_scales, scales_next = first_scales, held = 0;
+    // this lane's 16 codes of the wave's 8 keys, or (D = 64, upper half) of their values: from its place in a page, in LDS, as 32 bytes of a row
+    const int part = D == 64 ? lane & 31 : lane, row8 = part / (D / 16), piece = part % (D / 16);
+    const uint32_t page_off = ((wave & 1) * 8 + row8) * D + piece * 16;
+    const int row32 = (wave >> 1) * 16 + (wave & 1) * 8 + row8, to_row = row32 * R::kPitch;
+    // (a row's two pieces: rows of odd numbers write theirs the other way round, which takes 16 lanes to 16 places of the banks)
+    const int swap = row32 & 1, to_a = to_row + ((2 * piece + swap) ^ R::f(row32)) * 16, to_b = to_row + ((2 * piece + 1 - swap) ^ R::f(row32)) * 16;
+    auto issue = [&](int j, lds_u8 *slot) __attribute__((always_inline)) {
+        if ((j & 63) == 0 && j > 0) {
+            pages = pages_next;
+            pages_next = src.page_number(k_mine + (j + 64 + lane) * 32);
+        }
+        const int page = __builtin_amdgcn_readlane(pages, j & 63), g = k_mine + j * 32;
+        const uint8_t *k = uniform(src.k_page + page * src.page_bytes + (g & ((1 << p.page_shift) - 1)) * D);
+        if constexpr (D == 64) {
+            copy16((glb_u8 *)(k + (lane >= 32 ? src.to_v : 0)) + page_off, slot + wave * kSlot);
+        } else {
+            copy16((glb_u8 *)k + page_off, slot + wave * kSlot);
+            copy16((glb_u8 *)uniform(k + src.to_v) + page_off, slot + wave * kSlot + 1024);
+        }
+    };
+    // the scales of block j's group: to be asked for once for each block, in order
+    auto scales_of = [&](int j) __attribute__((always_inline)) {
+        if ((j & 63) == 0 && j > 0) scales = scales_next;
+        if ((j & 63) == 32) scales_next = src.scales(k_mine + ((j & ~63) + 64 + lane) * 32, pages_next);
+        return (uint32_t)__builtin_amdgcn_readlane(scales, j & 63);
+    };
+    auto codes_at = [&](lds_u8 *slot, int value) __attribute__((always_inline)) {
+        return *(const __attribute__((address_space(3))) u32x4 *)(slot + wave * kSlot + (D == 64 ? 0 : value * 1024) + lane * 16);
+    };
+    auto widen = [&](u32x4 x, float scale, lds_u8 *to) __attribute__((always_inline)) {
+        const u32x2 first = swap ? u32x2{x.z, x.w} : u32x2{x.x, x.y}, second = swap ? u32x2{x.x, x.y} : u32x2{x.z, x.w};
+        *(__attribute__((address_space(3))) u32x4 *)(to + to_a) = wide8(first, scale);
+        *(__attribute__((address_space(3))) u32x4 *)(to + to_b) = wide8(second, scale);
+    };
+    // keys of block j (slot kj) and values of the one before it (slot kv; of the same block: kj == kv in `whole_block`)
+    auto widen_keys = [&](lds_u8 *slot, uint32_t sc, lds_u8 *to) __attribute__((always_inline)) {
+        if (D == 128 || hf == 0) widen(codes_at(slot, 0), scale_of(sc), to);
+    };
+    auto widen_values = [&](lds_u8 *slot, uint32_t sc, lds_u8 *to) __attribute__((always_inline)) {
+        if (D == 128 || hf == 1) widen(codes_at(slot, 1), scale_of(sc >> 8), to);
+    };
+
+    Rows<D> at;
+    at.init(lane);
+    State<D, QB> st;
+    auto start = [&]() __attribute__((always_inline)) {
+        typename State<D, QB>::Row in[QB];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            const int r = min(r_wave + qb * 32 + l32, rows - 1);
+            st.template request<SUMI>(p, qb, s.row0 + r / p.G, w.hk * p.G + r % p.G, w.hk, hf, in[qb]);
+        }
+        if (n_blocks > 0) issue(0, room(0));
+        if (n_blocks > 1) issue(1, room(1));
+        if (n_blocks > 2) issue(2, room(2));
+        if (n_blocks > 3) issue(3, room(3));
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) st.template start<SUMI>(p, qb, hf, in[qb], w.split == 0);
+    };
+    // this wave's copies have landed but for those of `later` blocks, the last ones issued
+    auto landed8 = [&](int later) __attribute__((always_inline)) {
+        if (later >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * kCopies8) : "memory");
+        else if (later == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies8) : "memory");
+        else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies8) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    auto landed = [&](int later) __attribute__((always_inline)) {
+        if (later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * kCopies) : "memory");
+        else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    };
+    // (with this wave's reads and writes of LDS done: behind the barrier others write to what it has read, and read what it has written)
+    auto meet = [&]() __attribute__((always_inline)) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    // own rows, counted from the sequence's first: [n_lo, n_hi), of which all rows of the tile see the first n_clean blocks whole
+    int n_lo = 0, n_hi = 0, n_new = 0, n_clean = 0, top[QB], wave_hi = 0;
+    PagedSeq own = s;
+    own.n = 0;
+    if constexpr (!SUMI) {
+        n_lo = max(k_lo - s.n, 0), n_hi = max(k_hi - s.n, 0);
+        n_new = (n_hi - n_lo + 31) / 32;
+        n_clean = __builtin_amdgcn_readfirstlane(max(0, min(sees(r_tile) - s.n, n_hi) - n_lo) / 32);
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) top[qb] = min(sees(r_wave + qb * 32 + l32) - s.n, n_hi);
+        wave_hi = min(sees(r_wave + 32 * QB - 1) - s.n, n_hi);
+    }
+    bool odd = false, far[QB];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) far[qb] = false;
+    auto is_far = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) far[qb] |= !(st.l[qb] + other_half(st.l[qb]) < kFar);
+    };
+
+#pragma unroll 1
+    for (bool again = false;; again = true) {
+        start();
+        if (!again && n_whole > 0) {
+            f32x16 S0[QB], S1[QB];
+            bf16x8 P[QB][2];
+            landed8(n_whole > 1 ? min(n_blocks - 2, 2) : min(n_blocks - 1, 3));
+            held = scales_of(0);
+            widen_keys(room(0), held, room(4));
+            widen_values(room(0), held, room(6));
+            if (n_whole > 1) {
+                held = scales_of(1);
+                widen_keys(room(1), held, room(5));
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (n_blocks > 4) issue(4, room(0));
+            meet();
+            st.logits(read_k<D>(at, room(4)), S0);
+            st.reference(S0);
+            // block j (i = j % 4): its logits in Sc; behind the barrier the keys of block j + 1 and its own values are there, nobody reads the keys of
+            // block j or the values of block j - 1 any more, and their places are filled
+            auto step = [&](int j, int i, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
+                landed8(min(2, n_blocks - 3 - j));
+                meet();
+                const KFrags<D> k = read_k<D>(at, room(4 + ((i + 1) & 1)));
+                __builtin_amdgcn_sched_barrier(0);
+                st.weights(Sc, P, 0);
+                __builtin_amdgcn_sched_barrier(0);
+                st.logits(k, Sn);  // (behind the last block: not used)
+                st.weights(Sc, P, 1);
+                const VFrags<D> v0 = read_v<D>(at, room(6 + (i & 1))), v1 = read_v<D>(at, room(6 + (i & 1)) + 16 * R::kPitch);
+                if (j + 1 < n_whole) {
+                    widen_values(room((i + 1) & 3), held, room(6 + ((i + 1) & 1)));
+                    if (j + 2 < n_whole) {
+                        held = scales_of(j + 2);
+                        widen_keys(room((i + 2) & 3), held, room(4 + (i & 1)));
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0x40f);
+                st.add(v0, P, 0);
+                st.add(v1, P, 1);
+                if (j + 5 < n_blocks) {
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    issue(j + 5, room((i + 1) & 3));
+                }
+            };
+            for (int j = 0; j < n_whole;) {
+                step(j, 0, S0, S1);
+                if (++j == n_whole) break;
+                step(j, 1, S1, S0);
+                if (++j == n_whole) break;
+                step(j, 2, S0, S1);
+                if (++j == n_whole) break;
+                step(j, 3, S1, S0);
+                ++j;
+            }
+            // (now, and at the end: in the blocks to come the reference may move by more than 2^126, which makes zeros of the sums so far)
+            is_far();
+        }
+        // the block that is not whole, and all of them again
+#pragma unroll 1
+        for (int j = again ? 0 : n_whole; j < n_blocks; ++j) {
+            landed8(again || n_whole == 0 ? min(3, n_blocks - 1 - j) : 0);
+            const uint32_t sc = scales_of(j);
+            lds_u8 *const keys = room(4 + (j & 1)), *const values = room(6 + (j & 1)), *const slot = room(j & 3);
+            const bool here = c_lo + j * 32 + row32 < c_hi;  // (codes behind the cached keys may be no numbers)
+            const u32x4 none = {0, 0, 0, 0};
+            if (D == 128 || hf == 0) widen(here ? codes_at(slot, 0) : none, scale_of(sc), keys);
+            if (D == 128 || hf == 1) widen(here ? codes_at(slot, 1) : none, scale_of(sc >> 8), values);
+            meet();
+            if (again && j + 4 < n_blocks) issue(j + 4, slot);
+            f32x16 S[QB];
+            bf16x8 P[QB][2];
+            bool may[QB];
+            st.logits(read_k<D>(at, keys), S);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+                hide(S[qb], c_lo + j * 32, hf, c_hi);
+                may[qb] = j >= n_whole || j == 0 || far[qb];
+            }
+            st.reference(S, may);
+            st.weights(S, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, values + g * 16 * R::kPitch), P, g);
+        }
+        if constexpr (!SUMI) {
+            const Source<D, kCopies> rows_src(p, own, w.b, w.hk, n_hi, lane, (wave & 1) * kCopies);
+            auto issue_new = [&](int j) __attribute__((always_inline)) {
+                rows_src.issue(n_lo + (wave >> 1) * 16 + j * 32, 0, room(2 * (j & 3)) + wave * kShare, room(2 * (j & 3) + 1) + wave * kShare);
+            };
+            if (n_new > 0) {
+                meet();  // (all are done with the cached blocks' places)
+                issue_new(0);
+                if (n_new > 1) issue_new(1);
+                if (n_new > 2) issue_new(2);
+            }
+            if (!again && n_clean > 0) {
+                f32x16 S0[QB], S1[QB];
+                bf16x8 P[QB][2];
+                landed(min(n_new - 1, 2));
+                meet();
+                st.logits(read_k<D>(at, room(0)), S0);
+                st.reference(S0);
+                auto step = [&](int j, int i, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
+                    landed(min(1, n_new - 2 - j));
+                    meet();  // block j + 1 is here, and nobody reads block j - 1 any more
+                    if (j + 3 < n_new)
+                        rows_src.issue(n_lo + (wave >> 1) * 16 + (j + 3) * 32, 0, room(2 * ((i + 3) & 3)) + wave * kShare, room(2 * ((i + 3) & 3) + 1) + wave * kShare);
+                    const KFrags<D> k = read_k<D>(at, room(2 * ((i + 1) & 3)));
+                    __builtin_amdgcn_sched_barrier(0);
+                    st.weights(Sc, P, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    st.logits(k, Sn);  // (behind the last block: not used)
+                    st.weights(Sc, P, 1);
+                    const VFrags<D> v0 = read_v<D>(at, room(2 * i + 1)), v1 = read_v<D>(at, room(2 * i + 1) + 16 * R::kPitch);
+                    __builtin_amdgcn_sched_barrier(0x40f);
+                    st.add(v0, P, 0);
+                    st.add(v1, P, 1);
+                };
+                for (int j = 0; j < n_clean;) {
+                    step(j, 0, S0, S1);
+                    if (++j == n_clean) break;
+                    step(j, 1, S1, S0);
+                    if (++j == n_clean) break;
+                    step(j, 2, S0, S1);
+                    if (++j == n_clean) break;
+                    step(j, 3, S1, S0);
+                    ++j;
+                }
+                is_far();
+            }
+            // blocks that not every row sees whole
+#pragma unroll 1
+            for (int j = again ? 0 : n_clean; j < n_new; ++j) {
+                lds_u8 *const keys = room(2 * (j & 3)), *const values = room(2 * (j & 3) + 1);
+                landed(min(2, n_new - 1 - j));
+                if (j >= n_clean) odd |= clear_odd<kShare>(values + wave * kShare, lane);
+                meet();
+                if (j + 3 < n_new) issue_new(j + 3);
+                const int k0 = n_lo + j * 32;
+                if (k0 >= wave_hi) continue;
+                f32x16 S[QB];
+                bf16x8 P[QB][2];
+                bool may[QB];
+                st.logits(read_k<D>(at, keys), S);
+#pragma unroll
+                for (int qb = 0; qb < QB; ++qb) {
+                    hide(S[qb], k0, hf, top[qb]);
+                    may[qb] = j >= n_clean || j == 0 || far[qb];
+                }
+                st.reference(S, may);
+                st.weights(S, P);
+#pragma unroll
+                for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, values + g * 16 * R::kPitch), P, g);
+            }
+        }
+        if (again || n_whole + n_clean == 0) break;
+        // Weights far above the reference of the first block (or sums with them that passed the largest number): all of it again, block by
+        // block.  The reference of the rows that have them may move then; the others' results are made in the same way again, and do not
+        // depend on their neighbours.
+        bool some = false;
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) {
+            float nothing = 0.f;  // unless an output is no finite number
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) nothing = fmaf(st.O[qb][db][i], 0.f, nothing);
+            far[qb] |= !(st.l[qb] + other_half(st.l[qb]) < kFar) || !(nothing + other_half(nothing) == 0.f);
+            some |= far[qb];
+        }
+        const int wave_far = __builtin_amdgcn_ballot_w64(some) != 0;
+        if (lane == 0) flags[wave] = wave_far;
+        __syncthreads();
+        const bool any = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+        __syncthreads();
+        if (__builtin_expect(!any, 1)) break;
+        pages = first_pages, pages_next = next_pages, scales = first_scales;
+        odd = false;
+    }
+    store_tile<D, QB>(p, s, w, st, r_wave, rows);
+    if constexpr (!SUMI) {
+        if (lane == 0) flags[wave] = odd;
+        __syncthreads();
+        if (__builtin_expect(flags[0] | flags[1] | flags[2] | flags[3], 0))
+            put_odd<D>(p, s, w, s.n + n_lo + n_clean * 32, k_hi, r_wave, min(r_wave + 32 * QB, rows), sees);
+    }
+}
+
 // ---- few rows ------------------------------------------------------------------------------------
 // 32 packed rows; the waves of a workgroup take different blocks of 32 keys, each through a ring of its own, and are joined at the end.
 template <int D, bool SUMI>
@@ -362,8 +690,12 @@ template <int D, bool SUMI>
 hipError_t launch(Paged8Args p, hipStream_t s)
 {
     const int64_t rows = (int64_t)p.m_max * p.G;
-    p.n_tiles = (int)((rows + 31) / 32);
-    hipLaunchKernelGGL((attn_paged8_few_kernel<D, SUMI>), dim3(paged_grid(p)), dim3(256), 0, s, p);
+    const int tile = paged8_tile_rows(D, rows);
+    void (*kernel)(Paged8Args) = tile == 32 ? attn_paged8_few_kernel<D, SUMI> : attn_paged8_tile_kernel<D, 1, SUMI>;
+    if constexpr (D == 64)
+        if (tile == 256) kernel = attn_paged8_tile_kernel<D, 2, SUMI>;
+    p.n_tiles = (int)((rows + tile - 1) / tile);
+    hipLaunchKernelGGL(kernel, dim3(paged_grid(p)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

@@ -220,38 +220,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         if constexpr (D == 64) start();
     }
 
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int r = r_wave + qb * 32 + l32;
-        const float l = st.l[qb] + other_half(st.l[qb]);
-        const int64_t row = s.row0 + r / p.G, rh = row * p.H + w.hk * p.G + r % p.G;  // (r >= rows: not stored)
-        if (p.n_split > 1) {
-            if (r >= rows) continue;
-            float *po = p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D + 4 * hf;
-#pragma unroll
-            for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    *(f32x4 *)(po + 32 * db + 8 * g) =
-                        f32x4{st.O[qb][db][4 * g], st.O[qb][db][4 * g + 1], st.O[qb][db][4 * g + 2], st.O[qb][db][4 * g + 3]};
-            if (hf == 0) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{st.m[qb] * st.c[qb], l};
-            continue;
-        }
-        const float inv = 1.f / l;
-        __bf16 *op = (__bf16 *)(p.o + row * p.ld_o) + (int64_t)(w.hk * p.G + r % p.G) * D + 8 * hf;
-#pragma unroll
-        for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-            for (int g = 0; g < 4; g += 2) {
-                bf16x8 x;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = (__bf16)(st.O[qb][db][4 * g + e] * inv);
-                u32x4 y = __builtin_bit_cast(u32x4, x);
-                swap_pieces(y);
-                if (r < rows) *(u32x4 *)(op + 32 * db + 8 * g) = y;
-            }
-        if (hf == 0 && p.lse && r < rows) p.lse[rh] = float2{st.c[qb], st.m[qb] * st.c[qb] + __builtin_amdgcn_logf(l)};
-    }
+    store_tile<D, QB>(p, s, w, st, r_wave, rows);
     if (lane == 0) flags[wave] = odd;
     __syncthreads();
     if (__builtin_expect(flags[0] | flags[1] | flags[2] | flags[3], 0))

@@ -11,7 +11,7 @@ struct Paged8Args : PagedArgs {
 };
 
 // packed rows of a workgroup
-static inline int paged8_tile_rows(int d, int64_t rows) { return 32; }
+static inline int paged8_tile_rows(int d, int64_t rows) { return rows <= 32 ? 32 : d == 64 && rows > 128 ? 256 : 128; }
 
 hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t s);
 // The call's new tokens into their pages, behind everything that reads these.

@@ -310,6 +310,45 @@ static __device__ __forceinline__ void hide(f32x16 &S, int k, int hf, int top)
         if (k + 8 * (i >> 2) + 4 * hf + (i & 3) >= top) S[i] = -INFINITY;
 }
 
+// A wave's outputs of a tile, or its part of them.
+template <int D, int QB>
+static __device__ __forceinline__ void store_tile(const PagedArgs &p, const PagedSeq &s, const PagedWork &w, const State<D, QB> &st, int r_wave, int rows)
+{
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+        const int r = r_wave + qb * 32 + l32;
+        const float l = st.l[qb] + other_half(st.l[qb]);
+        const int64_t row = s.row0 + r / p.G, rh = row * p.H + w.hk * p.G + r % p.G;  // (r >= rows: not stored)
+        if (p.n_split > 1) {
+            if (r >= rows) continue;
+            float *po = p.part_o + ((int64_t)w.split * p.m_total * p.H + rh) * D + 4 * hf;
+#pragma unroll
+            for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    *(f32x4 *)(po + 32 * db + 8 * g) =
+                        f32x4{st.O[qb][db][4 * g], st.O[qb][db][4 * g + 1], st.O[qb][db][4 * g + 2], st.O[qb][db][4 * g + 3]};
+            if (hf == 0) *(float2 *)(p.part_ml + ((int64_t)w.split * p.m_total * p.H + rh) * 2) = float2{st.m[qb] * st.c[qb], l};
+            continue;
+        }
+        const float inv = 1.f / l;
+        __bf16 *op = (__bf16 *)(p.o + row * p.ld_o) + (int64_t)(w.hk * p.G + r % p.G) * D + 8 * hf;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; g += 2) {
+                bf16x8 x;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = (__bf16)(st.O[qb][db][4 * g + e] * inv);
+                u32x4 y = __builtin_bit_cast(u32x4, x);
+                swap_pieces(y);
+                if (r < rows) *(u32x4 *)(op + 32 * db + 8 * g) = y;
+            }
+        if (hf == 0 && p.lse && r < rows) p.lse[rh] = float2{st.c[qb], st.m[qb] * st.c[qb] + __builtin_amdgcn_logf(l)};
+    }
+}
+
 // The four waves of a workgroup have had different keys of the same 32 packed rows: their denominators and outputs in units of the largest
 // reference, added up and stored.  room(j): 32 D floats of LDS for wave j (whose copies have arrived and been read).
 struct JoinRoom {
