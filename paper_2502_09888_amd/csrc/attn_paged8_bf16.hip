@@ -180,11 +180,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
     int pages = first_pages, pages_next = next_pages;
     uint32_t scales = first_scales, scales_next = first_scales, held = 0;
     // this lane's 16 codes of the wave's 8 keys, or (D = 64, upper half) of their values: from its place in a page, in LDS, as 32 bytes of a row
-    const int part = D == 64 ? lane & 31 : lane, row8 = part / (D / 16), piece = part % (D / 16);
+    const int part = D == 64 ? lane & 31 : lane, x8 = part / (D / 16), piece = part % (D / 16);
+    // (16 lanes have rows whose pieces of even numbers lie in different places of the banks: 0 and 4, or 0, 1, 4 and 5)
+    const int row8 = D == 64 ? (x8 & 1) | (x8 & 2) << 1 | (x8 & 4) >> 1 : (x8 & 1) << 2 | x8 >> 1;
     const uint32_t page_off = ((wave & 1) * 8 + row8) * D + piece * 16;
     const int row32 = (wave >> 1) * 16 + (wave & 1) * 8 + row8, to_row = row32 * R::kPitch;
-    // (a row's two pieces: rows of odd numbers write theirs the other way round, which takes 16 lanes to 16 places of the banks)
-    const int swap = row32 & 1, to_a = to_row + ((2 * piece + swap) ^ R::f(row32)) * 16, to_b = to_row + ((2 * piece + 1 - swap) ^ R::f(row32)) * 16;
+    const int to_a = to_row + ((2 * piece) ^ R::f(row32)) * 16, to_b = to_row + ((2 * piece + 1) ^ R::f(row32)) * 16;
     auto issue = [&](int j, lds_u8 *slot) __attribute__((always_inline)) {
         if ((j & 63) == 0 && j > 0) {
             pages = pages_next;
@@ -205,20 +206,24 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
         if ((j & 63) == 32) scales_next = src.scales(k_mine + ((j & ~63) + 64 + lane) * 32, pages_next);
         return (uint32_t)__builtin_amdgcn_readlane(scales, j & 63);
     };
-    auto codes_at = [&](lds_u8 *slot, int value) __attribute__((always_inline)) {
-        return *(const __attribute__((address_space(3))) u32x4 *)(slot + wave * kSlot + (D == 64 ? 0 : value * 1024) + lane * 16);
-    };
     auto widen = [&](u32x4 x, float scale, lds_u8 *to) __attribute__((always_inline)) {
-        const u32x2 first = swap ? u32x2{x.z, x.w} : u32x2{x.x, x.y}, second = swap ? u32x2{x.x, x.y} : u32x2{x.z, x.w};
-        *(__attribute__((address_space(3))) u32x4 *)(to + to_a) = wide8(first, scale);
-        *(__attribute__((address_space(3))) u32x4 *)(to + to_b) = wide8(second, scale);
+        *(__attribute__((address_space(3))) u32x4 *)(to + to_a) = wide8(u32x2{x.x, x.y}, scale);
+        *(__attribute__((address_space(3))) u32x4 *)(to + to_b) = wide8(u32x2{x.z, x.w}, scale);
     };
-    // keys of block j (slot kj) and values of the one before it (slot kv; of the same block: kj == kv in `whole_block`)
-    auto widen_keys = [&](lds_u8 *slot, uint32_t sc, lds_u8 *to) __attribute__((always_inline)) {
-        if (D == 128 || hf == 0) widen(codes_at(slot, 0), scale_of(sc), to);
-    };
-    auto widen_values = [&](lds_u8 *slot, uint32_t sc, lds_u8 *to) __attribute__((always_inline)) {
-        if (D == 128 || hf == 1) widen(codes_at(slot, 1), scale_of(sc >> 8), to);
+    // the wave's keys in one slot and values in another become bf16 rows; the first `n` of each, zeros behind them
+    auto widen_both = [&](lds_u8 *key_slot, uint32_t key_scales, lds_u8 *keys, lds_u8 *value_slot, uint32_t value_scales, lds_u8 *values, bool here)
+                          __attribute__((always_inline)) {
+        const int mine = wave * kSlot + lane * 16;
+        if constexpr (D == 64) {  // (a half-wave has either)
+            u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)((hf ? value_slot : key_slot) + mine);
+            if (!here) x = u32x4{0, 0, 0, 0};
+            widen(x, scale_of(hf ? value_scales >> 8 : key_scales), hf ? values : keys);
+        } else {
+            u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)(key_slot + mine), y = *(const __attribute__((address_space(3))) u32x4 *)(value_slot + mine + 1024);
+            if (!here) x = y = u32x4{0, 0, 0, 0};
+            widen(x, scale_of(key_scales), keys);
+            widen(y, scale_of(value_scales >> 8), values);
+        }
     };
 
     Rows<D> at;
@@ -282,45 +287,35 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
         if (!again && n_whole > 0) {
             f32x16 S0[QB], S1[QB];
             bf16x8 P[QB][2];
-            landed8(n_whole > 1 ? min(n_blocks - 2, 2) : min(n_blocks - 1, 3));
+            landed8(min(n_blocks - 2, 2));
             held = scales_of(0);
-            widen_keys(room(0), held, room(4));
-            widen_values(room(0), held, room(6));
-            if (n_whole > 1) {
-                held = scales_of(1);
-                widen_keys(room(1), held, room(5));
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (n_blocks > 4) issue(4, room(0));
+            uint32_t next = n_whole > 1 ? scales_of(1) : held;
+            widen_both(room(0), held, room(4), room(0), held, room(6), true);
+            if (n_whole > 1) widen_both(room(1), next, room(5), room(0), held, room(6), true);
+            held = next;
             meet();
             st.logits(read_k<D>(at, room(4)), S0);
             st.reference(S0);
             // block j (i = j % 4): its logits in Sc; behind the barrier the keys of block j + 1 and its own values are there, nobody reads the keys of
             // block j or the values of block j - 1 any more, and their places are filled
             auto step = [&](int j, int i, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
-                landed8(min(2, n_blocks - 3 - j));
+                landed8(min(1, n_blocks - 3 - j));
                 meet();
+                if (j + 4 < n_blocks) issue(j + 4, room(i));
+                next = held;
+                if (j + 2 < n_whole) next = scales_of(j + 2);
                 const KFrags<D> k = read_k<D>(at, room(4 + ((i + 1) & 1)));
                 __builtin_amdgcn_sched_barrier(0);
                 st.weights(Sc, P, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                st.logits(k, Sn);  // (behind the last block: not used)
+                st.logits(k, Sn);  // (behind the last block: not used, as what is widened then)
                 st.weights(Sc, P, 1);
                 const VFrags<D> v0 = read_v<D>(at, room(6 + (i & 1))), v1 = read_v<D>(at, room(6 + (i & 1)) + 16 * R::kPitch);
-                if (j + 1 < n_whole) {
-                    widen_values(room((i + 1) & 3), held, room(6 + ((i + 1) & 1)));
-                    if (j + 2 < n_whole) {
-                        held = scales_of(j + 2);
-                        widen_keys(room((i + 2) & 3), held, room(4 + (i & 1)));
-                    }
-                }
+                widen_both(room((i + 2) & 3), next, room(4 + (i & 1)), room((i + 1) & 3), held, room(6 + ((i + 1) & 1)), true);
+                held = next;
                 __builtin_amdgcn_sched_barrier(0x40f);
                 st.add(v0, P, 0);
                 st.add(v1, P, 1);
-                if (j + 5 < n_blocks) {
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    issue(j + 5, room((i + 1) & 3));
-                }
             };
             for (int j = 0; j < n_whole;) {
                 step(j, 0, S0, S1);
@@ -341,10 +336,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
             landed8(again || n_whole == 0 ? min(3, n_blocks - 1 - j) : 0);
             const uint32_t sc = scales_of(j);
             lds_u8 *const keys = room(4 + (j & 1)), *const values = room(6 + (j & 1)), *const slot = room(j & 3);
-            const bool here = c_lo + j * 32 + row32 < c_hi;  // (codes behind the cached keys may be no numbers)
-            const u32x4 none = {0, 0, 0, 0};
-            if (D == 128 || hf == 0) widen(here ? codes_at(slot, 0) : none, scale_of(sc), keys);
-            if (D == 128 || hf == 1) widen(here ? codes_at(slot, 1) : none, scale_of(sc >> 8), values);
+            widen_both(slot, sc, keys, slot, sc, values, c_lo + j * 32 + row32 < c_hi);  // (codes behind the cached keys may be no numbers)
             meet();
             if (again && j + 4 < n_blocks) issue(j + 4, slot);
             f32x16 S[QB];
