@@ -7,6 +7,7 @@
 // probabilities to four bits.)  Every row sees all cached tokens of its sequence; masks only concern the call's own rows, which
 // are seen as they were brought.
 #include "paged8.h"
+#include "paged_combine.h"
 #include "paged_state_bf16.h"
 
 namespace climber {
@@ -308,6 +309,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
                 __builtin_amdgcn_sched_barrier(0);
                 st.weights(Sc, P, 0);
                 __builtin_amdgcn_sched_barrier(0);
+                // (from here on the matrix pipe has work: before the other wave of the SIMD, which makes its exponentials meanwhile.  us without / with:
+                // sessions 122.8 / 118.9, scoring 102.6 / 101.5, ragged scoring 143.6 / 142.1)
+                __builtin_amdgcn_s_setprio(1);
                 st.logits(k, Sn);  // (behind the last block: not used, as what is widened then)
                 st.weights(Sc, P, 1);
                 const VFrags<D> v0 = read_v<D>(at, room(6 + (i & 1))), v1 = read_v<D>(at, room(6 + (i & 1)) + 16 * R::kPitch);
@@ -316,6 +320,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
                 __builtin_amdgcn_sched_barrier(0x40f);
                 st.add(v0, P, 0);
                 st.add(v1, P, 1);
+                __builtin_amdgcn_s_setprio(0);
             };
             for (int j = 0; j < n_whole;) {
                 step(j, 0, S0, S1);
@@ -457,143 +462,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
     }
 }
 
-// ---- few rows ------------------------------------------------------------------------------------
-// 32 packed rows; the waves of a workgroup take different blocks of 32 keys, each through a ring of its own, and are joined at the end.
-template <int D, bool SUMI>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_paged8_few_kernel(const Paged8Args p)
-{
-    constexpr int kStage = 2 * 32 * D, kLoads = 4 * Rows8<D>::kLoads;  // a wave's, of a block of 32 keys
-    __shared__ __attribute__((aligned(1024))) uint8_t stage0[4 * kStage], stage1[4 * kStage], stage2[4 * kStage], stage3[4 * kStage];
-    __shared__ JoinRoom joined;
-    __shared__ int odd_seen[4];
-    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    PagedWork w;
-    PagedSeq s;
-    if (!paged_work(p, w, s)) return;
-    const int rows = s.T * p.G, r_tile = w.tile * 32;
-    if (r_tile >= rows) return;
-    const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
-    const int64_t row = s.row0 + t;
-    const bool causal = !SUMI && p.causal;
-    const int k_all = SUMI ? s.n : paged_keys(p, s);
-    auto sees = [&](int i) { return causal ? min(s.n + min(i, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row i sees keys below it
-    int k_lo, k_hi;
-    paged_part(p, w.split, sees(r_tile + 31), 128, k_lo, k_hi);
-    k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
-    const int c_lo = min(k_lo, s.n), c_hi = min(k_hi, s.n);            // the cached ones
-    const int n_blk = (c_hi - c_lo + 31) / 32, mine = n_blk > wave ? (n_blk - wave + 3) / 4 : 0;  // blocks wave, wave + 4, ...
-
-    const Source8<D> src(p, w.b, w.hk, c_hi, lane);
-    auto stage = [&](int i) __attribute__((always_inline)) {
-        return (lds_u8 *)((i & 3) == 0 ? stage0 : (i & 3) == 1 ? stage1 : (i & 3) == 2 ? stage2 : stage3) + wave * kStage;
-    };
-    // page numbers of 32 blocks: the lower 32 lanes have those of the first 16 keys, the upper those of the others; of the 32 after them
-    const int k_mine = c_lo + wave * 32 - (lane >> 5) * (32 * 128 - 16);
-    int pages = src.page_number(k_mine + lane * 128), pages_next = src.page_number(k_mine + (32 + lane) * 128);
-    uint32_t scales = src.scales(k_mine + lane * 128, pages), scales_next = scales;
-    auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
-        if ((i & 31) == 0 && i > 0) {
-            pages = pages_next;
-            pages_next = src.page_number(k_mine + (i + 32 + lane) * 128);
-        }
-        const int k0 = c_lo + (i * 4 + wave) * 32;
-        src.issue(k0, __builtin_amdgcn_readlane(pages, i & 31), to, to + 32 * D);
-        src.issue(k0 + 16, __builtin_amdgcn_readlane(pages, 32 + (i & 31)), to + 16 * D, to + 48 * D);
-    };
-    Rows8<D> at;
-    at.init(lane);
-    State<D, 1, true> st;
-    {
-        typename State<D, 1, true>::Row in;
-        st.template request<SUMI>(p, 0, row, h, w.hk, hf, in);
-        if (mine > 0) issue(0, stage(0));
-        if (mine > 1) issue(1, stage(1));
-        if (mine > 2) issue(2, stage(2));
-        st.template start<SUMI>(p, 0, hf, in, w.split == 0 && wave == 0);
-    }
-    auto block = [&](int i, lds_u8 *keys, lds_u8 *free) __attribute__((always_inline)) {
-        // (rows, page numbers and scales were asked for among the copies: this waits for more than it has to, never for less)
-        const int later = min(mine - 1 - i, 2);
-        if (later == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
-        else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (i + 3 < mine) issue(i + 3, free);
-        if ((i & 31) == 0 && i > 0) scales = scales_next;
-        if ((i & 31) == 16) scales_next = src.scales(k_mine + ((i & ~31) + 32 + lane) * 128, pages_next);
-        const uint32_t s0 = __builtin_amdgcn_readlane(scales, i & 31), s1 = __builtin_amdgcn_readlane(scales, 32 + (i & 31));
-        const int k0 = c_lo + (i * 4 + wave) * 32;
-        f32x16 S[1];
-        bf16x8 P[1][2];
-        st.logits(read_k8<D>(at, keys, scale_of(l32 < 16 ? s0 : s1)), S);
-        const bool whole = k0 + 32 <= c_hi;
-        if (!whole) hide(S[0], k0, hf, c_hi);
-        st.reference(S);
-        st.weights(S, P);
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const int left = c_hi - (k0 + 16 * g + 4 * hf);  // (codes of hidden keys may be no numbers)
-            st.add(read_v8<D>(at, keys + 32 * D + g * 16 * D, scale_of((g ? s1 : s0) >> 8), u32x2{first_bytes(left), first_bytes(left - 8)}), P, g);
-        }
-        // its place has been read
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    };
-#pragma unroll 1
-    for (int i = 0; i < mine; i += 4) {
-        block(i, stage(0), stage(3));
-        if (i + 1 < mine) block(i + 1, stage(1), stage(0));
-        if (i + 2 < mine) block(i + 2, stage(2), stage(1));
-        if (i + 3 < mine) block(i + 3, stage(3), stage(2));
-    }
-
-    bool odd = false;
-    int n_lo = 0;
-    if constexpr (!SUMI) {
-        // the call's own rows: blocks of 32 from the part's first one on
-        n_lo = max(k_lo - s.n, 0);
-        const int n_hi = max(k_hi - s.n, 0), n_new = (n_hi - n_lo + 31) / 32;
-        PagedSeq own = s;
-        own.n = 0;
-        const Source<D, Rows<D>::kLoads> rows_src(p, own, w.b, w.hk, n_hi, lane, 0);
-        Rows<D> vat;
-        vat.init(lane);
-        const int lim = sees(r) - s.n, lim_lo = sees(r_tile) - s.n;
-#pragma unroll 1
-        for (int i = wave; i < n_new; i += 4) {
-            const int k0 = n_lo + i * 32;
-            lds_u8 *const keys = stage(0), *const values = stage(1);
-            rows_src.issue(k0, 0, keys, values);
-            rows_src.issue(k0 + 16, 0, keys + 16 * Rows<D>::kPitch, values + 16 * Rows<D>::kPitch);
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            f32x16 S[1];
-            bf16x8 P[1][2];
-            st.logits(read_k_wide<D>(keys, lane), S);
-            if (k0 + 32 > min(lim_lo, n_hi)) {
-                odd |= clear_odd<32 * Rows<D>::kPitch>(values, lane);
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                hide(S[0], k0, hf, min(lim, n_hi));
-            }
-            st.reference(S);
-            st.weights(S, P);
-#pragma unroll
-            for (int g = 0; g < 2; ++g) st.add(read_v<D>(vat, values + g * 16 * Rows<D>::kPitch), P, g);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
-    }
-    if (lane == 0) odd_seen[wave] = odd;
-    // (each wave's outputs in units of its reference take the 2 x kStage bytes of two waves' places; all waves are done with theirs at the first barrier)
-    join_few<D, true>(p, s, w, st, joined, [&](int j) { return (float *)(j < 2 ? stage0 : stage1) + (j & 1) * 32 * D; }, row, h, r_tile, rows);
-    if constexpr (!SUMI) {
-        if (__builtin_expect(odd_seen[0] | odd_seen[1] | odd_seen[2] | odd_seen[3], 0)) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all waves' outputs are written
-            __syncthreads();
-            const int from = s.n + n_lo, clean = max(0, min(sees(r_tile), k_hi) - from) / 32 * 32;
-            if (wave == 0) put_odd<D>(p, s, w, from + clean, k_hi, r_tile, min(r_tile + 32, rows), sees);
-        }
-    }
-}
-
 // ---- new tokens ----------------------------------------------------------------------------------
-// A wave for a block of 16 tokens of a cache head.  The scale is the least with which all of the block's tokens, those that were
+// A wave for a block of 16 tokens of a cache head (the block-th that the sequence's new tokens touch).  The scale is the least with which all of the block's tokens, those that were
 // stored before too, stay within 448 of it; where it grows these are rounded again (by a power of two, so that only what lies near the
 // smallest numbers changes).  Infinities become no numbers.
 static __device__ __forceinline__ uint32_t wave_max(uint32_t x)
@@ -604,16 +474,11 @@ static __device__ __forceinline__ uint32_t wave_max(uint32_t x)
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void paged8_store_kernel(const Paged8Args p, int n_blk)
+static __device__ __forceinline__ void store_block(const Paged8Args &p, const PagedSeq &s, int b, int hk, int block)
 {
     constexpr int kLanes = D / 8, kRows = 64 / kLanes, kLoads = 16 / kRows;  // lanes of a row, 8 values each
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t unit = (int64_t)blockIdx.x * 4 + wave;
-    const int64_t bh = unit / n_blk;
-    if (bh >= (int64_t)p.n_seqs * p.Hkv) return;
-    const int b = (int)(bh / p.Hkv), hk = (int)(bh % p.Hkv);
-    const PagedSeq s = paged_seq(p, b);
-    const int end = min(s.n + s.T, p.max_len), slot0 = ((s.n >> 4) + (int)(unit % n_blk)) * 16;
+    const int lane = threadIdx.x & 63;
+    const int end = min(s.n + s.T, p.max_len), slot0 = ((s.n >> 4) + block) * 16;
     if (slot0 >= end || s.T == 0) return;
     const int page = p.table[(int64_t)b * p.table_ld + (slot0 >> p.page_shift)];
     if (page < 0 || page >= p.n_pages) return;
@@ -678,6 +543,158 @@ __global__ __launch_bounds__(256) void paged8_store_kernel(const Paged8Args p, i
     if (hk == 0 && p.stamp && lane >= old && lane < n) p.stamp[((int64_t)page << p.page_shift) + in + lane] = p.stamp_new[s.row0 + slot0 + lane - s.n];
 }
 
+template <int D>
+static __device__ __forceinline__ void store_unit(const Paged8Args &p, unsigned group)
+{
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t unit = (int64_t)group * 4 + wave, bh = unit / p.store_blocks;
+    if (bh >= (int64_t)p.n_seqs * p.Hkv) return;
+    const int b = (int)(bh / p.Hkv);
+    store_block<D>(p, paged_seq(p, b), b, (int)(bh % p.Hkv), (int)(unit % p.store_blocks));
+}
+template <int D>
+__global__ __launch_bounds__(256) void paged8_store_kernel(const Paged8Args p) { store_unit<D>(p, blockIdx.x); }
+// ... and the join of the parts of the keys, where there are any: nothing reads the cached tokens any more
+template <int D, int GROUPS>
+__global__ __launch_bounds__(256) void paged8_finish_kernel(const Paged8Args p, unsigned joins)
+{
+    if (blockIdx.x < joins) paged_join::combine_rows<__bf16, GROUPS>(p, blockIdx.x);
+    else store_unit<D>(p, blockIdx.x - joins);
+}
+
+// ---- few rows ------------------------------------------------------------------------------------
+// 32 packed rows; the waves of a workgroup take different blocks of 32 keys, each through a ring of its own, and are joined at the end.  Two
+// stages, so that a CU has two workgroups: us with four stages and one / this way, one token of 64 users 77 / 70, of one long cache 59 / 52.
+// Where a workgroup is the only one that reads its sequence's head it stores the new tokens itself.
+template <int D, bool SUMI>
+__global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Args p)
+{
+    constexpr int kStage = 2 * 32 * D, kLoads = 4 * Rows8<D>::kLoads;  // a wave's, of a block of 32 keys
+    __shared__ __attribute__((aligned(1024))) uint8_t stage0[4 * kStage], stage1[4 * kStage];
+    __shared__ JoinRoom joined;
+    __shared__ int odd_seen[4];
+    const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    PagedWork w;
+    PagedSeq s;
+    if (!paged_work(p, w, s)) return;
+    const int rows = s.T * p.G, r_tile = w.tile * 32;
+    if (r_tile >= rows) return;
+    const int r = min(r_tile + l32, rows - 1), t = r / p.G, h = w.hk * p.G + r % p.G;
+    const int64_t row = s.row0 + t;
+    const bool causal = !SUMI && p.causal;
+    const int k_all = SUMI ? s.n : paged_keys(p, s);
+    auto sees = [&](int i) { return causal ? min(s.n + min(i, rows - 1) / p.G + 1, k_all) : k_all; };  // packed row i sees keys below it
+    int k_lo, k_hi;
+    paged_part(p, w.split, sees(r_tile + 31), 128, k_lo, k_hi);
+    k_lo = __builtin_amdgcn_readfirstlane(k_lo), k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+    const int c_lo = min(k_lo, s.n), c_hi = min(k_hi, s.n);            // the cached ones
+    const int n_blk = (c_hi - c_lo + 31) / 32, mine = n_blk > wave ? (n_blk - wave + 3) / 4 : 0;  // blocks wave, wave + 4, ...
+
+    const Source8<D> src(p, w.b, w.hk, c_hi, lane);
+    lds_u8 *const at0 = (lds_u8 *)stage0 + wave * kStage, *const at1 = (lds_u8 *)stage1 + wave * kStage;
+    // page numbers of 32 blocks: the lower 32 lanes have those of the first 16 keys, the upper those of the others; of the 32 after them
+    const int k_mine = c_lo + wave * 32 - (lane >> 5) * (32 * 128 - 16);
+    int pages = src.page_number(k_mine + lane * 128), pages_next = src.page_number(k_mine + (32 + lane) * 128);
+    uint32_t scales = src.scales(k_mine + lane * 128, pages), scales_next = scales;
+    auto issue = [&](int i, lds_u8 *to) __attribute__((always_inline)) {
+        if ((i & 31) == 0 && i > 0) {
+            pages = pages_next;
+            pages_next = src.page_number(k_mine + (i + 32 + lane) * 128);
+        }
+        const int k0 = c_lo + (i * 4 + wave) * 32;
+        src.issue(k0, __builtin_amdgcn_readlane(pages, i & 31), to, to + 32 * D);
+        src.issue(k0 + 16, __builtin_amdgcn_readlane(pages, 32 + (i & 31)), to + 16 * D, to + 48 * D);
+    };
+    Rows8<D> at;
+    at.init(lane);
+    State<D, 1, true> st;
+    {
+        typename State<D, 1, true>::Row in;
+        st.template request<SUMI>(p, 0, row, h, w.hk, hf, in);
+        if (mine > 0) issue(0, at0);
+        if (mine > 1) issue(1, at1);
+        st.template start<SUMI>(p, 0, hf, in, w.split == 0 && wave == 0);
+    }
+    auto block = [&](int i, lds_u8 *keys) __attribute__((always_inline)) {
+        // (rows, page numbers and scales were asked for among the copies: this waits for more than it has to, never for less)
+        if (i + 1 < mine) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if ((i & 31) == 0 && i > 0) scales = scales_next;
+        if ((i & 31) == 16) scales_next = src.scales(k_mine + ((i & ~31) + 32 + lane) * 128, pages_next);
+        const uint32_t s0 = __builtin_amdgcn_readlane(scales, i & 31), s1 = __builtin_amdgcn_readlane(scales, 32 + (i & 31));
+        const int k0 = c_lo + (i * 4 + wave) * 32;
+        f32x16 S[1];
+        bf16x8 P[1][2];
+        st.logits(read_k8<D>(at, keys, scale_of(l32 < 16 ? s0 : s1)), S);
+        const bool whole = k0 + 32 <= c_hi;
+        if (!whole) hide(S[0], k0, hf, c_hi);
+        st.reference(S);
+        st.weights(S, P);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const int left = c_hi - (k0 + 16 * g + 4 * hf);  // (codes of hidden keys may be no numbers)
+            st.add(read_v8<D>(at, keys + 32 * D + g * 16 * D, scale_of((g ? s1 : s0) >> 8), u32x2{first_bytes(left), first_bytes(left - 8)}), P, g);
+        }
+        // its place has been read
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + 2 < mine) issue(i + 2, keys);
+    };
+#pragma unroll 1
+    for (int i = 0; i < mine; i += 2) {
+        block(i, at0);
+        if (i + 1 < mine) block(i + 1, at1);
+    }
+
+    bool odd = false;
+    int n_lo = 0;
+    if constexpr (!SUMI) {
+        // the call's own rows: blocks of 32 from the part's first one on
+        n_lo = max(k_lo - s.n, 0);
+        const int n_hi = max(k_hi - s.n, 0), n_new = (n_hi - n_lo + 31) / 32;
+        PagedSeq own = s;
+        own.n = 0;
+        const Source<D, Rows<D>::kLoads> rows_src(p, own, w.b, w.hk, n_hi, lane, 0);
+        Rows<D> vat;
+        vat.init(lane);
+        const int lim = sees(r) - s.n, lim_lo = sees(r_tile) - s.n;
+#pragma unroll 1
+        for (int i = wave; i < n_new; i += 4) {
+            const int k0 = n_lo + i * 32;
+            lds_u8 *const keys = at0, *const values = at1;
+            rows_src.issue(k0, 0, keys, values);
+            rows_src.issue(k0 + 16, 0, keys + 16 * Rows<D>::kPitch, values + 16 * Rows<D>::kPitch);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            f32x16 S[1];
+            bf16x8 P[1][2];
+            st.logits(read_k_wide<D>(keys, lane), S);
+            if (k0 + 32 > min(lim_lo, n_hi)) {
+                odd |= clear_odd<32 * Rows<D>::kPitch>(values, lane);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                hide(S[0], k0, hf, min(lim, n_hi));
+            }
+            st.reference(S);
+            st.weights(S, P);
+#pragma unroll
+            for (int g = 0; g < 2; ++g) st.add(read_v<D>(vat, values + g * 16 * Rows<D>::kPitch), P, g);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    }
+    if (lane == 0) odd_seen[wave] = odd;
+    // (each wave's outputs in units of its reference take the 2 x kStage bytes of two waves' places; all waves are done with theirs at the first barrier)
+    join_few<D, true>(p, s, w, st, joined, [&](int j) { return (float *)(j < 2 ? stage0 : stage1) + (j & 1) * 32 * D; }, row, h, r_tile, rows);
+    if constexpr (!SUMI) {
+        if (__builtin_expect(odd_seen[0] | odd_seen[1] | odd_seen[2] | odd_seen[3], 0)) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // all waves' outputs are written
+            __syncthreads();
+            const int from = s.n + n_lo, clean = max(0, min(sees(r_tile), k_hi) - from) / 32 * 32;
+            if (wave == 0) put_odd<D>(p, s, w, from + clean, k_hi, r_tile, min(r_tile + 32, rows), sees);
+        }
+        // (all of its waves have read the cached tokens, behind whose barrier they were joined)
+        if (p.n_split == 1)
+            for (int i = wave; i < p.store_blocks; i += 4) store_block<D>(p, s, w.b, w.hk, i);
+    }
+}
+
 template <int D, bool SUMI>
 hipError_t launch(Paged8Args p, hipStream_t s)
 {
@@ -687,7 +704,17 @@ hipError_t launch(Paged8Args p, hipStream_t s)
     if constexpr (D == 64)
         if (tile == 256) kernel = attn_paged8_tile_kernel<D, 2, SUMI>;
     p.n_tiles = (int)((rows + tile - 1) / tile);
+    p.store_blocks = SUMI ? 0 : (int)paged8_store_blocks(p.m_max);
     hipLaunchKernelGGL(kernel, dim3(paged_grid(p)), dim3(256), 0, s, p);
+    const unsigned stores = (unsigned)(((int64_t)p.n_seqs * p.Hkv * p.store_blocks + 3) / 4);
+    if (p.n_split > 1) {
+        const int64_t all = (int64_t)p.m_total * p.H;
+        const unsigned joins = (unsigned)(p.n_split <= 4 ? (all + 7) / 8 : all);
+        if (p.n_split <= 4) hipLaunchKernelGGL((paged8_finish_kernel<D, 1>), dim3(joins + stores), dim3(256), 0, s, p, joins);
+        else hipLaunchKernelGGL((paged8_finish_kernel<D, 8>), dim3(joins + stores), dim3(256), 0, s, p, joins);
+    } else if (!SUMI && tile != 32) {
+        hipLaunchKernelGGL(paged8_store_kernel<D>, dim3(stores), dim3(256), 0, s, p);
+    }
     return hipGetLastError();
 }
 
@@ -697,15 +724,6 @@ hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t s)
 {
     if (a.d == 64) return a.sumi ? launch<64, true>(a, s) : launch<64, false>(a, s);
     return a.sumi ? launch<128, true>(a, s) : launch<128, false>(a, s);
-}
-
-hipError_t launch_paged8_store(const Paged8Args &a, hipStream_t s)
-{
-    const int64_t n_blk = paged8_store_blocks(a.m_max), units = (int64_t)a.n_seqs * a.Hkv * n_blk;
-    const dim3 grid((unsigned)((units + 3) / 4));
-    if (a.d == 64) hipLaunchKernelGGL(paged8_store_kernel<64>, grid, dim3(256), 0, s, a, (int)n_blk);
-    else hipLaunchKernelGGL(paged8_store_kernel<128>, grid, dim3(256), 0, s, a, (int)n_blk);
-    return hipGetLastError();
 }
 
 }  // namespace climber

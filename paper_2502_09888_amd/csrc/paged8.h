@@ -8,15 +8,14 @@ constexpr int kScaleBlock = 16, kLeastScale = 10;  // tokens of a scale; the lea
 
 struct Paged8Args : PagedArgs {
     uint8_t *k_scale, *v_scale;  // [n_pages][Hkv][page / 16]
+    int store_blocks;            // blocks of 16 tokens that a sequence's new ones can touch; 0: nothing is stored
 };
 
 // packed rows of a workgroup
 static inline int paged8_tile_rows(int d, int64_t rows) { return rows <= 32 ? 32 : d == 64 && rows > 128 ? 256 : 128; }
-
-hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t s);
-// The call's new tokens into their pages, behind everything that reads these.
-hipError_t launch_paged8_store(const Paged8Args &a, hipStream_t s);
-// blocks of 16 tokens that a sequence's new tokens can touch
 static inline int64_t paged8_store_blocks(int64_t m_max) { return (m_max + 2 * kScaleBlock - 2) / kScaleBlock; }
+
+// attention, the join of its parts, and the call's new tokens into their pages
+hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t s);
 
 }  // namespace climber

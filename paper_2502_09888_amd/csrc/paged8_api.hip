@@ -34,10 +34,7 @@ int attn_paged8(const Call &c, const climber_paged_kv8 *kv8, void *workspace, si
     a.row_bytes = cfg->d_head;
     a.k_scale = kv8->k_scale;
     a.v_scale = kv8->v_scale;
-    const hipStream_t s = (hipStream_t)stream;
-    e = rt(launch_attn_paged8(a, s));
-    if (!e && a.n_split > 1) e = rt(launch_paged_combine(a, true, s));
-    return e || c.sumi ? e : rt(launch_paged8_store(a, s));
+    return rt(launch_attn_paged8(a, (hipStream_t)stream));
 }
 
 }  // namespace
