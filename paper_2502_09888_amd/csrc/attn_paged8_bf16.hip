@@ -705,7 +705,11 @@ hipError_t launch(Paged8Args p, hipStream_t s)
         if (tile == 256) kernel = attn_paged8_tile_kernel<D, 2, SUMI>;
     p.n_tiles = (int)((rows + tile - 1) / tile);
     p.store_blocks = SUMI ? 0 : (int)paged8_store_blocks(p.m_max);
-    hipLaunchKernelGGL(kernel, dim3(paged_grid(p)), dim3(256), 0, s, p);
+    const unsigned grid = paged_grid(p);
+    // All at once, two to a CU: the longest sequence is to be there with the shortest (one token of 64 users on 500 to 4000 64.7 / 61.4 us).
+    const int64_t per = (int64_t)p.Hkv * p.n_tiles * p.n_split, groups = per * p.n_seqs;
+    if (p.n_seqs > 1 && p.n_seqs <= 64 && groups > 256 && groups <= 512) p.by_work = 1, p.pair = (int)((255 + per) / per);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, p);
     const unsigned stores = (unsigned)(((int64_t)p.n_seqs * p.Hkv * p.store_blocks + 3) / 4);
     if (p.n_split > 1) {
         const int64_t all = (int64_t)p.m_total * p.H;

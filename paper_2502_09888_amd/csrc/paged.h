@@ -27,6 +27,7 @@ struct PagedArgs {
     float scale_log2e;
     // work split: tiles of packed rows, parts of the keys
     int n_tiles, n_split, bh_major, by_work;
+    int pair;  // by_work: sequences from this one of their order on come in ascending order; 0: all in descending
     float *part_o, *part_ml;  // [n_split][m_total H][d], [n_split][m_total H][2] (n_split > 1)
     float *logits;            // few rows: [n_seqs Hkv][m_max G][logits_ld] logits in log2 units for paged_mass_few, or nullptr
     int logits_ld;
@@ -99,6 +100,7 @@ static __device__ __forceinline__ bool paged_work(const PagedArgs &p, PagedWork 
     // (work in 26 bits, and the lane: no two alike)
     const uint32_t work = lane < n ? (__float_as_uint((float)mine.T * (float)(mine.n + mine.T)) & ~63u) | (uint32_t)(63 - lane) : 0;
     int at = w.b - b0;
+    if (p.pair && at >= p.pair) at = n - 1 - (at - p.pair);
     if (__builtin_amdgcn_ballot_w64(lane < n && (work >> 6) != (__builtin_amdgcn_readfirstlane(work) >> 6)) != 0) {
         int rank = 0;
         for (int j0 = 0; j0 < n; j0 += 16)

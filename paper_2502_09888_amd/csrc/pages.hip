@@ -76,11 +76,12 @@ static __device__ __forceinline__ void look(const int32_t *refs, int n_pages, in
 }
 
 // ---- fork ----------------------------------------------------------------------------------------
+constexpr int kForkFew = 32;  // rows of one workgroup
+
 // What rows become is read before any row is written: a wave for each row notes it and counts, another launch writes it.
-__global__ __launch_bounds__(256) void fork_read_kernel(const ForkArgs a)
+static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b)
 {
-    const int lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (b >= a.n_seqs) return;
+    const int lane = threadIdx.x & 63;
     const int par = a.parent[b];
     if (par >= a.n_seqs) {  // (no sequence: the row stays)
         if (lane == 0) atomicOr(a.status, CLIMBER_BAD_SEQ), a.new_held[b] = -1;
@@ -109,18 +110,36 @@ __global__ __launch_bounds__(256) void fork_read_kernel(const ForkArgs a)
     if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
     if (lane == 0) a.new_len[b] = n, a.new_held[b] = h;
 }
-__global__ __launch_bounds__(256) void fork_write_kernel(const ForkArgs a)
+static __device__ __forceinline__ void fork_write(const ForkArgs &a, int b)
 {
-    const int lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (b >= a.n_seqs) return;
+    const int lane = threadIdx.x & 63;
     const int h = a.new_held[b];
     if (h < 0) return;
     const int had = held_of(a, b);
     for (int i = lane; i < max(had, h); i += 64) a.table[(int64_t)b * a.table_ld + i] = a.rows[(int64_t)b * a.table_ld + i];
     if (lane == 0) a.len[b] = a.new_len[b], a.held[b] = h;
 }
+__global__ __launch_bounds__(256) void fork_read_kernel(const ForkArgs a)
+{
+    const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (b < a.n_seqs) fork_read(a, b);
+}
+__global__ __launch_bounds__(256) void fork_write_kernel(const ForkArgs a)
+{
+    const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (b < a.n_seqs) fork_write(a, b);
+}
+// ... few rows by one workgroup, a wave for each in turn
+__global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
+{
+    for (int b = threadIdx.x >> 6; b < a.n_seqs; b += 16) fork_read(a, b);
+    __syncthreads();
+    for (int b = threadIdx.x >> 6; b < a.n_seqs; b += 16) fork_write(a, b);
+}
 
 // ---- extend --------------------------------------------------------------------------------------
+constexpr int kFewSeqs = 1024, kFewUnits = 64, kListPages = 4096;  // what one workgroup takes; free pages that it keeps in LDS
+constexpr int kCompactFew = 256;
 constexpr int kNobody = 1 << 30;  // in last[]: a shared page that none of its writers keeps (n_seqs is less)
 
 // Sequence b's part of the call: pages [first, shared_to) that it holds and writes, [shared_to, need) that it has to get.
@@ -297,6 +316,134 @@ __global__ __launch_bounds__(256) void extend_write_kernel(const ExtendArgs a)
     if (lane == 0 && x.need > had) a.held[b] = x.need;
 }
 
+// All of it by one workgroup, a thread for each sequence: what it needs of its first page is requested with the bits of free pages, and the free
+// pages that are handed out stay in LDS.
+__global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
+{
+    __shared__ int sums[3][16], list[kListPages];
+    __shared__ uint64_t words[kFewUnits * 16];
+    __shared__ int unit_at[kFewUnits + 1];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, units = (int)pool_units(a.n_pages), b = t;
+    const bool mine = b < a.n_seqs;
+    Need x{};
+    int had = 0;
+    if (mine) x = need_of(a, b), had = held_of(a, b);
+    int32_t *const row = a.table + (int64_t)b * a.table_ld;
+    // bits and counts of the units
+    int n_used = 0;
+    for (int u = wave; u < units; u += 16) {
+        int r[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int64_t p = (int64_t)u * kUnitPages + i * 64 + lane;
+            r[i] = p < a.n_pages ? a.refs[p] : -1;
+        }
+        int n_free = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t f = __builtin_amdgcn_ballot_w64(r[i] == 0);
+            n_free += __popcll(f);
+            n_used += __popcll(__builtin_amdgcn_ballot_w64(r[i] > 0));
+            if (lane == 0) words[u * 16 + i] = f;
+        }
+        if (lane == 0) unit_at[u] = n_free;
+    }
+    // shared pages that are written
+    bool shared = false, bad = false;
+    for (int i = x.first; i < x.shared_to; ++i) {
+        const int page = row[i];
+        if (!in_pool(a, page)) bad = true;
+        else {
+            shared |= a.refs[page] > 1;
+            a.writers[page] = 0, a.last[page] = -1;
+        }
+    }
+    if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
+    const bool any_shared = __syncthreads_or(shared);
+    int c = max(0, x.need - max(x.shared_to, had)), copy = 0;
+    if (any_shared) {
+        if (shared)
+            for (int i = x.first; i < x.shared_to; ++i) {
+                const int page = row[i];
+                if (in_pool(a, page) && a.refs[page] > 1) atomicAdd(a.writers + page, 1), atomicMax(a.last + page, b);
+            }
+        __syncthreads();
+        if (shared)
+            for (int i = x.first; i < x.shared_to; ++i) {
+                if (!moves(a, b, row[i])) continue;
+                ++c;
+                copy |= i == x.first && x.part > 0;
+            }
+    }
+    const bool too_long = mine && x.too_long;
+    int all_new, all_copies, at = wave_before(c, all_new), at_copy = wave_before(copy, all_copies);
+    if (lane == 0) sums[0][wave] = all_new, sums[1][wave] = all_copies, sums[2][wave] = n_used;
+    const bool refused = __syncthreads_or(bad), full_row = __syncthreads_or(too_long);
+    int total = 0, n_copies = 0, in_use = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        if (i < wave) at += sums[0][i], at_copy += sums[1][i];
+        total += sums[0][i], n_copies += sums[1][i], in_use += sums[2][i];
+    }
+    int n_free = 0;
+    if (wave == 0) {
+        const int f = lane < units ? unit_at[lane] : 0, before = wave_before(f, n_free);
+        if (lane < units) unit_at[lane] = before;
+        if (lane == 0) unit_at[units] = n_free;
+    }
+    __syncthreads();
+    n_free = unit_at[units];
+    const bool full = full_row || total > n_free, go = !full && !refused;
+    if (t == 0) {
+        if (full) atomicOr(a.status, CLIMBER_POOL_FULL);
+        a.counts[0] = go ? n_copies : 0;
+        a.counts[1] = in_use + (go ? total : 0);
+    }
+    if (!go) return;
+    for (int u = wave; u < units; u += 16) {
+        int to0 = unit_at[u];
+        if (to0 >= total) break;
+#pragma unroll 1
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t w = words[u * 16 + i];
+            const int to = to0 + below(w);
+            if (((w >> lane) & 1) && to < total) {
+                const int page = u * kUnitPages + i * 64 + lane;
+                if (to < kListPages) list[to] = page;
+                else a.free_list[to] = page;
+            }
+            to0 += __popcll(w);
+        }
+    }
+    // refs change from the barrier on: whether a page stays with the last of its writers is noted before
+    if (shared)
+        for (int i = x.first; i < x.shared_to; ++i) {
+            const int page = row[i];
+            if (a.refs[page] > 1 && fresh(a.writers + page) != a.refs[page]) atomicOr(a.last + page, kNobody);
+        }
+    __syncthreads();
+    auto take = [&](int i) { return i < kListPages ? list[i] : fresh(a.free_list + i); };
+    if (shared)
+        for (int i = x.first; i < x.shared_to; ++i) {
+            const int page = row[i], last = fresh(a.last + page);
+            if (last < 0 || last == b) continue;
+            const int to = take(at++);
+            row[i] = to;
+            a.refs[to] = 1;
+            atomicSub(a.refs + page, 1);
+            if (i == x.first && x.part > 0) {
+                int32_t *const o = a.copies + 3 * (int64_t)at_copy;
+                o[0] = page, o[1] = to, o[2] = x.part;
+            }
+        }
+    for (int i = had; i < x.need; ++i) {
+        const int to = take(at++);
+        row[i] = to;
+        a.refs[to] = 1;
+    }
+    if (mine && x.need > had) a.held[b] = x.need;
+}
+
 // ---- compact -------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void compact_look_kernel(const CompactArgs a)
 {
@@ -361,6 +508,70 @@ __global__ __launch_bounds__(256) void compact_list_kernel(const CompactArgs a)
         }
         before += __popcll(w);
     }
+}
+// All of it by one workgroup: lists and bits in LDS but for the pages' new places.
+__global__ __launch_bounds__(1024) void compact_few_kernel(const CompactArgs a)
+{
+    __shared__ uint64_t words[kFewUnits * 16];
+    __shared__ int word_at[kFewUnits * 16], sums[16];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, units = (int)pool_units(a.n_pages), n_words = units * 16;
+    for (int u = wave; u < units; u += 16) {
+        int r[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int64_t p = (int64_t)u * kUnitPages + i * 64 + lane;
+            r[i] = p < a.n_pages ? a.refs[p] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint64_t w = __builtin_amdgcn_ballot_w64(r[i] > 0);
+            if (lane == 0) words[u * 16 + i] = w;
+        }
+    }
+    __syncthreads();
+    // pages in use before each word of 64 (kFewUnits * 16 words, a thread each)
+    int n_used;
+    const int before = group_before(t < n_words ? __popcll(words[t]) : 0, n_used, sums);
+    if (t < n_words) word_at[t] = before;
+    __syncthreads();
+    int low = n_used;  // pages in use below the end
+    if (n_used >> 6 < n_words) {
+        const int rest = n_used & 63;
+        low = word_at[n_used >> 6] + (rest ? __popcll(words[n_used >> 6] & ((1ull << rest) - 1)) : 0);
+    }
+    if (t == 0) a.counts[0] = n_used - low, a.counts[1] = n_used;
+    // pages in use behind the end, in order; free ones before it
+    for (int i = wave; i < n_words; i += 16) {
+        const uint64_t w = words[i];
+        const int page = i * 64 + lane, rank = word_at[i] + below(w);
+        const bool used = (w >> lane) & 1;
+        if (page >= a.n_pages) continue;
+        if (page < n_used && !used) a.holes[page - rank] = page;
+        if (page >= n_used && used) a.movers[rank - low] = page;
+    }
+    __syncthreads();
+    for (int i = t; i < n_used - low; i += 1024) {
+        const int from = a.movers[i], to = a.holes[i];
+        int32_t *const c = a.copies + 3 * (int64_t)i;
+        c[0] = from, c[1] = to, c[2] = 1 << a.page_shift;
+        a.refs[to] = a.refs[from];
+        a.refs[from] = 0;
+    }
+    bool bad = false;
+    for (int b = wave; b < a.n_seqs; b += 16) {
+        const int had = held_of(a, b);
+        for (int i = lane; i < had; i += 64) {
+            int32_t *const e = a.table + (int64_t)b * a.table_ld + i;
+            const int page = *e;
+            if (!in_pool(a, page)) bad = true;
+            else if (page >= n_used) {
+                const uint64_t w = words[page >> 6];
+                if ((w >> (page & 63)) & 1) *e = a.holes[word_at[page >> 6] + __popcll(w & ((1ull << (page & 63)) - 1)) - low];
+                else bad = true;  // (a page that nothing is said to hold)
+            }
+        }
+    }
+    if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
 }
 __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a, int pair_groups)
 {
@@ -431,6 +642,10 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(const CopyArgs a)
 
 hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t s)
 {
+    if (a.n_seqs <= kForkFew) {
+        hipLaunchKernelGGL(fork_few_kernel, dim3(1), dim3(1024), 0, s, a);
+        return hipGetLastError();
+    }
     const dim3 grid((unsigned)((a.n_seqs + 3) / 4));
     hipLaunchKernelGGL(fork_read_kernel, grid, dim3(256), 0, s, a);
     hipLaunchKernelGGL(fork_write_kernel, grid, dim3(256), 0, s, a);
@@ -439,6 +654,10 @@ hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t s)
 
 hipError_t launch_pages_extend(const ExtendArgs &a, hipStream_t s)
 {
+    if (a.n_seqs <= kFewSeqs && pool_units(a.n_pages) <= kFewUnits) {
+        hipLaunchKernelGGL(extend_few_kernel, dim3(1), dim3(1024), 0, s, a);
+        return hipGetLastError();
+    }
     const int unit_groups = (int)((pool_units(a.n_pages) + 3) / 4), seq_groups = std::min(1024, (a.n_seqs + 255) / 256);
     hipLaunchKernelGGL(extend_look_kernel, dim3((unsigned)(unit_groups + seq_groups)), dim3(256), 0, s, a, unit_groups);
     hipLaunchKernelGGL(extend_writers_kernel, dim3((unsigned)seq_groups), dim3(256), 0, s, a);
@@ -449,6 +668,10 @@ hipError_t launch_pages_extend(const ExtendArgs &a, hipStream_t s)
 
 hipError_t launch_pages_compact(const CompactArgs &a, hipStream_t s)
 {
+    if (a.n_seqs <= kCompactFew && pool_units(a.n_pages) <= kFewUnits) {
+        hipLaunchKernelGGL(compact_few_kernel, dim3(1), dim3(1024), 0, s, a);
+        return hipGetLastError();
+    }
     const unsigned units = (unsigned)((pool_units(a.n_pages) + 3) / 4);
     const int pair_groups = (int)std::min<int64_t>(1024, (a.n_pages / 2 + 255) / 256 + 1);
     hipLaunchKernelGGL(compact_look_kernel, dim3(units), dim3(256), 0, s, a);
