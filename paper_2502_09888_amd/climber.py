@@ -205,6 +205,10 @@ def _load_native(lib):
                 Config, RelBias, *current,
                 *(C.cast(f, C.c_void_p).value for f in (lib.climber_attn_history_paged, lib.climber_attn_sumi_paged, lib.climber_paged_evict)),
                 PagedKV, *(C.cast(f, C.c_void_p).value for f in (lib.climber_attn_history_paged8, lib.climber_attn_sumi_paged8)), PagedKV8)
+    if current[0] is not None:
+        native.bind_pages(*(C.cast(f, C.c_void_p).value for f in (lib.climber_pages_fork, lib.climber_pages_extend, lib.climber_pages_compact,
+                                                                  lib.climber_paged_copy, lib.climber_paged8_copy, lib.climber_rotary)),
+                          PagePool, RotaryPlan, torch.bfloat16, torch.float32)
     _native = native
     return native
 
@@ -648,44 +652,66 @@ def climber_pages_workspace_bytes(pool: PagePool) -> int:
     return int(load_library().climber_pages_workspace_bytes(C.byref(pool)))
 
 
-def _copies(t, least: int) -> Optional[int]:
+def _copies(t, least: int) -> None:
     if t is not None and not isinstance(t, int) and (t.numel() < 3 * least or not t.is_contiguous()):
         raise ValueError(f"copies needs room for {least} of three numbers")
-    return _ptr(t)
 
 
 def climber_pages_fork(pool: PagePool, parent, keep, status, workspace, stream=None) -> None:
     """Sequence b becomes what sequence parent[b] was (below 0: empty), up to its first keep[b] tokens; pages are shared."""
     _on_device(pool, stream)
-    _ok(load_library().climber_pages_fork(C.byref(pool), _ptr(parent), _ptr(keep), _ptr(status), _ptr(workspace), _nbytes(workspace), _stream(stream)),
-        "climber_pages_fork")
+    code = (_native or _load_native(load_library())).pages_fork(pool, parent, keep, status, workspace, stream)
+    if code is None:
+        code = load_library().climber_pages_fork(C.byref(pool), _ptr(parent), _ptr(keep), _ptr(status), _ptr(workspace), _nbytes(workspace),
+                                                 _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_pages_fork")
 
 
 def climber_pages_extend(pool: PagePool, rows, copies, counts, status, workspace, stream=None) -> None:
     """Pages for rows[b] more tokens of each sequence; shared pages that they go into are replaced, and copies says by which."""
     _on_device(pool, stream)
-    _ok(load_library().climber_pages_extend(C.byref(pool), _ptr(rows), _copies(copies, pool.n_seqs), _ptr(counts), _ptr(status), _ptr(workspace),
-                                            _nbytes(workspace), _stream(stream)), "climber_pages_extend")
+    _copies(copies, pool.n_seqs)
+    code = (_native or _load_native(load_library())).pages_extend(pool, rows, copies, counts, status, workspace, stream)
+    if code is None:
+        code = load_library().climber_pages_extend(C.byref(pool), _ptr(rows), _ptr(copies), _ptr(counts), _ptr(status), _ptr(workspace),
+                                                   _nbytes(workspace), _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_pages_extend")
 
 
 def climber_pages_compact(pool: PagePool, copies, counts, status, workspace, stream=None) -> None:
     """The pages in use move to the front of the pool; copies says which went where."""
     _on_device(pool, stream)
-    _ok(load_library().climber_pages_compact(C.byref(pool), _copies(copies, pool.n_pages // 2), _ptr(counts), _ptr(status), _ptr(workspace),
-                                             _nbytes(workspace), _stream(stream)), "climber_pages_compact")
+    _copies(copies, pool.n_pages // 2)
+    code = (_native or _load_native(load_library())).pages_compact(pool, copies, counts, status, workspace, stream)
+    if code is None:
+        code = load_library().climber_pages_compact(C.byref(pool), _ptr(copies), _ptr(counts), _ptr(status), _ptr(workspace), _nbytes(workspace),
+                                                    _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_pages_compact")
 
 
 def climber_paged_copy(cfg: Config, kv: PagedKV, copies, counts, max_copies: int, stream=None) -> None:
     """What climber_pages_extend or climber_pages_compact has left to copy, in one paged cache."""
     _on_device(kv, stream)
-    _ok(load_library().climber_paged_copy(C.byref(cfg), C.byref(kv), _copies(copies, 0), _ptr(counts), max_copies, _stream(stream)), "climber_paged_copy")
+    _copies(copies, 0)
+    code = (_native or _load_native(load_library())).paged_copy(cfg, kv, copies, counts, max_copies, stream)
+    if code is None:
+        code = load_library().climber_paged_copy(C.byref(cfg), C.byref(kv), _ptr(copies), _ptr(counts), max_copies, _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_paged_copy")
 
 
 def climber_paged8_copy(cfg: Config, kv8: PagedKV8, copies, counts, max_copies: int, stream=None) -> None:
     """climber_paged_copy in a cache in 8 bits."""
     _on_device(kv8, stream)
-    _ok(load_library().climber_paged8_copy(C.byref(cfg), C.byref(kv8), _copies(copies, 0), _ptr(counts), max_copies, _stream(stream)),
-        "climber_paged8_copy")
+    _copies(copies, 0)
+    code = (_native or _load_native(load_library())).paged8_copy(cfg, kv8, copies, counts, max_copies, stream)
+    if code is None:
+        code = load_library().climber_paged8_copy(C.byref(cfg), C.byref(kv8), _ptr(copies), _ptr(counts), max_copies, _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_paged8_copy")
 
 
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
@@ -713,13 +739,17 @@ def rotary(freq, rot_dims: int, interleaved: bool = False, scale: float = 1.0, i
 def climber_rotary(cfg: Config, rot: RotaryPlan, pos, n_kv_heads: int, q, k, q_out, k_out, stream=None) -> None:
     """Turn q and k rows by their positions (row r is [r] of the tensors, as many rows as q has; row pitches are taken from them)."""
     _on_device(rot, stream)
-    m, d, dk = q.shape[0], cfg.d_model, n_kv_heads * cfg.d_head
-    for t, wide in ((q, d), (q_out, d)) + (((k, dk), (k_out, dk)) if n_kv_heads else ()):
-        if t.shape[0] != m or t.numel() != m * wide:
-            raise ValueError("q, k, q_out and k_out have other rows")
-        if str(t.dtype) != ("torch.float32" if cfg.dtype == F32 else "torch.bfloat16"):
-            raise ValueError("q, k, q_out and k_out are of the configuration's type")
-    if str(pos.dtype) != "torch.int32" or not pos.is_contiguous() or pos.numel() != m:
+    if pos.numel() != q.shape[0] or str(pos.dtype) != "torch.int32" or not pos.is_contiguous():
         raise ValueError("pos is a contiguous int32 tensor with a position for each row")
-    _ok(load_library().climber_rotary(C.byref(cfg), C.byref(rot), _ptr(pos), m, n_kv_heads, _ptr(q), _pitch(q, d), _ptr(k), _pitch(k, dk), _ptr(q_out),
-                                      _pitch(q_out, d), _ptr(k_out), _pitch(k_out, dk), _stream(stream)), "climber_rotary")
+    code = (_native or _load_native(load_library())).rotary(cfg, rot, pos, n_kv_heads, q, k, q_out, k_out, stream)
+    if code is None:
+        m, d, dk = q.shape[0], cfg.d_model, n_kv_heads * cfg.d_head
+        for t, wide in ((q, d), (q_out, d)) + (((k, dk), (k_out, dk)) if n_kv_heads else ()):
+            if t.shape[0] != m or t.numel() != m * wide:
+                raise ValueError("q, k, q_out and k_out have other rows")
+            if str(t.dtype) != ("torch.float32" if cfg.dtype == F32 else "torch.bfloat16"):
+                raise ValueError("q, k, q_out and k_out are of the configuration's type")
+        code = load_library().climber_rotary(C.byref(cfg), C.byref(rot), _ptr(pos), m, n_kv_heads, _ptr(q), _pitch(q, d), _ptr(k), _pitch(k, dk),
+                                             _ptr(q_out), _pitch(q_out, d), _ptr(k_out), _pitch(k_out, dk), _stream(stream))
+    if code:
+        raise ClimberError(code, "climber_rotary")

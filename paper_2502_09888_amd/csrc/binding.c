@@ -1,4 +1,4 @@
-/* The attention entry points of include/climber.h, and the eviction, as Python calls, for callers whose calls are short: converts what a
+/* The attention entry points of include/climber.h, and those on pages and positions, as Python calls, for callers whose calls are short: converts what a
  * call passes (tensors, device pointers, None; numbers; ctypes structures) in C.  By ctypes the conversions took 1.6 of a call's 4.9 us on the
  * host (4.9 -> 3.6), and two fp32 calls of one small user 10.5 us as a pass for 8.3 in their kernels, 8.7 this way.
  *
@@ -19,6 +19,13 @@ static __typeof__(&climber_attn_sumi_paged) attn_sumi_paged_fn;
 static __typeof__(&climber_paged_evict) paged_evict_fn;
 static __typeof__(&climber_attn_history_paged8) attn_history_paged8_fn;
 static __typeof__(&climber_attn_sumi_paged8) attn_sumi_paged8_fn;
+static __typeof__(&climber_pages_fork) pages_fork_fn;
+static __typeof__(&climber_pages_extend) pages_extend_fn;
+static __typeof__(&climber_pages_compact) pages_compact_fn;
+static __typeof__(&climber_paged_copy) paged_copy_fn;
+static __typeof__(&climber_paged8_copy) paged8_copy_fn;
+static __typeof__(&climber_rotary) rotary_fn;
+static PyObject *pool_type, *rotary_type, *bf16_dtype, *f32_dtype, *s_dtype;
 static PyObject *config_type, *bias_type, *current_device, *raw_stream, *paged_type, *paged8_type, *s_data_ptr, *s_cuda_stream, *s_shape, *s_stride, *s_nbytes;
 
 static int unsigned_of(PyObject *o, void **p) /* takes the reference */
@@ -209,6 +216,141 @@ static PyObject *paged_evict(PyObject *m, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(code);
 }
 
+/* pool, n pointers, workspace, stream */
+static int pool_call(PyObject *const *a, Py_ssize_t n, int pointers, Py_buffer *pool, void **p, size_t *ws_bytes, void **s)
+{
+    if (n != pointers + 3 || !pool_type) return 0;
+    for (int i = 1; i <= pointers + 1; ++i)
+        if (!pointer(a[i], &p[i])) return 0;
+    return bytes_of(a[n - 2], ws_bytes) && stream_of(a[n - 1], s) && structure(a[0], pool_type, sizeof(climber_page_pool), pool);
+}
+static PyObject *pages_fork(PyObject *m, PyObject *const *a, Py_ssize_t n) /* parent, keep, status */
+{
+    Py_buffer pool;
+    void *p[5], *s;
+    size_t ws;
+    if (!pool_call(a, n, 3, &pool, p, &ws, &s)) return elsewhere();
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = pages_fork_fn(pool.buf, p[1], p[2], p[3], p[4], ws, s);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&pool);
+    return PyLong_FromLong(code);
+}
+static PyObject *pages_extend(PyObject *m, PyObject *const *a, Py_ssize_t n) /* rows, copies, counts, status */
+{
+    Py_buffer pool;
+    void *p[6], *s;
+    size_t ws;
+    if (!pool_call(a, n, 4, &pool, p, &ws, &s)) return elsewhere();
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = pages_extend_fn(pool.buf, p[1], p[2], p[3], p[4], p[5], ws, s);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&pool);
+    return PyLong_FromLong(code);
+}
+static PyObject *pages_compact(PyObject *m, PyObject *const *a, Py_ssize_t n) /* copies, counts, status */
+{
+    Py_buffer pool;
+    void *p[5], *s;
+    size_t ws;
+    if (!pool_call(a, n, 3, &pool, p, &ws, &s)) return elsewhere();
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = pages_compact_fn(pool.buf, p[1], p[2], p[3], p[4], ws, s);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&pool);
+    return PyLong_FromLong(code);
+}
+
+/* cfg, kv, copies, counts, max_copies, stream */
+static PyObject *copy(PyObject *const *a, Py_ssize_t n, int bits8)
+{
+    if (n != 6 || !paged8_type) return elsewhere();
+    Py_buffer cfg, kv;
+    void *copies, *counts, *s;
+    int32_t most;
+    if (!pointer(a[2], &copies) || !pointer(a[3], &counts) || !number(a[4], &most) || !stream_of(a[5], &s)) return elsewhere();
+    if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
+    if (bits8 ? !structure(a[1], paged8_type, sizeof(climber_paged_kv8), &kv) : !structure(a[1], paged_type, sizeof(climber_paged_kv), &kv))
+        return PyBuffer_Release(&cfg), elsewhere();
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = bits8 ? paged8_copy_fn(cfg.buf, kv.buf, copies, counts, most, s) : paged_copy_fn(cfg.buf, kv.buf, copies, counts, most, s);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&cfg);
+    PyBuffer_Release(&kv);
+    return PyLong_FromLong(code);
+}
+static PyObject *paged_copy(PyObject *m, PyObject *const *a, Py_ssize_t n) { return copy(a, n, 0); }
+static PyObject *paged8_copy(PyObject *m, PyObject *const *a, Py_ssize_t n) { return copy(a, n, 1); }
+
+/* A tensor of m (or, -1, any number of) rows of `width` elements of a type: its pointer and pitch. */
+static int rows_of(PyObject *o, int64_t width, PyObject *dtype, int64_t *m, void **p, int64_t *ld)
+{
+    PyObject *t = PyObject_GetAttr(o, s_dtype), *shape = t == dtype ? PyObject_GetAttr(o, s_shape) : NULL;
+    int ok = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) > 0;
+    if (ok) {
+        int64_t inner = 1;
+        for (Py_ssize_t i = PyTuple_GET_SIZE(shape) - 1; i > 0; --i) inner *= PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+        const int64_t rows = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0));
+        if (*m < 0) *m = rows;
+        ok = rows == *m && inner == width && !PyErr_Occurred();
+    }
+    Py_XDECREF(t);
+    Py_XDECREF(shape);
+    return ok && pitch(o, width, ld) && pointer(o, p);
+}
+
+/* cfg, plan, pos (its pointer: checked by the caller), n_kv_heads, q, k, q_out, k_out, stream */
+static PyObject *rotary(PyObject *m, PyObject *const *a, Py_ssize_t n)
+{
+    if (n != 9 || !rotary_type) return elsewhere();
+    Py_buffer cfg, plan;
+    void *pos, *p[4] = {NULL, NULL, NULL, NULL}, *s;
+    int32_t n_kv;
+    int64_t rows = -1, ld[4] = {0, 0, 0, 0};
+    if (!number(a[3], &n_kv) || n_kv < 0 || !stream_of(a[8], &s) || !structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
+    if (!structure(a[1], rotary_type, sizeof(climber_rotary_plan), &plan)) return PyBuffer_Release(&cfg), elsewhere();
+    const climber_config *c = cfg.buf;
+    const int64_t wide = c->d_model, kv_wide = (int64_t)n_kv * c->d_head;
+    PyObject *dtype = c->dtype == CLIMBER_BF16 ? bf16_dtype : f32_dtype;
+    int ok = rows_of(a[4], wide, dtype, &rows, &p[0], &ld[0]) && rows_of(a[6], wide, dtype, &rows, &p[2], &ld[2]);
+    if (ok && n_kv) ok = rows_of(a[5], kv_wide, dtype, &rows, &p[1], &ld[1]) && rows_of(a[7], kv_wide, dtype, &rows, &p[3], &ld[3]);
+    ok = ok && pointer(a[2], &pos);
+    int code = 0;
+    if (ok) {
+        Py_BEGIN_ALLOW_THREADS
+        code = rotary_fn(c, plan.buf, pos, rows, n_kv, p[0], ld[0], p[1], ld[1], p[2], ld[2], p[3], ld[3], s);
+        Py_END_ALLOW_THREADS
+    }
+    PyBuffer_Release(&cfg);
+    PyBuffer_Release(&plan);
+    return ok ? PyLong_FromLong(code) : elsewhere();
+}
+
+/* bind_pages(addresses of fork, extend, compact, the two copies and rotary, PagePool, RotaryPlan, torch.bfloat16, torch.float32) */
+static PyObject *bind_pages(PyObject *m, PyObject *args)
+{
+    unsigned long long f[6];
+    PyObject *t[4];
+    if (!PyArg_ParseTuple(args, "KKKKKKO!O!OO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &PyType_Type, &t[0], &PyType_Type, &t[1], &t[2], &t[3])) return NULL;
+    pages_fork_fn = (__typeof__(pages_fork_fn))(uintptr_t)f[0];
+    pages_extend_fn = (__typeof__(pages_extend_fn))(uintptr_t)f[1];
+    pages_compact_fn = (__typeof__(pages_compact_fn))(uintptr_t)f[2];
+    paged_copy_fn = (__typeof__(paged_copy_fn))(uintptr_t)f[3];
+    paged8_copy_fn = (__typeof__(paged8_copy_fn))(uintptr_t)f[4];
+    rotary_fn = (__typeof__(rotary_fn))(uintptr_t)f[5];
+    PyObject **const to[4] = {&pool_type, &rotary_type, &bf16_dtype, &f32_dtype};
+    for (int i = 0; i < 4; ++i) {
+        PyObject *was = *to[i];
+        *to[i] = Py_NewRef(t[i]);
+        Py_XDECREF(was);
+    }
+    Py_RETURN_NONE;
+}
+
 /* bind(addresses of the four entry points, Config, RelBias, torch.cuda.current_device, torch's raw current stream
  *      [, addresses of the three on a paged cache, PagedKV[, of the two on one in 8 bits, PagedKV8]]) */
 static PyObject *bind(PyObject *m, PyObject *args)
@@ -250,6 +392,13 @@ static PyMethodDef methods[] = {
     {"attn_sumi_paged", (PyCFunction)(void (*)(void))attn_sumi_paged, METH_FASTCALL, NULL},
     {"attn_history_paged8", (PyCFunction)(void (*)(void))attn_history_paged8, METH_FASTCALL, NULL},
     {"attn_sumi_paged8", (PyCFunction)(void (*)(void))attn_sumi_paged8, METH_FASTCALL, NULL},
+    {"bind_pages", bind_pages, METH_VARARGS, NULL},
+    {"pages_fork", (PyCFunction)(void (*)(void))pages_fork, METH_FASTCALL, NULL},
+    {"pages_extend", (PyCFunction)(void (*)(void))pages_extend, METH_FASTCALL, NULL},
+    {"pages_compact", (PyCFunction)(void (*)(void))pages_compact, METH_FASTCALL, NULL},
+    {"paged_copy", (PyCFunction)(void (*)(void))paged_copy, METH_FASTCALL, NULL},
+    {"paged8_copy", (PyCFunction)(void (*)(void))paged8_copy, METH_FASTCALL, NULL},
+    {"rotary", (PyCFunction)(void (*)(void))rotary, METH_FASTCALL, NULL},
     {"paged_evict", (PyCFunction)(void (*)(void))paged_evict, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL}};
 
@@ -262,5 +411,6 @@ PyMODINIT_FUNC PyInit__native(void)
     s_shape = PyUnicode_InternFromString("shape");
     s_stride = PyUnicode_InternFromString("stride");
     s_nbytes = PyUnicode_InternFromString("nbytes");
-    return s_data_ptr && s_cuda_stream && s_shape && s_stride && s_nbytes ? PyModule_Create(&module) : NULL;
+    s_dtype = PyUnicode_InternFromString("dtype");
+    return s_dtype && s_data_ptr && s_cuda_stream && s_shape && s_stride && s_nbytes ? PyModule_Create(&module) : NULL;
 }

@@ -139,7 +139,7 @@ __global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
 
 // ---- extend --------------------------------------------------------------------------------------
 constexpr int kFewSeqs = 1024, kFewUnits = 64, kListPages = 4096;  // what one workgroup takes; free pages that it keeps in LDS
-constexpr int kCompactFew = 256;
+constexpr int kCompactFew = 32;  // (256 sequences of 32 pages: 33 us by one workgroup, 17.5 in three launches; 2 of 3: 6 / 8)
 constexpr int kNobody = 1 << 30;  // in last[]: a shared page that none of its writers keeps (n_seqs is less)
 
 // Sequence b's part of the call: pages [first, shared_to) that it holds and writes, [shared_to, need) that it has to get.
