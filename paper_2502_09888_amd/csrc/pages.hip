@@ -138,7 +138,7 @@ __global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
 }
 
 // ---- extend --------------------------------------------------------------------------------------
-constexpr int kFewSeqs = 1024, kFewUnits = 64, kListPages = 4096;  // what one workgroup takes; free pages that it keeps in LDS
+constexpr int kFewSeqs = 1024, kFewUnits = 64, kFewWriters = 512, kListPages = 4096;  // what one workgroup takes; free pages that it keeps in LDS
 constexpr int kCompactFew = 32;  // (256 sequences of 32 pages: 33 us by one workgroup, 17.5 in three launches; 2 of 3: 6 / 8)
 constexpr int kNobody = 1 << 30;  // in last[]: a shared page that none of its writers keeps (n_seqs is less)
 
@@ -316,19 +316,24 @@ __global__ __launch_bounds__(256) void extend_write_kernel(const ExtendArgs a)
     if (lane == 0 && x.need > had) a.held[b] = x.need;
 }
 
-// All of it by one workgroup, a thread for each sequence: what it needs of its first page is requested with the bits of free pages, and the free
-// pages that are handed out stay in LDS.
+// All of it by one workgroup, a thread for each sequence; bound by its trips to memory, one behind the other: what a sequence needs, its
+// pages, what their refs are (the pool's are looked through meanwhile).  Who else writes a shared page is found in LDS where that is few
+// (one history forked four ways for each of 32 users, 128 writers: the call 10.5 us with counts in memory, 9 this way), and so are the pages handed out.
 __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
 {
-    __shared__ int sums[3][16], list[kListPages];
+    __shared__ int sums[3][16], list[kListPages], unit_at[kFewUnits + 1], n_listed, problems;
+    // a table of shared pages that are written, at most half full: page, its writers, the last of them
+    __shared__ int key[2 * kFewWriters], n_writers[2 * kFewWriters], last_writer[2 * kFewWriters];
     __shared__ uint64_t words[kFewUnits * 16];
-    __shared__ int unit_at[kFewUnits + 1];
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, units = (int)pool_units(a.n_pages), b = t;
     const bool mine = b < a.n_seqs;
     Need x{};
     int had = 0;
     if (mine) x = need_of(a, b), had = held_of(a, b);
+    if (t == 0) n_listed = 0, problems = 0;
+    if (t < 2 * kFewWriters) key[t] = -1, n_writers[t] = 0, last_writer[t] = -1;
     int32_t *const row = a.table + (int64_t)b * a.table_ld;
+    auto place = [](int page) { return (int)((uint32_t)page * 2654435769u >> 16) % (2 * kFewWriters); };
     // bits and counts of the units
     int n_used = 0;
     for (int u = wave; u < units; u += 16) {
@@ -348,43 +353,28 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
         }
         if (lane == 0) unit_at[u] = n_free;
     }
+    __syncthreads();
     // shared pages that are written
-    bool shared = false, bad = false;
+    bool shared = false;
+    int bad = x.too_long;
     for (int i = x.first; i < x.shared_to; ++i) {
         const int page = row[i];
-        if (!in_pool(a, page)) bad = true;
-        else {
-            shared |= a.refs[page] > 1;
-            a.writers[page] = 0, a.last[page] = -1;
+        if (!in_pool(a, page)) {
+            bad |= 2;
+        } else {
+            if (a.refs[page] > 1) {
+                if (atomicAdd(&n_listed, 1) < kFewWriters) {
+                    int at = place(page);
+                    for (int k; (k = atomicCAS(key + at, -1, page)) != -1 && k != page;) at = (at + 1) % (2 * kFewWriters);
+                    atomicAdd(n_writers + at, 1);
+                    atomicMax(last_writer + at, b);
+                }
+                shared = true;
+            }
+            a.writers[page] = 0, a.last[page] = -1;  // (for more of them than the list has room for)
         }
     }
-    if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
-    const bool any_shared = __syncthreads_or(shared);
-    int c = max(0, x.need - max(x.shared_to, had)), copy = 0;
-    if (any_shared) {
-        if (shared)
-            for (int i = x.first; i < x.shared_to; ++i) {
-                const int page = row[i];
-                if (in_pool(a, page) && a.refs[page] > 1) atomicAdd(a.writers + page, 1), atomicMax(a.last + page, b);
-            }
-        __syncthreads();
-        if (shared)
-            for (int i = x.first; i < x.shared_to; ++i) {
-                if (!moves(a, b, row[i])) continue;
-                ++c;
-                copy |= i == x.first && x.part > 0;
-            }
-    }
-    const bool too_long = mine && x.too_long;
-    int all_new, all_copies, at = wave_before(c, all_new), at_copy = wave_before(copy, all_copies);
-    if (lane == 0) sums[0][wave] = all_new, sums[1][wave] = all_copies, sums[2][wave] = n_used;
-    const bool refused = __syncthreads_or(bad), full_row = __syncthreads_or(too_long);
-    int total = 0, n_copies = 0, in_use = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        if (i < wave) at += sums[0][i], at_copy += sums[1][i];
-        total += sums[0][i], n_copies += sums[1][i], in_use += sums[2][i];
-    }
+    if (bad) atomicOr(&problems, bad);
     int n_free = 0;
     if (wave == 0) {
         const int f = lane < units ? unit_at[lane] : 0, before = wave_before(f, n_free);
@@ -392,14 +382,61 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
         if (lane == 0) unit_at[units] = n_free;
     }
     __syncthreads();
-    n_free = unit_at[units];
-    const bool full = full_row || total > n_free, go = !full && !refused;
+    const int listed = n_listed;
+    const bool in_list = listed <= kFewWriters;
+    if (!in_list) {
+        if (shared)
+            for (int i = x.first; i < x.shared_to; ++i) {
+                const int page = row[i];
+                if (in_pool(a, page) && a.refs[page] > 1) atomicAdd(a.writers + page, 1), atomicMax(a.last + page, b);
+            }
+        __syncthreads();
+    }
+    // whether the sequence's page i is shared and does not stay with it
+    auto goes = [&](int page) {
+        if (!in_list) return moves(a, b, page);
+        if (!in_pool(a, page)) return false;
+        const int r = a.refs[page];
+        if (r <= 1) return false;
+        int at = place(page);
+        while (key[at] != page) {
+            if (key[at] == -1) return false;  // (not in the table: its refs were others a moment ago)
+            at = (at + 1) % (2 * kFewWriters);
+        }
+        return !(n_writers[at] == r && last_writer[at] == b);
+    };
+    int c = max(0, x.need - max(x.shared_to, had)), copy = 0;
+    uint64_t which = 0;  // of the first 64 pages that are written, those that go; of those behind them the entry itself says it, as ~page
+    if (shared && !(problems & 2))
+        for (int i = x.first; i < x.shared_to; ++i) {
+            if (!goes(row[i])) continue;
+            ++c;
+            copy |= i == x.first && x.part > 0;
+            if (i - x.first < 64) which |= 1ull << (i - x.first);
+            else row[i] = ~row[i];
+        }
+    int all_new, all_copies, at = wave_before(c, all_new), at_copy = wave_before(copy, all_copies);
+    if (lane == 0) sums[0][wave] = all_new, sums[1][wave] = all_copies, sums[2][wave] = n_used;
+    __syncthreads();
+    int total = 0, n_copies = 0, in_use = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        if (i < wave) at += sums[0][i], at_copy += sums[1][i];
+        total += sums[0][i], n_copies += sums[1][i], in_use += sums[2][i];
+    }
+    const bool full = (problems & 1) || total > unit_at[units], go = !full && !(problems & 2);
     if (t == 0) {
-        if (full) atomicOr(a.status, CLIMBER_POOL_FULL);
+        const int found = (full ? CLIMBER_POOL_FULL : 0) | (problems & 2 ? CLIMBER_BAD_PAGE : 0);
+        if (found) atomicOr(a.status, found);
         a.counts[0] = go ? n_copies : 0;
         a.counts[1] = in_use + (go ? total : 0);
     }
-    if (!go) return;
+    if (!go) {
+        if (shared && !(problems & 2))
+            for (int i = x.first + 64; i < x.shared_to; ++i)
+                if (row[i] < 0) row[i] = ~row[i];
+        return;
+    }
     for (int u = wave; u < units; u += 16) {
         int to0 = unit_at[u];
         if (to0 >= total) break;
@@ -415,18 +452,12 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
             to0 += __popcll(w);
         }
     }
-    // refs change from the barrier on: whether a page stays with the last of its writers is noted before
-    if (shared)
-        for (int i = x.first; i < x.shared_to; ++i) {
-            const int page = row[i];
-            if (a.refs[page] > 1 && fresh(a.writers + page) != a.refs[page]) atomicOr(a.last + page, kNobody);
-        }
-    __syncthreads();
+    __syncthreads();  // (and all have made up their minds: refs change from here on)
     auto take = [&](int i) { return i < kListPages ? list[i] : fresh(a.free_list + i); };
     if (shared)
         for (int i = x.first; i < x.shared_to; ++i) {
-            const int page = row[i], last = fresh(a.last + page);
-            if (last < 0 || last == b) continue;
+            const int e = row[i], page = e < 0 ? ~e : e;
+            if (i - x.first < 64 ? !((which >> (i - x.first)) & 1) : e >= 0) continue;
             const int to = take(at++);
             row[i] = to;
             a.refs[to] = 1;

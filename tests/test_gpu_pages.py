@@ -73,6 +73,33 @@ def test_the_last_of_all_writers_keeps_a_shared_page(n):
                 assert len(copies) == n
 
 
+@pytest.mark.parametrize("n_seqs", [3, 300, 1500])
+@pytest.mark.parametrize("writers", [1, 2, 3])
+def test_many_shared_pages_are_written_at_once(n_seqs, writers):
+    # three sequences hold the same 150 pages, and tokens are taken back by their lengths alone; hundreds of others may have one each
+    for free, served in ((150 * writers + 2 * n_seqs, True), (100 * (writers - 1) + 40, False)):
+        host = Pool(150 + n_seqs + free, 16, n_seqs, 160)
+        for i in range(150):
+            host.table[0][i] = 3 + i
+            host.refs[3 + i] = 1
+        host.held[0], host.len[0] = 150, 2400
+        host.fork([0 if b < 3 else b for b in range(n_seqs)])
+        for b in range(3, n_seqs):                        # (all share one page, in which each writes)
+            host.table[b][0], host.held[b], host.len[b] = 153, 1, 5
+        host.refs[153] = n_seqs - 3
+        for b in range(3):
+            host.len[b] = 20 + b
+        rows = [2000 if b < writers else 0 if b < 3 else 1 for b in range(n_seqs)]
+        dev = DevicePool(host)
+        before = [list(x) for x in host.table]
+        copies = host.extend(rows)
+        assert (copies is not None) == served or not served and n_seqs == 3 and writers == 1
+        if copies is None:
+            assert host.table == before
+        dev.extend(rows)
+        dev.check(copies or [])
+
+
 def test_a_call_that_cannot_be_served_changes_nothing():
     host = Pool.random(3, 40, 16, 5, 12)
     for rows in ([10 ** 4, 0, 0, 0, 1], [2 ** 31 - 1] * 5, [1, 1, 1, 12 * 16, 1]):
