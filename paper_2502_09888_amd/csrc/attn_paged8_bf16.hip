@@ -139,19 +139,35 @@ static __device__ __forceinline__ KFrags<D> read_k_wide(const lds_u8 *base, int 
 }
 
 // ---- tiles ---------------------------------------------------------------------------------------
-// 4 waves of QB x 32 packed rows share the keys.  Cached blocks of 32 keys: each wave brings 8 keys and their values as codes, by copies that are
-// four to five blocks ahead, into a place that only it reads; two blocks ahead it makes bf16 rows of its keys, one block ahead of its values, in
-// buffers that all waves take their fragments from.  The codes are widened once for 128 or 256 rows that way.  The call's own rows
-// follow as in the bf16 paged cache, in the same LDS.
+// A block of 32 keys and their values as codes in LDS: 1 KiB of keys and of values of each wave's 8 keys, or (D = 64) one of both; pieces of a
+// row permuted as in Rows8.
+template <int D>
+struct Block8 {
+    static constexpr int kValues = D == 64 ? 512 : 4096, kGroup = 2048;  // from a key to its value; from 16 rows to the next
+    static __device__ __forceinline__ int row(int r) { return D == 64 ? (r >> 3) * 1024 + (r & 7) * 64 : r * 128; }
+    uint32_t k_at[D / 32], v_at[D / 32];
+    __device__ __forceinline__ void init(int lane)
+    {
+        const int l32 = lane & 31, hf = lane >> 5, G = lane >> 4, i16 = lane & 15, j = i16 >> 1, r = 8 * (j >> 2) + 4 * (G >> 1) + (j & 3);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+            k_at[e] = row(l32) + ((2 * e + hf) ^ Rows8<D>::f(l32)) * 16;
+            v_at[e] = kValues + row(r) + ((2 * e + (G & 1)) ^ Rows8<D>::f(r)) * 16 + 8 * (i16 & 1);
+        }
+    }
+};
+
+// 4 waves of QB x 32 packed rows share the keys.  Cached blocks of 32 keys travel as codes, by copies that are two blocks ahead, and each wave
+// widens the fragments that it takes from them: half the bytes through LDS, which all eight waves of a CU read their operands from.
+// The call's own rows follow as in the bf16 paged cache, in the same LDS.
 template <int D, int QB, bool SUMI>
 __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Args p)
 {
     using R = Rows<D>;
     constexpr int kRows = 128 * QB, kValues = 32 * R::kPitch;
     constexpr int kShare = 8 * R::kPitch, kCopies = kShare / 1024;  // own rows: a wave's part of either; copies of it
-    constexpr int kCopies8 = D / 64, kSlot = 16 * D;                // codes: copies of a wave's part of a block, keys and values; their bytes
-    // (arrays of their own: reads of one do not wait for copies into another.)  Codes in 0 .. 3, keys in 4 and 5, values in 6 and 7; own rows: keys
-    // and values of stage i in 2 i and 2 i + 1.
+    constexpr int kCopies8 = D / 64;                                // codes: copies of a wave's part of a block
+    // (arrays of their own: reads of one do not wait for copies into another.)  Codes in 0 .. 3; own rows: keys and values of stage i in 2 i and 2 i + 1.
     __shared__ __attribute__((aligned(1024))) uint8_t a0[kValues], a1[kValues], a2[kValues], a3[kValues], a4[kValues], a5[kValues], a6[kValues], a7[kValues];
     __shared__ int flags[4];
     auto room = [&](int i) __attribute__((always_inline)) {
@@ -173,65 +189,68 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
     // cached keys: all rows see them
     const int c_lo = min(k_lo, s.n), c_hi = min(k_hi, s.n), n_blocks = (c_hi - c_lo + 31) / 32, n_whole = (c_hi - c_lo) / 32;
 
-    const int k_mine = c_lo + (wave >> 1) * 16;  // this wave's group of 16 keys of block 0
     const Source8<D> src(p, w.b, w.hk, c_hi, lane);
-    // page numbers and scales of 64 of the wave's groups, one in each lane, and of the 64 after them
-    const int first_pages = src.page_number(k_mine + lane * 32), next_pages = src.page_number(k_mine + (64 + lane) * 32);
+    // page numbers and scales of 32 blocks: the lower 32 lanes have those of the first 16 keys, the upper those of the others; of the 32 after them
+    const int k_mine = c_lo - hf * (32 * 32 - 16);
+    const int first_pages = src.page_number(k_mine + lane * 32), next_pages = src.page_number(k_mine + (32 + lane) * 32);
     const uint32_t first_scales = src.scales(k_mine + lane * 32, first_pages);
     int pages = first_pages, pages_next = next_pages;
-    uint32_t scales = first_scales, scales_next = first_scales, held = 0;
-    // this lane's 16 codes of the wave's 8 keys, or (D = 64, upper half) of their values: from its place in a page, in LDS, as 32 bytes of a row
-    const int part = D == 64 ? lane & 31 : lane, x8 = part / (D / 16), piece = part % (D / 16);
-    // (16 lanes have rows whose pieces of even numbers lie in different places of the banks: 0 and 4, or 0, 1, 4 and 5)
-    const int row8 = D == 64 ? (x8 & 1) | (x8 & 2) << 1 | (x8 & 4) >> 1 : (x8 & 1) << 2 | x8 >> 1;
-    const uint32_t page_off = ((wave & 1) * 8 + row8) * D + piece * 16;
-    const int row32 = (wave >> 1) * 16 + (wave & 1) * 8 + row8, to_row = row32 * R::kPitch;
-    const int to_a = to_row + ((2 * piece) ^ R::f(row32)) * 16, to_b = to_row + ((2 * piece + 1) ^ R::f(row32)) * 16;
-    auto issue = [&](int j, lds_u8 *slot) __attribute__((always_inline)) {
-        if ((j & 63) == 0 && j > 0) {
+    uint32_t scales = first_scales, scales_next = first_scales;
+    // this lane's 16 codes of the wave's 8 keys, or (D = 64, upper half) of their values, in a page
+    const int part = D == 64 ? lane & 31 : lane, row16 = (wave & 1) * 8 + part / (D / 16);
+    const uint32_t page_off = row16 * D + ((part % (D / 16)) ^ Rows8<D>::f(row16)) * 16;
+    auto issue = [&](int j, lds_u8 *stage) __attribute__((always_inline)) {
+        if ((j & 31) == 0 && j > 0) {
             pages = pages_next;
-            pages_next = src.page_number(k_mine + (j + 64 + lane) * 32);
+            pages_next = src.page_number(k_mine + (j + 32 + lane) * 32);
         }
-        const int page = __builtin_amdgcn_readlane(pages, j & 63), g = k_mine + j * 32;
+        const int page = __builtin_amdgcn_readlane(pages, (wave >> 1) * 32 + (j & 31)), g = c_lo + j * 32 + (wave >> 1) * 16;
         const uint8_t *k = uniform(src.k_page + page * src.page_bytes + (g & ((1 << p.page_shift) - 1)) * D);
         if constexpr (D == 64) {
-            copy16((glb_u8 *)(k + (lane >= 32 ? src.to_v : 0)) + page_off, slot + wave * kSlot);
+            copy16((glb_u8 *)(k + (lane >= 32 ? src.to_v : 0)) + page_off, stage + wave * 1024);
         } else {
-            copy16((glb_u8 *)k + page_off, slot + wave * kSlot);
-            copy16((glb_u8 *)uniform(k + src.to_v) + page_off, slot + wave * kSlot + 1024);
+            copy16((glb_u8 *)k + page_off, stage + wave * 1024);
+            copy16((glb_u8 *)uniform(k + src.to_v) + page_off, stage + Block8<D>::kValues + wave * 1024);
         }
     };
-    // the scales of block j's group: to be asked for once for each block, in order
+    // the scales of a block's two groups: to be asked for once for each block, in order
+    struct Scales {
+        uint32_t a, b;
+    };
     auto scales_of = [&](int j) __attribute__((always_inline)) {
-        if ((j & 63) == 0 && j > 0) scales = scales_next;
-        if ((j & 63) == 32) scales_next = src.scales(k_mine + ((j & ~63) + 64 + lane) * 32, pages_next);
-        return (uint32_t)__builtin_amdgcn_readlane(scales, j & 63);
+        if ((j & 31) == 0 && j > 0) scales = scales_next;
+        if ((j & 31) == 16) scales_next = src.scales(k_mine + ((j & ~31) + 32 + lane) * 32, pages_next);
+        return Scales{(uint32_t)__builtin_amdgcn_readlane(scales, j & 31), (uint32_t)__builtin_amdgcn_readlane(scales, 32 + (j & 31))};
     };
-    auto widen = [&](u32x4 x, float scale, lds_u8 *to) __attribute__((always_inline)) {
-        *(__attribute__((address_space(3))) u32x4 *)(to + to_a) = wide8(u32x2{x.x, x.y}, scale);
-        *(__attribute__((address_space(3))) u32x4 *)(to + to_b) = wide8(u32x2{x.z, x.w}, scale);
-    };
-    // the wave's keys in one slot and values in another become bf16 rows; the first `n` of each, zeros behind them
-    auto widen_both = [&](lds_u8 *key_slot, uint32_t key_scales, lds_u8 *keys, lds_u8 *value_slot, uint32_t value_scales, lds_u8 *values, bool here)
-                          __attribute__((always_inline)) {
-        const int mine = wave * kSlot + lane * 16;
-        if constexpr (D == 64) {  // (a half-wave has either)
-            u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)((hf ? value_slot : key_slot) + mine);
-            if (!here) x = u32x4{0, 0, 0, 0};
-            widen(x, scale_of(hf ? value_scales >> 8 : key_scales), hf ? values : keys);
-        } else {
-            u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)(key_slot + mine), y = *(const __attribute__((address_space(3))) u32x4 *)(value_slot + mine + 1024);
-            if (!here) x = y = u32x4{0, 0, 0, 0};
-            widen(x, scale_of(key_scales), keys);
-            widen(y, scale_of(value_scales >> 8), values);
+    Block8<D> at8;
+    at8.init(lane);
+    auto keys_of = [&](lds_u8 *stage, const Scales &sc) __attribute__((always_inline)) {
+        const float scale = scale_of(l32 < 16 ? sc.a : sc.b);
+        KFrags<D> f;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+            const u32x4 x = *(const __attribute__((address_space(3))) u32x4 *)(stage + at8.k_at[e]);
+            f.a[2 * e] = frag(wide8(u32x2{x.x, x.y}, scale));
+            f.a[2 * e + 1] = frag(wide8(u32x2{x.z, x.w}, scale));
         }
+        return f;
+    };
+    auto values_of = [&](lds_u8 *stage, int g, const Scales &sc, u32x2 keep) __attribute__((always_inline)) {
+        const float scale = scale_of((g ? sc.b : sc.a) >> 8);
+        VFrags<D> f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2 *)(stage + g * Block8<D>::kGroup + at8.v_at[db])));
+            f.a[db] = wide8(x & keep, scale);
+        }
+        return f;
     };
 
     Rows<D> at;
     at.init(lane);
-    State<D, QB> st;
+    State<D, QB, true> st;
     auto start = [&]() __attribute__((always_inline)) {
-        typename State<D, QB>::Row in[QB];
+        typename State<D, QB, true>::Row in[QB];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             const int r = min(r_wave + qb * 32 + l32, rows - 1);
@@ -240,14 +259,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
         if (n_blocks > 0) issue(0, room(0));
         if (n_blocks > 1) issue(1, room(1));
         if (n_blocks > 2) issue(2, room(2));
-        if (n_blocks > 3) issue(3, room(3));
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) st.template start<SUMI>(p, qb, hf, in[qb], w.split == 0);
     };
     // this wave's copies have landed but for those of `later` blocks, the last ones issued
     auto landed8 = [&](int later) __attribute__((always_inline)) {
-        if (later >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * kCopies8) : "memory");
-        else if (later == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies8) : "memory");
+        if (later >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies8) : "memory");
         else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kCopies8) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
@@ -256,7 +273,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
         else if (later == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kCopies) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
-    // (with this wave's reads and writes of LDS done: behind the barrier others write to what it has read, and read what it has written)
+    // (with this wave's reads of a stage done: behind the barrier others copy into it)
     auto meet = [&]() __attribute__((always_inline)) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
@@ -288,34 +305,27 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
         if (!again && n_whole > 0) {
             f32x16 S0[QB], S1[QB];
             bf16x8 P[QB][2];
-            landed8(min(n_blocks - 2, 2));
-            held = scales_of(0);
-            uint32_t next = n_whole > 1 ? scales_of(1) : held;
-            widen_both(room(0), held, room(4), room(0), held, room(6), true);
-            if (n_whole > 1) widen_both(room(1), next, room(5), room(0), held, room(6), true);
-            held = next;
+            landed8(min(n_blocks - 1, 2));
             meet();
-            st.logits(read_k<D>(at, room(4)), S0);
+            Scales held = scales_of(0);
+            st.logits(keys_of(room(0), held), S0);
             st.reference(S0);
-            // block j (i = j % 4): its logits in Sc; behind the barrier the keys of block j + 1 and its own values are there, nobody reads the keys of
-            // block j or the values of block j - 1 any more, and their places are filled
+            // block j (i = j % 4): its logits in Sc, its values and the next one's keys behind the barrier, where nobody reads block j - 1 any more
             auto step = [&](int j, int i, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
-                landed8(min(1, n_blocks - 3 - j));
+                landed8(min(1, n_blocks - 2 - j));
                 meet();
-                if (j + 4 < n_blocks) issue(j + 4, room(i));
-                next = held;
-                if (j + 2 < n_whole) next = scales_of(j + 2);
-                const KFrags<D> k = read_k<D>(at, room(4 + ((i + 1) & 1)));
+                if (j + 3 < n_blocks) issue(j + 3, room((i + 3) & 3));
+                Scales next = held;
+                if (j + 1 < n_whole) next = scales_of(j + 1);
+                const KFrags<D> k = keys_of(room((i + 1) & 3), next);
                 __builtin_amdgcn_sched_barrier(0);
                 st.weights(Sc, P, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                // (from here on the matrix pipe has work: before the other wave of the SIMD, which makes its exponentials meanwhile.  us without / with:
-                // sessions 122.8 / 118.9, scoring 102.6 / 101.5, ragged scoring 143.6 / 142.1)
+                // (from here on the matrix pipe has work: before the other wave of the SIMD, which makes its exponentials meanwhile)
                 __builtin_amdgcn_s_setprio(1);
-                st.logits(k, Sn);  // (behind the last block: not used, as what is widened then)
+                st.logits(k, Sn);  // (behind the last block: not used)
                 st.weights(Sc, P, 1);
-                const VFrags<D> v0 = read_v<D>(at, room(6 + (i & 1))), v1 = read_v<D>(at, room(6 + (i & 1)) + 16 * R::kPitch);
-                widen_both(room((i + 2) & 3), next, room(4 + (i & 1)), room((i + 1) & 3), held, room(6 + ((i + 1) & 1)), true);
+                const VFrags<D> v0 = values_of(room(i), 0, held, u32x2{~0u, ~0u}), v1 = values_of(room(i), 1, held, u32x2{~0u, ~0u});
                 held = next;
                 __builtin_amdgcn_sched_barrier(0x40f);
                 st.add(v0, P, 0);
@@ -338,25 +348,28 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
         // the block that is not whole, and all of them again
 #pragma unroll 1
         for (int j = again ? 0 : n_whole; j < n_blocks; ++j) {
-            landed8(again || n_whole == 0 ? min(3, n_blocks - 1 - j) : 0);
-            const uint32_t sc = scales_of(j);
-            lds_u8 *const keys = room(4 + (j & 1)), *const values = room(6 + (j & 1)), *const slot = room(j & 3);
-            widen_both(slot, sc, keys, slot, sc, values, c_lo + j * 32 + row32 < c_hi);  // (codes behind the cached keys may be no numbers)
+            lds_u8 *const stage = room(j & 3);
+            landed8(min(2, n_blocks - 1 - j));
             meet();
-            if (again && j + 4 < n_blocks) issue(j + 4, slot);
+            if (j + 3 < n_blocks) issue(j + 3, room((j + 3) & 3));
+            const Scales sc = scales_of(j);
+            const int k0 = c_lo + j * 32;
             f32x16 S[QB];
             bf16x8 P[QB][2];
             bool may[QB];
-            st.logits(read_k<D>(at, keys), S);
+            st.logits(keys_of(stage, sc), S);
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) {
-                hide(S[qb], c_lo + j * 32, hf, c_hi);
+                hide(S[qb], k0, hf, c_hi);
                 may[qb] = j >= n_whole || j == 0 || far[qb];
             }
             st.reference(S, may);
             st.weights(S, P);
 #pragma unroll
-            for (int g = 0; g < 2; ++g) st.add(read_v<D>(at, values + g * 16 * R::kPitch), P, g);
+            for (int g = 0; g < 2; ++g) {
+                const int left = c_hi - (k0 + 16 * g + 4 * hf);  // (codes of hidden keys may be no numbers)
+                st.add(values_of(stage, g, sc, u32x2{first_bytes(left), first_bytes(left - 8)}), P, g);
+            }
         }
         if constexpr (!SUMI) {
             const Source<D, kCopies> rows_src(p, own, w.b, w.hk, n_hi, lane, (wave & 1) * kCopies);
@@ -374,14 +387,14 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
                 bf16x8 P[QB][2];
                 landed(min(n_new - 1, 2));
                 meet();
-                st.logits(read_k<D>(at, room(0)), S0);
+                st.logits(read_k_wide<D>(room(0), lane), S0);
                 st.reference(S0);
                 auto step = [&](int j, int i, f32x16 (&Sc)[QB], f32x16 (&Sn)[QB]) __attribute__((always_inline)) {
                     landed(min(1, n_new - 2 - j));
                     meet();  // block j + 1 is here, and nobody reads block j - 1 any more
                     if (j + 3 < n_new)
                         rows_src.issue(n_lo + (wave >> 1) * 16 + (j + 3) * 32, 0, room(2 * ((i + 3) & 3)) + wave * kShare, room(2 * ((i + 3) & 3) + 1) + wave * kShare);
-                    const KFrags<D> k = read_k<D>(at, room(2 * ((i + 1) & 3)));
+                    const KFrags<D> k = read_k_wide<D>(room(2 * ((i + 1) & 3)), lane);
                     __builtin_amdgcn_sched_barrier(0);
                     st.weights(Sc, P, 0);
                     __builtin_amdgcn_sched_barrier(0);
@@ -417,7 +430,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
                 f32x16 S[QB];
                 bf16x8 P[QB][2];
                 bool may[QB];
-                st.logits(read_k<D>(at, keys), S);
+                st.logits(read_k_wide<D>(keys, lane), S);
 #pragma unroll
                 for (int qb = 0; qb < QB; ++qb) {
                     hide(S[qb], k0, hf, top[qb]);
@@ -453,7 +466,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
         pages = first_pages, pages_next = next_pages, scales = first_scales;
         odd = false;
     }
-    store_tile<D, QB>(p, s, w, st, r_wave, rows);
+    store_tile<D>(p, s, w, st, r_wave, rows);
     if constexpr (!SUMI) {
         if (lane == 0) flags[wave] = odd;
         __syncthreads();

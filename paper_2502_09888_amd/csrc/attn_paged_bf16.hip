@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_tile_kernel(const PagedArgs
         if constexpr (D == 64) start();
     }
 
-    store_tile<D, QB>(p, s, w, st, r_wave, rows);
+    store_tile<D>(p, s, w, st, r_wave, rows);
     if (lane == 0) flags[wave] = odd;
     __syncthreads();
     if (__builtin_expect(flags[0] | flags[1] | flags[2] | flags[3], 0))

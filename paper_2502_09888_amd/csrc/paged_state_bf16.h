@@ -311,8 +311,8 @@ static __device__ __forceinline__ void hide(f32x16 &S, int k, int hf, int top)
 }
 
 // A wave's outputs of a tile, or its part of them.
-template <int D, int QB>
-static __device__ __forceinline__ void store_tile(const PagedArgs &p, const PagedSeq &s, const PagedWork &w, const State<D, QB> &st, int r_wave, int rows)
+template <int D, int QB, bool WIDE>
+static __device__ __forceinline__ void store_tile(const PagedArgs &p, const PagedSeq &s, const PagedWork &w, const State<D, QB, WIDE> &st, int r_wave, int rows)
 {
     const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
 #pragma unroll
