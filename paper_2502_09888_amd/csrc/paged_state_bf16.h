@@ -214,12 +214,25 @@ struct State {
         for (int qb = 0; qb < QB; ++qb) may[qb] = true;
         reference(S, may);
     }
-    // P: the operand of the value product for 16 of the 32 keys
+    // P: the operand of the value product for 16 of the 32 keys.  WIDE: the denominator takes them as they are rounded for it (two at a time, in
+    // fp32; nothing else is made of them)
     __device__ __forceinline__ void weights(const f32x16 (&S)[QB], bf16x8 (&P)[QB][2], int g)
     {
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb) {
             const float sub = m[qb] * c[qb];
+            if constexpr (WIDE) {
+                typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+                const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const bf16x2 x = {(__bf16)__builtin_amdgcn_exp2f(fmaf(S[qb][8 * g + e], c[qb], -sub)),
+                                      (__bf16)__builtin_amdgcn_exp2f(fmaf(S[qb][8 * g + e + 1], c[qb], -sub))};
+                    P[qb][g][e] = x[0], P[qb][g][e + 1] = x[1];
+                    l[qb] = __builtin_amdgcn_fdot2_f32_bf16(x, ones, l[qb], false);
+                }
+                continue;
+            }
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
