@@ -398,12 +398,14 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
                     __builtin_amdgcn_sched_barrier(0);
                     st.weights(Sc, P, 0);
                     __builtin_amdgcn_sched_barrier(0);
+                    __builtin_amdgcn_s_setprio(1);
                     st.logits(k, Sn);  // (behind the last block: not used)
                     st.weights(Sc, P, 1);
                     const VFrags<D> v0 = read_v<D>(at, room(2 * i + 1)), v1 = read_v<D>(at, room(2 * i + 1) + 16 * R::kPitch);
                     __builtin_amdgcn_sched_barrier(0x40f);
                     st.add(v0, P, 0);
                     st.add(v1, P, 1);
+                    __builtin_amdgcn_s_setprio(0);
                 };
                 for (int j = 0; j < n_clean;) {
                     step(j, 0, S0, S1);
@@ -712,7 +714,7 @@ template <int D, bool SUMI>
 hipError_t launch(Paged8Args p, hipStream_t s)
 {
     const int64_t rows = (int64_t)p.m_max * p.G;
-    const int tile = paged8_tile_rows(D, rows);
+    const int tile = paged8_tile_rows(D, rows, (int64_t)p.n_seqs * p.Hkv);
     void (*kernel)(Paged8Args) = tile == 32 ? attn_paged8_few_kernel<D, SUMI> : attn_paged8_tile_kernel<D, 1, SUMI>;
     if constexpr (D == 64)
         if (tile == 256) kernel = attn_paged8_tile_kernel<D, 2, SUMI>;

@@ -12,7 +12,7 @@ struct Paged8Args : PagedArgs {
 };
 
 // packed rows of a workgroup
-static inline int paged8_tile_rows(int d, int64_t rows) { return rows <= 32 ? 32 : d == 64 && rows > 128 ? 256 : 128; }
+static inline int paged8_tile_rows(int d, int64_t rows, int64_t groups) { return rows <= 32 ? 32 : d == 64 && rows > 128 && (rows + 255) / 256 * groups >= 256 ? 256 : 128; }
 static inline int64_t paged8_store_blocks(int64_t m_max) { return (m_max + 2 * kScaleBlock - 2) / kScaleBlock; }
 
 // attention, the join of its parts, and the call's new tokens into their pages

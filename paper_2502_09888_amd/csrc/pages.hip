@@ -76,7 +76,7 @@ static __device__ __forceinline__ void look(const int32_t *refs, int n_pages, in
 }
 
 // ---- fork ----------------------------------------------------------------------------------------
-constexpr int kForkFew = 32;  // rows of one workgroup
+constexpr int kForkFew = 2048;  // entries of a table that one workgroup takes
 
 // What rows become is read before any row is written: a wave for each row notes it and counts, another launch writes it.
 static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b)
@@ -129,17 +129,49 @@ __global__ __launch_bounds__(256) void fork_write_kernel(const ForkArgs a)
     const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (b < a.n_seqs) fork_write(a, b);
 }
-// ... few rows by one workgroup, a wave for each in turn
+// ... small tables by one workgroup, a thread for each entry in turn; bound by its trips to memory, one behind the other
 __global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
 {
-    for (int b = threadIdx.x >> 6; b < a.n_seqs; b += 16) fork_read(a, b);
+    const int all = a.n_seqs * a.table_ld;
+    int bits = 0;
+    for (int e0 = 0; e0 < all; e0 += 1024) {
+        const int e = e0 + threadIdx.x;
+        if (e >= all) continue;
+        const int b = e / a.table_ld, i = e - b * a.table_ld, par = a.parent[b], had = held_of(a, b), was = a.table[e];
+        int h = -1, n = 0;
+        if (par < a.n_seqs) {
+            h = 0;
+            if (par >= 0) {
+                const int there = max(a.len[par], 0);
+                n = a.keep ? min(there, max(a.keep[b], 0)) : there;
+                h = par == b && n == there ? -1 : min((int)(((int64_t)n + (1 << a.page_shift) - 1) >> a.page_shift), held_of(a, par));
+            }
+        } else {
+            bits |= CLIMBER_BAD_SEQ;
+        }
+        if (i == 0) a.new_held[b] = h, a.new_len[b] = n;
+        if (h < 0 || i >= max(had, h)) continue;
+        const int is = i < h ? a.table[(int64_t)par * a.table_ld + i] : -1;
+        a.rows[e] = is;
+        if (i < h && !in_pool(a, is)) bits |= CLIMBER_BAD_PAGE;
+        if (i < had && was == is) continue;
+        if (i < had && in_pool(a, was)) atomicSub(a.refs + was, 1);
+        if (in_pool(a, is)) atomicAdd(a.refs + is, 1);
+    }
+    if (bits) atomicOr(a.status, bits);
     __syncthreads();
-    for (int b = threadIdx.x >> 6; b < a.n_seqs; b += 16) fork_write(a, b);
+    for (int e = threadIdx.x; e < all; e += 1024) {
+        const int b = e / a.table_ld, i = e - b * a.table_ld, h = a.new_held[b];
+        if (h >= 0 && i < max(held_of(a, b), h)) a.table[e] = a.rows[e];
+    }
+    __syncthreads();  // (what rows held before is read above)
+    for (int b = threadIdx.x; b < a.n_seqs; b += 1024)
+        if (a.new_held[b] >= 0) a.len[b] = a.new_len[b], a.held[b] = a.new_held[b];
 }
 
 // ---- extend --------------------------------------------------------------------------------------
 constexpr int kFewSeqs = 1024, kFewUnits = 64, kFewWriters = 512, kListPages = 4096;  // what one workgroup takes; free pages that it keeps in LDS
-constexpr int kCompactFew = 32;  // (256 sequences of 32 pages: 33 us by one workgroup, 17.5 in three launches; 2 of 3: 6 / 8)
+constexpr int kCompactFew = 2048;  // entries of a table that one workgroup takes (us by it / in three launches: 8192 entries 23.5 / 17.5, 50 entries 7 / 14)
 constexpr int kNobody = 1 << 30;  // in last[]: a shared page that none of its writers keeps (n_seqs is less)
 
 // Sequence b's part of the call: pages [first, shared_to) that it holds and writes, [shared_to, need) that it has to get.
@@ -589,17 +621,16 @@ __global__ __launch_bounds__(1024) void compact_few_kernel(const CompactArgs a)
         a.refs[from] = 0;
     }
     bool bad = false;
-    for (int b = wave; b < a.n_seqs; b += 16) {
-        const int had = held_of(a, b);
-        for (int i = lane; i < had; i += 64) {
-            int32_t *const e = a.table + (int64_t)b * a.table_ld + i;
-            const int page = *e;
-            if (!in_pool(a, page)) bad = true;
-            else if (page >= n_used) {
-                const uint64_t w = words[page >> 6];
-                if ((w >> (page & 63)) & 1) *e = a.holes[word_at[page >> 6] + __popcll(w & ((1ull << (page & 63)) - 1)) - low];
-                else bad = true;  // (a page that nothing is said to hold)
-            }
+    const int all = a.n_seqs * a.table_ld;
+#pragma unroll 4
+    for (int e = t; e < all; e += 1024) {
+        const int b = e / a.table_ld, page = a.table[e];
+        if (e - b * a.table_ld >= held_of(a, b)) continue;
+        if (!in_pool(a, page)) bad = true;
+        else if (page >= n_used) {
+            const uint64_t w = words[page >> 6];
+            if ((w >> (page & 63)) & 1) a.table[e] = a.holes[word_at[page >> 6] + __popcll(w & ((1ull << (page & 63)) - 1)) - low];
+            else bad = true;  // (a page that nothing is said to hold)
         }
     }
     if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
@@ -673,7 +704,7 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(const CopyArgs a)
 
 hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t s)
 {
-    if (a.n_seqs <= kForkFew) {
+    if ((int64_t)a.n_seqs * a.table_ld <= kForkFew) {
         hipLaunchKernelGGL(fork_few_kernel, dim3(1), dim3(1024), 0, s, a);
         return hipGetLastError();
     }
@@ -699,7 +730,7 @@ hipError_t launch_pages_extend(const ExtendArgs &a, hipStream_t s)
 
 hipError_t launch_pages_compact(const CompactArgs &a, hipStream_t s)
 {
-    if (a.n_seqs <= kCompactFew && pool_units(a.n_pages) <= kFewUnits) {
+    if ((int64_t)a.n_seqs * a.table_ld <= kCompactFew && pool_units(a.n_pages) <= kFewUnits) {
         hipLaunchKernelGGL(compact_few_kernel, dim3(1), dim3(1024), 0, s, a);
         return hipGetLastError();
     }

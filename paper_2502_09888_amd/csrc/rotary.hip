@@ -45,28 +45,20 @@ static __device__ __forceinline__ float2 turn(double turns, float scale, int inv
     return float2{co * scale, (inverse ? -si : si) * scale};
 }
 
-template <typename T>
-struct Vec;
-template <>
-struct Vec<float> {
-    static constexpr int kN = 4;
-    typedef float type __attribute__((ext_vector_type(4)));
-};
-template <>
-struct Vec<__bf16> {
-    static constexpr int kN = 8;
-    typedef __attribute__((__vector_size__(16))) __bf16 type;
+// N elements of type T, of whichever alignment that makes.  N: elements that travel together, 16 bytes where rows, heads and halves allow it.
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Some {
+    T x[N];
 };
 
-// VECTOR: elements travel 16 bytes at a time; otherwise one by one (rows, heads or halves that are not multiples of 16 bytes).
-template <typename T, bool INTER, bool VECTOR>
+template <typename T, bool INTER, int N>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs p)
 {
-    constexpr int N = VECTOR ? Vec<T>::kN : 1;
+    typedef Some<T, N> V;
     __shared__ float2 cs[kMostRows * kMostHalf];
     const int heads = p.heads[0] + p.heads[1], rot = 2 * p.half;
     // pieces of a head: of pairs, then of elements that stay
-    const int pairs = INTER ? (VECTOR ? rot / N : p.half) : p.half / N, rest = (p.d - rot) / N, pieces = pairs + rest;
+    const int pairs = (INTER && N > 1 ? rot : p.half) / N, rest = (p.d - rot) / N, pieces = pairs + rest;
     const int64_t groups = (p.m + p.rows - 1) / p.rows;
     for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
         const int64_t row0 = g * p.rows;
@@ -85,57 +77,52 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs p)
             T *y = (T *)(p.out[which] + (row0 + r) * p.ld_out[which]) + (int64_t)h * p.d;
             const float2 *t = cs + r * p.half;
             if (piece >= pairs) {
-                if (x == y) continue;
                 const int at = rot + (piece - pairs) * N;
-                if constexpr (VECTOR) *(typename Vec<T>::type *)(y + at) = *(const typename Vec<T>::type *)(x + at);
-                else y[at] = x[at];
-                continue;
-            }
-            if constexpr (!VECTOR) {
-                const int ia = INTER ? 2 * piece : piece, ib = INTER ? 2 * piece + 1 : piece + p.half;
-                const float a = (float)x[ia], b = (float)x[ib];
-                const float2 e = t[piece];
-                y[ia] = (T)fmaf(a, e.x, -(b * e.y));
-                y[ib] = (T)fmaf(a, e.y, b * e.x);
-            } else if constexpr (INTER) {
-                typename Vec<T>::type v = *(const typename Vec<T>::type *)(x + piece * N);
+                if (x != y) *(V *)(y + at) = *(const V *)(x + at);
+            } else if constexpr (INTER && N > 1) {
+                V v = *(const V *)(x + piece * N);
 #pragma unroll
                 for (int e = 0; e < N / 2; ++e) {
                     const float2 w = t[piece * (N / 2) + e];
-                    const float a = (float)v[2 * e], b = (float)v[2 * e + 1];
-                    v[2 * e] = (T)fmaf(a, w.x, -(b * w.y));
-                    v[2 * e + 1] = (T)fmaf(a, w.y, b * w.x);
+                    const float a = (float)v.x[2 * e], b = (float)v.x[2 * e + 1];
+                    v.x[2 * e] = (T)fmaf(a, w.x, -(b * w.y));
+                    v.x[2 * e + 1] = (T)fmaf(a, w.y, b * w.x);
                 }
-                *(typename Vec<T>::type *)(y + piece * N) = v;
+                *(V *)(y + piece * N) = v;
             } else {
-                typename Vec<T>::type v = *(const typename Vec<T>::type *)(x + piece * N), z = *(const typename Vec<T>::type *)(x + p.half + piece * N);
+                // (neighbours of an odd alignment: one by one too)
+                const int ia = INTER ? 2 * piece : piece * N, ib = INTER ? 2 * piece + 1 : piece * N + p.half;
+                V v = *(const V *)(x + ia), z = *(const V *)(x + ib);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float2 w = t[piece * N + e];
-                    const float a = (float)v[e], b = (float)z[e];
-                    v[e] = (T)fmaf(a, w.x, -(b * w.y));
-                    z[e] = (T)fmaf(a, w.y, b * w.x);
+                    const float a = (float)v.x[e], b = (float)z.x[e];
+                    v.x[e] = (T)fmaf(a, w.x, -(b * w.y));
+                    z.x[e] = (T)fmaf(a, w.y, b * w.x);
                 }
-                *(typename Vec<T>::type *)(y + piece * N) = v;
-                *(typename Vec<T>::type *)(y + p.half + piece * N) = z;
+                *(V *)(y + ia) = v;
+                *(V *)(y + ib) = z;
             }
         }
     }
 }
 
-template <typename T>
-hipError_t launch(RotaryArgs p, bool interleaved, hipStream_t s)
+template <typename T, bool INTER>
+hipError_t launch(RotaryArgs p, hipStream_t s)
 {
-    const int n = Vec<T>::kN;
-    bool vector = (interleaved ? 2 * p.half : p.half) % n == 0 && p.d % n == 0;
+    // the most elements that a place in any of the rows is a multiple of
+    uint64_t odd = (uint64_t)(INTER ? 2 * p.half : p.half) * sizeof(T) | (uint64_t)p.d * sizeof(T) | 16;
     for (int i = 0; i < 2; ++i)
-        if (p.heads[i])
-            vector = vector && (uintptr_t)p.in[i] % 16 == 0 && (uintptr_t)p.out[i] % 16 == 0 && p.ld_in[i] % 16 == 0 && p.ld_out[i] % 16 == 0;
+        if (p.heads[i]) odd |= (uint64_t)p.in[i] | (uint64_t)p.out[i] | (uint64_t)p.ld_in[i] | (uint64_t)p.ld_out[i];
+    const int n = (int)((odd & -odd) / sizeof(T));
     p.rows = p.m >= 4096 ? kMostRows : 1;
     const int64_t groups = (p.m + p.rows - 1) / p.rows;
     const dim3 grid((unsigned)std::min<int64_t>(groups, 1 << 16));
-    void (*kernel)(RotaryArgs) = interleaved ? (vector ? rotary_kernel<T, true, true> : rotary_kernel<T, true, false>)
-                                             : (vector ? rotary_kernel<T, false, true> : rotary_kernel<T, false, false>);
+    void (*kernel)(RotaryArgs) = rotary_kernel<T, INTER, 1>;
+    if (n == 2) kernel = rotary_kernel<T, INTER, 2>;
+    if (n == 4) kernel = rotary_kernel<T, INTER, 4>;
+    if constexpr (sizeof(T) == 2)
+        if (n == 8) kernel = rotary_kernel<T, INTER, 8>;
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p);
     return hipGetLastError();
 }
@@ -217,8 +204,9 @@ int climber_rotary(const climber_config *cfg, const climber_rotary_plan *rot, co
     a.d = cfg->d_head;
     a.half = rot->rot_dims / 2;
     a.inverse = rot->inverse != 0;
-    return rt(cfg->dtype == CLIMBER_BF16 ? launch<__bf16>(a, rot->interleaved != 0, (hipStream_t)stream)
-                                         : launch<float>(a, rot->interleaved != 0, (hipStream_t)stream));
+    const hipStream_t s = (hipStream_t)stream;
+    if (cfg->dtype == CLIMBER_BF16) return rt(rot->interleaved ? launch<__bf16, true>(a, s) : launch<__bf16, false>(a, s));
+    return rt(rot->interleaved ? launch<float, true>(a, s) : launch<float, false>(a, s));
 }
 
 }  // extern "C"
