@@ -491,6 +491,13 @@ def _on_device(kv: PagedKV, stream) -> None:
         raise ValueError("the paged cache is on another device than the stream")
 
 
+def _there(desc, *tensors) -> None:
+    """What a call is given besides the described tensors lies on their device."""
+    at = desc._device
+    if at is not None and any(t is not None and not isinstance(t, int) and t.get_device() != at for t in tensors):
+        raise ValueError("the call's tensors are not on the device of what it works on")
+
+
 def climber_paged_workspace_bytes(cfg: Config, kv: PagedKV, m_total: int, m_max: int) -> int:
     return int(load_library().climber_paged_workspace_bytes(C.byref(cfg), C.byref(kv), m_total, m_max))
 
@@ -603,8 +610,9 @@ def climber_attn_history_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q, k, v, 
     """climber_attn_history_paged on a cache in 8 bits."""
     _on_device(kv8, stream)
     code = (_native or _load_native(load_library())).attn_history_paged8(cfg, tau_layer, kv8, q, k, v, off, m_total, m_max, scen, beh, stamp, o,
-                                                                         workspace, stream)
+                                                                         workspace, stream, kv8._device)
     if code is None:
+        _there(kv8, tau_layer, q, k, v, off, scen, beh, stamp, o, workspace)
         d, dk = cfg.d_model, kv8.kv.n_kv_heads * cfg.d_head
         code = load_library().climber_attn_history_paged8(
             C.byref(cfg), _ptr(tau_layer), C.byref(kv8), _ptr(q), _pitch(q, d), _ptr(k), _ptr(v), _same_pitch(k, v, dk), _ptr(off), m_total, m_max,
@@ -618,8 +626,9 @@ def climber_attn_sumi_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q_c, k_c, v_
     """climber_attn_sumi_paged on a cache in 8 bits."""
     _on_device(kv8, stream)
     code = (_native or _load_native(load_library())).attn_sumi_paged8(cfg, tau_layer, kv8, q_c, k_c, v_c, cand_off, m_total, m_max, cand_scen,
-                                                                      cand_beh, o_c, workspace, stream)
+                                                                      cand_beh, o_c, workspace, stream, kv8._device)
     if code is None:
+        _there(kv8, tau_layer, q_c, k_c, v_c, cand_off, cand_scen, cand_beh, o_c, workspace)
         d, dk = cfg.d_model, kv8.kv.n_kv_heads * cfg.d_head
         code = load_library().climber_attn_sumi_paged8(
             C.byref(cfg), _ptr(tau_layer), C.byref(kv8), _ptr(q_c), _pitch(q_c, d), _ptr(k_c), _ptr(v_c), _same_pitch(k_c, v_c, dk),
@@ -657,11 +666,18 @@ def _copies(t, least: int) -> None:
         raise ValueError(f"copies needs room for {least} of three numbers")
 
 
+def _room(copies, most: int) -> int:
+    """... and is read no further than it has any."""
+    _copies(copies, 0)
+    return most if copies is None or isinstance(copies, int) else min(most, copies.numel() // 3)
+
+
 def climber_pages_fork(pool: PagePool, parent, keep, status, workspace, stream=None) -> None:
     """Sequence b becomes what sequence parent[b] was (below 0: empty), up to its first keep[b] tokens; pages are shared."""
     _on_device(pool, stream)
-    code = (_native or _load_native(load_library())).pages_fork(pool, parent, keep, status, workspace, stream)
+    code = (_native or _load_native(load_library())).pages_fork(pool, parent, keep, status, workspace, stream, pool._device)
     if code is None:
+        _there(pool, parent, keep, status, workspace)
         code = load_library().climber_pages_fork(C.byref(pool), _ptr(parent), _ptr(keep), _ptr(status), _ptr(workspace), _nbytes(workspace),
                                                  _stream(stream))
     if code:
@@ -672,8 +688,9 @@ def climber_pages_extend(pool: PagePool, rows, copies, counts, status, workspace
     """Pages for rows[b] more tokens of each sequence; shared pages that they go into are replaced, and copies says by which."""
     _on_device(pool, stream)
     _copies(copies, pool.n_seqs)
-    code = (_native or _load_native(load_library())).pages_extend(pool, rows, copies, counts, status, workspace, stream)
+    code = (_native or _load_native(load_library())).pages_extend(pool, rows, copies, counts, status, workspace, stream, pool._device)
     if code is None:
+        _there(pool, rows, copies, counts, status, workspace)
         code = load_library().climber_pages_extend(C.byref(pool), _ptr(rows), _ptr(copies), _ptr(counts), _ptr(status), _ptr(workspace),
                                                    _nbytes(workspace), _stream(stream))
     if code:
@@ -684,8 +701,9 @@ def climber_pages_compact(pool: PagePool, copies, counts, status, workspace, str
     """The pages in use move to the front of the pool; copies says which went where."""
     _on_device(pool, stream)
     _copies(copies, pool.n_pages // 2)
-    code = (_native or _load_native(load_library())).pages_compact(pool, copies, counts, status, workspace, stream)
+    code = (_native or _load_native(load_library())).pages_compact(pool, copies, counts, status, workspace, stream, pool._device)
     if code is None:
+        _there(pool, copies, counts, status, workspace)
         code = load_library().climber_pages_compact(C.byref(pool), _ptr(copies), _ptr(counts), _ptr(status), _ptr(workspace), _nbytes(workspace),
                                                     _stream(stream))
     if code:
@@ -695,9 +713,10 @@ def climber_pages_compact(pool: PagePool, copies, counts, status, workspace, str
 def climber_paged_copy(cfg: Config, kv: PagedKV, copies, counts, max_copies: int, stream=None) -> None:
     """What climber_pages_extend or climber_pages_compact has left to copy, in one paged cache."""
     _on_device(kv, stream)
-    _copies(copies, 0)
-    code = (_native or _load_native(load_library())).paged_copy(cfg, kv, copies, counts, max_copies, stream)
+    max_copies = _room(copies, max_copies)
+    code = (_native or _load_native(load_library())).paged_copy(cfg, kv, copies, counts, max_copies, stream, kv._device)
     if code is None:
+        _there(kv, copies, counts)
         code = load_library().climber_paged_copy(C.byref(cfg), C.byref(kv), _ptr(copies), _ptr(counts), max_copies, _stream(stream))
     if code:
         raise ClimberError(code, "climber_paged_copy")
@@ -706,9 +725,10 @@ def climber_paged_copy(cfg: Config, kv: PagedKV, copies, counts, max_copies: int
 def climber_paged8_copy(cfg: Config, kv8: PagedKV8, copies, counts, max_copies: int, stream=None) -> None:
     """climber_paged_copy in a cache in 8 bits."""
     _on_device(kv8, stream)
-    _copies(copies, 0)
-    code = (_native or _load_native(load_library())).paged8_copy(cfg, kv8, copies, counts, max_copies, stream)
+    max_copies = _room(copies, max_copies)
+    code = (_native or _load_native(load_library())).paged8_copy(cfg, kv8, copies, counts, max_copies, stream, kv8._device)
     if code is None:
+        _there(kv8, copies, counts)
         code = load_library().climber_paged8_copy(C.byref(cfg), C.byref(kv8), _ptr(copies), _ptr(counts), max_copies, _stream(stream))
     if code:
         raise ClimberError(code, "climber_paged8_copy")
@@ -741,8 +761,9 @@ def climber_rotary(cfg: Config, rot: RotaryPlan, pos, n_kv_heads: int, q, k, q_o
     _on_device(rot, stream)
     if pos.numel() != q.shape[0] or str(pos.dtype) != "torch.int32" or not pos.is_contiguous():
         raise ValueError("pos is a contiguous int32 tensor with a position for each row")
-    code = (_native or _load_native(load_library())).rotary(cfg, rot, pos, n_kv_heads, q, k, q_out, k_out, stream)
+    code = (_native or _load_native(load_library())).rotary(cfg, rot, pos, n_kv_heads, q, k, q_out, k_out, stream, rot._device)
     if code is None:
+        _there(rot, pos, q, q_out, *((k, k_out) if n_kv_heads else ()))
         m, d, dk = q.shape[0], cfg.d_model, n_kv_heads * cfg.d_head
         for t, wide in ((q, d), (q_out, d)) + (((k, dk), (k_out, dk)) if n_kv_heads else ()):
             if t.shape[0] != m or t.numel() != m * wide:

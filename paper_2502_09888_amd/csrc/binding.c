@@ -25,7 +25,7 @@ static __typeof__(&climber_pages_compact) pages_compact_fn;
 static __typeof__(&climber_paged_copy) paged_copy_fn;
 static __typeof__(&climber_paged8_copy) paged8_copy_fn;
 static __typeof__(&climber_rotary) rotary_fn;
-static PyObject *pool_type, *rotary_type, *bf16_dtype, *f32_dtype, *s_dtype;
+static PyObject *pool_type, *rotary_type, *bf16_dtype, *f32_dtype, *s_dtype, *s_get_device;
 static PyObject *config_type, *bias_type, *current_device, *raw_stream, *paged_type, *paged8_type, *s_data_ptr, *s_cuda_stream, *s_shape, *s_stride, *s_nbytes;
 
 static int unsigned_of(PyObject *o, void **p) /* takes the reference */
@@ -157,9 +157,25 @@ static int bytes_of(PyObject *o, size_t *n)
     return 1;
 }
 
-/* cfg, tau, kv, q, k, v, off, m_total, m_max, scen, beh[, stamp], o, workspace, stream */
+/* A tensor on device `at` (a number; None: not known, then any tensor; pointers and None are taken as they are) */
+static int lies_on(PyObject *o, PyObject *at)
+{
+    if (at == Py_None || o == Py_None || PyLong_Check(o)) return 1;
+    PyObject *d = PyObject_CallMethodNoArgs(o, s_get_device);
+    const int ok = d && PyObject_RichCompareBool(d, at, Py_EQ) == 1;
+    Py_XDECREF(d);
+    return ok;
+}
+
+/* cfg, tau, kv, q, k, v, off, m_total, m_max, scen, beh[, stamp], o, workspace, stream[, device] */
 static PyObject *paged(PyObject *const *a, Py_ssize_t n, int appends, int bits8)
 {
+    if (bits8) {
+        if (n != 15 + appends) return elsewhere();
+        --n;
+        for (Py_ssize_t i = 1; i < n - 1; ++i)
+            if (i != 2 && i != 7 && i != 8 && !lies_on(a[i], a[n])) return elsewhere();
+    }
     if (n != 14 + appends) return elsewhere();
     void *p[14], *s;
     int32_t m_total, m_max;
@@ -216,13 +232,13 @@ static PyObject *paged_evict(PyObject *m, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(code);
 }
 
-/* pool, n pointers, workspace, stream */
+/* pool, n pointers, workspace, stream, device */
 static int pool_call(PyObject *const *a, Py_ssize_t n, int pointers, Py_buffer *pool, void **p, size_t *ws_bytes, void **s)
 {
-    if (n != pointers + 3 || !pool_type) return 0;
+    if (n != pointers + 4 || !pool_type) return 0;
     for (int i = 1; i <= pointers + 1; ++i)
-        if (!pointer(a[i], &p[i])) return 0;
-    return bytes_of(a[n - 2], ws_bytes) && stream_of(a[n - 1], s) && structure(a[0], pool_type, sizeof(climber_page_pool), pool);
+        if (!lies_on(a[i], a[n - 1]) || !pointer(a[i], &p[i])) return 0;
+    return bytes_of(a[n - 3], ws_bytes) && stream_of(a[n - 2], s) && structure(a[0], pool_type, sizeof(climber_page_pool), pool);
 }
 static PyObject *pages_fork(PyObject *m, PyObject *const *a, Py_ssize_t n) /* parent, keep, status */
 {
@@ -264,10 +280,10 @@ static PyObject *pages_compact(PyObject *m, PyObject *const *a, Py_ssize_t n) /*
     return PyLong_FromLong(code);
 }
 
-/* cfg, kv, copies, counts, max_copies, stream */
+/* cfg, kv, copies, counts, max_copies, stream, device */
 static PyObject *copy(PyObject *const *a, Py_ssize_t n, int bits8)
 {
-    if (n != 6 || !paged8_type) return elsewhere();
+    if (n != 7 || !paged8_type || !lies_on(a[2], a[6]) || !lies_on(a[3], a[6])) return elsewhere();
     Py_buffer cfg, kv;
     void *copies, *counts, *s;
     int32_t most;
@@ -303,10 +319,12 @@ static int rows_of(PyObject *o, int64_t width, PyObject *dtype, int64_t *m, void
     return ok && pitch(o, width, ld) && pointer(o, p);
 }
 
-/* cfg, plan, pos (its pointer: checked by the caller), n_kv_heads, q, k, q_out, k_out, stream */
+/* cfg, plan, pos (its pointer: checked by the caller), n_kv_heads, q, k, q_out, k_out, stream, device */
 static PyObject *rotary(PyObject *m, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 9 || !rotary_type) return elsewhere();
+    if (n != 10 || !rotary_type) return elsewhere();
+    for (int i = 2; i < 8; ++i)
+        if (i != 3 && !lies_on(a[i], a[9])) return elsewhere();
     Py_buffer cfg, plan;
     void *pos, *p[4] = {NULL, NULL, NULL, NULL}, *s;
     int32_t n_kv;
@@ -412,5 +430,6 @@ PyMODINIT_FUNC PyInit__native(void)
     s_stride = PyUnicode_InternFromString("stride");
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_dtype = PyUnicode_InternFromString("dtype");
-    return s_dtype && s_data_ptr && s_cuda_stream && s_shape && s_stride && s_nbytes ? PyModule_Create(&module) : NULL;
+    s_get_device = PyUnicode_InternFromString("get_device");
+    return s_dtype && s_get_device && s_data_ptr && s_cuda_stream && s_shape && s_stride && s_nbytes ? PyModule_Create(&module) : NULL;
 }

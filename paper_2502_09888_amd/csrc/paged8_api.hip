@@ -23,7 +23,8 @@ int attn_paged8(const Call &c, const climber_paged_kv8 *kv8, void *workspace, si
     const int64_t G = cfg->n_heads / kv->n_kv_heads, heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged8_tile_rows(cfg->d_head, c.m_max * G, heads);
     const int n_split = parts(cfg, kv, c.m_total, c.m_max, tile);
     if ((c.m_max * G + tile - 1) / tile * (heads + 7) * n_split >= kMostGroups) return CLIMBER_ERR_RANGE;
-    if (!c.sumi && (heads * paged8_store_blocks(c.m_max) + 3) / 4 >= kMostGroups) return CLIMBER_ERR_RANGE;
+    // (new tokens are stored in a launch of their own, or with the join of the parts, a workgroup for a row and head at most)
+    if (!c.sumi && (heads * paged8_store_blocks(c.m_max) + 3) / 4 + (n_split > 1 ? (int64_t)c.m_total * cfg->n_heads : 0) >= kMostGroups) return CLIMBER_ERR_RANGE;
     const Layout w = layout_of(cfg, kv, c.m_total, n_split > 1 ? (size_t)n_split * c.m_total * cfg->n_heads : 0);
     if (w.bytes > 0 && !workspace) return CLIMBER_ERR_NULL;
     if (!aligned(workspace, 256)) return CLIMBER_ERR_ALIGN;

@@ -77,6 +77,46 @@ def test_many_rows_on_a_longer_cache(d, sumi):
         check8(case, dev)
 
 
+@pytest.mark.parametrize("kind", ["plain", "far", "odd"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
+def test_the_largest_tiles(sumi, causal, kind):
+    # enough rows of enough sequences for tiles of 256 rows at d_head 64
+    g = torch.Generator().manual_seed(3)
+    lens, rows = (torch.randint(0, hi, (40,), generator=g).tolist() for hi in (200, 150))
+    lens[:3], rows[:3] = [199, 0, 64], [150, 150, 149]
+    case = Case8(lens, rows, H=8, Hkv=4, d=64, page=32, sumi=sumi, causal=causal, seed=91, scale=1.0 if kind == "far" else None)
+    if kind == "far":                                     # (as in test_weights_that_exceed_the_first_ones_by_far, in several rows)
+        case.q.mul_(0.05), case.tau.fill_(1.0)
+        case.q[20, 1, 0] = case.q[130, 5, 0] = case.q[160, 2, 0] = 24.0
+        for hit in (40, 198):
+            pg, s = case.at(0, hit)
+            case.k[pg, :, s] = 0.0
+            case.k[pg, :, s, 0] = 24.0
+        case.quantise()
+        case.kn[155] = 0.0
+        case.kn[155, :, 0] = 24.0
+    if kind == "odd":
+        case.vn[100, 1, 7], case.vn[140, 2, 9] = math.inf, math.nan
+    dev = Device8(case)
+    dev.attend()
+    if kind != "odd":
+        check8(case, dev)
+        return
+    clean = Case8(lens, rows, H=8, Hkv=4, d=64, page=32, sumi=sumi, causal=causal, seed=91)
+    other = Device8(clean)
+    other.attend()
+    x, y = dev.out(), other.out()
+    # of the first sequence's 150 rows, those that see row 100, and row 140
+    for at, heads, e, value in ((100, (2, 3), 7, math.inf), (140, (4, 5), 9, math.nan)):
+        sees = [at] if sumi else list(range(at if causal else 0, 150))
+        for h in heads:
+            got = x[sees, h, e]
+            assert (torch.isnan(got) if math.isnan(value) else got == value).all()
+            x[sees, h, e] = y[sees, h, e]
+    assert torch.equal(x, y)
+
+
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_large_logits(d, sumi):

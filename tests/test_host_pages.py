@@ -82,7 +82,24 @@ def test_pools_of_other_tensors_are_none():
             P.page_pool(**{**t, name: bad}, page_size=16)
     with pytest.raises(ValueError):                       # host memory, which no kernel can reach
         P.climber_pages_fork(p, None, None, None, None)
+    # tensors elsewhere than the pool
+    p._device = 0
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    other = torch.zeros(100, dtype=torch.int32)
+    for f, given in ((P.climber_pages_fork, (other, None, FAKE, FAKE)), (P.climber_pages_extend, (FAKE, FAKE, other, FAKE, FAKE)),
+                     (P.climber_pages_compact, (FAKE, FAKE, FAKE, ws))):
+        with pytest.raises(ValueError):
+            f(p, *given, stream=0)
     p._device = None
     for f, rows in ((P.climber_pages_extend, (None,)), (P.climber_pages_compact, ())):
         with pytest.raises(ValueError):                   # too short
             f(p, *rows, torch.zeros((2, 3), dtype=torch.int32), None, None, None, stream=0)
+
+
+def test_copies_are_read_no_further_than_they_go():
+    torch = pytest.importorskip("torch")
+    from paper_2502_09888_amd.climber import _room
+    assert _room(torch.zeros((7, 3), dtype=torch.int32), 100) == 7 and _room(torch.zeros((7, 3), dtype=torch.int32), 5) == 5
+    assert _room(FAKE, 100) == 100 and _room(None, 100) == 100
+    with pytest.raises(ValueError):
+        _room(torch.zeros((3, 7), dtype=torch.int32).t(), 5)

@@ -85,6 +85,9 @@ def test_tensors_of_other_kinds_are_refused():
     q, pos = torch.zeros(3, 8, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError):                       # frequencies in host memory, which no kernel can reach
         P.climber_rotary(cfg(), plan, pos, 0, q, None, q, None)
+    plan._device = 3                                      # ... and rows elsewhere than these
+    with pytest.raises(ValueError):
+        P.climber_rotary(cfg(), plan, pos, 0, q, None, q, None, stream=0)
     plan._device = None
     for bad in (dict(q=q[:2]), dict(q_out=q.float()), dict(pos=pos.long()), dict(pos=pos[:2]), dict(q=q.transpose(1, 2).contiguous().transpose(1, 2))):
         a = {**dict(pos=pos, q=q, q_out=q), **bad}
