@@ -489,75 +489,92 @@ static __device__ __forceinline__ uint32_t wave_max(uint32_t x)
 }
 
 template <int D>
-static __device__ __forceinline__ void store_block(const Paged8Args &p, const PagedSeq &s, int b, int hk, int block)
-{
-    constexpr int kLanes = D / 8, kRows = 64 / kLanes, kLoads = 16 / kRows;  // lanes of a row, 8 values each
-    const int lane = threadIdx.x & 63;
-    const int end = min(s.n + s.T, p.max_len), slot0 = ((s.n >> 4) + block) * 16;
-    if (slot0 >= end || s.T == 0) return;
-    const int page = p.table[(int64_t)b * p.table_ld + (slot0 >> p.page_shift)];
-    if (page < 0 || page >= p.n_pages) return;
-    const int in = slot0 & ((1 << p.page_shift) - 1), old = min(max(s.n - slot0, 0), 16), n = min(end - slot0, 16);  // tokens [0, old) stay, [old, n) come
-    const int64_t head = (int64_t)page * p.Hkv + hk, to = ((head << p.page_shift) + in) * D, at = (head << (p.page_shift - 4)) + (in >> 4);
+struct StoreBlock {
+    static constexpr int kLanes = D / 8, kRows = 64 / kLanes, kLoads = 16 / kRows;  // lanes of a row, 8 values each
+    bool any;
+    int page, in, slot0, old, n, was[2];
+    int64_t to, at;
     u32x4 x[2][kLoads];
+    // what it needs of the new rows, and the scales so far
+    __device__ __forceinline__ void load(const Paged8Args &p, const PagedSeq &s, int b, int hk, int block)
+    {
+        const int lane = threadIdx.x & 63, end = min(s.n + s.T, p.max_len);
+        slot0 = ((s.n >> 4) + block) * 16;
+        any = slot0 < end && s.T > 0;
+        if (!any) return;
+        old = min(max(s.n - slot0, 0), 16), n = min(end - slot0, 16);  // tokens [0, old) stay, [old, n) come
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int j = i * kRows + lane / kLanes;
-            x[kv][i] = u32x4{0, 0, 0, 0};
-            if (j >= old && j < n)
-                x[kv][i] = *(const u32x4 *)((kv ? p.v : p.k) + (s.row0 + slot0 + j - s.n) * p.ld_kv + (int64_t)hk * (2 * D) + (lane % kLanes) * 16);
-        }
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        uint8_t *const pages = kv ? p.v_pages : p.k_pages, *const scale = (kv ? p.v_scale : p.k_scale) + at;
-        uint32_t top = 0;  // largest finite magnitude, as bits of a bf16
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t lo = x[kv][i][e] & 0x7fffu, hi = (x[kv][i][e] >> 16) & 0x7fffu;
-                top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-            }
-        top = wave_max(top);
-        // 1.m 2^(e - 127) <= 448 2^s = 1.75 2^(s + 8)
-        const int was = old > 0 ? *scale : 0, mine = max((int)(top >> 7) - 8 + ((top & 127u) > 96u), kLeastScale), now = max(was, mine);
-        if (old > 0 && now > was) {
-            const float down = now - was > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (now - was)) << 23);
+        for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
                 const int j = i * kRows + lane / kLanes;
-                if (j >= old) continue;
-                u32x2 *const c = (u32x2 *)(pages + to + j * D + (lane % kLanes) * 8);
-                u32x2 y = *c;
+                x[kv][i] = u32x4{0, 0, 0, 0};
+                if (j >= old && j < n)
+                    x[kv][i] = *(const u32x4 *)((kv ? p.v : p.k) + (s.row0 + slot0 + j - s.n) * p.ld_kv + (int64_t)hk * (2 * D) + (lane % kLanes) * 16);
+            }
+        page = p.table[(int64_t)b * p.table_ld + (slot0 >> p.page_shift)];
+        any = page >= 0 && page < p.n_pages;
+        if (!any) return;
+        in = slot0 & ((1 << p.page_shift) - 1);
+        const int64_t head = (int64_t)page * p.Hkv + hk;
+        to = ((head << p.page_shift) + in) * D, at = (head << (p.page_shift - 4)) + (in >> 4);
+        was[0] = old > 0 ? p.k_scale[at] : 0, was[1] = old > 0 ? p.v_scale[at] : 0;
+    }
+    // (nobody reads the block any more)
+    __device__ __forceinline__ void write(const Paged8Args &p, const PagedSeq &s, int hk) const
+    {
+        if (!any) return;
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+            uint8_t *const pages = kv ? p.v_pages : p.k_pages;
+            uint32_t top = 0;  // largest finite magnitude, as bits of a bf16
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t lo = x[kv][i][e] & 0x7fffu, hi = (x[kv][i][e] >> 16) & 0x7fffu;
+                    top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+                }
+            top = wave_max(top);
+            // 1.m 2^(e - 127) <= 448 2^s = 1.75 2^(s + 8)
+            const int mine = max((int)(top >> 7) - 8 + ((top & 127u) > 96u), kLeastScale), now = max(was[kv], mine);
+            if (old > 0 && now > was[kv]) {
+                const float down = now - was[kv] > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (now - was[kv])) << 23);
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int j = i * kRows + lane / kLanes;
+                    if (j >= old) continue;
+                    u32x2 *const c = (u32x2 *)(pages + to + j * D + (lane % kLanes) * 8);
+                    u32x2 y = *c;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(y[e], false), b2 = __builtin_amdgcn_cvt_pk_f32_fp8(y[e], true);
+                        y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(b2[0] * down, b2[1] * down, __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * down, a[1] * down, 0, false), true);
+                    }
+                    *c = y;
+                }
+            }
+            const float up = __uint_as_float((uint32_t)(254 - now) << 23);  // 2^(127 - now)
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int j = i * kRows + lane / kLanes;
+                if (j < old || j >= n) continue;
+                u32x2 y;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const auto a = __builtin_amdgcn_cvt_pk_f32_fp8(y[e], false), b2 = __builtin_amdgcn_cvt_pk_f32_fp8(y[e], true);
-                    y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(b2[0] * down, b2[1] * down, __builtin_amdgcn_cvt_pk_fp8_f32(a[0] * down, a[1] * down, 0, false), true);
+                    const uint32_t u = x[kv][i][2 * e], v = x[kv][i][2 * e + 1];
+                    y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(u << 16) * up, __uint_as_float(u & 0xffff0000u) * up, 0, false);
+                    y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(v << 16) * up, __uint_as_float(v & 0xffff0000u) * up, y[e], true);
                 }
-                *c = y;
+                *(u32x2 *)(pages + to + j * D + (lane % kLanes) * 8) = y;
             }
+            if (lane == 0 && now != was[kv]) (kv ? p.v_scale : p.k_scale)[at] = (uint8_t)now;
         }
-        const float up = __uint_as_float((uint32_t)(254 - now) << 23);  // 2^(127 - now)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int j = i * kRows + lane / kLanes;
-            if (j < old || j >= n) continue;
-            u32x2 y;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint32_t u = x[kv][i][2 * e], v = x[kv][i][2 * e + 1];
-                y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(u << 16) * up, __uint_as_float(u & 0xffff0000u) * up, 0, false);
-                y[e] = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(v << 16) * up, __uint_as_float(v & 0xffff0000u) * up, y[e], true);
-            }
-            *(u32x2 *)(pages + to + j * D + (lane % kLanes) * 8) = y;
-        }
-        if (lane == 0 && now != was) *scale = (uint8_t)now;
+        if (hk == 0 && p.stamp && lane >= old && lane < n)
+            p.stamp[((int64_t)page << p.page_shift) + in + lane] = p.stamp_new[s.row0 + slot0 + lane - s.n];
     }
-    if (hk == 0 && p.stamp && lane >= old && lane < n) p.stamp[((int64_t)page << p.page_shift) + in + lane] = p.stamp_new[s.row0 + slot0 + lane - s.n];
-}
-
+};
 template <int D>
 static __device__ __forceinline__ void store_unit(const Paged8Args &p, unsigned group)
 {
@@ -565,7 +582,10 @@ static __device__ __forceinline__ void store_unit(const Paged8Args &p, unsigned 
     const int64_t unit = (int64_t)group * 4 + wave, bh = unit / p.store_blocks;
     if (bh >= (int64_t)p.n_seqs * p.Hkv) return;
     const int b = (int)(bh / p.Hkv);
-    store_block<D>(p, paged_seq(p, b), b, (int)(bh % p.Hkv), (int)(unit % p.store_blocks));
+    const PagedSeq s = paged_seq(p, b);
+    StoreBlock<D> block;
+    block.load(p, s, b, (int)(bh % p.Hkv), (int)(unit % p.store_blocks));
+    block.write(p, s, (int)(bh % p.Hkv));
 }
 template <int D>
 __global__ __launch_bounds__(256) void paged8_store_kernel(const Paged8Args p) { store_unit<D>(p, blockIdx.x); }
@@ -673,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Arg
         vat.init(lane);
         const int lim = sees(r) - s.n, lim_lo = sees(r_tile) - s.n;
 #pragma unroll 1
-        for (int i = wave; i < n_new; i += 4) {
+        for (int i = (wave - n_blk) & 3; i < n_new; i += 4) {  // (the waves that had fewer cached blocks first)
             const int k0 = n_lo + i * 32;
             lds_u8 *const keys = at0, *const values = at1;
             rows_src.issue(k0, 0, keys, values);
@@ -695,6 +715,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Arg
         }
     }
     if (lane == 0) odd_seen[wave] = odd;
+    StoreBlock<D> put;
+    const bool stores = !SUMI && p.n_split == 1;
+    if (stores && wave < p.store_blocks) put.load(p, s, w.b, w.hk, wave);
     // (each wave's outputs in units of its reference take the 2 x kStage bytes of two waves' places; all waves are done with theirs at the first barrier)
     join_few<D, true>(p, s, w, st, joined, [&](int j) { return (float *)(j < 2 ? stage0 : stage1) + (j & 1) * 32 * D; }, row, h, r_tile, rows);
     if constexpr (!SUMI) {
@@ -705,8 +728,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Arg
             if (wave == 0) put_odd<D>(p, s, w, from + clean, k_hi, r_tile, min(r_tile + 32, rows), sees);
         }
         // (all of its waves have read the cached tokens, behind whose barrier they were joined)
-        if (p.n_split == 1)
-            for (int i = wave; i < p.store_blocks; i += 4) store_block<D>(p, s, w.b, w.hk, i);
+        if (stores) {
+            if (wave < p.store_blocks) put.write(p, s, w.hk);
+            for (int i = wave + 4; i < p.store_blocks; i += 4) {
+                put.load(p, s, w.b, w.hk, i);
+                put.write(p, s, w.hk);
+            }
+        }
     }
 }
 

@@ -29,7 +29,7 @@ struct RotaryArgs {
     int d, half, rows, inverse;  // rows: of a workgroup
 };
 
-constexpr int kMostHalf = 256, kMostRows = 4;
+constexpr int kMostHalf = 256, kTurns = 1024;  // sines and cosines of a workgroup
 
 // cosine and sine of 2 pi turns, times scale
 static __device__ __forceinline__ float2 turn(double turns, float scale, int inverse)
@@ -55,7 +55,7 @@ template <typename T, bool INTER, int N>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs p)
 {
     typedef Some<T, N> V;
-    __shared__ float2 cs[kMostRows * kMostHalf];
+    __shared__ float2 cs[kTurns];
     const int heads = p.heads[0] + p.heads[1], rot = 2 * p.half;
     // pieces of a head: of pairs, then of elements that stay
     const int pairs = (INTER && N > 1 ? rot : p.half) / N, rest = (p.d - rot) / N, pieces = pairs + rest;
@@ -115,7 +115,10 @@ hipError_t launch(RotaryArgs p, hipStream_t s)
     for (int i = 0; i < 2; ++i)
         if (p.heads[i]) odd |= (uint64_t)p.in[i] | (uint64_t)p.out[i] | (uint64_t)p.ld_in[i] | (uint64_t)p.ld_out[i];
     const int n = (int)((odd & -odd) / sizeof(T));
-    p.rows = p.m >= 4096 ? kMostRows : 1;
+    // Rows of a workgroup: one where that has work for all of its threads, more of smaller ones where there are rows enough.  us with 1 / 2 / 4:
+    // 20000 rows of 40 heads of 128 70.6 / 74.8 / 77.7, 5000 of 12 heads of 64 in fp32 9.5 / 8.9 / 8.5.
+    const int64_t units = (int64_t)(p.heads[0] + p.heads[1]) * ((INTER && n > 1 ? 2 * p.half : p.half) / n + (p.d - 2 * p.half) / n);
+    p.rows = units >= 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(768 / units, kTurns / p.half), p.m / 1024));
     const int64_t groups = (p.m + p.rows - 1) / p.rows;
     const dim3 grid((unsigned)std::min<int64_t>(groups, 1 << 16));
     void (*kernel)(RotaryArgs) = rotary_kernel<T, INTER, 1>;
