@@ -208,7 +208,7 @@ def _load_native(lib):
     if current[0] is not None:
         native.bind_pages(*(C.cast(f, C.c_void_p).value for f in (lib.climber_pages_fork, lib.climber_pages_extend, lib.climber_pages_compact,
                                                                   lib.climber_paged_copy, lib.climber_paged8_copy, lib.climber_rotary)),
-                          PagePool, RotaryPlan, torch.bfloat16, torch.float32)
+                          PagePool, RotaryPlan, torch.bfloat16, torch.float32, torch.int32)
     _native = native
     return native
 
@@ -759,11 +759,11 @@ def rotary(freq, rot_dims: int, interleaved: bool = False, scale: float = 1.0, i
 def climber_rotary(cfg: Config, rot: RotaryPlan, pos, n_kv_heads: int, q, k, q_out, k_out, stream=None) -> None:
     """Turn q and k rows by their positions (row r is [r] of the tensors, as many rows as q has; row pitches are taken from them)."""
     _on_device(rot, stream)
-    if pos.numel() != q.shape[0] or str(pos.dtype) != "torch.int32" or not pos.is_contiguous():
-        raise ValueError("pos is a contiguous int32 tensor with a position for each row")
     code = (_native or _load_native(load_library())).rotary(cfg, rot, pos, n_kv_heads, q, k, q_out, k_out, stream, rot._device)
     if code is None:
         _there(rot, pos, q, q_out, *((k, k_out) if n_kv_heads else ()))
+        if pos.numel() != q.shape[0] or str(pos.dtype) != "torch.int32" or not pos.is_contiguous():
+            raise ValueError("pos is a contiguous int32 tensor with a position for each row")
         m, d, dk = q.shape[0], cfg.d_model, n_kv_heads * cfg.d_head
         for t, wide in ((q, d), (q_out, d)) + (((k, dk), (k_out, dk)) if n_kv_heads else ()):
             if t.shape[0] != m or t.numel() != m * wide:

@@ -25,7 +25,7 @@ static __typeof__(&climber_pages_compact) pages_compact_fn;
 static __typeof__(&climber_paged_copy) paged_copy_fn;
 static __typeof__(&climber_paged8_copy) paged8_copy_fn;
 static __typeof__(&climber_rotary) rotary_fn;
-static PyObject *pool_type, *rotary_type, *bf16_dtype, *f32_dtype, *s_dtype, *s_get_device;
+static PyObject *pool_type, *rotary_type, *bf16_dtype, *f32_dtype, *i32_dtype, *s_dtype, *s_get_device;
 static PyObject *config_type, *bias_type, *current_device, *raw_stream, *paged_type, *paged8_type, *s_data_ptr, *s_cuda_stream, *s_shape, *s_stride, *s_nbytes;
 
 static int unsigned_of(PyObject *o, void **p) /* takes the reference */
@@ -302,24 +302,31 @@ static PyObject *copy(PyObject *const *a, Py_ssize_t n, int bits8)
 static PyObject *paged_copy(PyObject *m, PyObject *const *a, Py_ssize_t n) { return copy(a, n, 0); }
 static PyObject *paged8_copy(PyObject *m, PyObject *const *a, Py_ssize_t n) { return copy(a, n, 1); }
 
-/* A tensor of m (or, -1, any number of) rows of `width` elements of a type: its pointer and pitch. */
+/* A tensor of m (or, -1, any number of) rows of `width` elements of a type, one behind the other: its pointer and pitch. */
 static int rows_of(PyObject *o, int64_t width, PyObject *dtype, int64_t *m, void **p, int64_t *ld)
 {
     PyObject *t = PyObject_GetAttr(o, s_dtype), *shape = t == dtype ? PyObject_GetAttr(o, s_shape) : NULL;
-    int ok = shape && PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) > 0;
+    PyObject *stride = shape ? PyObject_CallMethodNoArgs(o, s_stride) : NULL;
+    int ok = stride && PyTuple_Check(shape) && PyTuple_Check(stride) && PyTuple_GET_SIZE(shape) > 0 && PyTuple_GET_SIZE(shape) == PyTuple_GET_SIZE(stride);
     if (ok) {
         int64_t inner = 1;
-        for (Py_ssize_t i = PyTuple_GET_SIZE(shape) - 1; i > 0; --i) inner *= PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+        for (Py_ssize_t i = PyTuple_GET_SIZE(shape) - 1; ok && i > 0; --i) {
+            const int64_t n = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i));
+            ok = n == 1 || PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i)) == inner;
+            inner *= n;
+        }
         const int64_t rows = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0));
         if (*m < 0) *m = rows;
-        ok = rows == *m && inner == width && !PyErr_Occurred();
+        ok = ok && rows == *m && inner == width && !PyErr_Occurred();
+        *ld = rows > 1 ? PyLong_AsLongLong(PyTuple_GET_ITEM(stride, 0)) : width;
     }
     Py_XDECREF(t);
     Py_XDECREF(shape);
-    return ok && pitch(o, width, ld) && pointer(o, p);
+    Py_XDECREF(stride);
+    return ok && pointer(o, p);
 }
 
-/* cfg, plan, pos (its pointer: checked by the caller), n_kv_heads, q, k, q_out, k_out, stream, device */
+/* cfg, plan, pos, n_kv_heads, q, k, q_out, k_out, stream, device */
 static PyObject *rotary(PyObject *m, PyObject *const *a, Py_ssize_t n)
 {
     if (n != 10 || !rotary_type) return elsewhere();
@@ -336,7 +343,8 @@ static PyObject *rotary(PyObject *m, PyObject *const *a, Py_ssize_t n)
     PyObject *dtype = c->dtype == CLIMBER_BF16 ? bf16_dtype : f32_dtype;
     int ok = rows_of(a[4], wide, dtype, &rows, &p[0], &ld[0]) && rows_of(a[6], wide, dtype, &rows, &p[2], &ld[2]);
     if (ok && n_kv) ok = rows_of(a[5], kv_wide, dtype, &rows, &p[1], &ld[1]) && rows_of(a[7], kv_wide, dtype, &rows, &p[3], &ld[3]);
-    ok = ok && pointer(a[2], &pos);
+    int64_t ld_pos = 1;
+    ok = ok && rows_of(a[2], 1, i32_dtype, &rows, &pos, &ld_pos) && ld_pos == 1;
     int code = 0;
     if (ok) {
         Py_BEGIN_ALLOW_THREADS
@@ -348,20 +356,21 @@ static PyObject *rotary(PyObject *m, PyObject *const *a, Py_ssize_t n)
     return ok ? PyLong_FromLong(code) : elsewhere();
 }
 
-/* bind_pages(addresses of fork, extend, compact, the two copies and rotary, PagePool, RotaryPlan, torch.bfloat16, torch.float32) */
+/* bind_pages(addresses of fork, extend, compact, the two copies and rotary, PagePool, RotaryPlan, torch.bfloat16, torch.float32, torch.int32) */
 static PyObject *bind_pages(PyObject *m, PyObject *args)
 {
     unsigned long long f[6];
-    PyObject *t[4];
-    if (!PyArg_ParseTuple(args, "KKKKKKO!O!OO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &PyType_Type, &t[0], &PyType_Type, &t[1], &t[2], &t[3])) return NULL;
+    PyObject *t[5];
+    if (!PyArg_ParseTuple(args, "KKKKKKO!O!OOO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &PyType_Type, &t[0], &PyType_Type, &t[1], &t[2], &t[3], &t[4]))
+        return NULL;
     pages_fork_fn = (__typeof__(pages_fork_fn))(uintptr_t)f[0];
     pages_extend_fn = (__typeof__(pages_extend_fn))(uintptr_t)f[1];
     pages_compact_fn = (__typeof__(pages_compact_fn))(uintptr_t)f[2];
     paged_copy_fn = (__typeof__(paged_copy_fn))(uintptr_t)f[3];
     paged8_copy_fn = (__typeof__(paged8_copy_fn))(uintptr_t)f[4];
     rotary_fn = (__typeof__(rotary_fn))(uintptr_t)f[5];
-    PyObject **const to[4] = {&pool_type, &rotary_type, &bf16_dtype, &f32_dtype};
-    for (int i = 0; i < 4; ++i) {
+    PyObject **const to[5] = {&pool_type, &rotary_type, &bf16_dtype, &f32_dtype, &i32_dtype};
+    for (int i = 0; i < 5; ++i) {
         PyObject *was = *to[i];
         *to[i] = Py_NewRef(t[i]);
         Py_XDECREF(was);
