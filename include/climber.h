@@ -237,7 +237,7 @@ int climber_attn_sumi_bias(const climber_config *cfg, const float *tau_layer,
  *   page_table  dev int32 [n_seqs][table_ld]: token `slot` of sequence b is row slot % page_size of page
  *               page_table[b][slot / page_size].  Entries behind the pages in use may hold anything.
  *   len         dev int32 [n_seqs]: tokens in the cache before the call.  No call but climber_paged_evict
- *               changes a length: after an append the caller adds the chunk's rows.
+ *               and climber_pages_fork changes a length: after an append the caller adds the chunk's rows.
  *   max_len     host: no sequence has more tokens than this after the call.  It sizes the launches (a
  *               HIP graph keeps working while lengths grow up to it) and is at most table_ld * page_size.
  *   mass        dev fp32 [n_pages][page_size] or NULL: accumulated attention weight per token.  Where it is
@@ -328,8 +328,8 @@ int climber_check_paged(const climber_config *cfg, const climber_paged_kv *kv, c
  * and everything else as in climber_paged_kv.  CLIMBER_BF16 with d_head 64 or 128 (rows of a call are bf16); kv.mass must be NULL.
  * A block's scale is the least s >= 10 with which every finite element of its tokens is at most 448 * 2^(s - 127) in magnitude; elements
  * are rounded to the nearest e4m3 number, ties to even, and infinities and NaN become NaN.  A token that joins a block raises the scale
- * where it has to: the block's older elements are then rounded once more.  A scale never falls while its block has tokens; the first token of a block
- * (slot a multiple of 16) starts it anew.  Elements of keys and values have to stay below 2^127 in magnitude, and scales that the caller
+ * where it has to: the block's older elements are then rounded once more.  A scale never falls while its block has tokens (where some of them were cut
+ * off, or copied without the others, it stays as well); the first token of a block (slot a multiple of 16) starts it anew.  Elements of keys and values have to stay below 2^127 in magnitude, and scales that the caller
  * writes between 10 and 247.
  * Two sequences of a call may list the same page as long as no call writes it; the append writes to the blocks of slots len[b] .. len[b] + rows - 1
  * whole, the older tokens of the first one among them.  Eviction does not take this cache; climber_check_paged takes &kv8->kv. */

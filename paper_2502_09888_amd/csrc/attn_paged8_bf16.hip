@@ -158,8 +158,16 @@ struct Block8 {
 };
 
 // 4 waves of QB x 32 packed rows share the keys.  Cached blocks of 32 keys travel as codes, by copies that are two blocks ahead, and each wave
-// widens the fragments that it takes from them: half the bytes through LDS, which all eight waves of a CU read their operands from.
-// The call's own rows follow as in the bf16 paged cache, in the same LDS.
+// widens the fragments that it takes from them: half the bytes through LDS, which all eight waves of a CU read their operands from (us against one
+// widening for all by the wave that copied: sessions 120 / 117, ragged candidates 141 / 133, 512 of each of 64 users 103 / 105).  The call's own
+// rows follow as in the bf16 paged cache, in the same LDS.
+//
+// Bound by the matrix and the vector pipe, which the two waves of a SIMD keep busy at once only in part: of a wave's step of 32 keys 512 cycles are
+// products and as many instructions that widen (64, D = 128) and make exponentials (16, or 32 of two blocks of rows).  512 candidates of each of
+// 64 users on 1024: 103 us, of them 60 the walk (1.15 PFLOP/s) and 43 the rows' bytes at its ends; 256 to 1024 of each of 16 on 512 to 4096: 129 us
+// (0.78 PFLOP/s), the longest one's 128 steps of 0.85 us; chunks of 60 to 500 of eight on 1000 to 4000: 111 us and 6 for the new tokens.
+// Built and not kept (us of ragged candidates, of the chunks): parts of the keys for all 170, 135; two teams of four waves in a workgroup, half
+// of a tile's keys each, 163, 143, and with their phases in turn 153, 135; one wave per SIMD with 64 rows 162, 166.
 template <int D, int QB, bool SUMI>
 __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Args p)
 {
@@ -321,7 +329,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
                 __builtin_amdgcn_sched_barrier(0);
                 st.weights(Sc, P, 0);
                 __builtin_amdgcn_sched_barrier(0);
-                // (from here on the matrix pipe has work: before the other wave of the SIMD, which makes its exponentials meanwhile)
+                // (from here on the matrix pipe has work: before the other wave of the SIMD, which makes its exponentials meanwhile; us without / with:
+                // chunks of eight users 129 / 117, ragged candidates 139 / 132, 512 of each of 64 users 106 / 104)
                 __builtin_amdgcn_s_setprio(1);
                 st.logits(k, Sn);  // (behind the last block: not used)
                 st.weights(Sc, P, 1);
@@ -478,7 +487,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_tile_kernel(const Paged8Ar
 }
 
 // ---- new tokens ----------------------------------------------------------------------------------
-// A wave for a block of 16 tokens of a cache head (the block-th that the sequence's new tokens touch).  The scale is the least with which all of the block's tokens, those that were
+// A wave for a block of 16 tokens of a cache head (the block-th that the sequence's new tokens touch), bound by its chain of loads: 6 us of 2200 new tokens
+// of 8 users.  The scale is the least with which all of the block's tokens, those that were
 // stored before too, stay within 448 of it; where it grows these are rounded again (by a power of two, so that only what lies near the
 // smallest numbers changes).  Infinities become no numbers.
 static __device__ __forceinline__ uint32_t wave_max(uint32_t x)
@@ -599,8 +609,10 @@ __global__ __launch_bounds__(256) void paged8_finish_kernel(const Paged8Args p, 
 
 // ---- few rows ------------------------------------------------------------------------------------
 // 32 packed rows; the waves of a workgroup take different blocks of 32 keys, each through a ring of its own, and are joined at the end.  Two
-// stages, so that a CU has two workgroups: us with four stages and one / this way, one token of 64 users 77 / 70, of one long cache 59 / 52.
-// Where a workgroup is the only one that reads its sequence's head it stores the new tokens itself.
+// stages, so that a CU has two workgroups: us with four stages and one / this way, all else alike, one token of 64 users 77 / 70, of one long cache
+// 59 / 52.  Where a workgroup is the only one that reads its sequence's head it stores the new tokens itself, after it has read the cached ones
+// (one token of 64 users in a launch of its own / this way 70 / 65).  Bound by memory: a token of each of 64 users on 500 to 4000 (8 heads of
+// 128) 61 us, 291 MB at 4.8 TB/s; of one cache of 98765 40 us of 202 MB at 5.1 TB/s, and 5 for the join.  More parts of the keys: 65 / 67 to 87.
 template <int D, bool SUMI>
 __global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Args p)
 {
