@@ -363,6 +363,7 @@ int climber_attn_sumi_paged8(const climber_config *cfg, const float *tau_layer, 
  *   held        dev int32 [n_seqs]: pages that a sequence holds, its row's first entries
  *   len         dev int32 [n_seqs]: its tokens, as a climber_paged_kv's: at most held * page_size
  * Empty: all zeros.  page_size, and the limits of the sizes, as in climber_paged_kv; n_seqs * table_ld below 2^31, n_seqs below 2^24.
+ * A cache whose pages are shared has no mass (see climber_paged_kv), and eviction writes pages: of a sequence that shares none.
  * Results do not depend on the order in which the device works.  Values are device memory and cannot be checked on the host: whatever
  * they hold, nothing is read or written outside the arrays, and calls OR what they find into *status (dev int32, not cleared):
  *   CLIMBER_BAD_PAGE  a page number that is held lies outside the pool (or, compact, is of a page with refs 0)
@@ -380,10 +381,11 @@ typedef struct climber_page_pool {
 size_t climber_pages_workspace_bytes(const climber_page_pool *pool); /* 0 on an invalid argument */
 
 /* All rows at once: sequence b becomes what sequence parent[b] was before the call, up to its first keep[b] tokens (parent, keep: dev int32
- * [n_seqs]; keep NULL: all of them; below 0 counts as 0).  parent[b] = b and nothing cut: the row stays as it is, with the pages
+ * [n_seqs]; keep NULL: all of them; below 0 counts as 0).  parent[b] = b with keep NULL: the row stays as it is, with the pages
  * that it holds beyond its tokens.  parent[b] < 0: the sequence becomes empty.  Otherwise the pages that hold the tokens are shared
  * (held: as many), what the row held before is given up, and entries of it that are held no more become -1.  Branches of a history, beams that take
- * each other's place, a shared prefix, tokens taken back, users that leave are each one call. */
+ * each other's place, a shared prefix, tokens taken back, users that leave are each one call; after an eviction one with parent[b] = b and keep = len gives
+ * the pages back that hold no token any more. */
 int climber_pages_fork(const climber_page_pool *pool, const int32_t *parent, const int32_t *keep, int32_t *status, void *workspace,
                        size_t ws_bytes, void *stream);
 

@@ -93,11 +93,11 @@ static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b)
     if (par >= 0) {
         const int all = max(a.len[par], 0);
         n = a.keep ? min(all, max(a.keep[b], 0)) : all;
-        if (par == b && n == all) {
+        h = min((int)(((int64_t)n + (1 << a.page_shift) - 1) >> a.page_shift), held_of(a, par));
+        if (par == b && n == all && (!a.keep || h == had)) {
             if (lane == 0) a.new_held[b] = -1;
             return;
         }
-        h = min((int)(((int64_t)n + (1 << a.page_shift) - 1) >> a.page_shift), held_of(a, par));
     }
     bool bad = false;
     for (int i = lane; i < max(had, h); i += 64) {
@@ -145,7 +145,8 @@ __global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
             if (par >= 0) {
                 const int there = max(a.len[par], 0);
                 n = a.keep ? min(there, max(a.keep[b], 0)) : there;
-                h = par == b && n == there ? -1 : min((int)(((int64_t)n + (1 << a.page_shift) - 1) >> a.page_shift), held_of(a, par));
+                h = min((int)(((int64_t)n + (1 << a.page_shift) - 1) >> a.page_shift), held_of(a, par));
+                if (par == b && n == there && (!a.keep || h == had)) h = -1;
             }
         } else {
             bits |= CLIMBER_BAD_SEQ;

@@ -44,7 +44,7 @@ class Pool:
                 self.status |= BAD_SEQ
                 continue
             n = 0 if par < 0 else lens[par] if keep is None else min(lens[par], max(0, keep[b]))
-            if par == b and n == lens[b]:
+            if par == b and n == lens[b] and keep is None:
                 continue
             h = 0 if par < 0 else min(self.pages_of(n), helds[par])
             for i in range(helds[b]):

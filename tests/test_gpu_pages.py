@@ -210,6 +210,44 @@ def test_copies_behind_4_gib():
     assert torch.equal(k[290], k[299]) and not k[:290].any() and not k[291:299].any()
 
 
+@pytest.mark.parametrize("n_seqs,table_ld", [(5, 12), (40, 80)])
+def test_pages_of_evicted_tokens_go_back(n_seqs, table_ld):
+    """An eviction cuts the lengths; a fork of each row into itself, with keep, gives up the pages behind, and what stays is what was kept."""
+    import paper_2502_09888_amd as P
+    page, d, r = 16, 64, random.Random(n_seqs)
+    host = Pool.random(8, n_seqs * table_ld, page, n_seqs, table_ld)
+    dev = DevicePool(host)
+    g = torch.Generator(device="cuda:0").manual_seed(3)
+    k = torch.randn((host.n_pages, 2, page, d), generator=g, device="cuda:0").bfloat16()
+    v, rank = k.neg(), torch.rand((host.n_pages, page), generator=g, device="cuda:0")
+    cfg = P.Config(n_heads=2, d_head=d, n_scen=1, n_beh=1, dtype=P.BF16)
+    kv = P.paged_kv(k, v, dev.table, dev.len, table_ld * page)
+    ws = torch.empty(P.climber_paged_workspace_bytes(cfg, kv, 0, 0), dtype=torch.uint8, device="cuda:0")
+    before, old = k.clone(), [list(x) for x in host.table]
+    budget = [r.choice([0, 1, 16, 33, 10 ** 6]) for _ in range(n_seqs)]
+    src = torch.empty((n_seqs, table_ld * page), dtype=torch.int32, device="cuda:0")
+    P.climber_paged_evict(cfg, kv, rank, dev.ints(budget), None, dev.len, src, ws)
+    host.len = [min(n, x) for n, x in zip(host.len, budget)]
+    dev.check()
+    rows = list(range(n_seqs))
+    dev.fork(rows)                                        # (without keep a row stays as it is)
+    dev.check()
+    host.fork(rows, host.len)
+    P.climber_pages_fork(dev.pool, dev.ints(rows), dev.len, dev.status, dev.ws)
+    dev.check()
+    assert host.held == [host.pages_of(n) for n in host.len] and host.used() == sum(host.held)
+    src = src.tolist()
+    for b in range(n_seqs):
+        for slot in range(host.len[b]):
+            was = src[b][slot]
+            assert torch.equal(k[host.table[b][slot // page], :, slot % page], before[old[b][was // page], :, was % page]), (b, slot)
+    more = [20] * n_seqs
+    more = [min(x, table_ld * page - n) for x, n in zip(more, host.len)]
+    copies = host.extend(more)
+    dev.extend(more)
+    dev.check(copies)
+
+
 def test_captured_branches_and_streams():
     """Fork, extend and copy in a graph that is replayed, with eager work between, against the same calls made plainly; and on another stream."""
     import paper_2502_09888_amd as P
