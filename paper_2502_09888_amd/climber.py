@@ -661,23 +661,30 @@ def climber_pages_workspace_bytes(pool: PagePool) -> int:
     return int(load_library().climber_pages_workspace_bytes(C.byref(pool)))
 
 
-def _copies(t, least: int) -> None:
-    if t is not None and not isinstance(t, int) and (t.numel() < 3 * least or not t.is_contiguous()):
-        raise ValueError(f"copies needs room for {least} of three numbers")
+def _ints(**least) -> None:
+    """name=(tensor, integers that it has at least)"""
+    for name, (t, n) in least.items():
+        if t is not None and not isinstance(t, int) and (str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.numel() < n):
+            raise ValueError(f"{name} is a contiguous int32 tensor of {n} or more")
 
 
 def _room(copies, most: int) -> int:
-    """... and is read no further than it has any."""
-    _copies(copies, 0)
-    return most if copies is None or isinstance(copies, int) else min(most, copies.numel() // 3)
+    """Copies are read no further than there are any."""
+    if copies is None or isinstance(copies, int):
+        return most
+    if not copies.is_contiguous():
+        raise ValueError("copies are contiguous")
+    return min(most, copies.numel() // 3)
 
 
 def climber_pages_fork(pool: PagePool, parent, keep, status, workspace, stream=None) -> None:
-    """Sequence b becomes what sequence parent[b] was (below 0: empty), up to its first keep[b] tokens; pages are shared."""
+    """Sequence b becomes what sequence parent[b] was (below 0: empty), up to its first keep[b] tokens; pages are shared, and with keep no row holds
+    more of them than its tokens need."""
     _on_device(pool, stream)
     code = (_native or _load_native(load_library())).pages_fork(pool, parent, keep, status, workspace, stream, pool._device)
     if code is None:
         _there(pool, parent, keep, status, workspace)
+        _ints(parent=(parent, pool.n_seqs), keep=(keep, pool.n_seqs), status=(status, 1))
         code = load_library().climber_pages_fork(C.byref(pool), _ptr(parent), _ptr(keep), _ptr(status), _ptr(workspace), _nbytes(workspace),
                                                  _stream(stream))
     if code:
@@ -687,10 +694,10 @@ def climber_pages_fork(pool: PagePool, parent, keep, status, workspace, stream=N
 def climber_pages_extend(pool: PagePool, rows, copies, counts, status, workspace, stream=None) -> None:
     """Pages for rows[b] more tokens of each sequence; shared pages that they go into are replaced, and copies says by which."""
     _on_device(pool, stream)
-    _copies(copies, pool.n_seqs)
     code = (_native or _load_native(load_library())).pages_extend(pool, rows, copies, counts, status, workspace, stream, pool._device)
     if code is None:
         _there(pool, rows, copies, counts, status, workspace)
+        _ints(rows=(rows, pool.n_seqs), copies=(copies, 3 * pool.n_seqs), counts=(counts, 2), status=(status, 1))
         code = load_library().climber_pages_extend(C.byref(pool), _ptr(rows), _ptr(copies), _ptr(counts), _ptr(status), _ptr(workspace),
                                                    _nbytes(workspace), _stream(stream))
     if code:
@@ -700,10 +707,10 @@ def climber_pages_extend(pool: PagePool, rows, copies, counts, status, workspace
 def climber_pages_compact(pool: PagePool, copies, counts, status, workspace, stream=None) -> None:
     """The pages in use move to the front of the pool; copies says which went where."""
     _on_device(pool, stream)
-    _copies(copies, pool.n_pages // 2)
     code = (_native or _load_native(load_library())).pages_compact(pool, copies, counts, status, workspace, stream, pool._device)
     if code is None:
         _there(pool, copies, counts, status, workspace)
+        _ints(copies=(copies, pool.n_pages // 2 * 3), counts=(counts, 2), status=(status, 1))
         code = load_library().climber_pages_compact(C.byref(pool), _ptr(copies), _ptr(counts), _ptr(status), _ptr(workspace), _nbytes(workspace),
                                                     _stream(stream))
     if code:
@@ -717,6 +724,7 @@ def climber_paged_copy(cfg: Config, kv: PagedKV, copies, counts, max_copies: int
     code = (_native or _load_native(load_library())).paged_copy(cfg, kv, copies, counts, max_copies, stream, kv._device)
     if code is None:
         _there(kv, copies, counts)
+        _ints(copies=(copies, 3 * max_copies), counts=(counts, 1))
         code = load_library().climber_paged_copy(C.byref(cfg), C.byref(kv), _ptr(copies), _ptr(counts), max_copies, _stream(stream))
     if code:
         raise ClimberError(code, "climber_paged_copy")
@@ -729,6 +737,7 @@ def climber_paged8_copy(cfg: Config, kv8: PagedKV8, copies, counts, max_copies: 
     code = (_native or _load_native(load_library())).paged8_copy(cfg, kv8, copies, counts, max_copies, stream, kv8._device)
     if code is None:
         _there(kv8, copies, counts)
+        _ints(copies=(copies, 3 * max_copies), counts=(counts, 1))
         code = load_library().climber_paged8_copy(C.byref(cfg), C.byref(kv8), _ptr(copies), _ptr(counts), max_copies, _stream(stream))
     if code:
         raise ClimberError(code, "climber_paged8_copy")

@@ -25,7 +25,7 @@ static __typeof__(&climber_pages_compact) pages_compact_fn;
 static __typeof__(&climber_paged_copy) paged_copy_fn;
 static __typeof__(&climber_paged8_copy) paged8_copy_fn;
 static __typeof__(&climber_rotary) rotary_fn;
-static PyObject *pool_type, *rotary_type, *bf16_dtype, *f32_dtype, *i32_dtype, *s_dtype, *s_get_device;
+static PyObject *pool_type, *rotary_type, *bf16_dtype, *f32_dtype, *i32_dtype, *s_dtype, *s_get_device, *s_is_contiguous;
 static PyObject *config_type, *bias_type, *current_device, *raw_stream, *paged_type, *paged8_type, *s_data_ptr, *s_cuda_stream, *s_shape, *s_stride, *s_nbytes;
 
 static int unsigned_of(PyObject *o, void **p) /* takes the reference */
@@ -232,20 +232,43 @@ static PyObject *paged_evict(PyObject *m, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(code);
 }
 
-/* pool, n pointers, workspace, stream, device */
-static int pool_call(PyObject *const *a, Py_ssize_t n, int pointers, Py_buffer *pool, void **p, size_t *ws_bytes, void **s)
+/* A tensor of at least n 32-bit integers, one behind the other (pointers and None are taken as they are) */
+static int ints_of(PyObject *o, int64_t n, void **p)
+{
+    if (o != Py_None && !PyLong_Check(o)) {
+        PyObject *t = PyObject_GetAttr(o, s_dtype), *whole = t == i32_dtype ? PyObject_CallMethodNoArgs(o, s_is_contiguous) : NULL;
+        size_t bytes;
+        const int ok = whole == Py_True && bytes_of(o, &bytes) && bytes / 4 >= (uint64_t)n;
+        Py_XDECREF(t);
+        Py_XDECREF(whole);
+        if (!ok) return 0;
+    }
+    return pointer(o, p);
+}
+
+/* pool, n pointers (i: to n_seqs * seqs[i] + pages / 2 * halves[i] + more[i] integers), workspace, stream, device */
+static int pool_call(PyObject *const *a, Py_ssize_t n, int pointers, const int (*sizes)[3], Py_buffer *pool, void **p, size_t *ws_bytes, void **s)
 {
     if (n != pointers + 4 || !pool_type) return 0;
     for (int i = 1; i <= pointers + 1; ++i)
-        if (!lies_on(a[i], a[n - 1]) || !pointer(a[i], &p[i])) return 0;
-    return bytes_of(a[n - 3], ws_bytes) && stream_of(a[n - 2], s) && structure(a[0], pool_type, sizeof(climber_page_pool), pool);
+        if (!lies_on(a[i], a[n - 1])) return 0;
+    if (!pointer(a[pointers + 1], &p[pointers + 1]) || !bytes_of(a[n - 3], ws_bytes) || !stream_of(a[n - 2], s) ||
+        !structure(a[0], pool_type, sizeof(climber_page_pool), pool))
+        return 0;
+    const climber_page_pool *c = pool->buf;
+    for (int i = 1; i <= pointers; ++i) {
+        const int *x = sizes[i - 1];
+        if (!ints_of(a[i], (int64_t)x[0] * c->n_seqs + (int64_t)x[1] * (c->n_pages / 2) + x[2], &p[i])) return PyBuffer_Release(pool), 0;
+    }
+    return 1;
 }
 static PyObject *pages_fork(PyObject *m, PyObject *const *a, Py_ssize_t n) /* parent, keep, status */
 {
     Py_buffer pool;
     void *p[5], *s;
     size_t ws;
-    if (!pool_call(a, n, 3, &pool, p, &ws, &s)) return elsewhere();
+    static const int sizes[3][3] = {{1, 0, 0}, {1, 0, 0}, {0, 0, 1}};
+    if (!pool_call(a, n, 3, sizes, &pool, p, &ws, &s)) return elsewhere();
     int code;
     Py_BEGIN_ALLOW_THREADS
     code = pages_fork_fn(pool.buf, p[1], p[2], p[3], p[4], ws, s);
@@ -258,7 +281,8 @@ static PyObject *pages_extend(PyObject *m, PyObject *const *a, Py_ssize_t n) /* 
     Py_buffer pool;
     void *p[6], *s;
     size_t ws;
-    if (!pool_call(a, n, 4, &pool, p, &ws, &s)) return elsewhere();
+    static const int sizes[4][3] = {{1, 0, 0}, {3, 0, 0}, {0, 0, 2}, {0, 0, 1}};
+    if (!pool_call(a, n, 4, sizes, &pool, p, &ws, &s)) return elsewhere();
     int code;
     Py_BEGIN_ALLOW_THREADS
     code = pages_extend_fn(pool.buf, p[1], p[2], p[3], p[4], p[5], ws, s);
@@ -271,7 +295,8 @@ static PyObject *pages_compact(PyObject *m, PyObject *const *a, Py_ssize_t n) /*
     Py_buffer pool;
     void *p[5], *s;
     size_t ws;
-    if (!pool_call(a, n, 3, &pool, p, &ws, &s)) return elsewhere();
+    static const int sizes[3][3] = {{0, 3, 0}, {0, 0, 2}, {0, 0, 1}};
+    if (!pool_call(a, n, 3, sizes, &pool, p, &ws, &s)) return elsewhere();
     int code;
     Py_BEGIN_ALLOW_THREADS
     code = pages_compact_fn(pool.buf, p[1], p[2], p[3], p[4], ws, s);
@@ -287,7 +312,7 @@ static PyObject *copy(PyObject *const *a, Py_ssize_t n, int bits8)
     Py_buffer cfg, kv;
     void *copies, *counts, *s;
     int32_t most;
-    if (!pointer(a[2], &copies) || !pointer(a[3], &counts) || !number(a[4], &most) || !stream_of(a[5], &s)) return elsewhere();
+    if (!number(a[4], &most) || !ints_of(a[2], 3 * (int64_t)(most < 0 ? 0 : most), &copies) || !ints_of(a[3], 1, &counts) || !stream_of(a[5], &s)) return elsewhere();
     if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
     if (bits8 ? !structure(a[1], paged8_type, sizeof(climber_paged_kv8), &kv) : !structure(a[1], paged_type, sizeof(climber_paged_kv), &kv))
         return PyBuffer_Release(&cfg), elsewhere();
@@ -440,5 +465,6 @@ PyMODINIT_FUNC PyInit__native(void)
     s_nbytes = PyUnicode_InternFromString("nbytes");
     s_dtype = PyUnicode_InternFromString("dtype");
     s_get_device = PyUnicode_InternFromString("get_device");
-    return s_dtype && s_get_device && s_data_ptr && s_cuda_stream && s_shape && s_stride && s_nbytes ? PyModule_Create(&module) : NULL;
+    s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    return s_is_contiguous && s_dtype && s_get_device && s_data_ptr && s_cuda_stream && s_shape && s_stride && s_nbytes ? PyModule_Create(&module) : NULL;
 }

@@ -103,3 +103,26 @@ def test_copies_are_read_no_further_than_they_go():
     assert _room(FAKE, 100) == 100 and _room(None, 100) == 100
     with pytest.raises(ValueError):
         _room(torch.zeros((3, 7), dtype=torch.int32).t(), 5)
+
+
+def test_other_tensors_than_the_calls_read_are_refused():
+    """Too short, of another type, not one behind the other: each argument by itself, the others in order (no workspace: nothing would be launched)."""
+    torch = pytest.importorskip("torch")
+    p = P.page_pool(torch.zeros(10, dtype=torch.int32), torch.zeros((6, 4), dtype=torch.int32), torch.zeros(6, dtype=torch.int32),
+                    torch.zeros(6, dtype=torch.int32), 16)
+    p._device = None
+    for f, sizes in ((P.climber_pages_fork, (6, 6, 1)), (P.climber_pages_extend, (6, 18, 2, 1)), (P.climber_pages_compact, (15, 2, 1))):
+        right = [torch.zeros(n, dtype=torch.int32) for n in sizes]
+        with pytest.raises(P.ClimberError):
+            f(p, *right, None, stream=0)
+        for i, n in enumerate(sizes):
+            for bad in (torch.zeros(n - 1, dtype=torch.int32), torch.zeros(n, dtype=torch.int64), torch.zeros(4 * n, dtype=torch.uint8),
+                        torch.zeros(n, dtype=torch.float32), torch.zeros((n + 1, 2), dtype=torch.int32)[:, 0]):
+                with pytest.raises(ValueError):
+                    f(p, *(bad if i == j else t for j, t in enumerate(right)), None, stream=0)
+    for f, cache in ((P.climber_paged_copy, kv()), (P.climber_paged8_copy, kv8())):
+        for copies, counts in ((torch.zeros((4, 3), dtype=torch.int64), torch.zeros(2, dtype=torch.int32)),
+                               (torch.zeros((4, 3), dtype=torch.int32), torch.zeros(2, dtype=torch.int64)),
+                               (torch.zeros((4, 3), dtype=torch.int32), torch.zeros(0, dtype=torch.int32))):
+            with pytest.raises(ValueError):
+                f(cfg(), cache, copies, counts, 4, stream=0)
