@@ -728,7 +728,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Arg
     }
     if (lane == 0) odd_seen[wave] = odd;
     StoreBlock<D> put;
-    const bool stores = !SUMI && p.n_split == 1;
+    const bool stores = !SUMI && p.n_split == 1;  // (32 rows touch 3 blocks at most)
     if (stores && wave < p.store_blocks) put.load(p, s, w.b, w.hk, wave);
     // (each wave's outputs in units of its reference take the 2 x kStage bytes of two waves' places; all waves are done with theirs at the first barrier)
     join_few<D, true>(p, s, w, st, joined, [&](int j) { return (float *)(j < 2 ? stage0 : stage1) + (j & 1) * 32 * D; }, row, h, r_tile, rows);
@@ -740,13 +740,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Arg
             if (wave == 0) put_odd<D>(p, s, w, from + clean, k_hi, r_tile, min(r_tile + 32, rows), sees);
         }
         // (all of its waves have read the cached tokens, behind whose barrier they were joined)
-        if (stores) {
-            if (wave < p.store_blocks) put.write(p, s, w.hk);
-            for (int i = wave + 4; i < p.store_blocks; i += 4) {
-                put.load(p, s, w.b, w.hk, i);
-                put.write(p, s, w.hk);
-            }
-        }
+        if (stores && wave < p.store_blocks) put.write(p, s, w.hk);
     }
 }
 
