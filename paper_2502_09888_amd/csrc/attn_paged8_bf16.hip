@@ -728,7 +728,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged8_few_kernel(const Paged8Arg
     }
     if (lane == 0) odd_seen[wave] = odd;
     StoreBlock<D> put;
-    const bool stores = !SUMI && p.n_split == 1;  // (32 rows touch 3 blocks at most)
+    const bool stores = !SUMI && p.n_split == 1 && p.n_tiles == 1;  // (32 rows touch 3 blocks at most)
     if (stores && wave < p.store_blocks) put.load(p, s, w.b, w.hk, wave);
     // (each wave's outputs in units of its reference take the 2 x kStage bytes of two waves' places; all waves are done with theirs at the first barrier)
     join_few<D, true>(p, s, w, st, joined, [&](int j) { return (float *)(j < 2 ? stage0 : stage1) + (j & 1) * 32 * D; }, row, h, r_tile, rows);
@@ -748,7 +748,7 @@ template <int D, bool SUMI>
 hipError_t launch(Paged8Args p, hipStream_t s)
 {
     const int64_t rows = (int64_t)p.m_max * p.G;
-    const int tile = paged8_tile_rows(D, rows, (int64_t)p.n_seqs * p.Hkv);
+    const int tile = paged8_tile_rows(D, rows, (int64_t)p.n_seqs * p.Hkv, p.max_len);
     void (*kernel)(Paged8Args) = tile == 32 ? attn_paged8_few_kernel<D, SUMI> : attn_paged8_tile_kernel<D, 1, SUMI>;
     if constexpr (D == 64)
         if (tile == 256) kernel = attn_paged8_tile_kernel<D, 2, SUMI>;
@@ -765,7 +765,7 @@ hipError_t launch(Paged8Args p, hipStream_t s)
         const unsigned joins = (unsigned)(p.n_split <= 4 ? (all + 7) / 8 : all);
         if (p.n_split <= 4) hipLaunchKernelGGL((paged8_finish_kernel<D, 1>), dim3(joins + stores), dim3(256), 0, s, p, joins);
         else hipLaunchKernelGGL((paged8_finish_kernel<D, 8>), dim3(joins + stores), dim3(256), 0, s, p, joins);
-    } else if (!SUMI && tile != 32) {
+    } else if (!SUMI && (tile != 32 || p.n_tiles > 1)) {
         hipLaunchKernelGGL(paged8_store_kernel<D>, dim3(stores), dim3(256), 0, s, p);
     }
     return hipGetLastError();

@@ -20,7 +20,7 @@ int attn_paged8(const Call &c, const climber_paged_kv8 *kv8, void *workspace, si
     bool nothing;
     e = check_call(c, nothing);
     if (e || nothing) return e;
-    const int64_t G = cfg->n_heads / kv->n_kv_heads, heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged8_tile_rows(cfg->d_head, c.m_max * G, heads);
+    const int64_t G = cfg->n_heads / kv->n_kv_heads, heads = (int64_t)kv->n_seqs * kv->n_kv_heads, tile = paged8_tile_rows(cfg->d_head, c.m_max * G, heads, kv->max_len);
     const int n_split = parts(cfg, kv, c.m_total, c.m_max, tile);
     if ((c.m_max * G + tile - 1) / tile * (heads + 7) * n_split >= kMostGroups) return CLIMBER_ERR_RANGE;
     // (new tokens are stored in a launch of their own, or with the join of the parts, a workgroup for a row and head at most)

@@ -64,7 +64,7 @@ hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t)
     const int64_t out = (int64_t)a.m_total * a.H, rows = (int64_t)a.m_max * a.G, bh = (int64_t)a.n_seqs * a.Hkv;
     if (a.n_split > 1) in_workspace({{"part_o", u8(a.part_o), a.n_split * out * a.d * 4}, {"part_ml", u8(a.part_ml), a.n_split * out * 8}});
     if (!a.k_scale || !a.v_scale || a.row_bytes != a.d || a.mass) ++bad;
-    const int tile = paged8_tile_rows(a.d, rows, bh);
+    const int tile = paged8_tile_rows(a.d, rows, bh, a.max_len);
     threads("attention", (bh + 7) * ((rows + tile - 1) / tile) * a.n_split, 256);
     const int64_t after = (a.sumi ? 0 : (bh * paged8_store_blocks(a.m_max) + 3) / 4) + (a.n_split > 1 ? out : 0);
     if (after > 0) threads("new tokens and join", after, 256);

@@ -11,10 +11,16 @@ from test_gpu_paged import LENS
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(params=[0, 1100], ids=["few", "many"])
+def batch(request, monkeypatch):
+    """The case alone, and with 1100 sequences that have nothing: more than a few rows are then done in tiles of 128 or 256, not of 32."""
+    monkeypatch.setattr(Device8, "more", request.param)
+
+
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("lens", LENS)
-def test_attention_and_append(lens, d, sumi):
+def test_attention_and_append(lens, d, sumi, batch):
     case = Case8(*LENS[lens], d=d, sumi=sumi, seed=len(lens) + d)
     dev = Device8(case, stamp=True)
     dev.attend()
@@ -24,7 +30,7 @@ def test_attention_and_append(lens, d, sumi):
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("H,Hkv", [(1, 1), (3, 3), (5, 1), (8, 2), (40, 1), (64, 8)])
-def test_head_layouts(H, Hkv, d, sumi):
+def test_head_layouts(H, Hkv, d, sumi, batch):
     case = Case8([70, 9], [7, 33], H=H, Hkv=Hkv, d=d, sumi=sumi, seed=H)
     dev = Device8(case)
     dev.attend()
@@ -33,7 +39,7 @@ def test_head_layouts(H, Hkv, d, sumi):
 
 @pytest.mark.parametrize("page", [16, 32, 128, 1024])
 @pytest.mark.parametrize("d", [64, 128])
-def test_pages_strides_and_whole_chunks(page, d):
+def test_pages_strides_and_whole_chunks(page, d, batch):
     # without the causal flag every new token sees the whole chunk; rows are columns of wider rows; three rows belong to nobody
     for causal in (False, True):
         case = Case8([page - 1, 40, 2 * page + 5], [page + 3, 9, 70], page=page, d=d, causal=causal, tail=3, seed=page)
@@ -44,7 +50,7 @@ def test_pages_strides_and_whole_chunks(page, d):
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n", [2047, 5003, 9000])
-def test_long_cache(d, n):
+def test_long_cache(d, n, batch):
     # keys shared out over workgroups whose parts are joined; more page numbers and scales than a wave holds at once
     for chunk in (1, 50):
         case = Case8([n], [chunk], d=d, page=64, H=8, seed=n)
@@ -58,7 +64,7 @@ def test_long_cache(d, n):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_short_sequences_in_a_launch_for_long_ones(d):
+def test_short_sequences_in_a_launch_for_long_ones(d, batch):
     wide = Case8([37, 1], [1, 2], d=d, page=64, seed=4)
     wide.table = torch.cat([wide.table, torch.full((2, 1000), -1, dtype=torch.int32)], dim=1)
     dev = Device8(wide, max_len=60000)
@@ -68,7 +74,7 @@ def test_short_sequences_in_a_launch_for_long_ones(d):
 
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("d", [64, 128])
-def test_many_rows_on_a_longer_cache(d, sumi):
+def test_many_rows_on_a_longer_cache(d, sumi, batch):
     # whole tiles of rows over many blocks of cached keys and of the call's own
     for causal in (True, False):
         case = Case8([700, 33, 0, 512], [300, 140, 257, 64], H=4, Hkv=1, d=d, page=32, sumi=sumi, causal=causal, seed=d)
@@ -119,7 +125,7 @@ def test_the_largest_tiles(sumi, causal, kind):
 
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("d", [64, 128])
-def test_large_logits(d, sumi):
+def test_large_logits(d, sumi, batch):
     # one-hot rows, and logits far above and below those before them
     case = Case8([150, 80], [40, 100], d=d, std=6.0, scale=1.0, sumi=sumi, seed=11)
     case.tau.fill_(0.5)
@@ -131,7 +137,7 @@ def test_large_logits(d, sumi):
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("std,values", [(4.0, 1e30), (1.0, 1e32), (4.0, 1e-30)])
-def test_large_and_small_values(d, std, values, sumi):
+def test_large_and_small_values(d, std, values, sumi, batch):
     # weights of later keys that exceed those of the first by 2^30 and more, on values with which unscaled sums pass 2^128; 700 tokens
     # of at most 6e32 stay below 2^119
     case = Case8([500, 33], [190, 4], d=d, std=std, sumi=sumi, seed=53)
@@ -145,7 +151,7 @@ def test_large_and_small_values(d, std, values, sumi):
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("late", ["cached", "last cached", "own"])
-def test_weights_that_exceed_the_first_ones_by_far(d, late, sumi):
+def test_weights_that_exceed_the_first_ones_by_far(d, late, sumi, batch):
     # one row's logits rise by more than 2^100 in exp2 units behind the first blocks: the sums so far vanish against it, and its neighbours
     # keep theirs
     case = Case8([299, 0], [140, 130], H=4, Hkv=2, d=d, sumi=sumi, scale=1.0, seed=71)
@@ -168,7 +174,7 @@ def test_weights_that_exceed_the_first_ones_by_far(d, late, sumi):
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf, 3.0e38])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("cached,chunk,at", [(20, 100, 50), (4, 7, 3), (260, 150, 140)])
-def test_a_token_has_no_influence_on_rows_that_do_not_see_it(d, bad, cached, chunk, at):
+def test_a_token_has_no_influence_on_rows_that_do_not_see_it(d, bad, cached, chunk, at, batch):
     clean, case = (Case8([cached], [chunk], d=d, seed=5) for _ in range(2))
     for name in ("kn", "vn"):
         getattr(case, name)[at:] = bad
@@ -202,7 +208,7 @@ def test_a_cached_token_that_is_no_number_reaches_every_row():
     assert torch.isnan(got[:, 2:, 9]).all() and torch.isfinite(got[:, :2]).all()
 
 
-def test_candidates_do_not_see_each_other():
+def test_candidates_do_not_see_each_other(batch):
     clean, case = Case8([70], [90], sumi=True, seed=6), Case8([70], [90], sumi=True, seed=6)
     case.kn[30] = math.nan
     case.vn[31] = math.inf
@@ -272,7 +278,7 @@ def test_chunks_that_end_anywhere_give_the_same_cache_as_their_parts():
             assert np.all(np.abs(a - c) <= 2.0 ** -9)     # one step of the smallest codes
 
 
-def test_slots_behind_max_len_are_not_stored():
+def test_slots_behind_max_len_are_not_stored(batch):
     case = Case8([60, 20], [30, 9], page=16, seed=9)
     dev = Device8(case, stamp=True, max_len=70)
     dev.attend()
@@ -302,7 +308,7 @@ def test_lengths_and_page_numbers_that_break_the_contract_stay_in_bounds():
 
 
 @pytest.mark.parametrize("sumi", [False, True], ids=["history", "sumi"])
-@pytest.mark.parametrize("n_seqs,cached,chunk,Hkv", [(70, 150, 36, 8), (300, 40, 1, 2), (16, 600, 70, 2)])
+@pytest.mark.parametrize("n_seqs,cached,chunk,Hkv", [(70, 150, 36, 8), (300, 40, 1, 2), (16, 600, 70, 2), (70, 150, 100, 8), (20, 1500, 200, 1)])
 def test_batches_of_very_different_lengths(n_seqs, cached, chunk, Hkv, sumi):
     g = torch.Generator().manual_seed(50)
     lens, rows = (torch.randint(lo, hi + 1, (n_seqs,), generator=g).tolist() for lo, hi in ((0, cached), (int(chunk == 1), chunk)))
@@ -316,7 +322,7 @@ def test_batches_of_very_different_lengths(n_seqs, cached, chunk, Hkv, sumi):
     check8(case, dev)
 
 
-def test_pool_beyond_32_bits():
+def test_pool_beyond_32_bits(batch):
     # the same calls with their pages behind 4 GiB of others
     case = Case8([130, 40, 0], [5, 40, 17], page=256, d=128, seed=54)
     small, big = Device8(case, stamp=True), Device8(case, stamp=True)
@@ -330,7 +336,7 @@ def test_pool_beyond_32_bits():
     big.describe()
     for dev in (small, big):
         dev.history()
-        dev.len += torch.tensor(case.chunk, dtype=torch.int32, device="cuda:0")
+        dev.len[:3] += torch.tensor(case.chunk, dtype=torch.int32, device="cuda:0")
     check8(case, small)
     for dev in (small, big):
         dev.sumi()
@@ -341,7 +347,7 @@ def test_pool_beyond_32_bits():
 
 
 @pytest.mark.parametrize("chunk", [[1, 1, 1], [40, 3, 0]], ids=["decode", "chunks"])
-def test_captured_steps_of_two_caches(chunk):
+def test_captured_steps_of_two_caches(chunk, batch):
     # one graph per cache, with a workspace each: append, lengths, scores; replays alternate, with eager work between them
     def start(seed):
         case = Case8([60, 30, 200], chunk, H=8, seed=seed, free=8)
@@ -361,7 +367,7 @@ def test_captured_steps_of_two_caches(chunk):
 
     def step(dev, stream=None):
         dev.history(stream)
-        dev.len += more
+        dev.len[:3] += more
         dev.sumi(stream)
 
     more = torch.tensor(chunk, dtype=torch.int32, device="cuda:0")
@@ -396,7 +402,7 @@ def test_other_streams_and_two_calls_at_once():
         check8(c, d)
 
 
-def test_same_call_same_bits():
+def test_same_call_same_bits(batch):
     results = []
     for _ in range(2):
         dev = Device8(Case8([300, 800, 5], [100, 1, 40], H=8, seed=22))
