@@ -172,7 +172,7 @@ __global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
 }
 
 // ---- extend --------------------------------------------------------------------------------------
-constexpr int kFewSeqs = 1024, kFewUnits = 64, kFewWriters = 512, kListPages = 4096;  // what one workgroup takes; free pages that it keeps in LDS
+constexpr int kFewSeqs = 1024, kFewUnits = 64, kFewWriters = 512, kListPages = 4096, kFewNew = 4;  // what one workgroup takes; free pages that it keeps in LDS; new ones that a thread writes
 constexpr int kCompactFew = 2048;  // entries of a table that one workgroup takes (us by it / in three launches: 8192 entries 23.5 / 17.5, 50 entries 7 / 14)
 constexpr int kNobody = 1 << 30;  // in last[]: a shared page that none of its writers keeps (n_seqs is less)
 
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256) void extend_write_kernel(const ExtendArgs a)
 // us of a run with fork and copies, in the launches above / this way: one branch 25 / 15, four branches of 32 users 29 / 20, half of 256 users gone 153 / 150.
 __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
 {
-    __shared__ int sums[3][16], list[kListPages], unit_at[kFewUnits + 1], n_listed, problems;
+    __shared__ int sums[3][16], list[kListPages], unit_at[kFewUnits + 1], n_listed, problems, some_long;
     // a table of shared pages that are written, at most half full: page, its writers, the last of them
     __shared__ int key[2 * kFewWriters], n_writers[2 * kFewWriters], last_writer[2 * kFewWriters];
     __shared__ uint64_t words[kFewUnits * 16];
@@ -365,7 +365,7 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
     Need x{};
     int had = 0;
     if (mine) x = need_of(a, b), had = held_of(a, b);
-    if (t == 0) n_listed = 0, problems = 0;
+    if (t == 0) n_listed = 0, problems = 0, some_long = 0;
     if (t < 2 * kFewWriters) key[t] = -1, n_writers[t] = 0, last_writer[t] = -1;
     int32_t *const row = a.table + (int64_t)b * a.table_ld;
     auto place = [](int page) { return (int)((uint32_t)page * 2654435769u >> 16) % (2 * kFewWriters); };
@@ -487,6 +487,14 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
             to0 += __popcll(w);
         }
     }
+    // New pages of a sequence that gets more than a few: by all threads, each looking for the sequence of its page (eight sequences of 421 pages, half of
+    // which come back: the run 129 / 41 us).  In place of the table, which nobody reads any more: the sequence's first page of the call, what makes
+    // a page's place of its number, the first place.
+    static_assert(2 * kFewWriters >= kFewSeqs);
+    const int fresh_pages = max(0, x.need - had);
+    const bool is_long = fresh_pages > kFewNew;
+    key[t] = at, n_writers[t] = had - (at + c - fresh_pages), last_writer[t] = is_long ? had : 0x7fffffff;
+    if (is_long) some_long = 1;
     __syncthreads();  // (and all have made up their minds: refs change from here on)
     auto take = [&](int i) { return i < kListPages ? list[i] : fresh(a.free_list + i); };
     if (shared)
@@ -502,11 +510,26 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
                 o[0] = page, o[1] = to, o[2] = x.part;
             }
         }
-    for (int i = had; i < x.need; ++i) {
-        const int to = take(at++);
-        row[i] = to;
-        a.refs[to] = 1;
-    }
+    if (!is_long)
+        for (int i = had; i < x.need; ++i) {
+            const int to = take(at++);
+            row[i] = to;
+            a.refs[to] = 1;
+        }
+    if (some_long)
+        for (int j = t; j < total; j += 1024) {
+            int lo = 0, hi = a.n_seqs;  // (the last sequence whose first page is not behind page j)
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (key[mid] <= j) lo = mid;
+                else hi = mid;
+            }
+            const int i = j + n_writers[lo];
+            if (i < last_writer[lo]) continue;
+            const int to = take(j);
+            a.table[(int64_t)lo * a.table_ld + i] = to;
+            a.refs[to] = 1;
+        }
     if (mine && x.need > had) a.held[b] = x.need;
 }
 
