@@ -16,7 +16,7 @@ struct PoolArgs {
 struct ForkArgs : PoolArgs {
     const int32_t *parent, *keep;
     // workspace
-    int32_t *rows, *new_len, *new_held;  // [n_seqs][table_ld], [n_seqs], [n_seqs]
+    int32_t *rows, *new_len, *new_held, *entries;  // [n_seqs][table_ld], [n_seqs], [n_seqs], [n_seqs]
 };
 
 struct ExtendArgs : PoolArgs {

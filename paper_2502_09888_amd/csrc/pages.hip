@@ -78,14 +78,18 @@ static __device__ __forceinline__ void look(const int32_t *refs, int n_pages, in
 // ---- fork ----------------------------------------------------------------------------------------
 constexpr int kForkFew = 2048;  // entries of a table that one workgroup takes (us of a whole run, in two launches / this way: 6 entries 18 / 15, 8192 entries 150 / 166)
 
-// What rows become is read before any row is written: a wave for each row notes it and counts, another launch writes it.  Bound by its launches: 3 to 5 us
+// Waves for a row of a table: more than one where rows are long and few (us of a run that forks and moves two rows of 6173 entries and of the calls
+// around it, with one / with these 173 / 46).
+static int row_waves(const PoolArgs &a) { return (int)std::max<int64_t>(1, std::min<int64_t>((a.table_ld + 63) / 64, 1024 / a.n_seqs)); }
+
+// What rows become is read before any row is written: a row's waves note it and count, another launch writes it.  Bound by its launches: 3 to 5 us
 // each for 160 to 256 rows.
-static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b)
+static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b, int piece, int pieces)
 {
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, first = piece * 64 + lane;
     const int par = a.parent[b];
     if (par >= a.n_seqs) {  // (no sequence: the row stays)
-        if (lane == 0) atomicOr(a.status, CLIMBER_BAD_SEQ), a.new_held[b] = -1;
+        if (first == 0) atomicOr(a.status, CLIMBER_BAD_SEQ), a.new_held[b] = -1;
         return;
     }
     const int had = held_of(a, b);
@@ -95,12 +99,12 @@ static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b)
         n = a.keep ? min(all, max(a.keep[b], 0)) : all;
         h = min((int)(((int64_t)n + (1 << a.page_shift) - 1) >> a.page_shift), held_of(a, par));
         if (par == b && n == all && (!a.keep || h == had)) {
-            if (lane == 0) a.new_held[b] = -1;
+            if (first == 0) a.new_held[b] = -1;
             return;
         }
     }
     bool bad = false;
-    for (int i = lane; i < max(had, h); i += 64) {
+    for (int i = first; i < max(had, h); i += 64 * pieces) {
         const int was = i < had ? a.table[(int64_t)b * a.table_ld + i] : -1, is = i < h ? a.table[(int64_t)par * a.table_ld + i] : -1;
         a.rows[(int64_t)b * a.table_ld + i] = is;
         bad |= i < h && !in_pool(a, is);
@@ -109,26 +113,26 @@ static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b)
         if (in_pool(a, is)) atomicAdd(a.refs + is, 1);
     }
     if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
-    if (lane == 0) a.new_len[b] = n, a.new_held[b] = h;
+    if (first == 0) a.new_len[b] = n, a.new_held[b] = h, a.entries[b] = max(had, h);
 }
-static __device__ __forceinline__ void fork_write(const ForkArgs &a, int b)
+static __device__ __forceinline__ void fork_write(const ForkArgs &a, int b, int piece, int pieces)
 {
-    const int lane = threadIdx.x & 63;
+    const int first = piece * 64 + (threadIdx.x & 63);
     const int h = a.new_held[b];
     if (h < 0) return;
-    const int had = held_of(a, b);
-    for (int i = lane; i < max(had, h); i += 64) a.table[(int64_t)b * a.table_ld + i] = a.rows[(int64_t)b * a.table_ld + i];
-    if (lane == 0) a.len[b] = a.new_len[b], a.held[b] = h;
+    const int n = a.entries[b];  // (a.held changes here)
+    for (int i = first; i < n; i += 64 * pieces) a.table[(int64_t)b * a.table_ld + i] = a.rows[(int64_t)b * a.table_ld + i];
+    if (first == 0) a.len[b] = a.new_len[b], a.held[b] = h;
 }
 __global__ __launch_bounds__(256) void fork_read_kernel(const ForkArgs a)
 {
     const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (b < a.n_seqs) fork_read(a, b);
+    if (b < a.n_seqs) fork_read(a, b, blockIdx.y, gridDim.y);
 }
 __global__ __launch_bounds__(256) void fork_write_kernel(const ForkArgs a)
 {
     const int b = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (b < a.n_seqs) fork_write(a, b);
+    if (b < a.n_seqs) fork_write(a, b, blockIdx.y, gridDim.y);
 }
 // ... small tables by one workgroup, a thread for each entry in turn; bound by its trips to memory, one behind the other
 __global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
@@ -661,7 +665,7 @@ __global__ __launch_bounds__(1024) void compact_few_kernel(const CompactArgs a)
     }
     if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
 }
-__global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a, int pair_groups)
+__global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a, int pair_groups, int pieces)
 {
     const int n = a.counts[0], n_used = a.counts[1];
     if ((int)blockIdx.x < pair_groups) {
@@ -674,11 +678,11 @@ __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a, 
         }
         return;
     }
-    const int lane = threadIdx.x & 63, b = (blockIdx.x - pair_groups) * 4 + (threadIdx.x >> 6);
+    const int g = blockIdx.x - pair_groups, b = g / pieces * 4 + (threadIdx.x >> 6);
     if (b >= a.n_seqs) return;
     const int had = held_of(a, b);
     bool bad = false;
-    for (int i = lane; i < had; i += 64) {
+    for (int i = g % pieces * 64 + (threadIdx.x & 63); i < had; i += 64 * pieces) {
         int32_t *const e = a.table + (int64_t)b * a.table_ld + i;
         const int page = *e;
         if (!in_pool(a, page)) bad = true;
@@ -735,7 +739,7 @@ hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t s)
         hipLaunchKernelGGL(fork_few_kernel, dim3(1), dim3(1024), 0, s, a);
         return hipGetLastError();
     }
-    const dim3 grid((unsigned)((a.n_seqs + 3) / 4));
+    const dim3 grid((unsigned)((a.n_seqs + 3) / 4), (unsigned)row_waves(a));
     hipLaunchKernelGGL(fork_read_kernel, grid, dim3(256), 0, s, a);
     hipLaunchKernelGGL(fork_write_kernel, grid, dim3(256), 0, s, a);
     return hipGetLastError();
@@ -765,7 +769,7 @@ hipError_t launch_pages_compact(const CompactArgs &a, hipStream_t s)
     const int pair_groups = (int)std::min<int64_t>(1024, (a.n_pages / 2 + 255) / 256 + 1);
     hipLaunchKernelGGL(compact_look_kernel, dim3(units), dim3(256), 0, s, a);
     hipLaunchKernelGGL(compact_list_kernel, dim3(units), dim3(256), 0, s, a);
-    hipLaunchKernelGGL(compact_move_kernel, dim3((unsigned)(pair_groups + (a.n_seqs + 3) / 4)), dim3(256), 0, s, a, pair_groups);
+    hipLaunchKernelGGL(compact_move_kernel, dim3((unsigned)(pair_groups + (a.n_seqs + 3) / 4 * row_waves(a))), dim3(256), 0, s, a, pair_groups, row_waves(a));
     return hipGetLastError();
 }
 

@@ -28,7 +28,8 @@ PoolLayout fork_layout(const climber_page_pool *p)
     PoolLayout w{};
     w.b = up((size_t)p->n_seqs * p->table_ld * 4);
     w.c = w.b + up((size_t)p->n_seqs * 4);
-    w.bytes = w.c + up((size_t)p->n_seqs * 4);
+    w.d = w.c + up((size_t)p->n_seqs * 4);
+    w.bytes = w.d + up((size_t)p->n_seqs * 4);
     return w;
 }
 PoolLayout extend_layout(const climber_page_pool *p)
@@ -128,6 +129,7 @@ int climber_pages_fork(const climber_page_pool *pool, const int32_t *parent, con
     a.rows = (int32_t *)ws;
     a.new_len = (int32_t *)(ws + w.b);
     a.new_held = (int32_t *)(ws + w.c);
+    a.entries = (int32_t *)(ws + w.d);
     return rt(launch_pages_fork(a, (hipStream_t)stream));
 }
 

@@ -73,7 +73,8 @@ hipError_t launch_attn_paged8(const Paged8Args &a, hipStream_t)
 hipError_t launch_pages_fork(const ForkArgs &a, hipStream_t)
 {
     ++launches;
-    in_workspace({{"rows", u8(a.rows), (int64_t)a.n_seqs * a.table_ld * 4}, {"new_len", u8(a.new_len), a.n_seqs * 4ll}, {"new_held", u8(a.new_held), a.n_seqs * 4ll}});
+    in_workspace({{"rows", u8(a.rows), (int64_t)a.n_seqs * a.table_ld * 4}, {"new_len", u8(a.new_len), a.n_seqs * 4ll}, {"new_held", u8(a.new_held), a.n_seqs * 4ll},
+                  {"entries", u8(a.entries), a.n_seqs * 4ll}});
     threads("fork", (a.n_seqs + 3) / 4, 256);
     return hipSuccess;
 }
