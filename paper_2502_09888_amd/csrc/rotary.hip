@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
 #include "paged_host.h"
@@ -27,7 +28,7 @@ struct RotaryArgs {
     const int32_t *pos;
     float scale;
     int64_t m;
-    int d, half, rows, inverse;  // rows: of a workgroup
+    int d, half, rows, inverse, in_place;  // rows: of a workgroup
 };
 
 constexpr int kMostHalf = 256, kTurns = 1024;  // sines and cosines of a workgroup
@@ -46,20 +47,60 @@ static __device__ __forceinline__ float2 turn(double turns, float scale, int inv
     return float2{co * scale, (inverse ? -si : si) * scale};
 }
 
-// N elements of type T, of whichever alignment that makes.  N: elements that travel together, 16 bytes where rows, heads and halves allow it.
-template <typename T, int N>
-struct alignas(sizeof(T) * N) Some {
+// 16 bytes, at any element: a head's halves may begin at an odd one.
+typedef uint32_t Words2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t Words4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T>
+struct Some {
+    static constexpr int N = 16 / sizeof(T);
+    typedef std::conditional_t<sizeof(T) == 2, Words2, Words4> Words;
     T x[N];
+    __device__ __forceinline__ void load(const T *p) { *this = __builtin_bit_cast(Some, *(const Words *)p); }
+    __device__ __forceinline__ void store(T *p) const { *(Words *)p = __builtin_bit_cast(Words, *this); }
 };
+template <typename T>
+static __device__ __forceinline__ void turn_pair(T &a, T &b, float2 w)
+{
+    const float x = (float)a, y = (float)b;
+    a = (T)fmaf(x, w.x, -(y * w.y));
+    b = (T)fmaf(x, w.y, y * w.x);
+}
+// (an entry left out behind every eight: lanes that read eight each meet in different banks; 20000 rows of 40 heads of 64 in fp32, 32 of them turned, 86 / 75)
+static __device__ __forceinline__ int in_lds(int i) { return i + (i >> 3); }
 
-template <typename T, bool INTER, int N>
+// A thread has 16 bytes of a head, and those that they are turned with.  EVEN: they divide what is turned, and the rest.  Otherwise the last ones
+// overlap those before them, which is the same values twice; in place, where it would turn them twice, what is left over goes one by one.
+// us with as many elements together as the alignment allows / this way: 6458 rows of 72 heads of 256, 114 of them turned in halves of 57, 351 / 101, in
+// place 222 / 70.
+struct Pieces {
+    int pairs, singles, rest, stay;  // of a head: of pairs, pairs, of elements that stay, such elements
+    int part, all;
+};
+template <int N, bool INTER, bool EVEN>
+static __host__ __device__ __forceinline__ Pieces pieces_of(const RotaryArgs &p)
+{
+    Pieces x{};
+    const int rest = p.d - 2 * p.half;
+    x.part = INTER ? 2 * p.half : p.half;
+    x.pairs = x.part / N, x.rest = rest / N;
+    if (!EVEN) {
+        const int left = x.part % N, stay = rest % N;
+        if (left && x.pairs > 0 && !p.in_place) ++x.pairs;
+        else x.singles = INTER ? left / 2 : left;
+        if (stay && x.rest > 0) ++x.rest;
+        else x.stay = stay;
+    }
+    x.all = x.pairs + x.singles + x.rest + x.stay;
+    return x;
+}
+template <typename T, bool INTER, bool EVEN>
 __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs p)
 {
-    typedef Some<T, N> V;
-    __shared__ float2 cs[kTurns];
+    typedef Some<T> V;
+    constexpr int N = V::N;
+    __shared__ float2 cs[kTurns + kTurns / 8];
     const int heads = p.heads[0] + p.heads[1], rot = 2 * p.half;
-    // pieces of a head: of pairs, then of elements that stay
-    const int pairs = (INTER && N > 1 ? rot : p.half) / N, rest = (p.d - rot) / N, pieces = pairs + rest;
+    const Pieces n = pieces_of<N, INTER, EVEN>(p);
     const int64_t groups = (p.m + p.rows - 1) / p.rows;
     for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
         const int64_t row0 = g * p.rows;
@@ -67,42 +108,51 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs p)
         __syncthreads();
         for (int i = threadIdx.x; i < rows * p.half; i += 256) {
             const int r = i / p.half, j = i - r * p.half;
-            cs[i] = turn((double)p.pos[row0 + r] * p.freq[j] * 0.15915494309189535, p.scale, p.inverse);
+            cs[in_lds(i)] = turn((double)p.pos[row0 + r] * p.freq[j] * 0.15915494309189535, p.scale, p.inverse);
         }
         __syncthreads();
-        const int units = rows * heads * pieces;
+        const int units = rows * heads * n.all;
         for (int u = threadIdx.x; u < units; u += 256) {
-            const int rh = u / pieces, piece = u - rh * pieces, r = rh / heads, hh = rh - r * heads;
+            const int rh = u / n.all, r = rh / heads, hh = rh - r * heads;
+            int piece = u - rh * n.all;
             const int which = hh >= p.heads[0], h = which ? hh - p.heads[0] : hh;
             const T *x = (const T *)(p.in[which] + (row0 + r) * p.ld_in[which]) + (int64_t)h * p.d;
             T *y = (T *)(p.out[which] + (row0 + r) * p.ld_out[which]) + (int64_t)h * p.d;
-            const float2 *t = cs + r * p.half;
-            if (piece >= pairs) {
-                const int at = rot + (piece - pairs) * N;
-                if (x != y) *(V *)(y + at) = *(const V *)(x + at);
-            } else if constexpr (INTER && N > 1) {
-                V v = *(const V *)(x + piece * N);
+            const int t = r * p.half;
+            if (piece < n.pairs) {
+                const int at = EVEN ? piece * N : min(piece * N, n.part - N);
+                V v, z;
+                v.load(x + at);
+                if constexpr (INTER) {
 #pragma unroll
-                for (int e = 0; e < N / 2; ++e) {
-                    const float2 w = t[piece * (N / 2) + e];
-                    const float a = (float)v.x[2 * e], b = (float)v.x[2 * e + 1];
-                    v.x[2 * e] = (T)fmaf(a, w.x, -(b * w.y));
-                    v.x[2 * e + 1] = (T)fmaf(a, w.y, b * w.x);
+                    for (int e = 0; e < N; e += 2) turn_pair(v.x[e], v.x[e + 1], cs[in_lds(t + (at + e) / 2)]);
+                } else {
+                    z.load(x + at + p.half);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) turn_pair(v.x[e], z.x[e], cs[in_lds(t + at + e)]);
+                    z.store(y + at + p.half);
                 }
-                *(V *)(y + piece * N) = v;
+                v.store(y + at);
+                continue;
+            }
+            piece -= n.pairs;
+            if (!EVEN && piece < n.singles) {
+                const int j = (INTER ? p.half : n.part) - n.singles + piece, ia = INTER ? 2 * j : j, ib = INTER ? 2 * j + 1 : j + p.half;
+                T a = x[ia], b = x[ib];
+                turn_pair(a, b, cs[in_lds(t + j)]);
+                y[ia] = a, y[ib] = b;
+                continue;
+            }
+            piece -= n.singles;
+            if (x == y) continue;
+            if (EVEN || piece < n.rest) {
+                const int at = rot + (EVEN ? piece * N : min(piece * N, p.d - rot - N));
+                V v;
+                v.load(x + at);
+                v.store(y + at);
             } else {
-                // (neighbours of an odd alignment: one by one too)
-                const int ia = INTER ? 2 * piece : piece * N, ib = INTER ? 2 * piece + 1 : piece * N + p.half;
-                V v = *(const V *)(x + ia), z = *(const V *)(x + ib);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float2 w = t[piece * N + e];
-                    const float a = (float)v.x[e], b = (float)z.x[e];
-                    v.x[e] = (T)fmaf(a, w.x, -(b * w.y));
-                    z.x[e] = (T)fmaf(a, w.y, b * w.x);
-                }
-                *(V *)(y + ia) = v;
-                *(V *)(y + ib) = z;
+                const int at = rot + piece - n.rest;  // (fewer than 16 bytes of them)
+                y[at] = x[at];
             }
         }
     }
@@ -111,22 +161,16 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs p)
 template <typename T, bool INTER>
 hipError_t launch(RotaryArgs p, hipStream_t s)
 {
-    // the most elements that a place in any of the rows is a multiple of
-    uint64_t odd = (uint64_t)(INTER ? 2 * p.half : p.half) * sizeof(T) | (uint64_t)p.d * sizeof(T) | 16;
-    for (int i = 0; i < 2; ++i)
-        if (p.heads[i]) odd |= (uint64_t)p.in[i] | (uint64_t)p.out[i] | (uint64_t)p.ld_in[i] | (uint64_t)p.ld_out[i];
-    const int n = (int)((odd & -odd) / sizeof(T));
+    constexpr int N = Some<T>::N;
+    const bool even = (INTER ? 2 * p.half : p.half) % N == 0 && (p.d - 2 * p.half) % N == 0;
+    p.in_place = p.in[0] == p.out[0] || (p.heads[1] > 0 && p.in[1] == p.out[1]);
     // Rows of a workgroup: one where that has work for all of its threads, more of smaller ones where there are rows enough.  us with 1 / 2 / 4:
     // 20000 rows of 40 heads of 128 70.6 / 74.8 / 77.7, 5000 of 12 heads of 64 in fp32 9.5 / 8.9 / 8.5.
-    const int64_t units = (int64_t)(p.heads[0] + p.heads[1]) * ((INTER && n > 1 ? 2 * p.half : p.half) / n + (p.d - 2 * p.half) / n);
+    const int64_t units = (int64_t)(p.heads[0] + p.heads[1]) * (even ? pieces_of<N, INTER, true>(p) : pieces_of<N, INTER, false>(p)).all;
     p.rows = units >= 256 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(768 / units, kTurns / p.half), p.m / 1024));
     const int64_t groups = (p.m + p.rows - 1) / p.rows;
     const dim3 grid((unsigned)std::min<int64_t>(groups, 1 << 16));
-    void (*kernel)(RotaryArgs) = rotary_kernel<T, INTER, 1>;
-    if (n == 2) kernel = rotary_kernel<T, INTER, 2>;
-    if (n == 4) kernel = rotary_kernel<T, INTER, 4>;
-    if constexpr (sizeof(T) == 2)
-        if (n == 8) kernel = rotary_kernel<T, INTER, 8>;
+    void (*kernel)(RotaryArgs) = even ? rotary_kernel<T, INTER, true> : rotary_kernel<T, INTER, false>;
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p);
     return hipGetLastError();
 }

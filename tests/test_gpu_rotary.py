@@ -69,7 +69,8 @@ def turned(m, H, Hkv, d, rot, dtype, *, interleaved=False, kind="plain", inverse
 @pytest.mark.parametrize("place", ["out", "in"])
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("d,rot", [(64, 64), (128, 128), (128, 64), (64, 48), (64, 2), (80, 26), (32, 10), (7, 4), (2, 2), (256, 256), (512, 512), (600, 512)])
+@pytest.mark.parametrize("d,rot", [(64, 64), (128, 128), (128, 64), (64, 48), (64, 2), (80, 26), (32, 10), (7, 4), (2, 2), (256, 256), (512, 512), (600, 512),
+                                   (256, 114), (256, 26), (128, 78), (72, 66), (41, 18), (40, 34), (23, 16), (19, 18)])
 def test_widths(d, rot, dtype, interleaved, place):
     turned(37, 4, 2, d, rot, dtype, interleaved=interleaved, place=place, seed=d + rot)
 
