@@ -6,7 +6,7 @@
 // A position may be far, so the angle is made in 64 bits and its whole quarter turns are taken off there; what is left, at most an eighth of
 // a turn, fits 32 bits, and the sine's and cosine's Taylor sums to the powers 9 and 10 are off by less than 2e-9 on it.  They are made once per row and pair
 // and shared by all heads through LDS.  Bound by memory: every element is read and written once, 16 bytes a thread.
-// 20000 rows of 40 heads of 128 in bf16 71 us (410 MB at 5.8 TB/s), 64 rows 5.9 (the host's call; 3.7 on the device).
+// 20000 rows of 40 heads of 128 in bf16 71 us (410 MB at 5.8 TB/s), 64 rows 5.9 (the host's call; 3.8 on the device).
 #include "../../include/climber.h"
 
 #include <algorithm>
@@ -120,16 +120,18 @@ __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs p)
             T *y = (T *)(p.out[which] + (row0 + r) * p.ld_out[which]) + (int64_t)h * p.d;
             const int t = r * p.half;
             if (piece < n.pairs) {
-                const int at = EVEN ? piece * N : min(piece * N, n.part - N);
+                const int at = EVEN ? piece * N : min(piece * N, n.part - N), first = t + (INTER ? at / 2 : at), first_lds = in_lds(first);
+                // (EVEN: a piece's entries are all of the same eight)
+                auto entry = [&](int i) { return cs[EVEN ? first_lds + i : in_lds(first + i)]; };
                 V v, z;
                 v.load(x + at);
                 if constexpr (INTER) {
 #pragma unroll
-                    for (int e = 0; e < N; e += 2) turn_pair(v.x[e], v.x[e + 1], cs[in_lds(t + (at + e) / 2)]);
+                    for (int e = 0; e < N; e += 2) turn_pair(v.x[e], v.x[e + 1], entry(e / 2));
                 } else {
                     z.load(x + at + p.half);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) turn_pair(v.x[e], z.x[e], cs[in_lds(t + at + e)]);
+                    for (int e = 0; e < N; ++e) turn_pair(v.x[e], z.x[e], entry(e));
                     z.store(y + at + p.half);
                 }
                 v.store(y + at);
