@@ -439,7 +439,7 @@ int climber_rotary_frequencies(int32_t rot_dims, double base, int32_t kind, doub
                                double slow, double *freq, float *scale);
 
 /* q [m][ld_q] of cfg->n_heads * d_head, k [m][ld_k] of n_kv_heads * d_head (n_kv_heads 0: no k), elements of the config's dtype; pos: dev int32 [m].
- * Row pitches are free, and so is the alignment; rows of whole 16 bytes are faster.  q_out, k_out: of the same widths; q_out may be q
+ * Row pitches are free, and so is the alignment; heads whose turned halves and rest are whole 16 bytes are faster.  q_out, k_out: of the same widths; q_out may be q
  * with the same pitch (turned in place), and k_out k; otherwise what is written must not share an element with anything else.  Uses d_model,
  * n_heads, d_head and dtype of cfg; any d_head, rot_dims even, 2 .. min(d_head, 512).
  * Errors: CLIMBER_ERR_NULL, _SHAPE, _ALIGN, _RANGE, _UNSUPPORTED, _RUNTIME. */
