@@ -594,9 +594,9 @@ __global__ __launch_bounds__(256) void compact_list_kernel(const CompactArgs a)
         if (page < a.n_pages) {
             if (page < n_used) {
                 if (!used) a.holes[page - rank] = page;
-            } else {
-                a.to[page] = used ? rank - low : -1;
-                if (used) a.movers[rank - low] = page;
+            } else if (used) {
+                a.to[page] = rank - low;
+                a.movers[rank - low] = page;
             }
         }
         before += __popcll(w);
@@ -656,12 +656,9 @@ __global__ __launch_bounds__(1024) void compact_few_kernel(const CompactArgs a)
     for (int e = t; e < all; e += 1024) {
         const int b = e / a.table_ld, page = a.table[e];
         if (e - b * a.table_ld >= held_of(a, b)) continue;
-        if (!in_pool(a, page)) bad = true;
-        else if (page >= n_used) {
-            const uint64_t w = words[page >> 6];
-            if ((w >> (page & 63)) & 1) a.table[e] = a.holes[word_at[page >> 6] + __popcll(w & ((1ull << (page & 63)) - 1)) - low];
-            else bad = true;  // (a page that nothing is said to hold)
-        }
+        const uint64_t w = in_pool(a, page) ? words[page >> 6] : 0;
+        if (!((w >> (page & 63)) & 1)) bad = true;  // (no page, or one that nothing is said to hold)
+        else if (page >= n_used) a.table[e] = a.holes[word_at[page >> 6] + __popcll(w & ((1ull << (page & 63)) - 1)) - low];
     }
     if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
 }
@@ -685,12 +682,9 @@ __global__ __launch_bounds__(256) void compact_move_kernel(const CompactArgs a, 
     for (int i = g % pieces * 64 + (threadIdx.x & 63); i < had; i += 64 * pieces) {
         int32_t *const e = a.table + (int64_t)b * a.table_ld + i;
         const int page = *e;
-        if (!in_pool(a, page)) bad = true;
-        else if (page >= n_used) {
-            const int j = a.to[page];
-            if (j >= 0) *e = a.holes[j];
-            else bad = true;  // (a page that nothing is said to hold)
-        }
+        // (a.bits: what was in use before the moves that other workgroups make meanwhile)
+        if (!in_pool(a, page) || !((a.bits[page >> 6] >> (page & 63)) & 1)) bad = true;  // (no page, or one that nothing is said to hold)
+        else if (page >= n_used) *e = a.holes[a.to[page]];
     }
     if (bad) atomicOr(a.status, CLIMBER_BAD_PAGE);
 }
