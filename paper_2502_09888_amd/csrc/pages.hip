@@ -446,10 +446,12 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
     };
     int c = max(0, x.need - max(x.shared_to, had)), copy = 0;
     uint64_t which = 0;  // of the first 64 pages that are written, those that go; of those behind them the entry itself says it, as ~page
-    if (shared && !(problems & 2))
+    const bool some_bad = problems & 2;  // (nothing is handed out: counted all the same, for CLIMBER_POOL_FULL)
+    if (shared)
         for (int i = x.first; i < x.shared_to; ++i) {
             if (!goes(row[i])) continue;
             ++c;
+            if (some_bad) continue;
             copy |= i == x.first && x.part > 0;
             if (i - x.first < 64) which |= 1ull << (i - x.first);
             else row[i] = ~row[i];
@@ -463,15 +465,15 @@ __global__ __launch_bounds__(1024) void extend_few_kernel(const ExtendArgs a)
         if (i < wave) at += sums[0][i], at_copy += sums[1][i];
         total += sums[0][i], n_copies += sums[1][i], in_use += sums[2][i];
     }
-    const bool full = (problems & 1) || total > unit_at[units], go = !full && !(problems & 2);
+    const bool full = (problems & 1) || total > unit_at[units], go = !full && !some_bad;
     if (t == 0) {
-        const int found = (full ? CLIMBER_POOL_FULL : 0) | (problems & 2 ? CLIMBER_BAD_PAGE : 0);
+        const int found = (full ? CLIMBER_POOL_FULL : 0) | (some_bad ? CLIMBER_BAD_PAGE : 0);
         if (found) atomicOr(a.status, found);
         a.counts[0] = go ? n_copies : 0;
         a.counts[1] = in_use + (go ? total : 0);
     }
     if (!go) {
-        if (shared && !(problems & 2))
+        if (shared && !some_bad)
             for (int i = x.first + 64; i < x.shared_to; ++i)
                 if (row[i] < 0) row[i] = ~row[i];
         return;

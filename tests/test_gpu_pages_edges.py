@@ -3,7 +3,7 @@ import random
 
 import pytest
 
-from pages_ref import BAD_PAGE, DevicePool, Pool
+from pages_ref import BAD_PAGE, POOL_FULL, DevicePool, Pool
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,21 @@ def test_compact_reports_held_pages_without_refs(size, side):
     assert host.status == (0 if side == "none" else BAD_PAGE)
     dev.compact()
     dev.check(copies)
+
+
+@pytest.mark.parametrize("n_seqs", [5, 1024, 1025])
+@pytest.mark.parametrize("free", [0, 1, 2, 140, 141, 142, 300])
+def test_extend_reports_all_that_it_finds(n_seqs, free):
+    """A page outside the pool and too few free pages in one call: both, whatever the sizes; and nothing changes."""
+    # sequences 1 and 2 share 70 pages with somebody else, that both write: 140 pages; the last one needs two more of its own
+    host = Pool(70 + free, 16, n_seqs, 80)
+    for b in (1, 2):
+        host.table[b][:70] = range(70)
+        host.held[b], host.len[b] = 70, 5
+    host.refs[:70] = [3] * 70
+    host.table[0][0], host.held[0], host.len[0] = 10 ** 6, 1, 3
+    rows = [1, 69 * 16, 69 * 16] + [0] * (n_seqs - 4) + [20]
+    dev = DevicePool(host)
+    host.status = BAD_PAGE | (POOL_FULL if free < 142 else 0)
+    dev.extend(rows)
+    dev.check([])
