@@ -57,3 +57,28 @@ def test_extend_reports_all_that_it_finds(n_seqs, free):
     host.status = BAD_PAGE | (POOL_FULL if free < 142 else 0)
     dev.extend(rows)
     dev.check([])
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("n_seqs,most", [(60, 500), (900, 12)])
+def test_extend_hands_out_more_pages_than_it_keeps_at_hand(n_seqs, most, shared):
+    """One workgroup's list of free pages is 4096 long: those behind, for sequences that get many and few, and in the places of shared ones."""
+    r = random.Random(n_seqs)
+    host = Pool.random(6, 30000, 16, n_seqs, 600 if n_seqs < 100 else 30, fill=0.1)
+    if shared:
+        host.fork([b if b % 3 else (b + 1) % n_seqs for b in range(n_seqs)])
+    rows = [r.choice([r.randint(1, 16), r.randint(1, 64), 16 * most, r.randint(0, 16 * most)]) for b in range(n_seqs)]
+    rows[-1] = 16 * most
+    rows = [min(x, host.table_ld * 16 - n) for x, n in zip(rows, host.len)]
+    dev, held, used, before = DevicePool(host), list(host.held), host.used(), [list(x) for x in host.table]
+    copies = host.extend(rows)
+    # pages that each sequence got, in order: more than 4096, and one sequence has pages on both sides of the border
+    got = [sum(x != y for x, y in zip(now[:h], was[:h])) for now, was, h in zip(host.table, before, host.held)]
+    at = [sum(got[:b]) for b in range(n_seqs)]
+    assert copies is not None and sum(got) > 4200 and any(a < 4096 < a + g for a, g in zip(at, got))
+    assert any(a > 4096 and 0 < g <= 4 for a, g in zip(at, got)) and any(a > 4096 and g > 4 for a, g in zip(at, got))
+    if shared:
+        assert copies and any(host.table[b][:held[b]] != before[b][:held[b]] and at[b] > 4096 for b in range(n_seqs))
+    assert host.used() == used + sum(got)
+    dev.extend(rows)
+    dev.check(copies)
