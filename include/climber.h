@@ -401,7 +401,8 @@ int climber_pages_extend(const climber_page_pool *pool, const int32_t *rows, int
                          void *workspace, size_t ws_bytes, void *stream);
 
 /* Moves pages so that the pages in use are 0 .. counts[1] - 1: those behind go, in ascending order, to the free ones before.  Table and refs
- * follow; copies (dev int32 [n_pages / 2][3]) gets (old number, new number, page_size) of each, counts[0] of them. */
+ * follow; copies (dev int32 [n_pages / 2][3]; a pool of one page needs none, and takes NULL) gets (old number, new number, page_size) of each,
+ * counts[0] of them. */
 int climber_pages_compact(const climber_page_pool *pool, int32_t *copies, int32_t *counts, int32_t *status, void *workspace,
                           size_t ws_bytes, void *stream);
 

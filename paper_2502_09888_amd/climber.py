@@ -677,6 +677,14 @@ def _room(copies, most: int) -> int:
     return min(most, copies.numel() // 3)
 
 
+def _copies(copies, counts):
+    """An empty tensor has no address: one that there is, and of which nothing is read, in its place."""
+    if copies is None or isinstance(copies, int) or copies.numel() > 0:
+        return copies
+    _ints(copies=(copies, 0))
+    return counts
+
+
 def climber_pages_fork(pool: PagePool, parent, keep, status, workspace, stream=None) -> None:
     """Sequence b becomes what sequence parent[b] was (below 0: empty), up to its first keep[b] tokens; pages are shared, and with keep no row holds
     more of them than its tokens need."""
@@ -721,6 +729,8 @@ def climber_paged_copy(cfg: Config, kv: PagedKV, copies, counts, max_copies: int
     """What climber_pages_extend or climber_pages_compact has left to copy, in one paged cache."""
     _on_device(kv, stream)
     max_copies = _room(copies, max_copies)
+    if max_copies == 0:
+        copies = _copies(copies, counts)
     code = (_native or _load_native(load_library())).paged_copy(cfg, kv, copies, counts, max_copies, stream, kv._device)
     if code is None:
         _there(kv, copies, counts)
@@ -734,6 +744,8 @@ def climber_paged8_copy(cfg: Config, kv8: PagedKV8, copies, counts, max_copies: 
     """climber_paged_copy in a cache in 8 bits."""
     _on_device(kv8, stream)
     max_copies = _room(copies, max_copies)
+    if max_copies == 0:
+        copies = _copies(copies, counts)
     code = (_native or _load_native(load_library())).paged8_copy(cfg, kv8, copies, counts, max_copies, stream, kv8._device)
     if code is None:
         _there(kv8, copies, counts)

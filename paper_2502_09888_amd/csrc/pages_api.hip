@@ -168,7 +168,7 @@ int climber_pages_compact(const climber_page_pool *pool, int32_t *copies, int32_
     int e = check_pool(pool);
     if (e) return e;
     const PoolLayout w = compact_layout(pool);
-    e = check(pool, copies, counts, status, workspace, ws_bytes, w.bytes);
+    e = check(pool, pool->n_pages < 2 && !copies ? counts : copies, counts, status, workspace, ws_bytes, w.bytes);  // (of one page there are no copies)
     if (e) return e;
     uint8_t *ws = (uint8_t *)workspace;
     CompactArgs a{};

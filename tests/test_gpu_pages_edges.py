@@ -2,6 +2,7 @@
 import random
 
 import pytest
+import torch
 
 from pages_ref import BAD_PAGE, POOL_FULL, DevicePool, Pool
 
@@ -82,3 +83,29 @@ def test_extend_hands_out_more_pages_than_it_keeps_at_hand(n_seqs, most, shared)
     assert host.used() == used + sum(got)
     dev.extend(rows)
     dev.check(copies)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_a_pool_of_one_page(kind):
+    """Copies of exactly [n_pages / 2][3] integers, which are none."""
+    import paper_2502_09888_amd as P
+    host = Pool(1, 16, 2, 3)
+    dev = DevicePool(host)
+    dev.copies = torch.empty((2, 3), dtype=torch.int32, device="cuda:0")
+    none = torch.empty((0, 3), dtype=torch.int32, device="cuda:0")
+    k = torch.ones((1, 2, 16, 64), device="cuda:0").to(torch.bfloat16 if kind == "bf16" else torch.float8_e4m3fn)
+    s = torch.full((1, 2, 1), 127, dtype=torch.uint8, device="cuda:0")
+    kv = P.paged_kv(k, k.clone(), dev.table, dev.len, 48) if kind == "bf16" else P.paged_kv8(k, k.clone(), s, s.clone(), dev.table, dev.len, 48)
+    cfg, copy = P.Config(n_heads=2, d_head=64, dtype=P.BF16), P.climber_paged_copy if kind == "bf16" else P.climber_paged8_copy
+    for rows in ([16, 0], [-1, -1], [0, 3]):
+        if rows[0] < 0:
+            host.fork([-1, -1])
+            dev.fork([-1, -1])
+        else:
+            host.extend(rows)
+            dev.extend(rows)
+        assert host.compact() == []
+        P.climber_pages_compact(dev.pool, none, dev.counts, dev.status, dev.ws)
+        copy(cfg, kv, none, dev.counts, 10)
+        dev.check()
+        assert dev.counts.tolist() == [0, host.used()] and bool((k.float() == 1).all())
