@@ -366,8 +366,8 @@ int climber_attn_sumi_paged8(const climber_config *cfg, const float *tau_layer, 
  * A cache whose pages are shared has no mass (see climber_paged_kv), and eviction writes pages: of a sequence that shares none.
  * Results do not depend on the order in which the device works.  Values are device memory and cannot be checked on the host: whatever
  * they hold, nothing is read or written outside the arrays, and calls OR what they find into *status (dev int32, not cleared):
- *   CLIMBER_BAD_PAGE  a page number that is held lies outside the pool (or, compact, is of a page with refs 0: it counts as free, and a page may
- *                     have been moved into it)
+ *   CLIMBER_BAD_PAGE  a page number that is held lies outside the pool (fork: one that a row takes or gives up; extend: one that new tokens go into;
+ *                     compact: any), or, compact, is of a page with refs 0: it counts as free, and a page may have been moved into it
  *   CLIMBER_BAD_SEQ   fork: a parent from n_seqs on (the row stays as it is)
  *   CLIMBER_POOL_FULL extend: not enough free pages, or more than a row of the table has room for
  * A workspace belongs to one call at a time, and so does a pool.  workspace: climber_pages_workspace_bytes(), 256-byte aligned.

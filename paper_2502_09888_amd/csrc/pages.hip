@@ -107,7 +107,7 @@ static __device__ __forceinline__ void fork_read(const ForkArgs &a, int b, int p
     for (int i = first; i < max(had, h); i += 64 * pieces) {
         const int was = i < had ? a.table[(int64_t)b * a.table_ld + i] : -1, is = i < h ? a.table[(int64_t)par * a.table_ld + i] : -1;
         a.rows[(int64_t)b * a.table_ld + i] = is;
-        bad |= i < h && !in_pool(a, is);
+        bad |= (i < h && !in_pool(a, is)) || (i < had && !in_pool(a, was));
         if (was == is) continue;
         if (in_pool(a, was)) atomicSub(a.refs + was, 1);
         if (in_pool(a, is)) atomicAdd(a.refs + is, 1);
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(1024) void fork_few_kernel(const ForkArgs a)
         if (h < 0 || i >= max(had, h)) continue;
         const int is = i < h ? a.table[(int64_t)par * a.table_ld + i] : -1;
         a.rows[e] = is;
-        if (i < h && !in_pool(a, is)) bits |= CLIMBER_BAD_PAGE;
+        if ((i < h && !in_pool(a, is)) || (i < had && !in_pool(a, was))) bits |= CLIMBER_BAD_PAGE;
         if (i < had && was == is) continue;
         if (i < had && in_pool(a, was)) atomicSub(a.refs + was, 1);
         if (in_pool(a, is)) atomicAdd(a.refs + is, 1);

@@ -109,3 +109,30 @@ def test_a_pool_of_one_page(kind):
         copy(cfg, kv, none, dev.counts, 10)
         dev.check()
         assert dev.counts.tolist() == [0, host.used()] and bool((k.float() == 1).all())
+
+
+@pytest.mark.parametrize("n_seqs,table_ld", [(6, 9), (300, 9), (3, 1500)])
+@pytest.mark.parametrize("keep", [False, True])
+def test_fork_reports_pages_outside_the_pool_that_a_row_gives_up(n_seqs, table_ld, keep):
+    for page in (-1, 5000, 10 ** 9, -2 ** 31):
+        for row, parent, reported in ((1, -1, True), (1, 2, True), (1, 1, keep), (2, 2, keep), (0, 0, False)):
+            host = Pool.random(7, 5000, 16, n_seqs, table_ld, fill=0.5)
+            for b in (1, 2):                              # rows of two pages at least
+                host.fork([x if x != b else -1 for x in range(n_seqs)])
+                assert host.extend([40 if x == b else 0 for x in range(n_seqs)]) == []
+                host.len[b] = 40
+            dev, last = DevicePool(host), host.held[row] - 1
+            if row:
+                dev.table[row, last] = page
+                host.refs[host.table[row][last]] -= 1     # (nobody holds it any more)
+                dev.refs.copy_(dev.ints(host.refs))
+                host.table[row][last], host.held[row] = -1, last
+            parents = [parent if b == row else b for b in range(n_seqs)]
+            keeps = [20 if b == row else 10 ** 6 for b in range(n_seqs)] if keep else None
+            dev.fork(parents, keeps)
+            torch.cuda.synchronize()
+            assert dev.status.item() == (BAD_PAGE if reported else 0), (page, row, parent)
+            if reported:
+                host.fork(parents, keeps)
+                host.status = BAD_PAGE
+                dev.check()
