@@ -605,15 +605,29 @@ def climber_paged8_workspace_bytes(cfg: Config, kv8: PagedKV8, m_total: int, m_m
     return int(load_library().climber_paged8_workspace_bytes(C.byref(cfg), C.byref(kv8), m_total, m_max))
 
 
+def _read8(cfg: Config, kv8: PagedKV8, m_total: int, tau, off, ids, **rows) -> None:
+    """What a call reads of its tensors is there, and of its type (where the cache is described by tensors on a device, and there are rows)."""
+    if kv8._device is None or m_total <= 0:
+        return
+    _ints("float32", tau_layer=(tau, cfg.n_scen * cfg.n_beh))
+    _ints(off=(off, kv8.kv.n_seqs + 1), **{n: (t, m_total) for n, t in zip(("scen", "beh", "stamp"), ids)})
+    for name, (t, wide) in rows.items():
+        if t is not None and not isinstance(t, int) and \
+                (str(t.dtype) != "torch.bfloat16" or t.shape[0] < m_total or t.numel() < t.shape[0] * wide):
+            raise ValueError(f"{name} is a bfloat16 tensor of {m_total} rows of {wide} elements or more")
+
+
 def climber_attn_history_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q, k, v, off, m_total: int, m_max: int, scen, beh, stamp, o,
                                 workspace, stream=None) -> None:
-    """climber_attn_history_paged on a cache in 8 bits."""
+    """climber_attn_history_paged on a cache in 8 bits.  Tensors of other types than the call reads (rows bfloat16, off, ids and stamps int32, temperatures
+    float32), or with less in them, are a ValueError."""
     _on_device(kv8, stream)
     code = (_native or _load_native(load_library())).attn_history_paged8(cfg, tau_layer, kv8, q, k, v, off, m_total, m_max, scen, beh, stamp, o,
                                                                          workspace, stream, kv8._device)
     if code is None:
         _there(kv8, tau_layer, q, k, v, off, scen, beh, stamp, o, workspace)
         d, dk = cfg.d_model, kv8.kv.n_kv_heads * cfg.d_head
+        _read8(cfg, kv8, m_total, tau_layer, off, (scen, beh, stamp), q=(q, d), k=(k, dk), v=(v, dk), o=(o, d))
         code = load_library().climber_attn_history_paged8(
             C.byref(cfg), _ptr(tau_layer), C.byref(kv8), _ptr(q), _pitch(q, d), _ptr(k), _ptr(v), _same_pitch(k, v, dk), _ptr(off), m_total, m_max,
             _ptr(scen), _ptr(beh), _ptr(stamp), _ptr(o), _pitch(o, d), _ptr(workspace), _nbytes(workspace), _stream(stream))
@@ -623,13 +637,14 @@ def climber_attn_history_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q, k, v, 
 
 def climber_attn_sumi_paged8(cfg: Config, tau_layer, kv8: PagedKV8, q_c, k_c, v_c, cand_off, m_total: int, m_max: int, cand_scen, cand_beh,
                              o_c, workspace, stream=None) -> None:
-    """climber_attn_sumi_paged on a cache in 8 bits."""
+    """climber_attn_sumi_paged on a cache in 8 bits.  Tensors as in climber_attn_history_paged8."""
     _on_device(kv8, stream)
     code = (_native or _load_native(load_library())).attn_sumi_paged8(cfg, tau_layer, kv8, q_c, k_c, v_c, cand_off, m_total, m_max, cand_scen,
                                                                       cand_beh, o_c, workspace, stream, kv8._device)
     if code is None:
         _there(kv8, tau_layer, q_c, k_c, v_c, cand_off, cand_scen, cand_beh, o_c, workspace)
         d, dk = cfg.d_model, kv8.kv.n_kv_heads * cfg.d_head
+        _read8(cfg, kv8, m_total, tau_layer, cand_off, (cand_scen, cand_beh), q_c=(q_c, d), k_c=(k_c, dk), v_c=(v_c, dk), o_c=(o_c, d))
         code = load_library().climber_attn_sumi_paged8(
             C.byref(cfg), _ptr(tau_layer), C.byref(kv8), _ptr(q_c), _pitch(q_c, d), _ptr(k_c), _ptr(v_c), _same_pitch(k_c, v_c, dk),
             _ptr(cand_off), m_total, m_max, _ptr(cand_scen), _ptr(cand_beh), _ptr(o_c), _pitch(o_c, d), _ptr(workspace), _nbytes(workspace),
@@ -661,11 +676,11 @@ def climber_pages_workspace_bytes(pool: PagePool) -> int:
     return int(load_library().climber_pages_workspace_bytes(C.byref(pool)))
 
 
-def _ints(**least) -> None:
-    """name=(tensor, integers that it has at least)"""
+def _ints(kind: str = "int32", **least) -> None:
+    """name=(tensor, elements of the type that it has at least)"""
     for name, (t, n) in least.items():
-        if t is not None and not isinstance(t, int) and (str(t.dtype) != "torch.int32" or not t.is_contiguous() or t.numel() < n):
-            raise ValueError(f"{name} is a contiguous int32 tensor of {n} or more")
+        if t is not None and not isinstance(t, int) and (str(t.dtype) != "torch." + kind or not t.is_contiguous() or t.numel() < n):
+            raise ValueError(f"{name} is a contiguous {kind} tensor of {n} or more")
 
 
 def _room(copies, most: int) -> int:

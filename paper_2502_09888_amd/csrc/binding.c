@@ -44,10 +44,11 @@ static int pointer(PyObject *o, void **p)
     return unsigned_of(PyObject_CallMethodNoArgs(o, s_data_ptr), p);
 }
 
-static int stream_of(PyObject *o, void **p)
+/* at: the device whose current stream is meant, where the caller knows that it is the current one; None: not known */
+static int stream_of(PyObject *o, PyObject *at, void **p)
 {
     if (o == Py_None) { /* torch's current one */
-        PyObject *dev = PyObject_CallNoArgs(current_device);
+        PyObject *dev = at == Py_None ? PyObject_CallNoArgs(current_device) : Py_NewRef(at);
         PyObject *s = dev ? PyObject_CallOneArg(raw_stream, dev) : NULL;
         Py_XDECREF(dev);
         return unsigned_of(s, p);
@@ -89,7 +90,7 @@ static PyObject *history(PyObject *const *a, Py_ssize_t n, int with_bias)
     Py_buffer cfg, bias;
     for (int i = 1; i < 8; ++i)
         if (!pointer(a[i], &p[i])) return elsewhere();
-    if (!number(a[8], &layer) || !pointer(a[9], &o) || !stream_of(a[n - 1], &s)) return elsewhere();
+    if (!number(a[8], &layer) || !pointer(a[9], &o) || !stream_of(a[n - 1], Py_None, &s)) return elsewhere();
     if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
     if (with_bias && !structure(a[10], bias_type, sizeof(climber_rel_bias), &bias)) return PyBuffer_Release(&cfg), elsewhere();
     int code;
@@ -111,7 +112,7 @@ static PyObject *sumi(PyObject *const *a, Py_ssize_t n, int with_bias)
     Py_buffer cfg, bias;
     for (int i = 1; i < 13; ++i)
         if (i != 3 && i != 8 && i != 9 && !pointer(a[i], &p[i])) return elsewhere();
-    if (!number(a[3], &layer) || !number(a[8], &m_total) || !number(a[9], &m_max) || !stream_of(a[n - 1], &s)) return elsewhere();
+    if (!number(a[3], &layer) || !number(a[8], &m_total) || !number(a[9], &m_max) || !stream_of(a[n - 1], Py_None, &s)) return elsewhere();
     if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
     if (with_bias && !structure(a[13], bias_type, sizeof(climber_rel_bias), &bias)) return PyBuffer_Release(&cfg), elsewhere();
     int code;
@@ -129,10 +130,15 @@ static PyObject *attn_history_bias(PyObject *m, PyObject *const *a, Py_ssize_t n
 static PyObject *attn_sumi(PyObject *m, PyObject *const *a, Py_ssize_t n) { return sumi(a, n, 0); }
 static PyObject *attn_sumi_bias(PyObject *m, PyObject *const *a, Py_ssize_t n) { return sumi(a, n, 1); }
 
-/* elements from one row to the next, as climber.py's _pitch */
-static int pitch(PyObject *o, int64_t width, int64_t *ld)
+/* elements from one row to the next, as climber.py's _pitch; where a type is given, of m rows or more of `least` such elements or more */
+static int pitch(PyObject *o, int64_t width, PyObject *dtype, int64_t m, int64_t least, int64_t *ld)
 {
     if (o == Py_None || PyLong_Check(o)) return *ld = width, 1;
+    if (dtype) {
+        PyObject *t = PyObject_GetAttr(o, s_dtype);
+        Py_XDECREF(t);
+        if (t != dtype) return 0;
+    }
     PyObject *shape = PyObject_GetAttr(o, s_shape), *stride = shape ? PyObject_CallMethodNoArgs(o, s_stride) : NULL;
     int ok = stride && PyTuple_Check(shape) && PyTuple_Check(stride) && PyTuple_GET_SIZE(shape) > 0 && PyTuple_GET_SIZE(shape) == PyTuple_GET_SIZE(stride);
     if (ok) {
@@ -142,7 +148,9 @@ static int pitch(PyObject *o, int64_t width, int64_t *ld)
             ok = n == 1 || PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i)) == inner;
             inner *= n;
         }
-        *ld = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)) > 1 ? PyLong_AsLongLong(PyTuple_GET_ITEM(stride, 0)) : inner > width ? inner : width;
+        const int64_t rows = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0));
+        *ld = rows > 1 ? PyLong_AsLongLong(PyTuple_GET_ITEM(stride, 0)) : inner > width ? inner : width;
+        if (dtype) ok = ok && rows >= m && inner >= least;
     }
     Py_XDECREF(shape);
     Py_XDECREF(stride);
@@ -167,6 +175,19 @@ static int lies_on(PyObject *o, PyObject *at)
     return ok;
 }
 
+/* A tensor of at least n elements of a type of 4 bytes, one behind the other (pointers and None are taken as they are) */
+static int whole(PyObject *o, PyObject *dtype, int64_t n)
+{
+    if (o == Py_None || PyLong_Check(o)) return 1;
+    PyObject *t = PyObject_GetAttr(o, s_dtype), *one = t == dtype ? PyObject_CallMethodNoArgs(o, s_is_contiguous) : NULL;
+    size_t bytes;
+    const int ok = one == Py_True && bytes_of(o, &bytes) && bytes / 4 >= (uint64_t)n;
+    Py_XDECREF(t);
+    Py_XDECREF(one);
+    return ok;
+}
+static int ints_of(PyObject *o, int64_t n, void **p) { return whole(o, i32_dtype, n) && pointer(o, p); }
+
 /* cfg, tau, kv, q, k, v, off, m_total, m_max, scen, beh[, stamp], o, workspace, stream[, device] */
 static PyObject *paged(PyObject *const *a, Py_ssize_t n, int appends, int bits8)
 {
@@ -185,14 +206,22 @@ static PyObject *paged(PyObject *const *a, Py_ssize_t n, int appends, int bits8)
     const Py_ssize_t o = 11 + appends;
     for (Py_ssize_t i = 1; i < n - 1; ++i)
         if (i != 2 && i != 7 && i != 8 && !pointer(a[i], &p[i])) return elsewhere();
-    if (!number(a[7], &m_total) || !number(a[8], &m_max) || !bytes_of(a[o + 1], &ws_bytes) || !stream_of(a[n - 1], &s)) return elsewhere();
+    if (!number(a[7], &m_total) || !number(a[8], &m_max) || !bytes_of(a[o + 1], &ws_bytes) || !stream_of(a[n - 1], bits8 ? a[n] : Py_None, &s)) return elsewhere();
     if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
     if (bits8 ? !paged8_type || !structure(a[2], paged8_type, sizeof(climber_paged_kv8), &kv) : !structure(a[2], paged_type, sizeof(climber_paged_kv), &kv))
         return PyBuffer_Release(&cfg), elsewhere();
-    const climber_config *c = cfg.buf; /* (a climber_paged_kv8 begins with its climber_paged_kv) */
-    const int64_t wide = c->d_model, kv_wide = (int64_t)((const climber_paged_kv *)kv.buf)->n_kv_heads * c->d_head;
-    int code = 0;
-    const int ok = pitch(a[3], wide, &ld_q) && pitch(a[4], kv_wide, &ld_kv) && pitch(a[5], ld_kv, &ld_v) && ld_v == ld_kv && pitch(a[o], wide, &ld_o);
+    const climber_config *c = cfg.buf;
+    const climber_paged_kv *cache = kv.buf; /* (a climber_paged_kv8 begins with it) */
+    const int64_t wide = c->d_model, kv_wide = (int64_t)cache->n_kv_heads * c->d_head;
+    int code = 0, ok = 1;
+    PyObject *rows = NULL; /* their type, where it is looked at: in 8 bits, on a known device, with rows at all */
+    if (bits8 && a[n] != Py_None && m_total > 0 && bf16_dtype) {
+        rows = bf16_dtype;
+        ok = whole(a[1], f32_dtype, (int64_t)c->n_scen * c->n_beh) && whole(a[6], i32_dtype, (int64_t)cache->n_seqs + 1);
+        for (Py_ssize_t i = 9; ok && i < o; ++i) ok = whole(a[i], i32_dtype, m_total);
+    }
+    ok = ok && pitch(a[3], wide, rows, m_total, wide, &ld_q) && pitch(a[4], kv_wide, rows, m_total, kv_wide, &ld_kv) &&
+         pitch(a[5], ld_kv, rows, m_total, kv_wide, &ld_v) && ld_v == ld_kv && pitch(a[o], wide, rows, m_total, wide, &ld_o);
     if (ok) {
         Py_BEGIN_ALLOW_THREADS
         if (bits8 && appends) code = attn_history_paged8_fn(c, p[1], kv.buf, p[3], ld_q, p[4], p[5], ld_kv, p[6], m_total, m_max, p[9], p[10], p[11], p[12], ld_o, p[13], ws_bytes, s);
@@ -220,7 +249,7 @@ static PyObject *paged_evict(PyObject *m, PyObject *const *a, Py_ssize_t n)
     Py_buffer cfg, kv;
     for (int i = 2; i < 8; ++i)
         if (!pointer(a[i], &p[i])) return elsewhere();
-    if (!bytes_of(a[7], &ws_bytes) || !stream_of(a[8], &s)) return elsewhere();
+    if (!bytes_of(a[7], &ws_bytes) || !stream_of(a[8], Py_None, &s)) return elsewhere();
     if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
     if (!structure(a[1], paged_type, sizeof(climber_paged_kv), &kv)) return PyBuffer_Release(&cfg), elsewhere();
     int code;
@@ -232,27 +261,13 @@ static PyObject *paged_evict(PyObject *m, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(code);
 }
 
-/* A tensor of at least n 32-bit integers, one behind the other (pointers and None are taken as they are) */
-static int ints_of(PyObject *o, int64_t n, void **p)
-{
-    if (o != Py_None && !PyLong_Check(o)) {
-        PyObject *t = PyObject_GetAttr(o, s_dtype), *whole = t == i32_dtype ? PyObject_CallMethodNoArgs(o, s_is_contiguous) : NULL;
-        size_t bytes;
-        const int ok = whole == Py_True && bytes_of(o, &bytes) && bytes / 4 >= (uint64_t)n;
-        Py_XDECREF(t);
-        Py_XDECREF(whole);
-        if (!ok) return 0;
-    }
-    return pointer(o, p);
-}
-
 /* pool, n pointers (i: to n_seqs * seqs[i] + pages / 2 * halves[i] + more[i] integers), workspace, stream, device */
 static int pool_call(PyObject *const *a, Py_ssize_t n, int pointers, const int (*sizes)[3], Py_buffer *pool, void **p, size_t *ws_bytes, void **s)
 {
     if (n != pointers + 4 || !pool_type) return 0;
     for (int i = 1; i <= pointers + 1; ++i)
         if (!lies_on(a[i], a[n - 1])) return 0;
-    if (!pointer(a[pointers + 1], &p[pointers + 1]) || !bytes_of(a[n - 3], ws_bytes) || !stream_of(a[n - 2], s) ||
+    if (!pointer(a[pointers + 1], &p[pointers + 1]) || !bytes_of(a[n - 3], ws_bytes) || !stream_of(a[n - 2], a[n - 1], s) ||
         !structure(a[0], pool_type, sizeof(climber_page_pool), pool))
         return 0;
     const climber_page_pool *c = pool->buf;
@@ -312,7 +327,7 @@ static PyObject *copy(PyObject *const *a, Py_ssize_t n, int bits8)
     Py_buffer cfg, kv;
     void *copies, *counts, *s;
     int32_t most;
-    if (!number(a[4], &most) || !ints_of(a[2], 3 * (int64_t)(most < 0 ? 0 : most), &copies) || !ints_of(a[3], 1, &counts) || !stream_of(a[5], &s)) return elsewhere();
+    if (!number(a[4], &most) || !ints_of(a[2], 3 * (int64_t)(most < 0 ? 0 : most), &copies) || !ints_of(a[3], 1, &counts) || !stream_of(a[5], a[6], &s)) return elsewhere();
     if (!structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
     if (bits8 ? !structure(a[1], paged8_type, sizeof(climber_paged_kv8), &kv) : !structure(a[1], paged_type, sizeof(climber_paged_kv), &kv))
         return PyBuffer_Release(&cfg), elsewhere();
@@ -361,7 +376,7 @@ static PyObject *rotary(PyObject *m, PyObject *const *a, Py_ssize_t n)
     void *pos, *p[4] = {NULL, NULL, NULL, NULL}, *s;
     int32_t n_kv;
     int64_t rows = -1, ld[4] = {0, 0, 0, 0};
-    if (!number(a[3], &n_kv) || n_kv < 0 || !stream_of(a[8], &s) || !structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
+    if (!number(a[3], &n_kv) || n_kv < 0 || !stream_of(a[8], a[9], &s) || !structure(a[0], config_type, sizeof(climber_config), &cfg)) return elsewhere();
     if (!structure(a[1], rotary_type, sizeof(climber_rotary_plan), &plan)) return PyBuffer_Release(&cfg), elsewhere();
     const climber_config *c = cfg.buf;
     const int64_t wide = c->d_model, kv_wide = (int64_t)n_kv * c->d_head;
