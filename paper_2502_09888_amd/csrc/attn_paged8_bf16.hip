@@ -755,7 +755,11 @@ hipError_t launch(Paged8Args p, hipStream_t s)
     p.n_tiles = (int)((rows + tile - 1) / tile);
     p.store_blocks = SUMI ? 0 : (int)paged8_store_blocks(p.m_max);
     const unsigned grid = paged_grid(p);
-    // All at once, two to a CU: the longest sequence is to be there with the shortest (one token of 64 users on 500 to 4000 64.7 / 61.4 us).
+    // All at once, two to a CU: the longest sequence is to be there with the shortest (us without / with: one token of 64 users on 500 to 4000 64.7 / 61.4).
+    // Over 224 shapes of 257 to 512 workgroups it takes 0.94 of the time for few rows of ragged lengths (one token of 35 users on 1668 to 13342 102 / 80; but
+    // one candidate of each of 49 users on 11 to 91 6.6 / 7.7: there the ranks cost more than there is to gain), 0.98 to 1.00 for tiles (73 candidates of
+    // 18 users on 258 to 2064 66 / 56; 690 of 18 on 167 to 668 24.8 / 27.3) and with parts of the keys (one token of 59 users on 2067 to 8268 26.0 / 22.7; 22 of five on 914 to 7313
+    // 18.6 / 20.2), and 1.00 where lengths are equal.
     const int64_t per = (int64_t)p.Hkv * p.n_tiles * p.n_split, groups = per * p.n_seqs;
     if (p.n_seqs > 1 && p.n_seqs <= 64 && groups > 256 && groups <= 512) p.by_work = 1, p.pair = (int)((255 + per) / per);
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, s, p);

@@ -214,8 +214,10 @@ struct State {
         for (int qb = 0; qb < QB; ++qb) may[qb] = true;
         reference(S, may);
     }
-    // P: the operand of the value product for 16 of the 32 keys.  WIDE: the denominator takes them as they are rounded for it (two at a time, in
-    // fp32; nothing else is made of them)
+    // P: the operand of the value product for 16 of the 32 keys: weights rounded to bf16, since the matrix instruction takes both operands in one
+    // type and weights in two pieces would be twice the products.  It is what outputs are off by beside their own rounding: 2.0e-3 to 2.3e-3 (relative, root
+    // mean square) for 1.65e-3 with weights in fp32.  WIDE: the denominator takes them as they are rounded for it (two at a time, in
+    // fp32; nothing else is made of them), so that they are shares of one.
     __device__ __forceinline__ void weights(const f32x16 (&S)[QB], bf16x8 (&P)[QB][2], int g)
     {
 #pragma unroll

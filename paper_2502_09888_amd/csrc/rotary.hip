@@ -6,7 +6,7 @@
 // A position may be far, so the angle is made in 64 bits and its whole quarter turns are taken off there; what is left, at most an eighth of
 // a turn, fits 32 bits, and the sine's and cosine's Taylor sums to the powers 9 and 10 are off by less than 2e-9 on it.  They are made once per row and pair
 // and shared by all heads through LDS.  Bound by memory: every element is read and written once, 16 bytes a thread.
-// 20000 rows of 40 heads of 128 in bf16 71 us (410 MB at 5.8 TB/s), 64 rows 5.9 (the host's call; 3.8 on the device).
+// 20000 rows of 40 heads of 128 in bf16 71 us (410 MB at 5.8 TB/s), 64 rows 5.4 (the host's call; 3.8 on the device).
 #include "../../include/climber.h"
 
 #include <algorithm>
